@@ -366,6 +366,184 @@ SOLFP4_API int mxfp4_linear(const uint16_t* x, const uint8_t* w_codes, const uin
                  const uint16_t* bias, uint16_t* out, void* workspace, size_t workspace_bytes,
                  int64_t M, int64_t N, int64_t K, void* stream);
 
+/*
+ * ---- Operators around the linears ----------------------------------------
+ *
+ * What a denoiser block has next to its FP4 linears: the residual's addition
+ * with the norm, rotary positions, and linears of few tokens whose activations
+ * are not rounded to 4 bits.  Conventions as above, with these differences:
+ * `type` names the element type of the operands that are not packed, rows
+ * may be strided (strides in elements), and operands and strides that are not
+ * packed codes need only the alignment of their elements.  Arithmetic between
+ * a load and a store is FP32; each stored value is rounded once.
+ */
+#define SOLFP4_BF16 0
+#define SOLFP4_F16 1
+#define SOLFP4_F32 2
+
+/*
+ * Root-mean-square norm with the residual's addition:
+ *
+ *   s = x + residual,  rho = (mean(s^2) + eps)^(-1/2),  out = s rho gain
+ *
+ *   x        [rows][width], rows x_stride apart
+ *   residual [rows][width], rows residual_stride apart; or NULL (s = x)
+ *   gain     [groups][width], groups gain_stride apart; or NULL (all 1).
+ *            Rows are dealt to the groups evenly and in order: row i takes
+ *            gain row i / (rows / groups), so rows % groups == 0
+ *   sum      [rows][width], written with s rounded to `type`; required with a
+ *            residual, ignored without one.  May be x or residual (same
+ *            address and stride)
+ *   out      [rows][width], written; must not overlap the inputs or sum,
+ *            except that it may be x
+ *
+ * The norm is taken of the FP32 sum, not of its rounded form.  width is at
+ * most 24576.  A row with a NaN or an infinity gives NaN; the squares are
+ * FP32, so rows beyond 2^63 overflow.  rows == 0 or width == 0 launches
+ * nothing.  Strides of inputs may be 0 (one row for all); output rows must
+ * not overlap.
+ */
+SOLFP4_API int solfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual,
+                   int64_t residual_stride, const void* gain, int64_t gain_stride, int64_t groups,
+                   float eps, void* sum, int64_t sum_stride, void* out, int64_t out_stride,
+                   int64_t rows, int64_t width, void* stream);
+
+/*
+ * The same with the output quantized in the same pass, width % 32 == 0, from
+ * the FP32 result (no rounding to `type` in between):
+ *
+ *   mxfp8_add_rmsnorm  codes [rows][width] uint8, E4M3 (OCP E4M3FN);
+ *                      scales [rows][width/32] uint8, E8M0, with
+ *                      E = floor(log2(amax_b)) - 8, scale = clamp(E + 127, 0, 254),
+ *                      code = E4M3_RNE_SAT(y / 2^(scale - 127)) (saturating at 448)
+ *   mxfp4_add_rmsnorm  codes [rows][width/2] and scales [rows][width/32]
+ *                      as mxfp4_quantize writes them (mxfp4_gemm reads them)
+ *
+ * A NaN keeps its E4M3 code 0x7F or 0xFF; E2M1 has none.
+ */
+SOLFP4_API int mxfp8_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual,
+                   int64_t residual_stride, const void* gain, int64_t gain_stride, int64_t groups,
+                   float eps, void* sum, int64_t sum_stride, uint8_t* codes, uint8_t* scales,
+                   int64_t rows, int64_t width, void* stream);
+SOLFP4_API int mxfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual,
+                   int64_t residual_stride, const void* gain, int64_t gain_stride, int64_t groups,
+                   float eps, void* sum, int64_t sum_stride, uint8_t* codes, uint8_t* scales,
+                   int64_t rows, int64_t width, void* stream);
+
+/* Device workspace, in bytes, that solfp4_rmsnorm_backward needs for the
+ * gain's gradient.  Host only; 0 for invalid sizes. */
+SOLFP4_API size_t solfp4_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t width, int64_t groups);
+
+/*
+ * Backward pass of the norm.  With rho and s as above and G = dy gain:
+ *
+ *   dx    = rho (G - s rho^2 mean(G s)) + dsum
+ *   dgain = sum over the group's rows of dy s rho
+ *
+ *   dy     [rows][width], the output's gradient
+ *   x      [rows][width], s (the forward call's sum, or its x without a
+ *          residual)
+ *   gain, groups as in the forward call
+ *   dsum   [rows][width], what reaches s past the norm; or NULL
+ *   dx     [rows][width], written: the gradient of s, which is that of x and
+ *          of the residual alike; may be dy or dsum (same address and stride)
+ *   dgain  [groups][width] FP32 contiguous, written; or NULL (not computed).
+ *          Valid without a gain too
+ *   workspace  >= solfp4_rmsnorm_backward_workspace_bytes bytes, 16-byte
+ *          aligned; ignored when dgain is NULL
+ *
+ * Sums over rows are formed in an order that depends on the sizes and the
+ * device alone: results are the same on every call.
+ */
+SOLFP4_API int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const void* x,
+                   int64_t x_stride, const void* gain, int64_t gain_stride, int64_t groups,
+                   const void* dsum, int64_t dsum_stride, float eps, void* dx, int64_t dx_stride,
+                   float* dgain, void* workspace, size_t workspace_bytes, int64_t rows,
+                   int64_t width, void* stream);
+
+/*
+ * Table of cosines and sines for solfp4_rotary:
+ *
+ *   table[p][i]         = magnitude cos(position frequency_i)
+ *   table[p][pairs + i] = magnitude sin(position frequency_i)
+ *
+ *   positions   [rows][axes] int64 on the device, or NULL (axes must be 1:
+ *               row p is position p)
+ *   frequencies [pairs] double on the device (scaled ones for long contexts)
+ *   axis_pairs  [axes] host array (not kept): the first axis_pairs[0] pairs turn with
+ *               axis 0, the next with axis 1, ...; they add up to pairs.
+ *               NULL with one axis
+ *   axes        1 to 4
+ *   table       [rows][2 pairs] FP32, written
+ *
+ * Angles, cosines and sines are formed in 64 bits and rounded once.
+ */
+SOLFP4_API int solfp4_rotary_table(const int64_t* positions, int64_t rows, const double* frequencies,
+                   int64_t pairs, const int64_t* axis_pairs, int axes, double magnitude,
+                   float* table, void* stream);
+
+/*
+ * Rotary positions on q and k:  pair i of a head, (u, v), becomes
+ * (u cos - v sin, u sin + v cos).  Element e of head h of token t is at
+ * t token_stride + h head_stride + e, so q and k may be views of one packed
+ * QKV buffer.
+ *
+ *   q, q_out   [tokens][q_heads][dim], each with its own strides; q_out may
+ *              be q (same strides) and must not overlap it otherwise
+ *   k, k_out   [tokens][k_heads][dim] likewise; k_heads may be 0
+ *   rotated    even, at most dim: the first `rotated` elements of a head turn,
+ *              the others are copied
+ *   layout     SOLFP4_ROTARY_HALF: pairs (i, i + rotated/2);
+ *              SOLFP4_ROTARY_INTERLEAVED: pairs (2i, 2i + 1)
+ *   inverse    nonzero: the transposed rotation (sin negated), which takes
+ *              the outputs' gradients to the inputs'
+ *   table      [table_rows][rotated] FP32, contiguous
+ *   positions  [tokens], the table row of each token, as int32 or int64
+ *              (position_bytes 4 or 8); or NULL (position_bytes 0): token t
+ *              takes row t % table_rows, so sequences of table_rows tokens
+ *              follow each other
+ *
+ * A position outside [0, table_rows) gives NaN in the rotated elements of
+ * its token and reads nothing outside the table.
+ */
+#define SOLFP4_ROTARY_HALF 0
+#define SOLFP4_ROTARY_INTERLEAVED 1
+SOLFP4_API int solfp4_rotary(int type, int layout, int inverse,
+                   const void* q, int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                   int64_t q_out_token_stride, int64_t q_out_head_stride, int64_t q_heads,
+                   const void* k, int64_t k_token_stride, int64_t k_head_stride, void* k_out,
+                   int64_t k_out_token_stride, int64_t k_out_head_stride, int64_t k_heads,
+                   const float* table, int64_t table_rows, const void* positions,
+                   int position_bytes, int64_t tokens, int64_t dim, int64_t rotated, void* stream);
+
+/*
+ * Linears of few tokens against 4-bit weights, activations not rounded:
+ *
+ *   out[m][n] = bf16_rne(alpha sum_k x[m][k] (s q)[n][k] + bias[n])
+ *
+ *   nvfp4_weight_linear  x [M][K] BF16; weight as nvfp4_quantize writes it
+ *                        (alpha = w_global_scale)
+ *   mxfp4_weight_linear  x [M][K] BF16; weight as mxfp4_quantize writes it
+ *   mxfp8_linear         x_codes [M][K] E4M3, x_scales [M][K/32] E8M0 as
+ *                        mxfp8_add_rmsnorm writes them; MXFP4 weight
+ *
+ * Products are exact and sums FP32 in a fixed order; decoded weights,
+ * products or sums outside the FP32 range are unspecified.  Time is that of
+ * reading the weight once for up to 64 tokens, and again for every further
+ * 64 tokens: from a few hundred tokens on, nvfp4_linear and mxfp4_linear are
+ * the faster calls.  M, N or K equal to 0 are valid (K == 0 writes the bias,
+ * or zeros).  K must be below 2^24 and N below 2^22.  Packed operands, x, bias
+ * and out are contiguous and 16-byte aligned; no workspace.
+ */
+SOLFP4_API int nvfp4_weight_linear(const uint16_t* x, const uint8_t* w_codes, const uint8_t* w_scales,
+                   const float* w_global_scale, const uint16_t* bias, uint16_t* out,
+                   int64_t M, int64_t N, int64_t K, void* stream);
+SOLFP4_API int mxfp4_weight_linear(const uint16_t* x, const uint8_t* w_codes, const uint8_t* w_scales,
+                   const uint16_t* bias, uint16_t* out, int64_t M, int64_t N, int64_t K, void* stream);
+SOLFP4_API int mxfp8_linear(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes,
+                   const uint8_t* w_scales, const uint16_t* bias, uint16_t* out,
+                   int64_t M, int64_t N, int64_t K, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -70,12 +70,41 @@ lib.mxfp4_linear_workspace_bytes.argtypes = [_i64, _i64]
 lib.mxfp4_linear.restype = ctypes.c_int
 lib.mxfp4_linear.argtypes = [_p, _p, _p, _p, _p, _p, _sz, _i64, _i64, _i64, _p]
 
+_int, _f32, _f64 = ctypes.c_int, ctypes.c_float, ctypes.c_double
+_norm_in = [_int, _p, _i64, _p, _i64, _p, _i64, _i64, _f32, _p, _i64]
+lib.solfp4_add_rmsnorm.restype = _int
+lib.solfp4_add_rmsnorm.argtypes = [*_norm_in, _p, _i64, _i64, _i64, _p]
+lib.mxfp8_add_rmsnorm.restype = _int
+lib.mxfp8_add_rmsnorm.argtypes = [*_norm_in, _p, _p, _i64, _i64, _p]
+lib.mxfp4_add_rmsnorm.restype = _int
+lib.mxfp4_add_rmsnorm.argtypes = [*_norm_in, _p, _p, _i64, _i64, _p]
+lib.solfp4_rmsnorm_backward_workspace_bytes.restype = _sz
+lib.solfp4_rmsnorm_backward_workspace_bytes.argtypes = [_i64, _i64, _i64]
+lib.solfp4_rmsnorm_backward.restype = _int
+lib.solfp4_rmsnorm_backward.argtypes = [_int, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i64, _f32, _p, _i64, _p, _p,
+                                        _sz, _i64, _i64, _p]
+lib.solfp4_rotary_table.restype = _int
+lib.solfp4_rotary_table.argtypes = [_p, _i64, _p, _i64, _p, _int, _f64, _p, _p]
+lib.solfp4_rotary.restype = _int
+lib.solfp4_rotary.argtypes = [_int, _int, _int, *2 * [_p, _i64, _i64, _p, _i64, _i64, _i64], _p, _i64, _p, _int, _i64,
+                              _i64, _i64, _p]
+lib.nvfp4_weight_linear.restype = _int
+lib.nvfp4_weight_linear.argtypes = [*6 * [_p], _i64, _i64, _i64, _p]
+lib.mxfp4_weight_linear.restype = _int
+lib.mxfp4_weight_linear.argtypes = [*5 * [_p], _i64, _i64, _i64, _p]
+lib.mxfp8_linear.restype = _int
+lib.mxfp8_linear.argtypes = [*6 * [_p], _i64, _i64, _i64, _p]
+
 EXPORTED = ["solfp4_strerror", "solfp4_version", "solfp4_gemm_plan",
             "nvfp4_quantize_workspace_bytes", "nvfp4_quantize", "nvfp4_quantize_amax",
             "nvfp4_gelu_amax", "nvfp4_quantize_encode", "nvfp4_quantize_noalloc",
             "nvfp4_gemm",
             "nvfp4_gemm_workspace_bytes", "nvfp4_linear_workspace_bytes", "nvfp4_linear",
-            "mxfp4_quantize", "mxfp4_gemm", "mxfp4_linear_workspace_bytes", "mxfp4_linear"]
+            "mxfp4_quantize", "mxfp4_gemm", "mxfp4_linear_workspace_bytes", "mxfp4_linear",
+            "solfp4_add_rmsnorm", "mxfp8_add_rmsnorm", "mxfp4_add_rmsnorm",
+            "solfp4_rmsnorm_backward_workspace_bytes", "solfp4_rmsnorm_backward",
+            "solfp4_rotary_table", "solfp4_rotary",
+            "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear"]
 
 FORMAT_NVFP4, FORMAT_MXFP4 = 0, 1
 KERNEL_NAMES = {0: None, 1: "nvfp4_gemm_lane_kernel", 2: "nvfp4_gemm_kernel",
@@ -430,4 +459,390 @@ def mxfp4_linear(x, w_codes, w_scales, bias=None, out=None, workspace=None, stre
     _check(lib.mxfp4_linear(_ptr(x), _ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(out),
                             _ptr(workspace), workspace.numel(), M, N, K,
                             ctypes.c_void_p(st.cuda_stream)))
+    return out
+
+
+# ---- operators around the linears -----------------------------------------
+
+TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+def _type(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if t.dtype not in TYPES:
+        raise ValueError(f"{name}: expected bfloat16, float16 or float32, got {t.dtype}")
+    return TYPES[t.dtype]
+
+
+def _need_strided(t, dtype, shape, name, device):
+    """A GPU tensor of this type and shape whose last dimension is contiguous;
+    the others may have any stride."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if t.layout != torch.strided or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not _is_gpu(t) \
+            or t.device != device or (shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: expected CUDA {dtype} {tuple(shape)} on {device} with a contiguous last dimension, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+
+
+def _norm_operands(x, residual, gain, eps, sum_out):
+    """Checked: (type, rows, width, device, groups, gain stride)."""
+    kind = _type(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: expected a 2-D tensor")
+    rows, width = x.shape
+    dev = x.device
+    _need_strided(x, x.dtype, (rows, width), "x", dev)
+    if residual is not None:
+        _need_strided(residual, x.dtype, (rows, width), "residual", dev)
+    if sum_out is not None:
+        if residual is None:
+            raise ValueError("sum_out: given without a residual")
+        _need_strided(sum_out, x.dtype, (rows, width), "sum_out", dev)
+    groups, gain_stride = _gain(gain, x, rows, width, dev)
+    if not eps >= 0:
+        raise ValueError(f"eps: expected a number of at least 0, got {eps}")
+    return kind, rows, width, dev, groups, gain_stride
+
+
+def _gain(gain, x, rows, width, dev):
+    if gain is None:
+        return 1, 0
+    if not isinstance(gain, torch.Tensor) or gain.dim() not in (1, 2):
+        raise ValueError("gain: expected a tensor [width] or [groups, width]")
+    groups = 1 if gain.dim() == 1 else gain.shape[0]
+    _need_strided(gain, x.dtype, (width,) if gain.dim() == 1 else (groups, width), "gain", dev)
+    if groups < 1 or rows % groups:
+        raise ValueError(f"gain: {rows} rows cannot be dealt to {groups} groups evenly")
+    return groups, 0 if gain.dim() == 1 else gain.stride(0)
+
+
+def _rows_of(t):
+    """Pointer and row stride, as the C-ABI takes them."""
+    return (None, 0) if t is None else (_ptr(t), t.stride(0))
+
+
+def add_rmsnorm(x, residual=None, gain=None, eps=1e-6, out=None, sum_out=None, stream=None):
+    """Root-mean-square norm of the rows of x + residual, times gain
+    ([width], or [groups, width] with the rows dealt to the groups in order)
+    -> (out, sum); sum, x + residual rounded to x's type, is None without a
+    residual.  x [rows, width] BF16, FP16 or FP32, rows of any stride; sum_out
+    may be x or residual."""
+    if stream is None:
+        r = _host.add_rmsnorm(x, residual, gain, eps, out, sum_out)
+        if r is not None:
+            return _native(r)
+    kind, rows, width, dev, groups, gain_stride = _norm_operands(x, residual, gain, eps, sum_out)
+    if out is not None:
+        _need_strided(out, x.dtype, (rows, width), "out", dev)
+    st = _stream(stream, dev)
+    if out is None:
+        out = _alloc((rows, width), x.dtype, dev, st)
+    if residual is not None and sum_out is None:
+        sum_out = _alloc((rows, width), x.dtype, dev, st)
+    _check(lib.solfp4_add_rmsnorm(kind, *_rows_of(x), *_rows_of(residual), _ptr(gain), gain_stride, groups, eps,
+                                  *_rows_of(sum_out), *_rows_of(out), rows, width, ctypes.c_void_p(st.cuda_stream)))
+    return out, sum_out
+
+
+def _quantized_add_rmsnorm(fn, native, pack, x, residual, gain, eps, codes, scales, sum_out, stream):
+    if stream is None:
+        r = native(x, residual, gain, eps, codes, scales, sum_out)
+        if r is not None:
+            return _native(r)
+    kind, rows, width, dev, groups, gain_stride = _norm_operands(x, residual, gain, eps, sum_out)
+    if width % 32:
+        raise ValueError(f"x: width {width} is not a multiple of 32")
+    if codes is not None:
+        _need(codes, torch.uint8, (rows, width // pack), "codes", dev)
+    if scales is not None:
+        _need(scales, torch.uint8, (rows, width // 32), "scales", dev)
+    st = _stream(stream, dev)
+    if codes is None:
+        codes = _alloc((rows, width // pack), torch.uint8, dev, st)
+    if scales is None:
+        scales = _alloc((rows, width // 32), torch.uint8, dev, st)
+    if residual is not None and sum_out is None:
+        sum_out = _alloc((rows, width), x.dtype, dev, st)
+    _check(fn(kind, *_rows_of(x), *_rows_of(residual), _ptr(gain), gain_stride, groups, eps, *_rows_of(sum_out),
+              _ptr(codes), _ptr(scales), rows, width, ctypes.c_void_p(st.cuda_stream)))
+    return codes, scales, sum_out
+
+
+def mxfp8_add_rmsnorm(x, residual=None, gain=None, eps=1e-6, codes=None, scales=None, sum_out=None, stream=None):
+    """add_rmsnorm with its output in MXFP8 -> (codes uint8 [rows, width],
+    E4M3, scales uint8 [rows, width/32], E8M0, sum).  width % 32 == 0."""
+    return _quantized_add_rmsnorm(lib.mxfp8_add_rmsnorm, _host.mxfp8_add_rmsnorm, 1, x, residual, gain, eps, codes,
+                                  scales, sum_out, stream)
+
+
+def mxfp4_add_rmsnorm(x, residual=None, gain=None, eps=1e-6, codes=None, scales=None, sum_out=None, stream=None):
+    """add_rmsnorm with its output in MXFP4, as mxfp4_gemm takes it -> (codes
+    uint8 [rows, width/2], scales uint8 [rows, width/32], sum).  width % 32 == 0."""
+    return _quantized_add_rmsnorm(lib.mxfp4_add_rmsnorm, _host.mxfp4_add_rmsnorm, 2, x, residual, gain, eps, codes,
+                                  scales, sum_out, stream)
+
+
+def rmsnorm_backward_workspace_bytes(rows: int, width: int, groups: int = 1) -> int:
+    return lib.solfp4_rmsnorm_backward_workspace_bytes(rows, width, groups)
+
+
+def rmsnorm_backward(dy, x, gain=None, dsum=None, eps=1e-6, dx=None, dgain=None, workspace=None, stream=None):
+    """Backward pass of add_rmsnorm: dy, the output's gradient; x, the sum
+    (or the x of a call without a residual); dsum, what reaches the sum past
+    the norm -> (dx, dgain).  dx is the gradient of x and of the residual alike;
+    dgain is FP32 in gain's shape, None without a gain."""
+    if stream is None:
+        r = _host.rmsnorm_backward(dy, x, gain, dsum, eps, dx, dgain, workspace)
+        if r is not None:
+            return _native(r)
+    kind = _type(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: expected a 2-D tensor")
+    rows, width = x.shape
+    dev = x.device
+    _need_strided(x, x.dtype, (rows, width), "x", dev)
+    _need_strided(dy, x.dtype, (rows, width), "dy", dev)
+    if dsum is not None:
+        _need_strided(dsum, x.dtype, (rows, width), "dsum", dev)
+    if dx is not None:
+        _need_strided(dx, x.dtype, (rows, width), "dx", dev)
+    groups, gain_stride = _gain(gain, x, rows, width, dev)
+    if not eps >= 0:
+        raise ValueError(f"eps: expected a number of at least 0, got {eps}")
+    need = 0
+    if gain is None:
+        if dgain is not None:
+            raise ValueError("dgain: given without a gain")
+    else:
+        if dgain is not None:
+            _need(dgain, torch.float32, tuple(gain.shape), "dgain", dev)
+        need = rmsnorm_backward_workspace_bytes(rows, width, groups)
+        if workspace is not None:
+            _need_workspace(workspace, need, "workspace", dev)
+    st = _stream(stream, dev)
+    if dx is None:
+        dx = _alloc((rows, width), x.dtype, dev, st)
+    if gain is not None:
+        if dgain is None:
+            dgain = _alloc(tuple(gain.shape), torch.float32, dev, st)
+        if workspace is None:
+            workspace = _alloc((max(need, 256),), torch.uint8, dev, st)
+    _check(lib.solfp4_rmsnorm_backward(kind, *_rows_of(dy), *_rows_of(x), _ptr(gain), gain_stride, groups,
+                                       *_rows_of(dsum), eps, *_rows_of(dx), _ptr(dgain), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), rows, width,
+                                       ctypes.c_void_p(st.cuda_stream)))
+    return dx, dgain
+
+
+def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
+                       original_length: int = 0, low_turns: float = 1.0, high_turns: float = 32.0):
+    """Angle per position of each of the rotated/2 pairs, float64 on the host:
+    base ** (-2 i / rotated), and for contexts `factor` times longer than the
+    one a model was trained on
+
+        "linear"   every frequency divided by factor
+        "base"     base * factor ** (rotated / (rotated - 2)) as the base: the
+                   fastest pair keeps its frequency, the slowest is divided
+                   by factor
+        "by-parts" pairs that turn more than high_turns times over
+                   original_length keep their frequency, those under low_turns
+                   have it divided by factor, in between linearly mixed by
+                   their number of turns
+    """
+    if rotated < 0 or rotated % 2:
+        raise ValueError(f"rotated: expected an even number, got {rotated}")
+    if scaling not in (None, "linear", "base", "by-parts"):
+        raise ValueError(f"scaling: expected None, 'linear', 'base' or 'by-parts', got {scaling!r}")
+    if not base > 0 or not factor > 0:
+        raise ValueError("base and factor: expected positive numbers")
+    i = torch.arange(rotated // 2, dtype=torch.float64)
+    if scaling == "base":
+        if rotated <= 2:
+            raise ValueError("scaling 'base' needs more than one pair")
+        base = base * factor ** (rotated / (rotated - 2))
+    f = base ** (-2.0 * i / max(rotated, 1))
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "by-parts":
+        if original_length <= 0 or not high_turns > low_turns:
+            raise ValueError("scaling 'by-parts' needs original_length and high_turns above low_turns")
+        turns = original_length * f / (2 * torch.pi)
+        keep = ((turns - low_turns) / (high_turns - low_turns)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+    return f
+
+
+def rotary_table(frequencies, positions, axis_pairs=None, magnitude=1.0, device=None, out=None, stream=None):
+    """cos and sin of position x frequency, FP32 [rows, 2 pairs], for rotary.
+
+    frequencies: float64 [pairs].  positions: a row count (row p is position
+    p) or an int64 tensor [rows], or [rows, axes] with axis_pairs giving each
+    axis's number of pairs (image positions: the first axis_pairs[0] pairs turn
+    with axis 0, ...).  magnitude scales both.  The table is on the
+    device of a positions tensor, else on `device` (default: the current one)."""
+    if not isinstance(frequencies, torch.Tensor) or frequencies.dim() != 1 or frequencies.dtype != torch.float64:
+        raise ValueError("frequencies: expected a 1-D float64 tensor")
+    pairs = frequencies.numel()
+    axes = 1
+    if isinstance(positions, torch.Tensor):
+        dev = positions.device
+        if positions.dim() not in (1, 2):
+            raise ValueError("positions: expected [rows] or [rows, axes]")
+        _need(positions, torch.int64, positions.shape, "positions")
+        rows = positions.shape[0]
+        axes = 1 if positions.dim() == 1 else positions.shape[1]
+        at = positions
+    else:
+        rows, at = int(positions), None
+        if rows < 0:
+            raise ValueError(f"positions: expected at least 0 rows, got {rows}")
+        dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    if axes > 1 or axis_pairs is not None:
+        if axis_pairs is None or len(axis_pairs) != axes or sum(axis_pairs) != pairs or min(axis_pairs) < 0:
+            raise ValueError(f"axis_pairs: expected {axes} counts that add up to {pairs}")
+    if out is not None:
+        _need(out, torch.float32, (rows, 2 * pairs), "out", dev)
+    st = _stream(stream, dev)
+    with torch.cuda.stream(st):
+        f = frequencies.to(dev)
+    if out is None:
+        out = _alloc((rows, 2 * pairs), torch.float32, dev, st)
+    counts = None if axis_pairs is None else (ctypes.c_int64 * axes)(*axis_pairs)
+    _check(lib.solfp4_rotary_table(_ptr(at), rows, _ptr(f), pairs, counts, axes, float(magnitude), _ptr(out),
+                                   ctypes.c_void_p(st.cuda_stream)))
+    return out
+
+
+def _heads_of(t):
+    return (None, 0, 0) if t is None else (_ptr(t), t.stride(0), t.stride(1))
+
+
+def rotary(q, k, table, positions=None, layout="half", inverse=False, q_out=None, k_out=None, stream=None):
+    """Rotary positions on q [tokens, q_heads, dim] and k [tokens, k_heads,
+    dim] or None -> (q, k) in new tensors, or in q_out and k_out, which may be q
+    and k themselves.  Views of a packed QKV buffer are taken as they are.
+
+    table: FP32 [table_rows, rotated] from rotary_table; the first `rotated`
+    elements of a head turn.  positions: int32 or int64 [tokens], the table
+    row of each token; None: token t takes row t % table_rows.  A position
+    outside the table gives NaN.  layout: "half" (pairs i, i + rotated/2) or
+    "interleaved" (pairs 2i, 2i + 1).  inverse: the transposed rotation, which
+    takes the outputs' gradients to the inputs'."""
+    if stream is None:
+        r = _host.rotary(q, k, table, positions, LAYOUTS.get(layout, -1), inverse, q_out, k_out)
+        if r is not None:
+            return _native(r)
+    kind = _type(q, "q")
+    if q.dim() != 3:
+        raise ValueError("q: expected a 3-D tensor [tokens, heads, dim]")
+    tokens, heads, dim = q.shape
+    dev = q.device
+    _need_strided(q, q.dtype, (tokens, heads, dim), "q", dev)
+    k_heads = 0
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 3:
+            raise ValueError("k: expected a 3-D tensor [tokens, heads, dim] or None")
+        k_heads = k.shape[1]
+        _need_strided(k, q.dtype, (tokens, k_heads, dim), "k", dev)
+    elif k_out is not None:
+        raise ValueError("k_out: given without k")
+    if layout not in LAYOUTS:
+        raise ValueError(f"layout: expected 'half' or 'interleaved', got {layout!r}")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table: expected a 2-D tensor [rows, rotated]")
+    table_rows, rotated = table.shape
+    _need(table, torch.float32, (table_rows, rotated), "table", dev)
+    if rotated % 2 or rotated > dim:
+        raise ValueError(f"table: {rotated} elements to rotate, expected an even number of at most {dim}")
+    if table_rows == 0 and tokens > 0:
+        raise ValueError("table: no rows")
+    position_bytes = 0
+    if positions is not None:
+        if not isinstance(positions, torch.Tensor) or positions.dtype not in (torch.int32, torch.int64):
+            raise ValueError("positions: expected an int32 or int64 tensor")
+        _need(positions, positions.dtype, (tokens,), "positions", dev)
+        position_bytes = positions.element_size()
+    if q_out is not None:
+        _need_strided(q_out, q.dtype, (tokens, heads, dim), "q_out", dev)
+    if k_out is not None:
+        _need_strided(k_out, q.dtype, (tokens, k_heads, dim), "k_out", dev)
+    st = _stream(stream, dev)
+    if q_out is None:
+        q_out = _alloc((tokens, heads, dim), q.dtype, dev, st)
+    if k is not None and k_out is None:
+        k_out = _alloc((tokens, k_heads, dim), q.dtype, dev, st)
+    _check(lib.solfp4_rotary(kind, LAYOUTS[layout], int(bool(inverse)), *_heads_of(q), *_heads_of(q_out), heads,
+                             *_heads_of(k), *_heads_of(k_out), k_heads, _ptr(table), table_rows, _ptr(positions),
+                             position_bytes, tokens, dim, rotated, ctypes.c_void_p(st.cuda_stream)))
+    return q_out, k_out
+
+
+def nvfp4_weight_linear(x, w_codes, w_scales, w_global_scale, bias=None, out=None, stream=None):
+    """Linear of few tokens with BF16 activations x [M, K] (not quantized) and
+    a packed NVFP4 weight [N, K], plus bias -> BF16 [M, N]."""
+    if stream is None:
+        r = _host.nvfp4_weight_linear(x, w_codes, w_scales, w_global_scale, bias, out)
+        if r is not None:
+            return _native(r)
+    M, K = _dims(x, "x", 16)
+    N = _dims(w_codes, "w_codes", 1)[0]
+    dev = x.device
+    _need(x, torch.bfloat16, (M, K), "x")
+    _need(w_codes, torch.uint8, (N, K // 2), "w_codes (x and w must agree on K)", dev)
+    _need(w_scales, torch.uint8, (N, K // 16), "w_scales", dev)
+    _need(w_global_scale, torch.float32, (1,), "w_global_scale", dev)
+    st, out = _weight_linear_out(bias, out, M, N, dev, stream)
+    _check(lib.nvfp4_weight_linear(_ptr(x), _ptr(w_codes), _ptr(w_scales), _ptr(w_global_scale), _ptr(bias),
+                                   _ptr(out), M, N, K, ctypes.c_void_p(st.cuda_stream)))
+    return out
+
+
+def _weight_linear_out(bias, out, M, N, dev, stream):
+    if bias is not None:
+        _need(bias, torch.bfloat16, (N,), "bias", dev)
+    if out is not None:
+        _need(out, torch.bfloat16, (M, N), "out", dev)
+    st = _stream(stream, dev)
+    return st, _alloc((M, N), torch.bfloat16, dev, st) if out is None else out
+
+
+def mxfp4_weight_linear(x, w_codes, w_scales, bias=None, out=None, stream=None):
+    """Linear of few tokens with BF16 activations x [M, K] (not quantized) and
+    a packed MXFP4 weight [N, K], plus bias -> BF16 [M, N]."""
+    if stream is None:
+        r = _host.mxfp4_weight_linear(x, w_codes, w_scales, bias, out)
+        if r is not None:
+            return _native(r)
+    M, K = _dims(x, "x", 32)
+    N = _dims(w_codes, "w_codes", 1)[0]
+    dev = x.device
+    _need(x, torch.bfloat16, (M, K), "x")
+    _need(w_codes, torch.uint8, (N, K // 2), "w_codes (x and w must agree on K)", dev)
+    _need(w_scales, torch.uint8, (N, K // 32), "w_scales", dev)
+    st, out = _weight_linear_out(bias, out, M, N, dev, stream)
+    _check(lib.mxfp4_weight_linear(_ptr(x), _ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(out), M, N, K,
+                                   ctypes.c_void_p(st.cuda_stream)))
+    return out
+
+
+def mxfp8_linear(x_codes, x_scales, w_codes, w_scales, bias=None, out=None, stream=None):
+    """Linear of few tokens with MXFP8 activations [M, K] (as mxfp8_add_rmsnorm
+    writes them) and a packed MXFP4 weight [N, K], plus bias -> BF16 [M, N]."""
+    if stream is None:
+        r = _host.mxfp8_linear(x_codes, x_scales, w_codes, w_scales, bias, out)
+        if r is not None:
+            return _native(r)
+    M, K = _dims(x_codes, "x_codes", 32)
+    N = _dims(w_codes, "w_codes", 1)[0]
+    dev = x_codes.device
+    _need(x_codes, torch.uint8, (M, K), "x_codes")
+    _need(x_scales, torch.uint8, (M, K // 32), "x_scales", dev)
+    _need(w_codes, torch.uint8, (N, K // 2), "w_codes (x and w must agree on K)", dev)
+    _need(w_scales, torch.uint8, (N, K // 32), "w_scales", dev)
+    st, out = _weight_linear_out(bias, out, M, N, dev, stream)
+    _check(lib.mxfp8_linear(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(out),
+                            M, N, K, ctypes.c_void_p(st.cuda_stream)))
     return out

@@ -20,8 +20,8 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsolfp4.so")
 HOST_LIB = os.path.join(PKG, "_host.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "gemm_small.hip", "gemm_wavek.hip", "mx_quantize.hip",
-           "mx_gemm.hip"]
-HEADERS = ["device_common.h", "kernels.h", "nvfp4_gemm_common.h"]
+           "mx_gemm.hip", "api_operators.hip", "norm.hip", "rotary.hip", "weight_linear.hip"]
+HEADERS = ["device_common.h", "elements.h", "kernels.h", "nvfp4_gemm_common.h"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,0 +1,326 @@
+// C-ABI entry points of the operators around the linears (declared and
+// documented in solfp4.h).  Every argument check happens on the host before
+// the first HIP call.
+#include <math.h>
+
+#include "solfp4.h"
+#include "kernels.h"
+
+namespace {
+
+constexpr int64_t kMaxDim = (int64_t)1 << 31;
+constexpr int64_t kMaxK = (int64_t)1 << 24, kMaxN = (int64_t)1 << 22;
+// a launch has at most 2^31 workgroups
+constexpr int64_t kMaxGroups = kMaxDim - 1;
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+bool type_ok(int type) { return type == SOLFP4_BF16 || type == SOLFP4_F16 || type == SOLFP4_F32; }
+
+bool element_aligned(int type, const void* p) { return ((uintptr_t)p & (type == SOLFP4_F32 ? 3u : 1u)) == 0; }
+
+int check_dims(int64_t a, int64_t b) {
+  if (a < 0 || b < 0) return SOLFP4_EINVAL;
+  if (a >= kMaxDim || b >= kMaxDim) return SOLFP4_ESHAPE;
+  return SOLFP4_OK;
+}
+
+// Whether an operand of this many rows stays within kMaxSpan elements.
+constexpr int64_t kMaxSpan = (int64_t)1 << 46;
+bool span_ok(int64_t stride, int64_t rows) { return stride == 0 || rows - 1 <= kMaxSpan / stride; }
+
+// Rows of an operand that the call reads or, with `written`, writes (whose
+// rows must not overlap).
+int check_rows(int type, const void* p, int64_t stride, int64_t rows, int64_t width, bool written) {
+  if (!p || stride < 0) return SOLFP4_EINVAL;
+  if (!span_ok(stride, rows)) return SOLFP4_ESHAPE;
+  if (!element_aligned(type, p)) return SOLFP4_EALIGN;
+  if (written && rows > 1 && stride < width) return SOLFP4_EINVAL;
+  return SOLFP4_OK;
+}
+
+// [a, a + bytes) of rows x width elements
+struct Extent {
+  uintptr_t lo, hi;
+};
+
+Extent extent(int type, const void* p, int64_t stride, int64_t rows, int64_t width) {
+  const uint64_t bytes = type == SOLFP4_F32 ? 4 : 2;
+  const uintptr_t lo = (uintptr_t)p;
+  return {lo, lo + (uintptr_t)(((uint64_t)(rows - 1) * (uint64_t)stride + (uint64_t)width) * bytes)};
+}
+
+bool overlap(Extent a, Extent b) { return a.lo < b.hi && b.lo < a.hi; }
+
+// The two are one operand (each element is read before it is written) or apart.
+bool same_or_apart(int type, const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t rows,
+                   int64_t width) {
+  if (in == out && (in_stride == out_stride || rows == 1)) return true;
+  return !overlap(extent(type, in, in_stride, rows, width), extent(type, out, out_stride, rows, width));
+}
+
+int norm_checks(int type, const solfp4::NormArgs& a, int64_t groups, int out) {
+  if (!type_ok(type)) return SOLFP4_EINVAL;
+  int rc = check_dims(a.rows, a.width);
+  if (rc) return rc;
+  if (groups < 1 || !(a.eps >= 0.0f)) return SOLFP4_EINVAL;
+  if (a.width > solfp4::kNormMaxWidth || a.rows % groups || (out != solfp4::kNormSame && a.width % 32))
+    return SOLFP4_ESHAPE;
+  if (a.rows == 0 || a.width == 0) return SOLFP4_OK;
+  if ((rc = check_rows(type, a.x, a.x_stride, a.rows, a.width, false))) return rc;
+  if (a.residual) {
+    if ((rc = check_rows(type, a.residual, a.residual_stride, a.rows, a.width, false))) return rc;
+    if ((rc = check_rows(type, a.sum, a.sum_stride, a.rows, a.width, true))) return rc;
+    if (!same_or_apart(type, a.x, a.x_stride, a.sum, a.sum_stride, a.rows, a.width) ||
+        !same_or_apart(type, a.residual, a.residual_stride, a.sum, a.sum_stride, a.rows, a.width))
+      return SOLFP4_EINVAL;
+  }
+  if (a.gain && (rc = check_rows(type, a.gain, a.gain_stride, groups, a.width, false))) return rc;
+  if (out == solfp4::kNormSame) {
+    if ((rc = check_rows(type, a.out, a.out_stride, a.rows, a.width, true))) return rc;
+    const Extent o = extent(type, a.out, a.out_stride, a.rows, a.width);
+    if (!same_or_apart(type, a.x, a.x_stride, a.out, a.out_stride, a.rows, a.width)) return SOLFP4_EINVAL;
+    if (a.residual && (overlap(o, extent(type, a.residual, a.residual_stride, a.rows, a.width)) ||
+                       overlap(o, extent(type, a.sum, a.sum_stride, a.rows, a.width))))
+      return SOLFP4_EINVAL;
+    return SOLFP4_OK;
+  }
+  if (!a.codes || !a.scales) return SOLFP4_EINVAL;
+  return aligned16(a.codes) && aligned16(a.scales) ? SOLFP4_OK : SOLFP4_EALIGN;
+}
+
+int add_rmsnorm(int type, int kind, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                const void* gain, int64_t gain_stride, int64_t groups, float eps, void* sum, int64_t sum_stride,
+                void* out, int64_t out_stride, uint8_t* codes, uint8_t* scales, int64_t rows, int64_t width,
+                void* stream) {
+  const solfp4::NormArgs a = {x, x_stride, residual, residual_stride, gain, gain_stride,
+                              groups > 0 && rows > 0 ? rows / groups : 1, eps, sum, sum_stride, out, out_stride,
+                              codes, scales, rows, width};
+  const int rc = norm_checks(type, a, groups, kind);
+  if (rc) return rc;
+  const hipError_t e = solfp4::launch_add_rmsnorm(type, kind, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
+size_t back_workspace(int64_t rows, int64_t width, int64_t groups) {
+  const size_t bytes = (size_t)(solfp4::rmsnorm_backward_parts(rows, groups) * groups) * (size_t)width * sizeof(float);
+  return (bytes + 255) / 256 * 256;
+}
+
+int back_dims(int64_t rows, int64_t width, int64_t groups) {
+  const int rc = check_dims(rows, width);
+  if (rc) return rc;
+  if (groups < 1) return SOLFP4_EINVAL;
+  return width > solfp4::kNormMaxWidth || groups > 65535 || rows % groups ? SOLFP4_ESHAPE : SOLFP4_OK;
+}
+
+int linear_checks(const void* x, const void* x_scales, bool scaled_x, const void* wc, const void* ws, const float* wg,
+                  bool has_global, const uint16_t* bias, const uint16_t* out, int64_t M, int64_t N, int64_t K,
+                  int64_t block) {
+  int rc = check_dims(M, N);
+  if (rc) return rc;
+  rc = check_dims(K, 0);
+  if (rc) return rc;
+  if (K % block || K >= kMaxK || N >= kMaxN) return SOLFP4_ESHAPE;
+  if (solfp4::weight_linear_groups(M, N) > kMaxGroups) return SOLFP4_ESHAPE;
+  if (M == 0 || N == 0) return SOLFP4_OK;
+  if (!out || (has_global && !wg)) return SOLFP4_EINVAL;
+  if (K > 0 && (!x || !wc || !ws || (scaled_x && !x_scales))) return SOLFP4_EINVAL;
+  if (!aligned16(out) || (bias && !aligned16(bias)) || (has_global && !aligned16(wg))) return SOLFP4_EALIGN;
+  if (K > 0 && (!aligned16(x) || !aligned16(wc) || !aligned16(ws) || (scaled_x && !aligned16(x_scales))))
+    return SOLFP4_EALIGN;
+  return SOLFP4_OK;
+}
+
+int run_linear(int format, bool x8, const solfp4::WeightLinearArgs& a, void* stream) {
+  const hipError_t e = solfp4::launch_weight_linear(format, x8, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
+int rotary_operand(int type, solfp4::RotaryOperand* o, const void* in, int64_t it, int64_t ih, void* out, int64_t ot,
+                   int64_t oh, int64_t heads, int64_t tokens, int64_t dim) {
+  if (heads < 0) return SOLFP4_EINVAL;
+  if (heads >= 1 << 20) return SOLFP4_ESHAPE;
+  *o = {in, it, ih, out, ot, oh, (int)heads};
+  if (heads == 0 || tokens == 0 || dim == 0) return SOLFP4_OK;
+  if (!in || !out || it < 0 || ih < 0 || ot < 0 || oh < 0) return SOLFP4_EINVAL;
+  if (!span_ok(it, tokens) || !span_ok(ih, heads) || !span_ok(ot, tokens) || !span_ok(oh, heads)) return SOLFP4_ESHAPE;
+  if (!element_aligned(type, in) || !element_aligned(type, out)) return SOLFP4_EALIGN;
+  // heads of the output must not overlap: either order of tokens and heads
+  const bool by_token = (heads == 1 || oh >= dim) && (tokens == 1 || ot >= (heads - 1) * oh + dim);
+  const bool by_head = (tokens == 1 || ot >= dim) && (heads == 1 || oh >= (tokens - 1) * ot + dim);
+  return by_token || by_head ? SOLFP4_OK : SOLFP4_EINVAL;
+}
+
+bool rotary_apart(int type, const solfp4::RotaryOperand& in, const solfp4::RotaryOperand& out, int64_t tokens,
+                  int64_t dim) {
+  if (!in.heads || !out.heads) return true;
+  const int64_t in_span = (tokens - 1) * in.in_token + (in.heads - 1) * in.in_head + dim;
+  const int64_t out_span = (tokens - 1) * out.out_token + (out.heads - 1) * out.out_head + dim;
+  if (!overlap(extent(type, in.in, 0, 1, in_span), extent(type, out.out, 0, 1, out_span))) return true;
+  // two views of one buffer whose heads lie side by side in every token
+  const int64_t s = in.in_token;
+  if (s != out.out_token || s <= 0) return false;
+  const int64_t bytes = type == SOLFP4_F32 ? 4 : 2;
+  const int64_t d = ((const char*)out.out - (const char*)in.in) / bytes;
+  const int64_t iw = (in.heads - 1) * in.in_head + dim, ow = (out.heads - 1) * out.out_head + dim;
+  const int64_t r = ((d % s) + s) % s;   // where the output's heads start in the input's token
+  return r >= iw && r + ow <= s;
+}
+
+bool rotary_in_place(const solfp4::RotaryOperand& o, int64_t tokens) {
+  return o.in == o.out && (o.in_token == o.out_token || tokens == 1) && (o.in_head == o.out_head || o.heads == 1);
+}
+
+}  // namespace
+
+extern "C" {
+
+int solfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                       const void* gain, int64_t gain_stride, int64_t groups, float eps, void* sum,
+                       int64_t sum_stride, void* out, int64_t out_stride, int64_t rows, int64_t width, void* stream) {
+  return add_rmsnorm(type, solfp4::kNormSame, x, x_stride, residual, residual_stride, gain, gain_stride, groups, eps,
+                     sum, sum_stride, out, out_stride, nullptr, nullptr, rows, width, stream);
+}
+
+int mxfp8_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                      const void* gain, int64_t gain_stride, int64_t groups, float eps, void* sum, int64_t sum_stride,
+                      uint8_t* codes, uint8_t* scales, int64_t rows, int64_t width, void* stream) {
+  return add_rmsnorm(type, solfp4::kNormMxfp8, x, x_stride, residual, residual_stride, gain, gain_stride, groups, eps,
+                     sum, sum_stride, nullptr, 0, codes, scales, rows, width, stream);
+}
+
+int mxfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                      const void* gain, int64_t gain_stride, int64_t groups, float eps, void* sum, int64_t sum_stride,
+                      uint8_t* codes, uint8_t* scales, int64_t rows, int64_t width, void* stream) {
+  return add_rmsnorm(type, solfp4::kNormMxfp4, x, x_stride, residual, residual_stride, gain, gain_stride, groups, eps,
+                     sum, sum_stride, nullptr, 0, codes, scales, rows, width, stream);
+}
+
+size_t solfp4_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t width, int64_t groups) {
+  return back_dims(rows, width, groups) ? 0 : back_workspace(rows, width, groups);
+}
+
+int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                            const void* gain, int64_t gain_stride, int64_t groups, const void* dsum,
+                            int64_t dsum_stride, float eps, void* dx, int64_t dx_stride, float* dgain,
+                            void* workspace, size_t workspace_bytes, int64_t rows, int64_t width, void* stream) {
+  if (!type_ok(type)) return SOLFP4_EINVAL;
+  int rc = back_dims(rows, width, groups);
+  if (rc) return rc;
+  if (!(eps >= 0.0f)) return SOLFP4_EINVAL;
+  if (width == 0) return SOLFP4_OK;
+  if (rows > 0) {
+    if ((rc = check_rows(type, dy, dy_stride, rows, width, false))) return rc;
+    if ((rc = check_rows(type, x, x_stride, rows, width, false))) return rc;
+    if (gain && (rc = check_rows(type, gain, gain_stride, groups, width, false))) return rc;
+    if (dsum && (rc = check_rows(type, dsum, dsum_stride, rows, width, false))) return rc;
+    if ((rc = check_rows(type, dx, dx_stride, rows, width, true))) return rc;
+    if (!same_or_apart(type, dy, dy_stride, dx, dx_stride, rows, width) ||
+        !same_or_apart(type, x, x_stride, dx, dx_stride, rows, width) ||
+        (dsum && !same_or_apart(type, dsum, dsum_stride, dx, dx_stride, rows, width)))
+      return SOLFP4_EINVAL;
+  }
+  if (dgain) {
+    if ((uintptr_t)dgain & 3u) return SOLFP4_EALIGN;
+    const size_t need = back_workspace(rows, width, groups);
+    if (need && !workspace) return SOLFP4_EWORKSPACE;
+    if (!aligned16(workspace)) return SOLFP4_EALIGN;
+    if (workspace_bytes < need) return SOLFP4_EWORKSPACE;
+  }
+  solfp4::NormBackArgs a = {};
+  a.dy = dy, a.dy_stride = dy_stride, a.x = x, a.x_stride = x_stride;
+  a.gain = gain, a.gain_stride = gain_stride, a.groups = groups;
+  a.dsum = dsum, a.dsum_stride = dsum_stride, a.eps = eps;
+  a.dx = dx, a.dx_stride = dx_stride;
+  a.partial = dgain ? static_cast<float*>(workspace) : nullptr;
+  a.rows = rows, a.width = width;
+  const hipError_t e = solfp4::launch_rmsnorm_backward(type, a, dgain, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
+int solfp4_rotary_table(const int64_t* positions, int64_t rows, const double* frequencies, int64_t pairs,
+                        const int64_t* axis_pairs, int axes, double magnitude, float* table, void* stream) {
+  int rc = check_dims(rows, pairs);
+  if (rc) return rc;
+  if (axes < 1 || (axes > 1 && (!axis_pairs || !positions))) return SOLFP4_EINVAL;
+  if (axes > solfp4::kRotaryMaxAxes || pairs >= 1 << 20 || rows * pairs > kMaxGroups * 256) return SOLFP4_ESHAPE;
+  solfp4::RotaryTableArgs a = {positions, frequencies, rows, (int)pairs, axes, {}, magnitude, table};
+  int64_t end = axis_pairs ? 0 : pairs;
+  for (int i = 0; i < axes; ++i) {
+    if (axis_pairs) {
+      if (axis_pairs[i] < 0) return SOLFP4_EINVAL;
+      if (axis_pairs[i] > pairs - end) return SOLFP4_ESHAPE;
+      end += axis_pairs[i];
+    }
+    a.axis_end[i] = (int)end;
+  }
+  if (end != pairs) return SOLFP4_ESHAPE;
+  if (rows == 0 || pairs == 0) return SOLFP4_OK;
+  if (!frequencies || !table) return SOLFP4_EINVAL;
+  if (((uintptr_t)positions & 7u) || ((uintptr_t)frequencies & 7u) || ((uintptr_t)table & 3u)) return SOLFP4_EALIGN;
+  const hipError_t e = solfp4::launch_rotary_table(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
+int solfp4_rotary(int type, int layout, int inverse, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                  void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, int64_t q_heads, const void* k,
+                  int64_t k_token_stride, int64_t k_head_stride, void* k_out, int64_t k_out_token_stride,
+                  int64_t k_out_head_stride, int64_t k_heads, const float* table, int64_t table_rows,
+                  const void* positions, int position_bytes, int64_t tokens, int64_t dim, int64_t rotated,
+                  void* stream) {
+  if (!type_ok(type) || (layout != SOLFP4_ROTARY_HALF && layout != SOLFP4_ROTARY_INTERLEAVED)) return SOLFP4_EINVAL;
+  int rc = check_dims(tokens, dim);
+  if (rc) return rc;
+  if (rotated < 0 || table_rows < 0) return SOLFP4_EINVAL;
+  if (rotated % 2 || rotated > dim || dim >= 1 << 20) return SOLFP4_ESHAPE;
+  if (position_bytes != 0 && position_bytes != 4 && position_bytes != 8) return SOLFP4_EINVAL;
+  solfp4::RotaryArgs a = {};
+  if ((rc = rotary_operand(type, &a.q, q, q_token_stride, q_head_stride, q_out, q_out_token_stride, q_out_head_stride,
+                           q_heads, tokens, dim)))
+    return rc;
+  if ((rc = rotary_operand(type, &a.k, k, k_token_stride, k_head_stride, k_out, k_out_token_stride, k_out_head_stride,
+                           k_heads, tokens, dim)))
+    return rc;
+  if (tokens == 0 || dim == 0 || q_heads + k_heads == 0) return SOLFP4_OK;
+  if ((position_bytes != 0) != (positions != nullptr)) return SOLFP4_EINVAL;
+  if (rotated > 0 && (!table || table_rows == 0)) return SOLFP4_EINVAL;
+  if ((uintptr_t)table & 3u) return SOLFP4_EALIGN;
+  if (position_bytes && ((uintptr_t)positions & (uintptr_t)(position_bytes - 1))) return SOLFP4_EALIGN;
+  if ((!rotary_in_place(a.q, tokens) && !rotary_apart(type, a.q, a.q, tokens, dim)) ||
+      (!rotary_in_place(a.k, tokens) && !rotary_apart(type, a.k, a.k, tokens, dim)) ||
+      !rotary_apart(type, a.q, a.k, tokens, dim) || !rotary_apart(type, a.k, a.q, tokens, dim))
+    return SOLFP4_EINVAL;
+  if (tokens * dim > kMaxGroups * 64) return SOLFP4_ESHAPE;
+  a.table = table, a.table_rows = table_rows > 0 ? table_rows : 1;
+  a.positions = positions, a.tokens = tokens, a.dim = (int)dim, a.rotated = (int)rotated;
+  const hipError_t e = solfp4::launch_rotary(type, layout == SOLFP4_ROTARY_INTERLEAVED, inverse != 0, position_bytes,
+                                             a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
+int nvfp4_weight_linear(const uint16_t* x, const uint8_t* w_codes, const uint8_t* w_scales,
+                        const float* w_global_scale, const uint16_t* bias, uint16_t* out, int64_t M, int64_t N,
+                        int64_t K, void* stream) {
+  const int rc = linear_checks(x, nullptr, false, w_codes, w_scales, w_global_scale, true, bias, out, M, N, K, 16);
+  if (rc) return rc;
+  return run_linear(SOLFP4_FORMAT_NVFP4, false, {x, nullptr, w_codes, w_scales, w_global_scale, bias, out, M, N, K},
+                    stream);
+}
+
+int mxfp4_weight_linear(const uint16_t* x, const uint8_t* w_codes, const uint8_t* w_scales, const uint16_t* bias,
+                        uint16_t* out, int64_t M, int64_t N, int64_t K, void* stream) {
+  const int rc = linear_checks(x, nullptr, false, w_codes, w_scales, nullptr, false, bias, out, M, N, K, 32);
+  if (rc) return rc;
+  return run_linear(SOLFP4_FORMAT_MXFP4, false, {x, nullptr, w_codes, w_scales, nullptr, bias, out, M, N, K}, stream);
+}
+
+int mxfp8_linear(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                 const uint16_t* bias, uint16_t* out, int64_t M, int64_t N, int64_t K, void* stream) {
+  const int rc = linear_checks(x_codes, x_scales, true, w_codes, w_scales, nullptr, false, bias, out, M, N, K, 32);
+  if (rc) return rc;
+  return run_linear(SOLFP4_FORMAT_MXFP4, true, {x_codes, x_scales, w_codes, w_scales, nullptr, bias, out, M, N, K},
+                    stream);
+}
+
+}  // extern "C"

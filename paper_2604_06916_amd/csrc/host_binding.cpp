@@ -275,6 +275,287 @@ PyObject* mxfp4_linear_(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- operators around the linears -----------------------------------------
+
+int type_of(const Tensor& t) {
+  switch (t.scalar_type()) {
+    case at::kBFloat16: return SOLFP4_BF16;
+    case at::kHalf: return SOLFP4_F16;
+    case at::kFloat: return SOLFP4_F32;
+    default: throw NotTaken{};
+  }
+}
+
+// A GPU tensor like `like` in type and device, of this shape, whose last
+// dimension is contiguous.
+void need_strided(const Tensor& t, const Tensor& like, at::IntArrayRef shape) {
+  need(t.is_cuda() && t.layout() == at::kStrided && t.scalar_type() == like.scalar_type() && t.sizes() == shape &&
+       t.device() == like.device() && (shape.back() <= 1 || t.stride(-1) == 1));
+}
+
+// An operand with strides that the caller may leave out.
+struct Strided {
+  Tensor t;
+  PyObject* given = nullptr;   // borrowed
+  Strided(PyObject* o, const Tensor& like, at::IntArrayRef shape) {
+    if (o == Py_None) return;
+    t = tensor(o);
+    need_strided(t, like, shape);
+    given = o;
+  }
+  int64_t stride(int64_t d) const { return t.defined() ? t.stride(d) : 0; }
+  void allocate(const Tensor& like, at::IntArrayRef shape) {
+    if (!given) t = make(shape, like.scalar_type(), like.device());
+  }
+  PyObject* object() const {
+    if (!t.defined()) Py_RETURN_NONE;
+    if (!given) return THPVariable_Wrap(t);
+    Py_INCREF(given);
+    return given;
+  }
+};
+
+double number(PyObject* o) {
+  need(PyFloat_CheckExact(o) || PyLong_CheckExact(o));
+  const double v = PyFloat_AsDouble(o);
+  need(!PyErr_Occurred());
+  return v;
+}
+
+struct Gain {
+  Tensor t;
+  int64_t groups = 1, stride = 0;
+  Gain(PyObject* o, const Tensor& x, int64_t rows, int64_t width) {
+    if (o == Py_None) return;
+    t = tensor(o);
+    need(t.layout() == at::kStrided && (t.dim() == 1 || t.dim() == 2));
+    if (t.dim() == 1) {
+      need_strided(t, x, {width});
+    } else {
+      groups = t.size(0);
+      need_strided(t, x, {groups, width});
+      stride = t.stride(0);
+    }
+    need(groups >= 1 && rows % groups == 0);
+  }
+};
+
+const Tensor& matrix_operand(PyObject* o) {
+  const Tensor& x = tensor(o);
+  need_matrix(x);
+  type_of(x);
+  need_strided(x, x, x.sizes());
+  return x;
+}
+
+// (x, residual, gain, eps, out, sum_out) -> (out, sum)
+PyObject* add_rmsnorm_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 6, [&]() -> PyObject* {
+    const Tensor& x = matrix_operand(a[0]);
+    const int64_t rows = x.size(0), width = x.size(1);
+    Strided r(a[1], x, {rows, width}), out(a[4], x, {rows, width}), sum(a[5], x, {rows, width});
+    Gain g(a[2], x, rows, width);
+    const double eps = number(a[3]);
+    need(eps >= 0);
+    need(r.given || !sum.given);
+    void* stream = stream_of(x.device());
+    out.allocate(x, {rows, width});
+    if (r.given) sum.allocate(x, {rows, width});
+    const int rc = call([&] {
+      return solfp4_add_rmsnorm(type_of(x), ptr(x), x.stride(0), ptr(r.t), r.stride(0), ptr(g.t), g.stride, g.groups,
+                                (float)eps, ptr(sum.t), sum.stride(0), ptr(out.t), out.stride(0), rows, width, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NN)", out.object(), sum.object());
+  });
+}
+
+// (x, residual, gain, eps, codes, scales, sum_out) -> (codes, scales, sum)
+template <typename F>
+PyObject* quantized_norm(PyObject* const* a, Py_ssize_t n, int pack, F f) {
+  return entry(n, 7, [&]() -> PyObject* {
+    const Tensor& x = matrix_operand(a[0]);
+    const int64_t rows = x.size(0), width = x.size(1);
+    need(width % 32 == 0);
+    const at::Device dev = x.device();
+    Strided r(a[1], x, {rows, width}), sum(a[6], x, {rows, width});
+    Gain g(a[2], x, rows, width);
+    const double eps = number(a[3]);
+    need(eps >= 0);
+    Operand codes(a[4], at::kByte, {rows, width / pack}, dev), scales(a[5], at::kByte, {rows, width / 32}, dev);
+    need(r.given || !sum.given);
+    void* stream = stream_of(dev);
+    codes.allocate(at::kByte, {rows, width / pack}, dev);
+    scales.allocate(at::kByte, {rows, width / 32}, dev);
+    if (r.given) sum.allocate(x, {rows, width});
+    const int rc = call([&] {
+      return f(type_of(x), ptr(x), x.stride(0), ptr(r.t), r.stride(0), ptr(g.t), g.stride, g.groups, (float)eps,
+               ptr(sum.t), sum.stride(0), u8(codes.t), u8(scales.t), rows, width, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NNN)", codes.object(), scales.object(), sum.object());
+  });
+}
+
+PyObject* mxfp8_add_rmsnorm_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return quantized_norm(a, n, 1, mxfp8_add_rmsnorm);
+}
+PyObject* mxfp4_add_rmsnorm_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return quantized_norm(a, n, 2, mxfp4_add_rmsnorm);
+}
+
+// (dy, x, gain, dsum, eps, dx, dgain, workspace) -> (dx, dgain)
+PyObject* rmsnorm_backward_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 8, [&]() -> PyObject* {
+    const Tensor& x = matrix_operand(a[1]);
+    const int64_t rows = x.size(0), width = x.size(1);
+    const Tensor& dy = tensor(a[0]);
+    need_strided(dy, x, {rows, width});
+    Gain g(a[2], x, rows, width);
+    Strided dsum(a[3], x, {rows, width}), dx(a[5], x, {rows, width});
+    const double eps = number(a[4]);
+    need(eps >= 0);
+    const at::Device dev = x.device();
+    const at::IntArrayRef shape = g.t.defined() ? g.t.sizes() : at::IntArrayRef();
+    need(g.t.defined() || a[6] == Py_None);
+    Operand dgain(a[6], at::kFloat, shape, dev);
+    const size_t bytes = g.t.defined() ? solfp4_rmsnorm_backward_workspace_bytes(rows, width, g.groups) : 0;
+    Tensor ws = g.t.defined() ? workspace_arg(a[7], bytes, dev) : Tensor();
+    void* stream = stream_of(dev);
+    dx.allocate(x, {rows, width});
+    if (g.t.defined()) {
+      dgain.allocate(at::kFloat, shape, dev);
+      if (!ws.defined()) ws = make({(int64_t)std::max<size_t>(bytes, 256)}, at::kByte, dev);
+    }
+    const int rc = call([&] {
+      return solfp4_rmsnorm_backward(type_of(x), ptr(dy), dy.stride(0), ptr(x), x.stride(0), ptr(g.t), g.stride,
+                                     g.groups, ptr(dsum.t), dsum.stride(0), (float)eps, ptr(dx.t), dx.stride(0),
+                                     f32(dgain.t), ptr(ws), ws.defined() ? (size_t)ws.numel() : 0, rows, width, stream);
+    });
+    if (rc) return failed(rc);
+    if (g.t.defined()) return Py_BuildValue("(NN)", dx.object(), dgain.object());
+    return Py_BuildValue("(NO)", dx.object(), Py_None);
+  });
+}
+
+// (q, k, table, positions, layout, inverse, q_out, k_out) -> (q, k)
+PyObject* rotary_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 8, [&]() -> PyObject* {
+    const Tensor& q = tensor(a[0]);
+    need(q.layout() == at::kStrided && q.dim() == 3);
+    type_of(q);
+    need_strided(q, q, q.sizes());
+    const int64_t tokens = q.size(0), heads = q.size(1), dim = q.size(2);
+    const at::Device dev = q.device();
+    Tensor k;
+    int64_t k_heads = 0;
+    if (a[1] != Py_None) {
+      k = tensor(a[1]);
+      need(k.layout() == at::kStrided && k.dim() == 3);
+      k_heads = k.size(1);
+      need_strided(k, q, {tokens, k_heads, dim});
+    }
+    const Tensor& table = tensor(a[2]);
+    need_matrix(table);
+    const int64_t table_rows = table.size(0), rotated = table.size(1);
+    need_tensor(table, at::kFloat, {table_rows, rotated}, &dev);
+    need(rotated % 2 == 0 && rotated <= dim && (table_rows > 0 || tokens == 0));
+    Tensor at_;
+    int position_bytes = 0;
+    if (a[3] != Py_None) {
+      at_ = tensor(a[3]);
+      need(at_.scalar_type() == at::kInt || at_.scalar_type() == at::kLong);
+      need_tensor(at_, at_.scalar_type(), {tokens}, &dev);
+      position_bytes = at_.scalar_type() == at::kInt ? 4 : 8;
+    }
+    need(PyLong_CheckExact(a[4]) && (PyBool_Check(a[5]) || PyLong_CheckExact(a[5])));
+    const long layout = PyLong_AsLong(a[4]);
+    need(layout == SOLFP4_ROTARY_HALF || layout == SOLFP4_ROTARY_INTERLEAVED);
+    const int inverse = PyObject_IsTrue(a[5]);
+    need(k.defined() || a[7] == Py_None);
+    Strided q_out(a[6], q, {tokens, heads, dim}), k_out(a[7], q, {tokens, k_heads, dim});
+    void* stream = stream_of(dev);
+    q_out.allocate(q, {tokens, heads, dim});
+    if (k.defined()) k_out.allocate(q, {tokens, k_heads, dim});
+    const int rc = call([&] {
+      return solfp4_rotary(type_of(q), (int)layout, inverse, ptr(q), q.stride(0), q.stride(1), ptr(q_out.t),
+                           q_out.stride(0), q_out.stride(1), heads, ptr(k), k.defined() ? k.stride(0) : 0,
+                           k.defined() ? k.stride(1) : 0, ptr(k_out.t), k_out.stride(0), k_out.stride(1), k_heads,
+                           f32(table), table_rows, ptr(at_), position_bytes, tokens, dim, rotated, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NN)", q_out.object(), k_out.object());
+  });
+}
+
+// (x, w_codes, w_scales, w_gs, bias, out) -> out
+PyObject* nvfp4_weight_linear_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 6, [&]() -> PyObject* {
+    const Tensor &x = tensor(a[0]), &wc = tensor(a[1]), &ws = tensor(a[2]), &wg = tensor(a[3]);
+    need_matrix(x);
+    need_matrix(wc);
+    const int64_t M = x.size(0), K = x.size(1), N = wc.size(0);
+    need(K % 16 == 0);
+    need_tensor(x, at::kBFloat16, {M, K}, nullptr);
+    const at::Device dev = x.device();
+    need_tensor(wc, at::kByte, {N, K / 2}, &dev);
+    need_tensor(ws, at::kByte, {N, K / 16}, &dev);
+    need_tensor(wg, at::kFloat, {1}, &dev);
+    Operand bias(a[4], at::kBFloat16, {N}, dev), out(a[5], at::kBFloat16, {M, N}, dev);
+    void* stream = stream_of(dev);
+    out.allocate(at::kBFloat16, {M, N}, dev);
+    const int rc = call([&] {
+      return nvfp4_weight_linear(u16(x), u8(wc), u8(ws), f32(wg), u16(bias.t), u16(out.t), M, N, K, stream);
+    });
+    return rc ? failed(rc) : out.object();
+  });
+}
+
+// (x, w_codes, w_scales, bias, out) -> out
+PyObject* mxfp4_weight_linear_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 5, [&]() -> PyObject* {
+    const Tensor &x = tensor(a[0]), &wc = tensor(a[1]), &ws = tensor(a[2]);
+    need_matrix(x);
+    need_matrix(wc);
+    const int64_t M = x.size(0), K = x.size(1), N = wc.size(0);
+    need(K % 32 == 0);
+    need_tensor(x, at::kBFloat16, {M, K}, nullptr);
+    const at::Device dev = x.device();
+    need_tensor(wc, at::kByte, {N, K / 2}, &dev);
+    need_tensor(ws, at::kByte, {N, K / 32}, &dev);
+    Operand bias(a[3], at::kBFloat16, {N}, dev), out(a[4], at::kBFloat16, {M, N}, dev);
+    void* stream = stream_of(dev);
+    out.allocate(at::kBFloat16, {M, N}, dev);
+    const int rc = call([&] {
+      return mxfp4_weight_linear(u16(x), u8(wc), u8(ws), u16(bias.t), u16(out.t), M, N, K, stream);
+    });
+    return rc ? failed(rc) : out.object();
+  });
+}
+
+// (x_codes, x_scales, w_codes, w_scales, bias, out) -> out
+PyObject* mxfp8_linear_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 6, [&]() -> PyObject* {
+    const Tensor &xc = tensor(a[0]), &xs = tensor(a[1]), &wc = tensor(a[2]), &ws = tensor(a[3]);
+    need_matrix(xc);
+    need_matrix(wc);
+    const int64_t M = xc.size(0), K = xc.size(1), N = wc.size(0);
+    need(K % 32 == 0);
+    need_tensor(xc, at::kByte, {M, K}, nullptr);
+    const at::Device dev = xc.device();
+    need_tensor(xs, at::kByte, {M, K / 32}, &dev);
+    need_tensor(wc, at::kByte, {N, K / 2}, &dev);
+    need_tensor(ws, at::kByte, {N, K / 32}, &dev);
+    Operand bias(a[4], at::kBFloat16, {N}, dev), out(a[5], at::kBFloat16, {M, N}, dev);
+    void* stream = stream_of(dev);
+    out.allocate(at::kBFloat16, {M, N}, dev);
+    const int rc = call([&] {
+      return mxfp8_linear(u8(xc), u8(xs), u8(wc), u8(ws), u16(bias.t), u16(out.t), M, N, K, stream);
+    });
+    return rc ? failed(rc) : out.object();
+  });
+}
+
 PyMethodDef methods[] = {
     {"nvfp4_quantize", (PyCFunction)(void*)nvfp4_quantize_, METH_FASTCALL, nullptr},
     {"mxfp4_quantize", (PyCFunction)(void*)mxfp4_quantize_, METH_FASTCALL, nullptr},
@@ -282,6 +563,14 @@ PyMethodDef methods[] = {
     {"mxfp4_gemm", (PyCFunction)(void*)mxfp4_gemm_, METH_FASTCALL, nullptr},
     {"nvfp4_linear", (PyCFunction)(void*)nvfp4_linear_, METH_FASTCALL, nullptr},
     {"mxfp4_linear", (PyCFunction)(void*)mxfp4_linear_, METH_FASTCALL, nullptr},
+    {"add_rmsnorm", (PyCFunction)(void*)add_rmsnorm_, METH_FASTCALL, nullptr},
+    {"mxfp8_add_rmsnorm", (PyCFunction)(void*)mxfp8_add_rmsnorm_, METH_FASTCALL, nullptr},
+    {"mxfp4_add_rmsnorm", (PyCFunction)(void*)mxfp4_add_rmsnorm_, METH_FASTCALL, nullptr},
+    {"rmsnorm_backward", (PyCFunction)(void*)rmsnorm_backward_, METH_FASTCALL, nullptr},
+    {"rotary", (PyCFunction)(void*)rotary_, METH_FASTCALL, nullptr},
+    {"nvfp4_weight_linear", (PyCFunction)(void*)nvfp4_weight_linear_, METH_FASTCALL, nullptr},
+    {"mxfp4_weight_linear", (PyCFunction)(void*)mxfp4_weight_linear_, METH_FASTCALL, nullptr},
+    {"mxfp8_linear", (PyCFunction)(void*)mxfp8_linear_, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "Native checks, allocation and calls of the binding.",

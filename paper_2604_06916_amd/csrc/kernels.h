@@ -197,4 +197,96 @@ hipError_t launch_mx_gemm_wavek(const uint8_t* a_codes, const uint8_t* a_scales,
                                 const uint16_t* bias, uint16_t* out, int64_t M, int64_t N,
                                 int64_t K, hipStream_t stream);
 
+// ---- norm (norm.hip) ------------------------------------------------------
+constexpr int kNormMaxRuns = 6;    // runs of 8 elements a lane holds of a row
+constexpr int kNormMaxWaves = 8;   // waves of a row
+constexpr int64_t kNormMaxWidth = (int64_t)kNormMaxRuns * kNormMaxWaves * 64 * 8;
+// what the norm writes: the rows' type, MXFP8 or MXFP4
+constexpr int kNormSame = 0, kNormMxfp8 = 1, kNormMxfp4 = 2;
+
+// Strides in elements; gain row of a row: row / group_rows.
+struct NormArgs {
+  const void* x;
+  int64_t x_stride;
+  const void* residual;   // NULL: none (then no sum either)
+  int64_t residual_stride;
+  const void* gain;       // NULL: 1
+  int64_t gain_stride, group_rows;
+  float eps;
+  void* sum;
+  int64_t sum_stride;
+  void* out;              // kNormSame
+  int64_t out_stride;
+  uint8_t *codes, *scales;   // kNormMxfp8, kNormMxfp4: contiguous
+  int64_t rows, width;
+};
+hipError_t launch_add_rmsnorm(int type, int out, const NormArgs& a, hipStream_t stream);
+
+struct NormBackArgs {
+  const void* dy;
+  int64_t dy_stride;
+  const void* x;
+  int64_t x_stride;
+  const void* gain;
+  int64_t gain_stride, groups;
+  const void* dsum;   // NULL: none
+  int64_t dsum_stride;
+  float eps;
+  void* dx;
+  int64_t dx_stride;
+  float* partial;     // [groups * parts][width], NULL: no gain gradient
+  int64_t rows, width;
+  int64_t group_rows, part_rows;   // set by the launch
+  int parts;
+};
+// Workgroups that each group's rows are dealt to (host only).
+int64_t rmsnorm_backward_parts(int64_t rows, int64_t groups);
+hipError_t launch_rmsnorm_backward(int type, NormBackArgs a, float* dgain, hipStream_t stream);
+
+// ---- rotary positions (rotary.hip) ----------------------------------------
+struct RotaryOperand {
+  const void* in;
+  int64_t in_token, in_head;   // strides in elements
+  void* out;
+  int64_t out_token, out_head;
+  int heads;
+};
+struct RotaryArgs {
+  RotaryOperand q, k;          // k.heads may be 0
+  const float* table;          // [table_rows][rotated]: cos of every pair, then sin
+  int64_t table_rows;
+  const void* positions;       // NULL: token % table_rows
+  int64_t tokens;
+  int dim, rotated;
+};
+hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,
+                         hipStream_t stream);
+
+constexpr int kRotaryMaxAxes = 4;
+struct RotaryTableArgs {
+  const int64_t* positions;    // [rows][axes], NULL: the row's index on one axis
+  const double* frequencies;   // [pairs]
+  int64_t rows;
+  int pairs, axes;
+  int axis_end[kRotaryMaxAxes];   // pairs before axis_end[a] and not before axis_end[a - 1] turn with axis a
+  double magnitude;
+  float* table;
+};
+hipError_t launch_rotary_table(const RotaryTableArgs& a, hipStream_t stream);
+
+// ---- few tokens with 4-bit weights (weight_linear.hip) --------------------
+struct WeightLinearArgs {
+  const void* x;               // [M][K] BF16, or MXFP8 codes
+  const uint8_t* x_scales;     // MXFP8: [M][K/32]
+  const uint8_t* w_codes;      // [N][K/2]
+  const uint8_t* w_scales;     // [N][K/16] E4M3 or [N][K/32] E8M0
+  const float* w_global;       // NVFP4's tensor scale, else NULL
+  const uint16_t* bias;        // [N] or NULL
+  uint16_t* out;               // [M][N]
+  int64_t M, N, K;
+};
+// Workgroups of the launch (host only).
+int64_t weight_linear_groups(int64_t M, int64_t N);
+hipError_t launch_weight_linear(int w_format, bool x_mxfp8, const WeightLinearArgs& a, hipStream_t stream);
+
 }  // namespace solfp4
