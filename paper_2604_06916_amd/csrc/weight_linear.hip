@@ -21,7 +21,7 @@
 // any order of FP32 sums can be, at K = 160.
 //
 // Tokens are the columns of the matrix instruction, so up to 16 cost what
-// one does; token rows past M repeat the last one and are not stored.
+// one does; columns past M hold anything and are not stored.
 #include "elements.h"
 #include "kernels.h"
 
@@ -66,40 +66,129 @@ __device__ __forceinline__ bf16x8_t weights8(uint32_t c, float s) {
   return __builtin_bit_cast(bf16x8_t, r);
 }
 
-// A lane's operands of one step
-template <bool kX8, int MT, int NT>
-struct Step {
-  u32x4_t w[NT];
-  uint32_t ws[NT];                 // scale bytes of the lane's 32 weights
-  u32x4_t x[MT][kX8 ? 2 : 4];
-  uint32_t xs[MT];                 // kX8
-};
-
-template <int kFormat, bool kX8, int MT, int NT, int W, int U>
+// A workgroup's waves work alone until the end: each moves its steps from
+// memory to a buffer of its own in LDS and reads the matrix instructions'
+// operands from there.  Loads straight into operand order put every lane of
+// a load on another row, one cache line a lane, and the address path (one
+// line a cycle) took longer than the memory: 4 x 18432 x 3072 19 us that
+// way.  Here 4 (weights), 16 (BF16) or 8 (MXFP8) neighbouring lanes read one
+// row's 64, 256 or 128 bytes of a step.
+//
+// U steps are in flight in registers; the LDS buffer holds one.  Pieces of
+// 16 bytes are stored at their number XOR the row's, so that 16 lanes that
+// read one piece of 16 rows reach all banks.
+template <int kFormat, bool kX8, int MT, int NT, int XR, int W, int U>
 __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearArgs a, int tiles_m) {
-  __shared__ floatx4_t part[W][NT * MT][kWave];
+  constexpr bool kNv = kFormat == SOLFP4_FORMAT_NVFP4;
+  constexpr int kScaleStep = kNv ? 8 : 4;              // scale bytes of a row's step
+  constexpr int kScaleRow = 4 * kScaleStep;            // of four steps: one batch
+  constexpr int kStage = (NT + XR) * 1024, kPart = NT * MT * 1024, kScales = NT * 16 * kScaleRow;
+  constexpr int kBuf = (kStage + kScales > kPart ? kStage + kScales : kPart);
+  __shared__ __attribute__((aligned(16))) uint8_t lds[W][kBuf];
+
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int r = lane & 15, g = lane >> 4;
   const int64_t n0 = (int64_t)(blockIdx.x / tiles_m) * (16 * NT);
   const int64_t m0 = (int64_t)(blockIdx.x % tiles_m) * (16 * MT);
-  constexpr int kBlocks = kFormat == SOLFP4_FORMAT_NVFP4 ? 2 : 1;   // scale bytes of 32 weights
   const int K = (int)a.K;
   const int steps = (K + kWLStep - 1) / kWLStep;
   const int first = steps * wave / W, last = steps * (wave + 1) / W;
+  uint8_t* const lw = lds[wave];
+  uint8_t* const lx = lw + NT * 1024;
+  uint8_t* const ls = lw + kStage;
 
-  const uint8_t *wc[NT], *ws[NT], *x[MT], *xs[MT];
+  // weights: lane l moves piece l % 4 (32 weights) of row l / 4
+  const int w_row = K / 2;
+  const __amdgpu_buffer_rsrc_t rw = uniform_rsrc(a.w_codes + n0 * w_row, min<int64_t>(a.N - n0, 16 * NT) * w_row);
+  const int wr = lane >> 2, wp = lane & 3;
+  const uint32_t w_off = (uint32_t)(wr * w_row + 16 * wp);
+  uint8_t* const w_to = lw + wr * 64 + 16 * (wp ^ (wr >> 2));
+  const uint8_t* const w_from = lw + r * 64 + 16 * (g ^ (r >> 2));
+  // activations: lane l moves piece l % P of row l / P (+ 64 / P a load)
+  constexpr int P = kX8 ? 8 : 16;
+  constexpr int kTokens = XR * 64 / P;   // rows in LDS: fewer than 16 MT where M has no more; others repeat them
+  const int x_row = K * (kX8 ? 1 : 2);
+  const __amdgpu_buffer_rsrc_t rx =
+      uniform_rsrc(static_cast<const uint8_t*>(a.x) + m0 * x_row, min<int64_t>(a.M - m0, 16 * MT) * x_row);
+  const int xr = lane / P, xp = lane % P;
+  const uint32_t x_off = (uint32_t)(xr * x_row + 16 * xp);
+  // MXFP8's scales: lane (r, g) holds block g of token r
+  const uint8_t* xs[MT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int64_t n = min(n0 + 16 * t + r, a.N - 1);
-    wc[t] = a.w_codes + n * (K / 2) + 16 * g;
-    ws[t] = a.w_scales + n * (K / (32 / kBlocks)) + kBlocks * g;
-  }
+  for (int t = 0; t < MT; ++t) xs[t] = kX8 ? a.x_scales + min(m0 + 16 * t + r, a.M - 1) * (K / 32) + g : nullptr;
+  // weight scales: a batch's kScaleRow bytes of a row in pieces of 16
+  constexpr int kScalePieces = kScaleRow / 16;
+  constexpr int kScaleLoads = (NT * 16 * kScalePieces + kWave - 1) / kWave;
+  const int scale_row = K / (kNv ? 16 : 32);
+  const uint8_t* sp[kScaleLoads];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int64_t m = min(m0 + 16 * t + r, a.M - 1);
-    x[t] = static_cast<const uint8_t*>(a.x) + m * K * (kX8 ? 1 : 2) + (kX8 ? 32 : 64) * g;
-    xs[t] = kX8 ? a.x_scales + m * (K / 32) + g : nullptr;
+  for (int i = 0; i < kScaleLoads; ++i) {
+    const int p = i * kWave + lane;
+    sp[i] = a.w_scales + min(n0 + p / kScalePieces, a.N - 1) * scale_row + 16 * (p % kScalePieces);
   }
+
+  struct Regs {
+    u32x4_t w[NT], x[XR];
+    uint32_t xs[MT];
+  };
+  // Step s into registers.  Where K ends inside it, pieces past the end are
+  // zeros: the activations' too, since zero times what lies there could be NaN.
+  auto load = [&](Regs& o, int s) {
+    const int left = K - s * kWLStep;
+    const bool whole = left >= kWLStep;
+    constexpr uint32_t kOutside = 0x80000000u;   // beyond any operand's range (below 2^31): reads zero
+    const uint32_t wv = whole || 32 * wp < left ? w_off : kOutside;
+    const uint32_t xv = whole || (kX8 ? 16 : 8) * xp < left ? x_off : kOutside;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      o.w[t] = __builtin_amdgcn_raw_buffer_load_b128(rw, wv + (uint32_t)(s * (kWLStep / 2) + t * 16 * w_row), 0, 0);
+#pragma unroll
+    for (int j = 0; j < XR; ++j)
+      o.x[j] = __builtin_amdgcn_raw_buffer_load_b128(
+          rx, xv + (uint32_t)(s * (kWLStep * (kX8 ? 1 : 2)) + j * (64 / P) * x_row), 0, 0);
+    if constexpr (kX8) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t) o.xs[t] = whole || 32 * g < left ? xs[t][s * (kWLStep / 32)] : 0u;
+    }
+  };
+  // half of the last 32 weights can be the next row's (K % 32 == 16)
+  auto trim = [&](Regs& o, int s) {
+    if constexpr (kNv) {
+      if (K - s * kWLStep - 32 * wp == 16) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o.w[t][2] = o.w[t][3] = 0;
+      }
+    }
+  };
+  // scales of the four steps from s on; bytes past the row's end are zeros
+  auto load_scales = [&](u32x4_t (&o)[kScaleLoads], int s) {
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+      const int p = i * kWave + lane;
+      const uint8_t* q = sp[i] + s * kScaleStep;
+      const int n = scale_row - s * kScaleStep - 16 * (p % kScalePieces);
+      o[i] = u32x4_t{0, 0, 0, 0};
+      if (p >= NT * 16 * kScalePieces) continue;
+      typedef u32x4_t u32x4_at1 __attribute__((aligned(1)));
+      typedef uint32_t u32_at1 __attribute__((aligned(1)));
+      if (n >= 16) {
+        o[i] = *reinterpret_cast<const u32x4_at1*>(q);
+      } else {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          uint32_t v = 0;
+          if (n >= 4 * d + 4) {
+            v = *reinterpret_cast<const u32_at1*>(q + 4 * d);
+          } else {
+#pragma unroll
+            for (int b = 0; b < 3; ++b)
+              if (4 * d + b < n) v |= (uint32_t)q[4 * d + b] << (8 * b);
+          }
+          o[i][d] = v;
+        }
+      }
+    }
+  };
 
   floatx4_t acc[NT][MT];
 #pragma unroll
@@ -107,126 +196,90 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
 #pragma unroll
     for (int u = 0; u < MT; ++u) acc[t][u] = floatx4_t{0, 0, 0, 0};
 
-  // loads of step s; a step that K ends in loads only what is there and
-  // leaves zeros (weights and activations both: zero times what lies
-  // past the end could be a NaN)
-  auto load = [&](Step<kX8, MT, NT>& o, int s) {
-    const int left = K - s * kWLStep;
-    if (left >= kWLStep) {
+  u32x4_t sreg[kScaleLoads];
+  Regs o[U];
+  if (first < last) load_scales(sreg, first);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        o.w[t] = *reinterpret_cast<const u32x4_at2*>(wc[t] + s * (kWLStep / 2));
-        const uint8_t* p = ws[t] + s * (kWLStep / 32 * kBlocks);
-        if constexpr (kBlocks == 2) {
-          typedef uint16_t u16_at1 __attribute__((aligned(1)));
-          o.ws[t] = *reinterpret_cast<const u16_at1*>(p);
-        } else {
-          o.ws[t] = *p;
-        }
+  for (int u = 0; u < U; ++u)
+    if (first + u < last) load(o[u], first + u);
+
+  for (int s = first; s < last; s += 4) {
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i)
+      if (i * kWave + lane < NT * 16 * kScalePieces)
+        *reinterpret_cast<u32x4_t*>(ls + 16 * (i * kWave + lane)) = sreg[i];
+    if (s + 4 < last) load_scales(sreg, s + 4);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      if (s + v >= last) break;
+      Regs& c = o[v % U];
+      if (s + v == steps - 1) trim(c, s + v);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) *reinterpret_cast<u32x4_t*>(w_to + t * 1024) = c.w[t];
+#pragma unroll
+      for (int j = 0; j < XR; ++j) {
+        const int row = j * (64 / P) + xr;
+        *reinterpret_cast<u32x4_t*>(lx + row * (16 * P) + 16 * (xp ^ (row & (P - 1)))) = c.x[j];
       }
+      uint32_t sx[MT];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
+      for (int t = 0; t < MT; ++t) sx[t] = kX8 ? c.xs[t] : 0u;
+      if (s + v + U < last) load(c, s + v + U);
+
+      bf16x8_t x[MT][4];
+#pragma unroll
+      for (int u = 0; u < MT; ++u) {
+        const int row = (16 * u + r) & (kTokens - 1);
         if constexpr (kX8) {
-          o.x[t][0] = *reinterpret_cast<const u32x4_at2*>(x[t] + s * kWLStep);
-          o.x[t][1] = *reinterpret_cast<const u32x4_at2*>(x[t] + s * kWLStep + 16);
-          o.xs[t] = xs[t][s * (kWLStep / 32)];
+          u32x4_t h[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            h[j] = *reinterpret_cast<const u32x4_t*>(lx + row * 128 + 16 * ((2 * g + j) ^ (row & 7)));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            x[u][j] = activations8(h[j / 2][2 * (j & 1)], h[j / 2][2 * (j & 1) + 1], e8m0_float(sx[u]));
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            o.x[t][j] = *reinterpret_cast<const u32x4_at2*>(x[t] + s * (2 * kWLStep) + 16 * j);
+            x[u][j] = *reinterpret_cast<const bf16x8_t*>(lx + row * 256 + 16 * ((4 * g + j) ^ (row & 15)));
         }
       }
-      return;
-    }
-    const int mine = left - 32 * g;   // of the lane's 32 elements, those inside K: a multiple of 16
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      o.w[t] = u32x4_t{0, 0, 0, 0};
-      o.ws[t] = 0;
-      const uint8_t* p = ws[t] + s * (kWLStep / 32 * kBlocks);
-      const uint8_t* c = wc[t] + s * (kWLStep / 2);
-      if (mine >= 32) {
-        o.w[t] = *reinterpret_cast<const u32x4_at2*>(c);
-        o.ws[t] = p[0] | (kBlocks == 2 ? (uint32_t)p[kBlocks - 1] << 8 : 0u);
-      } else if (mine > 0) {
-        typedef u32x2_t u32x2_at2 __attribute__((aligned(2)));
-        const u32x2_t h = *reinterpret_cast<const u32x2_at2*>(c);
-        o.w[t][0] = h.x;
-        o.w[t][1] = h.y;
-        o.ws[t] = p[0];
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      o.xs[t] = 0;
-      if constexpr (kX8) {
-        o.x[t][0] = o.x[t][1] = u32x4_t{0, 0, 0, 0};
-        if (mine > 0) {   // whole blocks
-          o.x[t][0] = *reinterpret_cast<const u32x4_at2*>(x[t] + s * kWLStep);
-          o.x[t][1] = *reinterpret_cast<const u32x4_at2*>(x[t] + s * kWLStep + 16);
-          o.xs[t] = xs[t][s * (kWLStep / 32)];
+      for (int t = 0; t < NT; ++t) {
+        const u32x4_t w = *reinterpret_cast<const u32x4_t*>(w_from + t * 1024);
+        const uint8_t* sc = ls + (16 * t + r) * kScaleRow + v * kScaleStep;
+        float f[2];
+        if constexpr (kNv) {
+          const int two = *reinterpret_cast<const uint16_t*>(sc + 2 * g);
+          f[0] = __builtin_amdgcn_cvt_f32_fp8(two, 0);
+          f[1] = __builtin_amdgcn_cvt_f32_fp8(two, 1);
+        } else {
+          f[0] = f[1] = e8m0_float(sc[g]);
         }
-      } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          o.x[t][j] = u32x4_t{0, 0, 0, 0};
-          if (8 * j < mine) o.x[t][j] = *reinterpret_cast<const u32x4_at2*>(x[t] + s * (2 * kWLStep) + 16 * j);
+          const bf16x8_t b = weights8<kFormat>(w[j], f[j / 2]);
+#pragma unroll
+          for (int u = 0; u < MT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, x[u][j], acc[t][u], 0, 0, 0);
         }
       }
     }
-  };
-
-  auto compute = [&](const Step<kX8, MT, NT>& o) {
-    bf16x8_t x[MT][4];
-#pragma unroll
-    for (int u = 0; u < MT; ++u)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (kX8)
-          x[u][j] = activations8(o.x[u][j / 2][2 * (j & 1)], o.x[u][j / 2][2 * (j & 1) + 1], e8m0_float(o.xs[u]));
-        else
-          x[u][j] = __builtin_bit_cast(bf16x8_t, o.x[u][j]);
-      }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float s[2];
-      if constexpr (kBlocks == 2) {
-        s[0] = __builtin_amdgcn_cvt_f32_fp8((int)o.ws[t], 0);
-        s[1] = __builtin_amdgcn_cvt_f32_fp8((int)o.ws[t], 1);
-      } else {
-        s[0] = s[1] = e8m0_float(o.ws[t]);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bf16x8_t w = weights8<kFormat>(o.w[t][j], s[j / 2]);
-#pragma unroll
-        for (int u = 0; u < MT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[u][j], acc[t][u], 0, 0, 0);
-      }
-    }
-  };
-
-  for (int s = first; s < last; s += U) {
-    Step<kX8, MT, NT> o[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s + u < last) load(o[u], s + u);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s + u < last) compute(o[u]);
   }
 
+  // each wave's sums in place of its buffer (its reads are done: one wave's
+  // LDS operations keep their order)
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int u = 0; u < MT; ++u) part[wave][t * MT + u][lane] = acc[t][u];
+    for (int u = 0; u < MT; ++u) reinterpret_cast<floatx4_t*>(lw)[(t * MT + u) * kWave + lane] = acc[t][u];
   __syncthreads();
 
   // a lane of tile (t, u) holds outputs n0 + 16 t + 4 g .. + 3 of token m0 + 16 u + r
-  const float alpha = kFormat == SOLFP4_FORMAT_NVFP4 ? a.w_global[0] : 1.0f;
+  const float alpha = kNv ? a.w_global[0] : 1.0f;
   for (int q = wave; q < NT * MT; q += W) {
-    floatx4_t v = part[0][q][lane];
+    floatx4_t v = reinterpret_cast<const floatx4_t*>(lds[0])[q * kWave + lane];
 #pragma unroll
-    for (int w = 1; w < W; ++w) v += part[w][q][lane];
+    for (int w = 1; w < W; ++w) v += reinterpret_cast<const floatx4_t*>(lds[w])[q * kWave + lane];
     const int64_t n = n0 + 16 * (q / MT) + 4 * g, m = m0 + 16 * (q % MT) + r;
     if (m >= a.M || n >= a.N) continue;
     float y[4];
@@ -261,27 +314,32 @@ int64_t weight_linear_groups(int64_t M, int64_t N) {
   return ((N + 16 * nt - 1) / (16 * nt)) * ((M + 16 * mt - 1) / (16 * mt));
 }
 
-template <int kFormat, bool kX8, int MT, int NT>
+template <int kFormat, bool kX8, int MT, int NT, int XR, int W, int U>
 static hipError_t launch_tile(const WeightLinearArgs& a, hipStream_t stream) {
-  constexpr int W = 8, U = MT == 1 ? 4 : 2;
   const int tiles_m = (int)((a.M + 16 * MT - 1) / (16 * MT));
-  return launch_kernel(weight_linear_kernel<kFormat, kX8, MT, NT, W, U>, dim3((unsigned)weight_linear_groups(a.M, a.N)),
-                       dim3(W * kWave), stream, a, tiles_m);
+  return launch_kernel(weight_linear_kernel<kFormat, kX8, MT, NT, XR, W, U>,
+                       dim3((unsigned)weight_linear_groups(a.M, a.N)), dim3(W * kWave), stream, a, tiles_m);
+}
+
+template <int kFormat, bool kX8, int NT>
+static hipError_t launch_format(const WeightLinearArgs& a, hipStream_t stream) {
+  constexpr int kFull = kX8 ? 2 : 4;   // loads of 16 tokens' step
+  if (a.M <= 16 / kFull) return launch_tile<kFormat, kX8, 1, NT, 1, 8, 4>(a, stream);
+  if (a.M <= 16) return launch_tile<kFormat, kX8, 1, NT, kFull, 8, 2>(a, stream);
+  if (a.M <= 32) return launch_tile<kFormat, kX8, 2, NT, 2 * kFull, 8, 2>(a, stream);
+  return launch_tile<kFormat, kX8, 4, NT, 4 * kFull, kX8 ? 8 : 4, 1>(a, stream);
 }
 
 template <int kFormat, bool kX8>
-static hipError_t launch_format(const WeightLinearArgs& a, hipStream_t stream) {
-  const int mt = tokens_tile(a.M), nt = column_tiles(a.M, a.N);
-  if (mt == 1) return nt == 1 ? launch_tile<kFormat, kX8, 1, 1>(a, stream) : launch_tile<kFormat, kX8, 1, 2>(a, stream);
-  if (mt == 2) return nt == 1 ? launch_tile<kFormat, kX8, 2, 1>(a, stream) : launch_tile<kFormat, kX8, 2, 2>(a, stream);
-  return nt == 1 ? launch_tile<kFormat, kX8, 4, 1>(a, stream) : launch_tile<kFormat, kX8, 4, 2>(a, stream);
+static hipError_t launch_columns(const WeightLinearArgs& a, hipStream_t stream) {
+  return column_tiles(a.M, a.N) == 1 ? launch_format<kFormat, kX8, 1>(a, stream) : launch_format<kFormat, kX8, 2>(a, stream);
 }
 
 hipError_t launch_weight_linear(int w_format, bool x_mxfp8, const WeightLinearArgs& a, hipStream_t stream) {
   if (a.M == 0 || a.N == 0) return hipSuccess;
-  if (x_mxfp8) return launch_format<SOLFP4_FORMAT_MXFP4, true>(a, stream);
-  if (w_format == SOLFP4_FORMAT_NVFP4) return launch_format<SOLFP4_FORMAT_NVFP4, false>(a, stream);
-  return launch_format<SOLFP4_FORMAT_MXFP4, false>(a, stream);
+  if (x_mxfp8) return launch_columns<SOLFP4_FORMAT_MXFP4, true>(a, stream);
+  if (w_format == SOLFP4_FORMAT_NVFP4) return launch_columns<SOLFP4_FORMAT_NVFP4, false>(a, stream);
+  return launch_columns<SOLFP4_FORMAT_MXFP4, false>(a, stream);
 }
 
 }  // namespace solfp4
