@@ -20,5 +20,7 @@ __all__ = list(_NAMES)
 def __getattr__(name):
     if name in _NAMES:
         from . import _binding
-        return getattr(_binding, name)
+        # found once: a call through the package costs no lookup here afterwards
+        value = globals()[name] = getattr(_binding, name)
+        return value
     raise AttributeError(name)
