@@ -528,10 +528,9 @@ SOLFP4_API int solfp4_rotary(int type, int layout, int inverse,
  *                        mxfp8_add_rmsnorm writes them; MXFP4 weight
  *
  * Products are exact and sums FP32 in a fixed order; decoded weights,
- * products or sums outside the FP32 range are unspecified.  Time is that of
- * reading the weight once for up to 64 tokens, and again for every further
- * 64 tokens: from a few hundred tokens on, nvfp4_linear and mxfp4_linear are
- * the faster calls.  M, N or K equal to 0 are valid (K == 0 writes the bias,
+ * products or sums outside the FP32 range are unspecified.  Every 32 tokens
+ * read the weight once (from L2 after the first): from a few hundred tokens
+ * on, nvfp4_linear and mxfp4_linear are the faster calls.  M, N or K equal to 0 are valid (K == 0 writes the bias,
  * or zeros).  K must be below 2^24 and N below 2^22.  Packed operands, x, bias
  * and out are contiguous and 16-byte aligned; no workspace.
  */

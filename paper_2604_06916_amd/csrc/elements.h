@@ -1,6 +1,8 @@
 // Runs of 8 elements of the operators' types (BF16, FP16, FP32) as FP32 values.
 #pragma once
 
+#include <type_traits>
+
 #include "device_common.h"
 #include "solfp4.h"
 
@@ -33,11 +35,22 @@ __device__ __forceinline__ Run<kType> zero_run() {
   return r;
 }
 
+// Row `row` of an operand (both uniform over the wave, so the address stays
+// scalar and a lane adds its 32-bit offset).
+template <int kType>
+__device__ __forceinline__ const uint8_t* row_of(const void* base, int64_t row, int64_t stride) {
+  return static_cast<const uint8_t*>(base) + row * stride * kElemBytes<kType>;
+}
+template <int kType>
+__device__ __forceinline__ uint8_t* row_of(void* base, int64_t row, int64_t stride) {
+  return static_cast<uint8_t*>(base) + row * stride * kElemBytes<kType>;
+}
+
 // The run at element `at` of `base`, of which the first n elements exist
 // (n >= 8: one vector load per piece; else element loads, zeros after them).
 template <int kType>
-__device__ __forceinline__ Run<kType> load_run(const void* base, int64_t at, int64_t n) {
-  const uint8_t* a = static_cast<const uint8_t*>(base) + at * kElemBytes<kType>;
+__device__ __forceinline__ Run<kType> load_run(const uint8_t* base, uint32_t at, int n) {
+  const uint8_t* a = base + at * kElemBytes<kType>;
   Run<kType> r = zero_run<kType>();
   if (n >= 8) {
 #pragma unroll
@@ -51,11 +64,11 @@ __device__ __forceinline__ Run<kType> load_run(const void* base, int64_t at, int
   }
 #pragma unroll
   for (int e = 0; e < 7; ++e) {
-    if (e >= n) break;
-    if constexpr (kType == SOLFP4_F32)
-      r.p[e / 4][e % 4] = reinterpret_cast<const uint32_t*>(a)[e];
-    else
-      r.p[0][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(a)[e] << (16 * (e & 1));
+    if constexpr (kType == SOLFP4_F32) {
+      if (e < n) r.p[e / 4][e % 4] = reinterpret_cast<const uint32_t*>(a)[e];
+    } else {
+      if (e < n) r.p[0][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(a)[e] << (16 * (e & 1));
+    }
   }
   return r;
 }
@@ -94,8 +107,8 @@ __device__ __forceinline__ Run<kType> from_f32(const float (&v)[8]) {
 }
 
 template <int kType>
-__device__ __forceinline__ void store_run(void* base, int64_t at, int64_t n, const Run<kType>& r) {
-  uint8_t* a = static_cast<uint8_t*>(base) + at * kElemBytes<kType>;
+__device__ __forceinline__ void store_run(uint8_t* base, uint32_t at, int n, const Run<kType>& r) {
+  uint8_t* a = base + at * kElemBytes<kType>;
   if (n >= 8) {
 #pragma unroll
     for (int i = 0; i < kRunPieces<kType>; ++i) {
@@ -108,18 +121,60 @@ __device__ __forceinline__ void store_run(void* base, int64_t at, int64_t n, con
   }
 #pragma unroll
   for (int e = 0; e < 7; ++e) {
-    if (e >= n) break;
-    if constexpr (kType == SOLFP4_F32)
-      reinterpret_cast<uint32_t*>(a)[e] = r.p[e / 4][e % 4];
-    else
-      reinterpret_cast<uint16_t*>(a)[e] = (uint16_t)(r.p[0][e / 2] >> (16 * (e & 1)));
+    if constexpr (kType == SOLFP4_F32) {
+      if (e < n) reinterpret_cast<uint32_t*>(a)[e] = r.p[e / 4][e % 4];
+    } else {
+      if (e < n) reinterpret_cast<uint16_t*>(a)[e] = (uint16_t)(r.p[0][e / 2] >> (16 * (e & 1)));
+    }
   }
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
+// Hides that the run is as it was, so that its conversion is made again
+// where it is used again and no FP32 copy is kept in between.
+template <int kType>
+__device__ __forceinline__ void forget(Run<kType>& r) {
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
-  return v;
+  for (int i = 0; i < kRunPieces<kType>; ++i) asm volatile("" : "+v"(r.p[i]));
+}
+
+// Sums over the wave, in every lane, without LDS: neighbours, quads and half
+// rows by DPP, then rows of 16 and halves of 32 by lane swaps.
+template <int kCtrl, typename T>
+__device__ __forceinline__ T dpp_of(T v) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), kCtrl, 0xF, 0xF, false));
+  } else {
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+    return __builtin_bit_cast(T, u32x2_t{(uint32_t)__builtin_amdgcn_mov_dpp((int)w.x, kCtrl, 0xF, 0xF, false),
+                                         (uint32_t)__builtin_amdgcn_mov_dpp((int)w.y, kCtrl, 0xF, 0xF, false)});
+  }
+}
+
+template <int kLanes, typename T>
+__device__ __forceinline__ T swapped_sum(T v) {
+  auto swap = [](uint32_t w) {
+    if constexpr (kLanes == 16) return __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    else return __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  };
+  if constexpr (sizeof(T) == 4) {
+    const auto h = swap(__builtin_bit_cast(uint32_t, v));
+    return __builtin_bit_cast(T, (uint32_t)h[0]) + __builtin_bit_cast(T, (uint32_t)h[1]);
+  } else {
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+    const auto x = swap(w.x), y = swap(w.y);
+    return __builtin_bit_cast(T, u32x2_t{(uint32_t)x[0], (uint32_t)y[0]}) +
+           __builtin_bit_cast(T, u32x2_t{(uint32_t)x[1], (uint32_t)y[1]});
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v) {
+  v += dpp_of<0xB1>(v);     // quad_perm 1,0,3,2
+  v += dpp_of<0x4E>(v);     // quad_perm 2,3,0,1
+  v += dpp_of<0x141>(v);    // row_half_mirror
+  v += dpp_of<0x140>(v);    // row_mirror
+  v = swapped_sum<16>(v);
+  return swapped_sum<32>(v);
 }
 
 }  // namespace solfp4

@@ -20,21 +20,39 @@ namespace solfp4 {
 
 // max over the aligned lane quad (quad_perm DPP: lanes 1,0,3,2 then 2,3,0,1)
 __device__ __forceinline__ uint32_t quad_max_bits(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, false));
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, false));
-  return v;
+  v = max(v, dpp_of<0xB1>(v));
+  return max(v, dpp_of<0x4E>(v));
 }
 
-// The E8M0 byte of a 32-element block held by a lane quad, 8 values a lane:
-// floor(log2(amax)) - kEmax + 127, at least 0, for elements whose largest
-// exponent is kEmax.  A NaN has the largest pattern of all, so it gives the
-// largest scale and stays a NaN where the elements have one.
+// The E8M0 byte of a 32-element block held by a lane quad, 8 values y = s rho g
+// a lane: floor(log2(amax)) - kEmax + 127, at least 0, for elements whose
+// largest exponent is kEmax.  A NaN has the largest pattern of all, so it
+// gives the largest scale and stays a NaN where the elements have one.
+//
+// An FP32 amax next to a power of two may lie on the wrong side of it, which
+// would double or halve the scale: within 4 units (y is within 2) the
+// comparison is made in 64 bits.  That takes a rho of more than 32 bits, for
+// which the row's squares are summed in 64.
 template <int kEmax>
-__device__ __forceinline__ uint32_t block_scale(const float (&y)[8]) {
+__device__ __forceinline__ uint32_t block_scale(const float (&y)[8], const float (&s)[8], const float (&g)[8],
+                                                double rho) {
   uint32_t m = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(y[e]) & 0x7FFFFFFFu);
-  const uint32_t f = quad_max_bits(m) >> 23;
+  m = quad_max_bits(m);
+  uint32_t f = m >> 23;
+  if (((m + 4u) & 0x7FFFFFu) < 8u) {   // alike in the quad
+    f = (m + 4u) >> 23;
+    const double power = __uint_as_float(f << 23);
+    uint32_t reached = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float t = s[e];
+      asm volatile("" : "+v"(t));   // converted here, where it is rarely needed, and not kept in 64 bits
+      reached |= __builtin_fabs((double)t * rho * (double)g[e]) >= power;
+    }
+    if (!quad_max_bits(reached)) --f;
+  }
   return f > kEmax ? f - kEmax : 0u;
 }
 
@@ -66,101 +84,121 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float (&y)[8], float inv) {
   return c;
 }
 
-// y, the 8 values at column `col` of a row (n of them inside it), to the output.
-template <int kType, int kOut>
-__device__ __forceinline__ void emit(const NormArgs& a, int64_t row, int64_t col, int64_t n, const float (&y)[8]) {
-  if constexpr (kOut == kNormSame) {
-    store_run<kType>(a.out, row * a.out_stride + col, n, from_f32<kType>(y));
-  } else {
-    // the four lanes of a block are inside the row or outside it together
-    const uint32_t sc = block_scale<(kOut == kNormMxfp8 ? 8 : 2)>(y);
-    const float inv = inverse_scale(sc);
-    if constexpr (kOut == kNormMxfp8)
-      *reinterpret_cast<u32x2_t*>(a.codes + row * a.width + col) = e4m3_codes(y, inv);
-    else
-      *reinterpret_cast<uint32_t*>(a.codes + (row * a.width + col) / 2) = e2m1_codes(y, inv);
-    if ((threadIdx.x & 3) == 0) a.scales[(row * a.width + col) / 32] = (uint8_t)sc;
-  }
-}
-
-// The sum of v over the `wpr` waves of this wave's row; every wave of the
-// workgroup calls it.
-__device__ __forceinline__ float row_sum(float v, float* lds, int wpr) {
-  v = wave_sum(v);
-  if (wpr == 1) return v;
-  const int wave = threadIdx.x / kWave, first = wave / wpr * wpr;
+// The sums of v[0 .. n) over the `wpr` waves of this wave's row, in wave
+// order; every wave of the workgroup calls it.
+template <int n, typename T>
+__device__ __forceinline__ void row_sum(T (&v)[n], T (*lds)[n], int wave, int wpr) {
+#pragma unroll
+  for (int i = 0; i < n; ++i) v[i] = wave_sum(v[i]);
+  if (wpr == 1) return;
   __syncthreads();
-  if ((threadIdx.x & (kWave - 1)) == 0) lds[wave] = v;
+  if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+    for (int i = 0; i < n; ++i) lds[wave][i] = v[i];
   __syncthreads();
-  float t = 0.0f;
-  for (int w = 0; w < wpr; ++w) t += lds[first + w];
-  return t;
+  const int first = wave & -wpr;
+#pragma unroll
+  for (int i = 0; i < n; ++i) v[i] = lds[first][i];
+  for (int w = 1; w < wpr; ++w)
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] += lds[first + w][i];
 }
 
 template <int kType, int kOut, int kRuns>
-__global__ __launch_bounds__(512) void add_rmsnorm_kernel(NormArgs a, int wpr) {
-  __shared__ float lds[kNormMaxWaves];
-  const int waves = blockDim.x / kWave;
-  const int wave = threadIdx.x / kWave;
-  const int64_t row = (int64_t)blockIdx.x * (waves / wpr) + wave / wpr;
-  const int lane = (wave % wpr) * kWave + (threadIdx.x & (kWave - 1));
+__global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(NormArgs a, int wpr) {
+  using Sum = std::conditional_t<kOut == kNormSame, float, double>;   // block_scale
+  __shared__ Sum lds[kNormMaxWaves][1];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int slots = (blockDim.x / kWave) / wpr;   // powers of two
+  const int64_t row = (int64_t)blockIdx.x * slots + wave / wpr;
+  const int lane = (wave & (wpr - 1)) * kWave + (threadIdx.x & (kWave - 1));
   const int step = wpr * kWave * 8;
-  const bool in = row < a.rows;
-  float s[kRuns][8];
+  const int width = row < a.rows ? (int)a.width : 0;   // no elements of a row past the last
+  const int64_t at = row < a.rows ? row : 0;
+  const uint8_t* xr = row_of<kType>(a.x, at, a.x_stride);
+  const uint8_t* rr = row_of<kType>(a.residual, at, a.residual_stride);
+  const uint8_t* gr = row_of<kType>(a.gain, (uint32_t)at / (uint32_t)a.group_rows, a.gain_stride);
   Run<kType> x[kRuns], r[kRuns], g[kRuns];
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    const int64_t col = (int64_t)i * step + lane * 8, n = in ? a.width - col : 0;
+    const int col = i * step + lane * 8, n = width - col;
     x[i] = r[i] = g[i] = zero_run<kType>();
     if (n > 0) {
-      x[i] = load_run<kType>(a.x, row * a.x_stride + col, n);
-      if (a.residual) r[i] = load_run<kType>(a.residual, row * a.residual_stride + col, n);
-      if (a.gain) g[i] = load_run<kType>(a.gain, row / a.group_rows * a.gain_stride + col, n);
+      x[i] = load_run<kType>(xr, col, n);
+      if (a.residual) r[i] = load_run<kType>(rr, col, n);
+      if (a.gain) g[i] = load_run<kType>(gr, col, n);
     }
   }
-  float q = 0.0f;
+  float s[kRuns][8];
+  Sum q[1] = {0};
+  uint8_t* sr = row_of<kType>(a.sum, at, a.sum_stride);
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    const int64_t col = (int64_t)i * step + lane * 8, n = in ? a.width - col : 0;
+    const int col = i * step + lane * 8, n = width - col;
     to_f32<kType>(x[i], s[i]);
     if (a.residual) {
       float v[8];
       to_f32<kType>(r[i], v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[i][e] += v[e];
-      if (n > 0) store_run<kType>(a.sum, row * a.sum_stride + col, n, from_f32<kType>(s[i]));
+      if (n > 0) store_run<kType>(sr, col, n, from_f32<kType>(s[i]));
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q += s[i][e] * s[i][e];
+    for (int e = 0; e < 8; ++e) q[0] += (Sum)s[i][e] * (Sum)s[i][e];
   }
-  q = row_sum(q, lds, wpr);
-  const float rho = 1.0f / __builtin_sqrtf(q / (float)a.width + a.eps);
+  row_sum(q, lds, wave, wpr);
+  Sum rho;
+  if constexpr (kOut == kNormSame) {
+    rho = 1.0f / __builtin_sqrtf(q[0] / (float)a.width + a.eps);
+  } else {
+    // an FP32 root and two Newton steps: 2^-22, 2^-43, beyond 2^-50
+    const double v = q[0] / (double)a.width + (double)a.eps;
+    rho = 1.0f / __builtin_sqrtf((float)v);
+    if (rho < 0x1p126f)   // else v is 0, a subnormal FP32 or NaN: rho as it is
+#pragma unroll
+      for (int i = 0; i < 2; ++i) rho = rho * (1.5 - 0.5 * v * rho * rho);
+  }
+  const float rho32 = (float)rho;
+  uint8_t* outr = row_of<kType>(a.out, at, a.out_stride);
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    const int64_t col = (int64_t)i * step + lane * 8, n = in ? a.width - col : 0;
-    float v[8];
+    const int col = i * step + lane * 8, n = width - col;
+    float v[8], y[8];
+    forget(g[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 1.0f;
     if (a.gain) to_f32<kType>(g[i], v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      s[i][e] *= rho;
-      if (a.gain) s[i][e] *= v[e];
+    for (int e = 0; e < 8; ++e) y[e] = s[i][e] * rho32 * v[e];
+    if (n <= 0) continue;
+    if constexpr (kOut == kNormSame) {
+      store_run<kType>(outr, col, n, from_f32<kType>(y));
+    } else {
+      // the four lanes of a block are inside the row or outside it together
+      const uint32_t sc = block_scale<(kOut == kNormMxfp8 ? 8 : 2)>(y, s[i], v, rho);
+      const float inv = inverse_scale(sc);
+      if constexpr (kOut == kNormMxfp8)
+        *reinterpret_cast<u32x2_t*>(a.codes + at * a.width + col) = e4m3_codes(y, inv);
+      else
+        *reinterpret_cast<uint32_t*>(a.codes + (at * a.width + col) / 2) = e2m1_codes(y, inv);
+      if ((threadIdx.x & 3) == 0) a.scales[(at * a.width + col) / 32] = (uint8_t)sc;
     }
-    if (n > 0) emit<kType, kOut>(a, row, col, n, s[i]);
   }
 }
 
-// Waves of a row, and runs a lane, for this width.
-static void row_shape(int64_t width, int* wpr, int* runs) {
+// Waves of a row, and runs a lane, for this width: the fewest waves that
+// need at most `most` runs a lane.
+static void row_shape(int64_t width, int most, int* wpr, int* runs) {
   const int64_t all = (width + 7) / 8;
   *wpr = 1;
-  while (*wpr < kNormMaxWaves && all > (int64_t)*wpr * kWave * kNormMaxRuns) *wpr *= 2;
+  while (*wpr < kNormMaxWaves && all > (int64_t)*wpr * kWave * most) *wpr *= 2;
   *runs = (int)((all + *wpr * kWave - 1) / (*wpr * kWave));
 }
 
 template <int kType, int kOut>
 static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
   int wpr, runs;
-  row_shape(a.width, &wpr, &runs);
+  row_shape(a.width, kNormMaxRuns, &wpr, &runs);
   const int waves = wpr > 4 ? wpr : 4, slots = waves / wpr;
   const dim3 grid((unsigned)((a.rows + slots - 1) / slots)), block(waves * kWave);
   switch (runs) {
@@ -189,86 +227,106 @@ hipError_t launch_add_rmsnorm(int type, int out, const NormArgs& a, hipStream_t 
 
 // ---- backward -------------------------------------------------------------
 
-// ds of every row, and each workgroup's share of dg: a workgroup takes the
-// rows [part * part_rows, ...) of one group, its row slots one row after
-// another, and keeps dg of its columns in registers; at the end the slots'
-// sums are added in slot order and stored as one row of the workspace.
+// ds of every row, and each workgroup's share of dg: a workgroup of eight
+// waves takes the rows [part * part_rows, ...) of one group, its row slots
+// one row after another, and keeps dg of its columns in registers; at the end
+// the slots' sums are added in slot order and stored as one row of the
+// workspace.  All of a row's loads go out before the first use and stay as
+// they were read (converted again after the reduction: half the registers
+// of FP32 copies, twice the waves).
 template <int kType, int kRuns>
-__global__ __launch_bounds__(512) void rmsnorm_backward_kernel(NormBackArgs a, int wpr) {
-  __shared__ float lds[kNormMaxWaves];
-  __shared__ __attribute__((aligned(16))) float fold[512 * 8];
-  const int waves = blockDim.x / kWave, slots = waves / wpr;
-  const int slot = threadIdx.x / kWave / wpr;
-  const int lane = threadIdx.x - slot * wpr * kWave;
+__global__ __launch_bounds__(kNormMaxWaves * kWave) void rmsnorm_backward_kernel(NormBackArgs a, int wpr) {
+  __shared__ float lds[kNormMaxWaves][2];
+  __shared__ __attribute__((aligned(16))) float fold[kNormMaxWaves * kWave * 8];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int slots = kNormMaxWaves / wpr, slot = wave / wpr;
+  const int lane = (wave & (wpr - 1)) * kWave + (threadIdx.x & (kWave - 1));
   const int step = wpr * kWave * 8;
-  const int64_t group = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  const int64_t first = group * a.group_rows + part * a.part_rows;
-  const int64_t last = min(first + a.part_rows, (group + 1) * a.group_rows);
+  const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
+  const int first = part * (int)a.part_rows;   // in the group
+  const int last = first + (int)a.part_rows < (int)a.group_rows ? first + (int)a.part_rows : (int)a.group_rows;
+  const int64_t row0 = group * a.group_rows;
+  Run<kType> g[kRuns];
+  const uint8_t* gr = row_of<kType>(a.gain, group, a.gain_stride);
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
+    const int col = i * step + lane * 8, n = (int)a.width - col;
+    g[i] = zero_run<kType>();
+    if (a.gain && n > 0) g[i] = load_run<kType>(gr, col, n);
+  }
   float dg[kRuns][8] = {};
-  for (int64_t base = first; base < last; base += slots) {
-    const int64_t row = base + slot;
-    const bool in = row < last;
-    float s[kRuns][8], G[kRuns][8];
-    float q = 0.0f, b = 0.0f;
+  for (int base = first; base < last; base += slots) {
+    const bool in = base + slot < last;
+    const int64_t row = row0 + (in ? base + slot : first);
+    const int width = in ? (int)a.width : 0;
+    const uint8_t* xr = row_of<kType>(a.x, row, a.x_stride);
+    const uint8_t* dr = row_of<kType>(a.dy, row, a.dy_stride);
+    const uint8_t* er = row_of<kType>(a.dsum, row, a.dsum_stride);
+    Run<kType> x[kRuns], d[kRuns], ex[kRuns];
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const int64_t col = (int64_t)i * step + lane * 8, n = in ? a.width - col : 0;
-      Run<kType> x = zero_run<kType>(), d = x, g = x;
+      const int col = i * step + lane * 8, n = width - col;
+      x[i] = d[i] = ex[i] = zero_run<kType>();
       if (n > 0) {
-        x = load_run<kType>(a.x, row * a.x_stride + col, n);
-        d = load_run<kType>(a.dy, row * a.dy_stride + col, n);
-        if (a.gain) g = load_run<kType>(a.gain, group * a.gain_stride + col, n);
-      }
-      to_f32<kType>(x, s[i]);
-      to_f32<kType>(d, G[i]);
-      float v[8];
-      to_f32<kType>(g, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float w = a.gain ? G[i][e] * v[e] : G[i][e];
-        q += s[i][e] * s[i][e];
-        b += w * s[i][e];
+        x[i] = load_run<kType>(xr, col, n);
+        d[i] = load_run<kType>(dr, col, n);
+        if (a.dsum) ex[i] = load_run<kType>(er, col, n);
       }
     }
-    q = row_sum(q, lds, wpr);
-    b = row_sum(b, lds, wpr);
-    const float rho = 1.0f / __builtin_sqrtf(q / (float)a.width + a.eps);
-    const float k = b / (float)a.width * rho * rho;
+    float qb[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const int64_t col = (int64_t)i * step + lane * 8, n = in ? a.width - col : 0;
-      if (n <= 0) continue;
-      float v[8], out[8];
-      if (a.gain) to_f32<kType>(load_run<kType>(a.gain, group * a.gain_stride + col, n), v);
+      float s[8], D[8], v[8];
+      to_f32<kType>(x[i], s);
+      to_f32<kType>(d[i], D);
+      to_f32<kType>(g[i], v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float w = a.gain ? G[i][e] * v[e] : G[i][e];
-        dg[i][e] += G[i][e] * (s[i][e] * rho);
-        out[e] = rho * (w - s[i][e] * k);
+        qb[0] += s[e] * s[e];
+        qb[1] += (a.gain ? D[e] * v[e] : D[e]) * s[e];
       }
-      if (a.dsum) {
-        to_f32<kType>(load_run<kType>(a.dsum, row * a.dsum_stride + col, n), v);
+    }
+    row_sum(qb, lds, wave, wpr);
+    const float rho = 1.0f / __builtin_sqrtf(qb[0] / (float)a.width + a.eps);
+    const float k = qb[1] / (float)a.width * rho * rho;
+    uint8_t* outr = row_of<kType>(a.dx, row, a.dx_stride);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] += v[e];
+    for (int i = 0; i < kRuns; ++i) {
+      const int col = i * step + lane * 8, n = width - col;
+      float s[8], D[8], v[8], out[8];
+      forget(x[i]);
+      forget(d[i]);
+      forget(g[i]);
+      to_f32<kType>(x[i], s);
+      to_f32<kType>(d[i], D);
+      to_f32<kType>(g[i], v);
+      to_f32<kType>(ex[i], out);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dg[i][e] += D[e] * (s[e] * rho);
+        out[e] += rho * ((a.gain ? D[e] * v[e] : D[e]) - s[e] * k);
       }
-      store_run<kType>(a.dx, row * a.dx_stride + col, n, from_f32<kType>(out));
+      if (n > 0) store_run<kType>(outr, col, n, from_f32<kType>(out));
     }
   }
   if (!a.partial) return;
+  float* part_row = a.partial + (int64_t)blockIdx.x * a.width;
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    __syncthreads();
+    const int col = i * step + lane * 8;
+    if (slots > 1) {
+      __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) fold[threadIdx.x * 8 + e] = dg[i][e];
-    __syncthreads();
-    if (slot) continue;
-    const int64_t col = (int64_t)i * step + lane * 8;
-    if (col >= a.width) continue;
-    for (int z = 1; z < slots; ++z)
+      for (int e = 0; e < 8; ++e) fold[e * (kNormMaxWaves * kWave) + threadIdx.x] = dg[i][e];
+      __syncthreads();
+      if (slot) continue;
+      for (int z = 1; z < slots; ++z)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dg[i][e] += fold[(z * wpr * kWave + lane) * 8 + e];
+        for (int e = 0; e < 8; ++e) dg[i][e] += fold[e * (kNormMaxWaves * kWave) + z * wpr * kWave + lane];
+    }
+#pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (col + e < a.width) a.partial[(int64_t)blockIdx.x * a.width + col + e] = dg[i][e];
+      if (col + e < a.width) part_row[col + e] = dg[i][e];
   }
 }
 
@@ -283,11 +341,15 @@ __global__ __launch_bounds__(kFoldCols * kFoldSlices) void dgain_kernel(const fl
   const int c = threadIdx.x % kFoldCols, z = threadIdx.x / kFoldCols;
   const int64_t col = (int64_t)blockIdx.x * kFoldCols + c, group = blockIdx.y;
   float t = 0.0f;
-  if (col < width)
-    for (int p = z; p < parts; p += kFoldSlices) t += partial[(group * parts + p) * width + col];
+  if (col < width) {
+    const float* p = partial + group * parts * width + col;
+#pragma unroll 8
+    for (int i = z; i < parts; i += kFoldSlices) t += p[i * width];
+  }
   sums[z][c] = t;
   __syncthreads();
   if (z || col >= width) return;
+#pragma unroll
   for (int i = 1; i < kFoldSlices; ++i) t += sums[i][c];
   dgain[group * width + col] = t;
 }
@@ -309,9 +371,8 @@ int64_t rmsnorm_backward_parts(int64_t rows, int64_t groups) {
 template <int kType>
 static hipError_t launch_back(const NormBackArgs& a, int64_t groups, hipStream_t stream) {
   int wpr, runs;
-  row_shape(a.width, &wpr, &runs);
-  const int waves = wpr > 4 ? wpr : 4;
-  const dim3 grid((unsigned)(groups * a.parts)), block(waves * kWave);
+  row_shape(a.width, kType == SOLFP4_F32 ? 3 : kNormMaxRuns, &wpr, &runs);
+  const dim3 grid((unsigned)(groups * a.parts)), block(kNormMaxWaves * kWave);
   switch (runs) {
     case 1: return launch_kernel(rmsnorm_backward_kernel<kType, 1>, grid, block, stream, a, wpr);
     case 2: return launch_kernel(rmsnorm_backward_kernel<kType, 2>, grid, block, stream, a, wpr);

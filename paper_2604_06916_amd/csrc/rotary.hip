@@ -62,7 +62,7 @@ __device__ __forceinline__ u32x4_t load_piece(const uint8_t* p, int n) {
   u32x4_t r = u32x4_t{0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < VE - 1; ++e) {
-    if (e >= n) break;
+    if (e >= n) continue;
     if constexpr (kType == SOLFP4_F32)
       r[e] = reinterpret_cast<const uint32_t*>(p)[e];
     else
@@ -82,7 +82,7 @@ __device__ __forceinline__ void store_piece(uint8_t* p, int n, u32x4_t r) {
   }
 #pragma unroll
   for (int e = 0; e < VE - 1; ++e) {
-    if (e >= n) break;
+    if (e >= n) continue;
     if constexpr (kType == SOLFP4_F32)
       reinterpret_cast<uint32_t*>(p)[e] = r[e];
     else

@@ -74,10 +74,10 @@ __device__ __forceinline__ bf16x8_t weights8(uint32_t c, float s) {
 // way.  Here 4 (weights), 16 (BF16) or 8 (MXFP8) neighbouring lanes read one
 // row's 64, 256 or 128 bytes of a step.
 //
-// U steps are in flight in registers; the LDS buffer holds one.  Pieces of
+// kWhole: K % 128 == 0, no partial step.  U steps are in flight in registers; the LDS buffer holds one.  Pieces of
 // 16 bytes are stored at their number XOR the row's, so that 16 lanes that
 // read one piece of 16 rows reach all banks.
-template <int kFormat, bool kX8, int MT, int NT, int XR, int W, int U>
+template <int kFormat, bool kX8, bool kWhole, int MT, int NT, int XR, int W>
 __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearArgs a, int tiles_m) {
   constexpr bool kNv = kFormat == SOLFP4_FORMAT_NVFP4;
   constexpr int kScaleStep = kNv ? 8 : 4;              // scale bytes of a row's step
@@ -86,10 +86,15 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
   constexpr int kBuf = (kStage + kScales > kPart ? kStage + kScales : kPart);
   __shared__ __attribute__((aligned(16))) uint8_t lds[W][kBuf];
 
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);   // uniform: offsets by step stay scalar
   const int r = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t)(blockIdx.x / tiles_m) * (16 * NT);
-  const int64_t m0 = (int64_t)(blockIdx.x % tiles_m) * (16 * MT);
+  const int tile_n = tiles_m == 1 ? blockIdx.x : blockIdx.x / tiles_m;
+  const int64_t n0 = (int64_t)tile_n * (16 * NT);
+  const int64_t m0 = (int64_t)(blockIdx.x - tile_n * tiles_m) * (16 * MT);
+  // rows of this tile inside the operands
+  const int rows_n = a.N - n0 < 16 * NT ? (int)(a.N - n0) : 16 * NT;
+  const int rows_m = a.M - m0 < 16 * MT ? (int)(a.M - m0) : 16 * MT;
   const int K = (int)a.K;
   const int steps = (K + kWLStep - 1) / kWLStep;
   const int first = steps * wave / W, last = steps * (wave + 1) / W;
@@ -99,9 +104,11 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
 
   // weights: lane l moves piece l % 4 (32 weights) of row l / 4
   const int w_row = K / 2;
-  const __amdgpu_buffer_rsrc_t rw = uniform_rsrc(a.w_codes + n0 * w_row, min<int64_t>(a.N - n0, 16 * NT) * w_row);
+  const __amdgpu_buffer_rsrc_t rw = uniform_rsrc(a.w_codes + n0 * w_row, (int64_t)rows_n * w_row);
   const int wr = lane >> 2, wp = lane & 3;
-  const uint32_t w_off = (uint32_t)(wr * w_row + 16 * wp);
+  uint32_t w_off[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) w_off[t] = (uint32_t)((16 * t + wr) * w_row + 16 * wp);
   uint8_t* const w_to = lw + wr * 64 + 16 * (wp ^ (wr >> 2));
   const uint8_t* const w_from = lw + r * 64 + 16 * (g ^ (r >> 2));
   // activations: lane l moves piece l % P of row l / P (+ 64 / P a load)
@@ -109,22 +116,26 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
   constexpr int kTokens = XR * 64 / P;   // rows in LDS: fewer than 16 MT where M has no more; others repeat them
   const int x_row = K * (kX8 ? 1 : 2);
   const __amdgpu_buffer_rsrc_t rx =
-      uniform_rsrc(static_cast<const uint8_t*>(a.x) + m0 * x_row, min<int64_t>(a.M - m0, 16 * MT) * x_row);
+      uniform_rsrc(static_cast<const uint8_t*>(a.x) + m0 * x_row, (int64_t)rows_m * x_row);
   const int xr = lane / P, xp = lane % P;
-  const uint32_t x_off = (uint32_t)(xr * x_row + 16 * xp);
+  uint32_t x_off[XR];
+#pragma unroll
+  for (int j = 0; j < XR; ++j) x_off[j] = (uint32_t)((j * (64 / P) + xr) * x_row + 16 * xp);
   // MXFP8's scales: lane (r, g) holds block g of token r
   const uint8_t* xs[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) xs[t] = kX8 ? a.x_scales + min(m0 + 16 * t + r, a.M - 1) * (K / 32) + g : nullptr;
+  for (int t = 0; t < MT; ++t) xs[t] = kX8 ? a.x_scales + (m0 + (16 * t + r < rows_m ? 16 * t + r : rows_m - 1)) * (K / 32) + g : nullptr;
   // weight scales: a batch's kScaleRow bytes of a row in pieces of 16
   constexpr int kScalePieces = kScaleRow / 16;
   constexpr int kScaleLoads = (NT * 16 * kScalePieces + kWave - 1) / kWave;
   const int scale_row = K / (kNv ? 16 : 32);
-  const uint8_t* sp[kScaleLoads];
+  const __amdgpu_buffer_rsrc_t rs =
+      uniform_rsrc(a.w_scales + n0 * scale_row, (int64_t)rows_n * scale_row);
+  uint32_t s_off[kScaleLoads];
 #pragma unroll
   for (int i = 0; i < kScaleLoads; ++i) {
     const int p = i * kWave + lane;
-    sp[i] = a.w_scales + min(n0 + p / kScalePieces, a.N - 1) * scale_row + 16 * (p % kScalePieces);
+    s_off[i] = (uint32_t)(p / kScalePieces * scale_row + 16 * (p % kScalePieces));
   }
 
   struct Regs {
@@ -134,58 +145,76 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
   // Step s into registers.  Where K ends inside it, pieces past the end are
   // zeros: the activations' too, since zero times what lies there could be NaN.
   auto load = [&](Regs& o, int s) {
+    if (kWhole || K - s * kWLStep >= kWLStep) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o.w[t] = __builtin_amdgcn_raw_buffer_load_b128(rw, w_off[t], s * (kWLStep / 2), 0);
+#pragma unroll
+      for (int j = 0; j < XR; ++j)
+        o.x[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, x_off[j], s * (kWLStep * (kX8 ? 1 : 2)), 0);
+      if constexpr (kX8) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) o.xs[t] = xs[t][s * (kWLStep / 32)];
+      }
+      return;
+    }
     const int left = K - s * kWLStep;
-    const bool whole = left >= kWLStep;
     constexpr uint32_t kOutside = 0x80000000u;   // beyond any operand's range (below 2^31): reads zero
-    const uint32_t wv = whole || 32 * wp < left ? w_off : kOutside;
-    const uint32_t xv = whole || (kX8 ? 16 : 8) * xp < left ? x_off : kOutside;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
-      o.w[t] = __builtin_amdgcn_raw_buffer_load_b128(rw, wv + (uint32_t)(s * (kWLStep / 2) + t * 16 * w_row), 0, 0);
+      o.w[t] = __builtin_amdgcn_raw_buffer_load_b128(rw, 32 * wp < left ? w_off[t] + s * (kWLStep / 2) : kOutside, 0, 0);
 #pragma unroll
     for (int j = 0; j < XR; ++j)
       o.x[j] = __builtin_amdgcn_raw_buffer_load_b128(
-          rx, xv + (uint32_t)(s * (kWLStep * (kX8 ? 1 : 2)) + j * (64 / P) * x_row), 0, 0);
+          rx, (kX8 ? 16 : 8) * xp < left ? x_off[j] + s * (kWLStep * (kX8 ? 1 : 2)) : kOutside, 0, 0);
     if constexpr (kX8) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t) o.xs[t] = whole || 32 * g < left ? xs[t][s * (kWLStep / 32)] : 0u;
+      for (int t = 0; t < MT; ++t) o.xs[t] = 32 * g < left ? xs[t][s * (kWLStep / 32)] : 0u;
     }
   };
   // half of the last 32 weights can be the next row's (K % 32 == 16)
   auto trim = [&](Regs& o, int s) {
-    if constexpr (kNv) {
+    if constexpr (kNv && !kWhole) {
       if (K - s * kWLStep - 32 * wp == 16) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) o.w[t][2] = o.w[t][3] = 0;
       }
     }
   };
-  // scales of the four steps from s on; bytes past the row's end are zeros
+  // Scales of the four steps from s on; bytes past the row's end are zeros.
+  // Near it the load starts early enough to end with the row (a load's range
+  // check would drop bytes that share a word with the operand's end) and the
+  // bytes are moved down; rows under 16 bytes go byte by byte.
   auto load_scales = [&](u32x4_t (&o)[kScaleLoads], int s) {
+    const int at = s * kScaleStep;
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
       const int p = i * kWave + lane;
-      const uint8_t* q = sp[i] + s * kScaleStep;
-      const int n = scale_row - s * kScaleStep - 16 * (p % kScalePieces);
-      o[i] = u32x4_t{0, 0, 0, 0};
-      if (p >= NT * 16 * kScalePieces) continue;
-      typedef u32x4_t u32x4_at1 __attribute__((aligned(1)));
-      typedef uint32_t u32_at1 __attribute__((aligned(1)));
-      if (n >= 16) {
-        o[i] = *reinterpret_cast<const u32x4_at1*>(q);
-      } else {
+      if (kScaleLoads * kWave > NT * 16 * kScalePieces && p >= NT * 16 * kScalePieces) continue;
+      if (at + kScaleRow <= scale_row) {
+        o[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, s_off[i], at, 0);
+        continue;
+      }
+      const int n = scale_row - at - 16 * (p % kScalePieces);   // bytes from the piece to the row's end
+      if (scale_row >= 16) {
+        const int back = n >= 16 ? 0 : n > 0 ? 16 - n : 16;
+        u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(rs, n > 0 ? s_off[i] + at - back : s_off[i], 0, 0);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          uint32_t v = 0;
-          if (n >= 4 * d + 4) {
-            v = *reinterpret_cast<const u32_at1*>(q + 4 * d);
-          } else {
+        for (int d = 0; d < 4; ++d) v[d] = __builtin_amdgcn_alignbyte(d < 3 ? v[d + 1] : 0u, v[d], back & 3);
 #pragma unroll
-            for (int b = 0; b < 3; ++b)
-              if (4 * d + b < n) v |= (uint32_t)q[4 * d + b] << (8 * b);
-          }
-          o[i][d] = v;
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) v[d] = back & (4 << h) ? (d + (1 << h) < 4 ? v[d + (1 << h)] : 0u) : v[d];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[i][d] = back & 16 ? 0u : v[d];
+        continue;
+      }
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        uint32_t v = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          if (4 * d + b < n) v |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, s_off[i] + at + 4 * d + b, 0, 0) << (8 * b);
+        o[i][d] = v;
       }
     }
   };
@@ -197,11 +226,11 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
     for (int u = 0; u < MT; ++u) acc[t][u] = floatx4_t{0, 0, 0, 0};
 
   u32x4_t sreg[kScaleLoads];
-  Regs o[U];
-  if (first < last) load_scales(sreg, first);
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (first + u < last) load(o[u], first + u);
+  Regs c;
+  if (first < last) {
+    load_scales(sreg, first);
+    load(c, first);
+  }
 
   for (int s = first; s < last; s += 4) {
 #pragma unroll
@@ -212,7 +241,6 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       if (s + v >= last) break;
-      Regs& c = o[v % U];
       if (s + v == steps - 1) trim(c, s + v);
 #pragma unroll
       for (int t = 0; t < NT; ++t) *reinterpret_cast<u32x4_t*>(w_to + t * 1024) = c.w[t];
@@ -224,7 +252,7 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
       uint32_t sx[MT];
 #pragma unroll
       for (int t = 0; t < MT; ++t) sx[t] = kX8 ? c.xs[t] : 0u;
-      if (s + v + U < last) load(c, s + v + U);
+      if (s + v + 1 < last) load(c, s + v + 1);
 
       bf16x8_t x[MT][4];
 #pragma unroll
@@ -282,16 +310,23 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
     for (int w = 1; w < W; ++w) v += reinterpret_cast<const floatx4_t*>(lds[w])[q * kWave + lane];
     const int64_t n = n0 + 16 * (q / MT) + 4 * g, m = m0 + 16 * (q % MT) + r;
     if (m >= a.M || n >= a.N) continue;
+    typedef u32x2_t u32x2_at2 __attribute__((aligned(2)));
     float y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float b = a.bias && n + e < a.N ? __uint_as_float((uint32_t)a.bias[n + e] << 16) : 0.0f;
-      y[e] = __builtin_fmaf(alpha, v[e], b);
+    u32x2_t b = u32x2_t{0, 0};
+    if (a.bias) {
+      if (n + 4 <= a.N) {
+        b = *reinterpret_cast<const u32x2_at2*>(a.bias + n);
+      } else {
+        b.x = a.bias[n] | (n + 1 < a.N ? (uint32_t)a.bias[n + 1] << 16 : 0u);
+        b.y = n + 2 < a.N ? a.bias[n + 2] : 0u;
+      }
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = __builtin_fmaf(alpha, v[e], __uint_as_float(e & 1 ? b[e / 2] & 0xFFFF0000u : b[e / 2] << 16));
     const uint32_t p0 = pack_bf16(y[0], y[1]), p1 = pack_bf16(y[2], y[3]);
     uint16_t* o = a.out + m * a.N + n;
     if (n + 4 <= a.N) {
-      typedef u32x2_t u32x2_at2 __attribute__((aligned(2)));
       *reinterpret_cast<u32x2_at2*>(o) = u32x2_t{p0, p1};
     } else {
       o[0] = (uint16_t)p0;
@@ -301,45 +336,56 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
   }
 }
 
-static int tokens_tile(int64_t M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }
+// The tile of a shape: up to 16 tokens 16 x 16 outputs a workgroup; beyond,
+// 32 tokens and 16 or 32 columns (more than 32 tokens a tile won nowhere by
+// more than a tenth, 64 x 9728 x 2432).  Of these, 32 columns halve the
+// activations' way from L2 but also the workgroups; with at most half a
+// workgroup a CU 16 are faster (32 x 2432 x 2432 NVFP4 5.4 against 6.3 us), and
+// past one a CU four waves, three workgroups of which fit a CU, beat eight
+// (64 x 9728 x 2432 13.1 against 17.0; below, eight win: 32 x 4864 x 2432 6.5
+// against 7.1).
+struct Tile {
+  int mt, nt, waves;
+};
 
-// 16-column tiles of a workgroup
-static int column_tiles(int64_t M, int64_t N) {
-  (void)M;
-  return N >= 4096 ? 2 : 1;
+static Tile tile_of(int64_t M, int64_t N) {
+  if (M <= 16) return {1, 1, 8};
+  const int64_t wide = ((M + 31) / 32) * ((N + 31) / 32), cus = device_cu_count();
+  if (wide <= cus / 2) return {2, 1, 8};
+  return {2, 2, wide <= cus ? 8 : 4};
 }
 
 int64_t weight_linear_groups(int64_t M, int64_t N) {
-  const int mt = tokens_tile(M), nt = column_tiles(M, N);
-  return ((N + 16 * nt - 1) / (16 * nt)) * ((M + 16 * mt - 1) / (16 * mt));
+  const Tile t = tile_of(M, N);
+  return ((N + 16 * t.nt - 1) / (16 * t.nt)) * ((M + 16 * t.mt - 1) / (16 * t.mt));
 }
 
-template <int kFormat, bool kX8, int MT, int NT, int XR, int W, int U>
+template <int kFormat, bool kX8, int MT, int NT, int XR, int W>
 static hipError_t launch_tile(const WeightLinearArgs& a, hipStream_t stream) {
   const int tiles_m = (int)((a.M + 16 * MT - 1) / (16 * MT));
-  return launch_kernel(weight_linear_kernel<kFormat, kX8, MT, NT, XR, W, U>,
-                       dim3((unsigned)weight_linear_groups(a.M, a.N)), dim3(W * kWave), stream, a, tiles_m);
-}
-
-template <int kFormat, bool kX8, int NT>
-static hipError_t launch_format(const WeightLinearArgs& a, hipStream_t stream) {
-  constexpr int kFull = kX8 ? 2 : 4;   // loads of 16 tokens' step
-  if (a.M <= 16 / kFull) return launch_tile<kFormat, kX8, 1, NT, 1, 8, 4>(a, stream);
-  if (a.M <= 16) return launch_tile<kFormat, kX8, 1, NT, kFull, 8, 2>(a, stream);
-  if (a.M <= 32) return launch_tile<kFormat, kX8, 2, NT, 2 * kFull, 8, 2>(a, stream);
-  return launch_tile<kFormat, kX8, 4, NT, 4 * kFull, kX8 ? 8 : 4, 1>(a, stream);
+  const dim3 grid((unsigned)weight_linear_groups(a.M, a.N)), block(W * kWave);
+  if (a.K % kWLStep == 0)
+    return launch_kernel(weight_linear_kernel<kFormat, kX8, true, MT, NT, XR, W>, grid, block, stream, a, tiles_m);
+  return launch_kernel(weight_linear_kernel<kFormat, kX8, false, MT, NT, XR, W>, grid, block, stream, a, tiles_m);
 }
 
 template <int kFormat, bool kX8>
-static hipError_t launch_columns(const WeightLinearArgs& a, hipStream_t stream) {
-  return column_tiles(a.M, a.N) == 1 ? launch_format<kFormat, kX8, 1>(a, stream) : launch_format<kFormat, kX8, 2>(a, stream);
+static hipError_t launch_format(const WeightLinearArgs& a, hipStream_t stream) {
+  constexpr int kFull = kX8 ? 2 : 4;   // loads of 16 tokens' step
+  const Tile t = tile_of(a.M, a.N);
+  // as few activation rows as one load brings need no more LDS than that
+  if (a.M <= 16 / kFull) return launch_tile<kFormat, kX8, 1, 1, 1, 8>(a, stream);
+  if (t.mt == 1) return launch_tile<kFormat, kX8, 1, 1, kFull, 8>(a, stream);
+  if (t.nt == 1) return launch_tile<kFormat, kX8, 2, 1, 2 * kFull, 8>(a, stream);
+  if (t.waves == 8) return launch_tile<kFormat, kX8, 2, 2, 2 * kFull, 8>(a, stream);
+  return launch_tile<kFormat, kX8, 2, 2, 2 * kFull, 4>(a, stream);
 }
 
 hipError_t launch_weight_linear(int w_format, bool x_mxfp8, const WeightLinearArgs& a, hipStream_t stream) {
   if (a.M == 0 || a.N == 0) return hipSuccess;
-  if (x_mxfp8) return launch_columns<SOLFP4_FORMAT_MXFP4, true>(a, stream);
-  if (w_format == SOLFP4_FORMAT_NVFP4) return launch_columns<SOLFP4_FORMAT_NVFP4, false>(a, stream);
-  return launch_columns<SOLFP4_FORMAT_MXFP4, false>(a, stream);
+  if (x_mxfp8) return launch_format<SOLFP4_FORMAT_MXFP4, true>(a, stream);
+  if (w_format == SOLFP4_FORMAT_NVFP4) return launch_format<SOLFP4_FORMAT_NVFP4, false>(a, stream);
+  return launch_format<SOLFP4_FORMAT_MXFP4, false>(a, stream);
 }
 
 }  // namespace solfp4
