@@ -35,6 +35,16 @@ __device__ __forceinline__ Run<kType> zero_run() {
   return r;
 }
 
+// Eight ones.
+template <int kType>
+__device__ __forceinline__ Run<kType> one_run() {
+  constexpr uint32_t k = kType == SOLFP4_F32 ? 0x3F800000u : kType == SOLFP4_BF16 ? 0x3F803F80u : 0x3C003C00u;
+  Run<kType> r;
+#pragma unroll
+  for (int i = 0; i < kRunPieces<kType>; ++i) r.p[i] = u32x4_t{k, k, k, k};
+  return r;
+}
+
 // Row `row` of an operand (both uniform over the wave, so the address stays
 // scalar and a lane adds its 32-bit offset).
 template <int kType>

@@ -236,7 +236,7 @@ struct NormBackArgs {
   int64_t dx_stride;
   float* partial;     // [groups * parts][width], NULL: no gain gradient
   int64_t rows, width;
-  int64_t group_rows, part_rows;   // set by the launch
+  int64_t group_rows;   // set by the launch
   int parts;
 };
 // Workgroups that each group's rows are dealt to (host only).

@@ -104,6 +104,11 @@ __device__ __forceinline__ void row_sum(T (&v)[n], T (*lds)[n], int wave, int wp
     for (int i = 0; i < n; ++i) v[i] += lds[first + w][i];
 }
 
+// a b + c, one rounding (the build contracts nothing by itself)
+__device__ __forceinline__ float fused(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ __forceinline__ double fused(double a, double b, double c) { return __builtin_fma(a, b, c); }
+__device__ __forceinline__ double fused(float a, float b, double c) { return fused((double)a, (double)b, c); }
+
 template <int kType, int kOut, int kRuns>
 __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(NormArgs a, int wpr) {
   using Sum = std::conditional_t<kOut == kNormSame, float, double>;   // block_scale
@@ -122,7 +127,8 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
     const int col = i * step + lane * 8, n = width - col;
-    x[i] = r[i] = g[i] = zero_run<kType>();
+    x[i] = r[i] = zero_run<kType>();
+    g[i] = one_run<kType>();
     if (n > 0) {
       x[i] = load_run<kType>(xr, col, n);
       if (a.residual) r[i] = load_run<kType>(rr, col, n);
@@ -144,7 +150,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
       if (n > 0) store_run<kType>(sr, col, n, from_f32<kType>(s[i]));
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[0] += (Sum)s[i][e] * (Sum)s[i][e];
+    for (int e = 0; e < 8; ++e) q[0] = fused(s[i][e], s[i][e], q[0]);
   }
   row_sum(q, lds, wave, wpr);
   Sum rho;
@@ -165,9 +171,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
     const int col = i * step + lane * 8, n = width - col;
     float v[8], y[8];
     forget(g[i]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 1.0f;
-    if (a.gain) to_f32<kType>(g[i], v);
+    to_f32<kType>(g[i], v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = s[i][e] * rho32 * v[e];
     if (n <= 0) continue;
@@ -228,10 +232,10 @@ hipError_t launch_add_rmsnorm(int type, int out, const NormArgs& a, hipStream_t 
 // ---- backward -------------------------------------------------------------
 
 // ds of every row, and each workgroup's share of dg: a workgroup of eight
-// waves takes the rows [part * part_rows, ...) of one group, its row slots
-// one row after another, and keeps dg of its columns in registers; at the end
-// the slots' sums are added in slot order and stored as one row of the
-// workspace.  All of a row's loads go out before the first use and stay as
+// waves (8 / wpr row slots) takes every `parts`-th run of slots rows of one
+// group, so that the chip reads one window of the operands at a time, and
+// keeps dg of its columns in registers; at the end the slots' sums are added
+// in slot order and stored as one row of the workspace.  All of a row's loads go out before the first use and stay as
 // they were read (converted again after the reduction: half the registers
 // of FP32 copies, twice the waves).
 template <int kType, int kRuns>
@@ -243,21 +247,20 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void rmsnorm_backward_kernel
   const int lane = (wave & (wpr - 1)) * kWave + (threadIdx.x & (kWave - 1));
   const int step = wpr * kWave * 8;
   const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
-  const int first = part * (int)a.part_rows;   // in the group
-  const int last = first + (int)a.part_rows < (int)a.group_rows ? first + (int)a.part_rows : (int)a.group_rows;
+  const int rows = (int)a.group_rows;
   const int64_t row0 = group * a.group_rows;
   Run<kType> g[kRuns];
   const uint8_t* gr = row_of<kType>(a.gain, group, a.gain_stride);
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
     const int col = i * step + lane * 8, n = (int)a.width - col;
-    g[i] = zero_run<kType>();
+    g[i] = one_run<kType>();
     if (a.gain && n > 0) g[i] = load_run<kType>(gr, col, n);
   }
   float dg[kRuns][8] = {};
-  for (int base = first; base < last; base += slots) {
-    const bool in = base + slot < last;
-    const int64_t row = row0 + (in ? base + slot : first);
+  for (int base = part * slots; base < rows; base += a.parts * slots) {
+    const bool in = base + slot < rows;
+    const int64_t row = row0 + (in ? base + slot : base);
     const int width = in ? (int)a.width : 0;
     const uint8_t* xr = row_of<kType>(a.x, row, a.x_stride);
     const uint8_t* dr = row_of<kType>(a.dy, row, a.dy_stride);
@@ -282,8 +285,8 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void rmsnorm_backward_kernel
       to_f32<kType>(g[i], v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        qb[0] += s[e] * s[e];
-        qb[1] += (a.gain ? D[e] * v[e] : D[e]) * s[e];
+        qb[0] = fused(s[e], s[e], qb[0]);
+        qb[1] = fused(D[e] * v[e], s[e], qb[1]);
       }
     }
     row_sum(qb, lds, wave, wpr);
@@ -303,30 +306,28 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void rmsnorm_backward_kernel
       to_f32<kType>(ex[i], out);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dg[i][e] += D[e] * (s[e] * rho);
-        out[e] += rho * ((a.gain ? D[e] * v[e] : D[e]) - s[e] * k);
+        dg[i][e] = fused(D[e], s[e] * rho, dg[i][e]);
+        out[e] = fused(rho, fused(s[e], -k, D[e] * v[e]), out[e]);
       }
       if (n > 0) store_run<kType>(outr, col, n, from_f32<kType>(out));
     }
   }
   if (!a.partial) return;
   float* part_row = a.partial + (int64_t)blockIdx.x * a.width;
+  // run by run: every slot's sums to LDS, then each thread adds `wpr` columns'
+  const int cols = wpr * kWave * 8;
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    const int col = i * step + lane * 8;
-    if (slots > 1) {
-      __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) fold[e * (kNormMaxWaves * kWave) + threadIdx.x] = dg[i][e];
-      __syncthreads();
-      if (slot) continue;
-      for (int z = 1; z < slots; ++z)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dg[i][e] += fold[e * (kNormMaxWaves * kWave) + z * wpr * kWave + lane];
+    __syncthreads();
+    floatx4_t* to = reinterpret_cast<floatx4_t*>(fold + slot * cols + lane * 8);
+    to[0] = floatx4_t{dg[i][0], dg[i][1], dg[i][2], dg[i][3]};
+    to[1] = floatx4_t{dg[i][4], dg[i][5], dg[i][6], dg[i][7]};
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += kNormMaxWaves * kWave) {
+      float t = fold[c];
+      for (int z = 1; z < slots; ++z) t += fold[z * cols + c];
+      if (i * step + c < a.width) part_row[i * step + c] = t;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (col + e < a.width) part_row[col + e] = dg[i][e];
   }
 }
 
@@ -362,10 +363,9 @@ constexpr int64_t kPartMinRows = 8;
 int64_t rmsnorm_backward_parts(int64_t rows, int64_t groups) {
   if (rows == 0 || groups == 0) return 0;
   const int64_t per = rows / groups;
-  int64_t parts = (2 * (int64_t)device_cu_count() + groups - 1) / groups;
-  if (parts > (per + kPartMinRows - 1) / kPartMinRows) parts = (per + kPartMinRows - 1) / kPartMinRows;
-  const int64_t part_rows = (per + parts - 1) / parts;
-  return (per + part_rows - 1) / part_rows;
+  const int64_t parts = (2 * (int64_t)device_cu_count() + groups - 1) / groups;
+  const int64_t most = (per + kPartMinRows - 1) / kPartMinRows;
+  return parts < most ? parts : most;
 }
 
 template <int kType>
@@ -391,7 +391,6 @@ hipError_t launch_rmsnorm_backward(int type, NormBackArgs a, float* dgain, hipSt
   if (parts) {
     a.group_rows = a.rows / groups;
     a.parts = (int)parts;
-    a.part_rows = (a.group_rows + parts - 1) / parts;
     if (type == SOLFP4_BF16) e = launch_back<SOLFP4_BF16>(a, groups, stream);
     else if (type == SOLFP4_F16) e = launch_back<SOLFP4_F16>(a, groups, stream);
     else e = launch_back<SOLFP4_F32>(a, groups, stream);
