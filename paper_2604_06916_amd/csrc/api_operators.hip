@@ -291,7 +291,10 @@ int solfp4_rotary(int type, int layout, int inverse, const void* q, int64_t q_to
       (!rotary_in_place(a.k, tokens) && !rotary_apart(type, a.k, a.k, tokens, dim)) ||
       !rotary_apart(type, a.q, a.k, tokens, dim) || !rotary_apart(type, a.k, a.q, tokens, dim))
     return SOLFP4_EINVAL;
-  if (tokens * dim > kMaxGroups * 64) return SOLFP4_ESHAPE;
+  // waves are numbered in 32 bits
+  if (solfp4::rotary_waves(type, layout == SOLFP4_ROTARY_INTERLEAVED, tokens, dim, rotated, q_heads + k_heads) >
+      kMaxGroups)
+    return SOLFP4_ESHAPE;
   a.table = table, a.table_rows = table_rows > 0 ? table_rows : 1;
   a.positions = positions, a.tokens = tokens, a.dim = (int)dim, a.rotated = (int)rotated;
   const hipError_t e = solfp4::launch_rotary(type, layout == SOLFP4_ROTARY_INTERLEAVED, inverse != 0, position_bytes,

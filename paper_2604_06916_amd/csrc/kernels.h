@@ -259,6 +259,8 @@ struct RotaryArgs {
   int64_t tokens;
   int dim, rotated;
 };
+// Waves of the launch (host only; all sizes positive).
+int64_t rotary_waves(int type, bool interleaved, int64_t tokens, int64_t dim, int64_t rotated, int64_t heads);
 hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,
                          hipStream_t stream);
 

@@ -355,23 +355,29 @@ __global__ __launch_bounds__(kFoldCols * kFoldSlices) void dgain_kernel(const fl
   dgain[group * width + col] = t;
 }
 
-// Workgroups a group's rows are dealt to: two a compute unit over all
-// groups, but at least kPartMinRows rows each, so that the partial sums stay
-// a small share of the rows' bytes.
+// Runs a lane above which a row gets more waves: with these the kernel takes
+// at most 128 registers, and two workgroups share a CU.
+template <int kType>
+constexpr int kBackRuns = kType == SOLFP4_F32 ? 2 : 3;
+
+// Workgroups a group's rows are dealt to: at most two a compute unit over all
+// groups (one round: with 516 on 256 CUs, 26574 x 2432 took 126 us, with 510
+// 107), but at least kPartMinRows rows each, so that the partial sums stay a
+// small share of the rows' bytes.
 constexpr int64_t kPartMinRows = 8;
 
 int64_t rmsnorm_backward_parts(int64_t rows, int64_t groups) {
   if (rows == 0 || groups == 0) return 0;
   const int64_t per = rows / groups;
-  const int64_t parts = (2 * (int64_t)device_cu_count() + groups - 1) / groups;
+  const int64_t parts = 2 * (int64_t)device_cu_count() / groups;
   const int64_t most = (per + kPartMinRows - 1) / kPartMinRows;
-  return parts < most ? parts : most;
+  return parts < 1 ? 1 : parts < most ? parts : most;
 }
 
 template <int kType>
 static hipError_t launch_back(const NormBackArgs& a, int64_t groups, hipStream_t stream) {
   int wpr, runs;
-  row_shape(a.width, kType == SOLFP4_F32 ? 3 : kNormMaxRuns, &wpr, &runs);
+  row_shape(a.width, kBackRuns<kType>, &wpr, &runs);
   const dim3 grid((unsigned)(groups * a.parts)), block(kNormMaxWaves * kWave);
   switch (runs) {
     case 1: return launch_kernel(rmsnorm_backward_kernel<kType, 1>, grid, block, stream, a, wpr);

@@ -7,9 +7,10 @@
 // inputs'.  Elements R.. of a head are copied.  FP32 between a load and a
 // store.
 //
-// A lane takes the same 16-byte pieces of every head of its token that its
-// slot reaches, so the table's row is read once per slot and not once per
-// head (a row is 2 R FP32 bytes against 2 R of a BF16 head).  Bound by
+// A wave takes the heads of one token (or, where they are few, of several):
+// a lane one 16-byte piece of every `slots`-th head, or the piece and its
+// partner R/2 elements further on, so its cosines and sines are read once for
+// all of them, and the loads of kRotaryHeads heads go out together.  Bound by
 // memory: each element is read and written once.
 #include "elements.h"
 #include "kernels.h"
@@ -17,11 +18,6 @@
 namespace solfp4 {
 
 constexpr int kRotaryThreads = 256;
-
-template <typename T>
-__device__ __forceinline__ float load_elem(const T* p) {
-  return (float)*p;
-}
 
 // 16-byte piece of VE elements as FP32
 template <int kType, int VE>
@@ -90,55 +86,112 @@ __device__ __forceinline__ void store_piece(uint8_t* p, int n, u32x4_t r) {
   }
 }
 
-// One lane's unit: piece `c` of the heads slot, slot + slots, ... of a token.
-// Pieces below `turning` hold pairs (half: VE pairs in two pieces R/2
-// elements apart; interleaved: VE/2 pairs in one), the others copy.
+constexpr int kRotaryHeads = 4;   // heads of a lane at most, all in flight together
+
+// n of the kPairs floats at p, the rest zero
+template <int kPairs>
+__device__ __forceinline__ void load_turns(const float* p, int n, float (&v)[kPairs]) {
+  if (n >= kPairs) {
+    if constexpr (kPairs == 2) {
+      typedef u32x2_t u32x2_at4 __attribute__((aligned(4)));
+      const u32x2_t w = *reinterpret_cast<const u32x2_at4*>(p);
+      v[0] = __uint_as_float(w.x);
+      v[1] = __uint_as_float(w.y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPairs; i += 4) {
+        const u32x4_t w = *reinterpret_cast<const u32x4_at4*>(p + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i + e] = __uint_as_float(w[e]);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) v[i] = i < n ? p[i] : 0.0f;
+}
+
+// How a launch's lanes share the work.  A head has `pieces` pieces: below
+// `turning` they hold pairs (half: VE pairs in two pieces R/2 elements apart;
+// interleaved: VE/2 pairs in one), the others copy.  A wave holds `lanes` of
+// them at a time (all, or 64 in each of `blocks` waves), `slots` heads of
+// `packed` tokens; `parts` waves share a token's heads.
+struct RotaryShape {
+  int turning, pieces, lanes, blocks, slots, packed, parts;
+};
+
 template <int kType, bool kInterleaved>
-__global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a, int position_bytes, float sign,
-                                                                int turning, int pieces, int slots) {
+__global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a, RotaryShape sh, int position_bytes,
+                                                                float sign) {
   constexpr int VE = 16 / kElemBytes<kType>;
   constexpr int kPairs = kInterleaved ? VE / 2 : VE;
-  const int64_t unit = (int64_t)blockIdx.x * kRotaryThreads + threadIdx.x;
-  const int c = (int)(unit % pieces);
-  const int64_t rest = unit / pieces;
-  const int slot = (int)(rest % slots);
-  const int64_t token = rest / slots;
-  if (token >= a.tokens) return;
+  uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kRotaryThreads / kWave) + threadIdx.x / kWave);
+  const int lane = threadIdx.x & (kWave - 1);
+  uint32_t block = 0, part = 0;
+  if (sh.blocks > 1) block = unit % sh.blocks, unit /= sh.blocks;
+  if (sh.parts > 1) part = unit % sh.parts, unit /= sh.parts;
+  const int at_slot = lane / sh.lanes, c = (int)block * sh.lanes + lane - at_slot * sh.lanes;
+  const int sub = at_slot / sh.slots;
+  const int64_t token = (int64_t)unit * sh.packed + sub;
+  if (c >= sh.pieces || sub >= sh.packed || token >= a.tokens) return;
   const int half = a.rotated / 2;
-  const bool copies = c >= turning;
-  // first element and count of the lane's piece (and of its partner R/2 further on)
-  const int at = copies ? a.rotated + (c - turning) * VE : kInterleaved ? c * VE : c * VE;
-  const int n = min(VE, copies ? a.dim - at : kInterleaved ? a.rotated - at : half - at);
+  const bool copies = c >= sh.turning;
+  // First element and count of the lane's piece (and of its partner R/2
+  // further on).  The last piece of a span that it does not fill starts early
+  // instead: a whole vector that repeats elements of the lane before.  Both
+  // lanes have read them before either writes (one wave, one instruction), and
+  // write the same values.
+  const int span = copies ? a.dim - a.rotated : kInterleaved ? a.rotated : half;
+  int at = (copies ? c - sh.turning : c) * VE;
+  if (sh.blocks == 1 && span >= VE) at = min(at, span - VE);
+  const int n = min(VE, span - at);
+  if (copies) at += a.rotated;
   float cs[kPairs], sn[kPairs];
   if (!copies) {
-    int64_t p = token % a.table_rows;
+    int64_t p = token;
     if (position_bytes == 4) p = static_cast<const int32_t*>(a.positions)[token];
-    if (position_bytes == 8) p = static_cast<const int64_t*>(a.positions)[token];
+    else if (position_bytes == 8) p = static_cast<const int64_t*>(a.positions)[token];
+    else if (a.table_rows < a.tokens) p = (uint32_t)token % (uint32_t)a.table_rows;
     const bool known = p >= 0 && p < a.table_rows;
     const float* t = a.table + (known ? p : 0) * a.rotated + (kInterleaved ? at / 2 : at);
-    const int pairs = kInterleaved ? n / 2 : n;
+    load_turns<kPairs>(t, kInterleaved ? n / 2 : n, cs);
+    load_turns<kPairs>(t + half, kInterleaved ? n / 2 : n, sn);
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       // a position outside the table turns into NaN
-      cs[i] = !known ? __builtin_nanf("") : i < pairs ? t[i] : 0.0f;
-      sn[i] = !known ? __builtin_nanf("") : i < pairs ? sign * t[half + i] : 0.0f;
+      cs[i] = known ? cs[i] : __builtin_nanf("");
+      sn[i] = known ? sign * sn[i] : __builtin_nanf("");
     }
   }
-  const int heads = a.q.heads + a.k.heads;
-  for (int h = slot; h < heads; h += slots) {
+  const uint8_t* qi = static_cast<const uint8_t*>(a.q.in) + (token * a.q.in_token + at) * kElemBytes<kType>;
+  const uint8_t* ki = static_cast<const uint8_t*>(a.k.in) + (token * a.k.in_token + at) * kElemBytes<kType>;
+  uint8_t* qo = static_cast<uint8_t*>(a.q.out) + (token * a.q.out_token + at) * kElemBytes<kType>;
+  uint8_t* ko = static_cast<uint8_t*>(a.k.out) + (token * a.k.out_token + at) * kElemBytes<kType>;
+  const int64_t apart = (int64_t)half * kElemBytes<kType>;
+  const int heads = a.q.heads + a.k.heads, hop = sh.slots * sh.parts;
+  const int h0 = at_slot - sub * sh.slots + (int)part * sh.slots;
+  u32x4_t pu[kRotaryHeads], pv[kRotaryHeads];
+  uint8_t* out[kRotaryHeads];
+#pragma unroll
+  for (int j = 0; j < kRotaryHeads; ++j) {
+    const int h = h0 + j * hop;
+    if (h >= heads) continue;
     const bool first = h < a.q.heads;
-    const RotaryOperand& o = first ? a.q : a.k;
-    const int hh = first ? h : h - a.q.heads;
-    const uint8_t* in = static_cast<const uint8_t*>(o.in) +
-                        (token * o.in_token + hh * o.in_head + at) * kElemBytes<kType>;
-    uint8_t* out = static_cast<uint8_t*>(o.out) + (token * o.out_token + hh * o.out_head + at) * kElemBytes<kType>;
-    const u32x4_t pu = load_piece<kType, VE>(in, n);
+    const int64_t hh = first ? h : h - a.q.heads;
+    const uint8_t* in = (first ? qi : ki) + hh * (first ? a.q.in_head : a.k.in_head) * kElemBytes<kType>;
+    out[j] = (first ? qo : ko) + hh * (first ? a.q.out_head : a.k.out_head) * kElemBytes<kType>;
+    pu[j] = load_piece<kType, VE>(in, n);
+    if (!kInterleaved && !copies) pv[j] = load_piece<kType, VE>(in + apart, n);
+  }
+#pragma unroll
+  for (int j = 0; j < kRotaryHeads; ++j) {
+    if (h0 + j * hop >= heads) continue;
     if (copies) {
-      store_piece<kType, VE>(out, n, pu);
+      store_piece<kType, VE>(out[j], n, pu[j]);
       continue;
     }
     float u[VE];
-    piece_to_f32<kType, VE>(pu, u);
+    piece_to_f32<kType, VE>(pu[j], u);
     if constexpr (kInterleaved) {
       float r[VE];
 #pragma unroll
@@ -146,38 +199,60 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a, in
         r[2 * i] = u[2 * i] * cs[i] - u[2 * i + 1] * sn[i];
         r[2 * i + 1] = u[2 * i] * sn[i] + u[2 * i + 1] * cs[i];
       }
-      store_piece<kType, VE>(out, n, piece_from_f32<kType, VE>(r));
+      store_piece<kType, VE>(out[j], n, piece_from_f32<kType, VE>(r));
     } else {
-      const int64_t apart = (int64_t)half * kElemBytes<kType>;
       float v[VE], ru[VE], rv[VE];
-      piece_to_f32<kType, VE>(load_piece<kType, VE>(in + apart, n), v);
+      piece_to_f32<kType, VE>(pv[j], v);
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
         ru[i] = u[i] * cs[i] - v[i] * sn[i];
         rv[i] = u[i] * sn[i] + v[i] * cs[i];
       }
-      store_piece<kType, VE>(out, n, piece_from_f32<kType, VE>(ru));
-      store_piece<kType, VE>(out + apart, n, piece_from_f32<kType, VE>(rv));
+      store_piece<kType, VE>(out[j], n, piece_from_f32<kType, VE>(ru));
+      store_piece<kType, VE>(out[j] + apart, n, piece_from_f32<kType, VE>(rv));
     }
   }
+}
+
+// Waves wanted a CU; with fewer tokens their heads are split.
+constexpr int64_t kRotaryWaves = 16;
+
+// The shape of a launch and its waves, for vectors of VE elements.
+static RotaryShape rotary_shape(int VE, bool interleaved, int64_t tokens, int64_t dim, int64_t rotated, int64_t heads,
+                                int64_t* waves) {
+  const int64_t span = interleaved ? rotated : rotated / 2;
+  RotaryShape sh;
+  sh.turning = (int)((span + VE - 1) / VE);
+  sh.pieces = sh.turning + (int)((dim - rotated + VE - 1) / VE);
+  sh.blocks = (sh.pieces + kWave - 1) / kWave;
+  sh.lanes = sh.blocks > 1 ? kWave : sh.pieces;
+  const int fit = kWave / sh.lanes;
+  sh.slots = heads < fit ? (int)heads : fit;
+  sh.packed = fit / sh.slots;
+  const int64_t rounds = (heads + sh.slots - 1) / sh.slots, units = (tokens + sh.packed - 1) / sh.packed;
+  const int64_t least = (rounds + kRotaryHeads - 1) / kRotaryHeads;
+  const int64_t wanted = (kRotaryWaves * device_cu_count() + units - 1) / units;
+  sh.parts = (int)(wanted < least ? least : wanted < rounds ? wanted : rounds);
+  *waves = units * sh.parts * sh.blocks;
+  return sh;
+}
+
+int64_t rotary_waves(int type, bool interleaved, int64_t tokens, int64_t dim, int64_t rotated, int64_t heads) {
+  int64_t waves;
+  rotary_shape(type == SOLFP4_F32 ? 4 : 8, interleaved, tokens, dim, rotated, heads, &waves);
+  return waves;
 }
 
 template <int kType>
 static hipError_t launch_rotary_type(bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,
                                      hipStream_t stream) {
-  constexpr int VE = 16 / kElemBytes<kType>;
-  const int span = interleaved ? a.rotated : a.rotated / 2;
-  const int turning = (span + VE - 1) / VE;
-  const int pieces = turning + (a.dim - a.rotated + VE - 1) / VE;
-  const int heads = a.q.heads + a.k.heads;
-  const int slots = heads < 4 ? heads : 4;
-  const int64_t units = a.tokens * slots * pieces;
-  const dim3 grid((unsigned)((units + kRotaryThreads - 1) / kRotaryThreads)), block(kRotaryThreads);
+  int64_t waves;
+  const RotaryShape sh = rotary_shape(16 / kElemBytes<kType>, interleaved, a.tokens, a.dim, a.rotated,
+                                      (int64_t)a.q.heads + a.k.heads, &waves);
+  const dim3 grid((unsigned)((waves + kRotaryThreads / kWave - 1) / (kRotaryThreads / kWave))), block(kRotaryThreads);
   const float sign = inverse ? -1.0f : 1.0f;
-  return interleaved ? launch_kernel(rotary_kernel<kType, true>, grid, block, stream, a, position_bytes, sign,
-                                     turning, pieces, slots)
-                     : launch_kernel(rotary_kernel<kType, false>, grid, block, stream, a, position_bytes, sign,
-                                     turning, pieces, slots);
+  return interleaved ? launch_kernel(rotary_kernel<kType, true>, grid, block, stream, a, sh, position_bytes, sign)
+                     : launch_kernel(rotary_kernel<kType, false>, grid, block, stream, a, sh, position_bytes, sign);
 }
 
 hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,
