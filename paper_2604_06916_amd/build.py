@@ -65,7 +65,7 @@ def _link_host(obj: str) -> None:
     torch_lib = os.path.join(importlib.util.find_spec("torch").submodule_search_locations[0], "lib")
     tmp = HOST_LIB + ".tmp"
     cmd = ["g++", "-shared", obj, "-o", tmp, "-L", PKG, "-l:libsolfp4.so", "-Wl,-rpath,$ORIGIN",
-           "-L", torch_lib, "-lc10", "-ltorch_cpu", "-ltorch_python"]
+           "-L", torch_lib, "-lc10", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")

@@ -17,7 +17,7 @@
 // with a kept output and workspace, in MXFP4, 14.5 -> 8.2.
 #include <torch/csrc/autograd/python_variable.h>
 
-#include <ATen/ops/empty.h>
+#include <ATen/hip/EmptyTensor.h>
 
 #include "solfp4.h"
 
@@ -47,8 +47,9 @@ void need_tensor(const Tensor& t, at::ScalarType type, at::IntArrayRef shape, co
 
 void need_matrix(const Tensor& t) { need(t.layout() == at::kStrided && t.dim() == 2); }
 
+// The device's allocation itself, without the dispatcher's way to it.
 Tensor make(at::IntArrayRef shape, at::ScalarType type, const at::Device& dev) {
-  return at::empty(shape, at::TensorOptions().dtype(type).device(dev));
+  return at::detail::empty_cuda(shape, type, dev, std::nullopt);
 }
 
 // An operand that the caller gives or leaves to the call, and its Python object.

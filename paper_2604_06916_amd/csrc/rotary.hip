@@ -86,7 +86,7 @@ __device__ __forceinline__ void store_piece(uint8_t* p, int n, u32x4_t r) {
   }
 }
 
-constexpr int kRotaryHeads = 4;   // heads of a lane at most, all in flight together
+constexpr int kRotaryHeads = 2;   // heads of a lane at most, all in flight together
 
 // n of the kPairs floats at p, the rest zero
 template <int kPairs>
