@@ -20,6 +20,16 @@ library's own, one pass with the next quantizer's amax).
 Block (pre-norm, no modulation):
     h = rmsnorm(x); qkv = linear(h); a = attention(q, k, v); x = x + linear(a)
     h = rmsnorm(x); u = gelu_tanh(linear(h)); x = x + linear(u)
+With Stage1Config(conditioned=True) the blocks are conditioned and know their
+tokens' positions, as a denoiser's do, and everything between their linears
+and the attention runs in the library:
+    c = rmsnorm(time[step] + text[rollout])              (MXFP8 for "mxfp4")
+    (g1, g2) = mod(c)        one row a rollout; few-token linear, 4-bit weight
+    x, h = add_rmsnorm(x, d of the block before, g1); qkv = linear(h)
+    q, k rotated in place, interleaved pairs at positions 0 .. tokens - 1
+    x, h = add_rmsnorm(x, linear(a), g2); d = linear(gelu_tanh(linear(h)))
+"mxfp4" norms write the linears' codes (no quantizer pass of their own).
+
 Euler step with T steps: x <- x + (1/T) * (blocks(x) - x).
 Reward of rollout i: mean over its tokens of <x_final[token], u> for a fixed
 direction u.
@@ -51,6 +61,7 @@ class Stage1Config:
     keep: int = 4            # K: K/2 highest- and K/2 lowest-rewarded rollouts
     w_sigma: float = 0.015
     seed: int = 5000
+    conditioned: bool = False   # norms modulated per rollout and step, rotary positions
 
     @property
     def head_dim(self):
@@ -61,6 +72,11 @@ def layer_shapes(cfg):
     """(name, N, K) of one block's linears."""
     return [("qkv", 3 * cfg.hidden, cfg.hidden), ("out", cfg.hidden, cfg.hidden),
             ("up", cfg.mlp, cfg.hidden), ("down", cfg.hidden, cfg.mlp)]
+
+
+def condition_shape(cfg):
+    """(N, K) of a conditioned block's modulation: two gains from the condition."""
+    return 2 * cfg.hidden, cfg.hidden
 
 
 def linear_flops(cfg):
@@ -101,8 +117,21 @@ def make_weights(cfg, device):
             w = draw_weights(N, K, cfg.w_sigma, seed)
             bias = draw_bias(N, cfg.w_sigma, seed + 1)
             blk[name] = (_bf16_dev(w, device), _bf16_dev(bias, device))
+        if cfg.conditioned:
+            N, K = condition_shape(cfg)
+            w = _bf16_dev(draw_weights(N, K, cfg.w_sigma, cfg.seed + 100 * b + 90), device)
+            # gains around 1
+            blk["mod"] = (w, 1 + _bf16_dev(draw_bias(N, cfg.w_sigma, cfg.seed + 100 * b + 91), device))
         model.append(blk)
     return model
+
+
+def make_condition(cfg, device):
+    """BF16 embeddings of the Euler steps [steps, hidden] and of the rollouts'
+    prompts [rollouts, hidden] (random, like the weights)."""
+    from workloads import draw_activations
+    return (_bf16_dev(draw_activations("normal", cfg.steps, cfg.hidden, cfg.seed + 11), device),
+            _bf16_dev(draw_activations("normal", cfg.rollouts, cfg.hidden, cfg.seed + 13), device))
 
 
 def _bf16_dev(bits, device):
@@ -142,10 +171,106 @@ class Runner:
         H, D = cfg.hidden, cfg.mlp
         self.buf = {n: torch.empty((M, c), dtype=torch.bfloat16, device=device)
                     for n, c in [("qkv", 3 * H), ("o", H), ("u", D), ("d", H)]}
+        if cfg.conditioned:
+            self._prepare_condition(model)
         self.linear_events = None
         self.op_events = None    # dict: op kind -> [(start, end)] of HIP events, when timing
         self.trace = None        # list: (stage name, tensor copy) of every block stage
         self.step_trace = None   # list: {"y": blocks output, "x": latents after} per Euler step
+
+    def _prepare_condition(self, model):
+        """The modulations' weights, the condition's buffers, the residual
+        stream and the norm's output, and the table of positions."""
+        cfg, dev = self.cfg, self.device
+        H, R = cfg.hidden, cfg.rollouts
+        bf16 = dict(dtype=torch.bfloat16, device=dev)
+        u8 = dict(dtype=torch.uint8, device=dev)
+        quantize = {"nvfp4": sol.nvfp4_quantize, "mxfp4": sol.mxfp4_quantize,
+                    "bf16": lambda w: (w.t().contiguous(),)}[self.backend]
+        for L, blk in zip(self.layers, model):
+            L["mod"] = (quantize(blk["mod"][0]), blk["mod"][1])
+        self.time, self.text = make_condition(cfg, dev)
+        self.gains = torch.empty((R, 2 * H), **bf16)
+        self.buf["x"] = torch.empty((self.M, H), **bf16)
+        if self.backend == "mxfp4":
+            self.c = (torch.empty((R, H), **u8), torch.empty((R, H // 32), **u8))
+            self.h = (torch.empty((self.M, H // 2), **u8), torch.empty((self.M, H // 32), **u8))
+        else:
+            self.c = (torch.empty((R, H), **bf16),)
+            self.h = (torch.empty((self.M, H), **bf16),)
+        self.table = sol.rotary_table(sol.rotary_frequencies(cfg.head_dim), cfg.tokens, device=dev)
+        self.set_step(0)
+
+    def set_step(self, step):
+        """Conditioned blocks: the condition of Euler step `step`, for the
+        blocks that run from here on (a captured step replays with the
+        condition set last)."""
+        time = self.time[step: step + 1].expand(self.cfg.rollouts, -1)
+        if self.backend == "mxfp4":
+            sol.mxfp8_add_rmsnorm(time, self.text, None, EPS, *self.c)
+        else:
+            sol.add_rmsnorm(time, self.text, None, EPS, *self.c)
+
+    def _modulate(self, layer):
+        """The two gains [rollouts, hidden] of one block."""
+        q, b = layer
+        H = self.cfg.hidden
+        if self.backend == "mxfp4":
+            sol.mxfp8_linear(*self.c, *q, b, self.gains)
+        elif self.backend == "nvfp4":
+            sol.nvfp4_weight_linear(*self.c, *q, b, self.gains)
+        else:
+            torch.addmm(b, *self.c, *q, out=self.gains)
+        return self.gains[:, :H], self.gains[:, H:]
+
+    def _norm(self, x, residual, gain):
+        """(x + residual, its norm as the linears take it)."""
+        total = None if residual is None else self.buf["x"]
+        if self.backend == "mxfp4":
+            sol.mxfp4_add_rmsnorm(x, residual, gain, EPS, *self.h, total)
+        else:
+            sol.add_rmsnorm(x, residual, gain, EPS, *self.h, total)
+        return x if residual is None else total
+
+    def _trace_norm(self, name):
+        for t, part in zip(self.h, ("", " scales")):
+            self._t(name + part, t)
+
+    def _linear_of_norm(self, layer, out):
+        if self.backend != "mxfp4":
+            return self.linear(self.h[0], layer, out)
+        q, b, _, _ = layer
+        return sol.mxfp4_gemm(*self.h, *q, b, out)
+
+    def _conditioned_blocks(self, x):
+        cfg, B = self.cfg, self.buf
+        R, T, Hh, hd = cfg.rollouts, cfg.tokens, cfg.heads, cfg.head_dim
+        d = None
+        for L in self.layers:
+            g1, g2 = self._modulate(L["mod"])
+            self._t("gains", self.gains)
+            x = self._t("x", self._norm(x, None, g1) if d is None else self._norm(d, x, g1))
+            self._trace_norm("h1")
+            qkv = self._linear_of_norm(L["qkv"], B["qkv"])
+            self._t("qkv", qkv)
+            heads = qkv.view(R * T, 3, Hh, hd)
+            sol.rotary(heads[:, 0], heads[:, 1], self.table, layout="interleaved", q_out=heads[:, 0], k_out=heads[:, 1])
+            self._t("rotated", qkv)
+            q, k, v = (qkv.view(R, T, 3, Hh, hd)[:, :, i].transpose(1, 2) for i in range(3))
+            with sdpa_kernel([SDPBackend.FLASH_ATTENTION, SDPBackend.EFFICIENT_ATTENTION]):
+                a = F.scaled_dot_product_attention(q, k, v)
+            a = self._t("a", a.transpose(1, 2).reshape(R * T, cfg.hidden))
+            o = self._t("o", self.linear(a, L["out"], B["o"]))
+            x = self._t("x2", self._norm(o, x, g2))
+            self._trace_norm("h2")
+            u = self._t("up", self._linear_of_norm(L["up"], B["u"]))
+            fused = self.backend == "nvfp4"
+            if fused:
+                sol.nvfp4_gelu_amax(u, self.down_amax)
+            else:
+                torch.ops.aten.gelu_(u, approximate="tanh")
+            d = self._t("d", self.linear(B["u"], L["down"], B["d"], fused))
+        return x if d is None else self._t("x3", x + d)
 
     def _down_views(self, cfg):
         """The regions of the workspace that the down layer's quantizer and
@@ -202,6 +327,8 @@ class Runner:
         return out
 
     def blocks(self, x):
+        if self.cfg.conditioned:
+            return self._conditioned_blocks(x)
         cfg, B = self.cfg, self.buf
         R, T, Hh, hd = cfg.rollouts, cfg.tokens, cfg.heads, cfg.head_dim
         def end(ev):
@@ -254,7 +381,9 @@ class Runner:
         """T Euler steps from x0 [rollouts * tokens, hidden] (BF16)."""
         x = x0
         dt = 1.0 / self.cfg.steps
-        for _ in range(self.cfg.steps):
+        for t in range(self.cfg.steps):
+            if self.cfg.conditioned:
+                self.set_step(t)
             y = self.blocks(x)
             ev = self._op("euler")
             x = (x.float() + dt * (y.float() - x.float())).to(torch.bfloat16)
