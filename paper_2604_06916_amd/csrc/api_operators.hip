@@ -103,7 +103,10 @@ int add_rmsnorm(int type, int kind, const void* x, int64_t x_stride, const void*
 }
 
 size_t back_workspace(int64_t rows, int64_t width, int64_t groups) {
-  const size_t bytes = (size_t)(solfp4::rmsnorm_backward_parts(rows, groups) * groups) * (size_t)width * sizeof(float);
+  const int64_t parts = solfp4::rmsnorm_backward_parts(rows, width, groups);
+  if (parts == 0) return 0;
+  // one part needs none, but a caller need not tell its sizes apart
+  const size_t bytes = parts == 1 ? 1 : (size_t)(parts * groups) * (size_t)width * sizeof(float);
   return (bytes + 255) / 256 * 256;
 }
 

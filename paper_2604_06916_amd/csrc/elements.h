@@ -147,7 +147,7 @@ __device__ __forceinline__ void forget(Run<kType>& r) {
   for (int i = 0; i < kRunPieces<kType>; ++i) asm volatile("" : "+v"(r.p[i]));
 }
 
-// Sums over the wave, in every lane, without LDS: neighbours, quads and half
+// Sums over lanes, in every lane, without LDS: neighbours, quads and half
 // rows by DPP, then rows of 16 and halves of 32 by lane swaps.
 template <int kCtrl, typename T>
 __device__ __forceinline__ T dpp_of(T v) {
@@ -177,14 +177,16 @@ __device__ __forceinline__ T swapped_sum(T v) {
   }
 }
 
+// Over each aligned group of `lanes` lanes (a power of two, uniform).
 template <typename T>
-__device__ __forceinline__ T wave_sum(T v) {
-  v += dpp_of<0xB1>(v);     // quad_perm 1,0,3,2
-  v += dpp_of<0x4E>(v);     // quad_perm 2,3,0,1
-  v += dpp_of<0x141>(v);    // row_half_mirror
-  v += dpp_of<0x140>(v);    // row_mirror
-  v = swapped_sum<16>(v);
-  return swapped_sum<32>(v);
+__device__ __forceinline__ T lanes_sum(T v, int lanes) {
+  if (lanes > 1) v += dpp_of<0xB1>(v);      // quad_perm 1,0,3,2
+  if (lanes > 2) v += dpp_of<0x4E>(v);      // quad_perm 2,3,0,1
+  if (lanes > 4) v += dpp_of<0x141>(v);     // row_half_mirror
+  if (lanes > 8) v += dpp_of<0x140>(v);     // row_mirror
+  if (lanes > 16) v = swapped_sum<16>(v);
+  if (lanes > 32) v = swapped_sum<32>(v);
+  return v;
 }
 
 }  // namespace solfp4

@@ -239,8 +239,8 @@ struct NormBackArgs {
   int64_t group_rows;   // set by the launch
   int parts;
 };
-// Workgroups that each group's rows are dealt to (host only).
-int64_t rmsnorm_backward_parts(int64_t rows, int64_t groups);
+// Workgroups that each group's rows are dealt to (host only); 1: no workspace.
+int64_t rmsnorm_backward_parts(int64_t rows, int64_t width, int64_t groups);
 hipError_t launch_rmsnorm_backward(int type, NormBackArgs a, float* dgain, hipStream_t stream);
 
 // ---- rotary positions (rotary.hip) ----------------------------------------

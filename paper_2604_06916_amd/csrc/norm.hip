@@ -11,7 +11,8 @@
 // A row belongs to `wpr` waves (1, 2, 4 or 8; as few as hold it in
 // kNormMaxRuns runs of 8 elements a lane), so a row is read once, stays in
 // registers, and for most widths is reduced inside one wave without a
-// barrier.  Bound by memory: 8 bytes an element in BF16 (7.03 with MXFP8
+// barrier.  Rows of at most 256 elements (a head's q or k) share a wave: 4 to
+// 32 lanes a row, or fewer (kRuns == 1).  Bound by memory: 8 bytes an element in BF16 (7.03 with MXFP8
 // output).
 #include "elements.h"
 #include "kernels.h"
@@ -84,22 +85,47 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float (&y)[8], float inv) {
   return c;
 }
 
-// The sums of v[0 .. n) over the `wpr` waves of this wave's row, in wave
-// order; every wave of the workgroup calls it.
+// How rows lie on the waves of a workgroup: a row on `wpr` whole waves, or
+// on `lanes` lanes of one (both powers of two; kRuns == 1 only).
+struct RowShape {
+  int wpr, lanes, runs;
+  __host__ __device__ int waves_slots(int waves) const { return waves / wpr * (kWave / lanes); }   // rows of a workgroup
+};
+
+// This thread's row slot in its workgroup, its lane in the row, and the
+// columns between its runs.
+template <int kRuns>
+struct Place {
+  int wave, slot, lane, step;
+  __device__ __forceinline__ explicit Place(RowShape sh) {
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int l = threadIdx.x & (kWave - 1);
+    slot = wave / sh.wpr;
+    lane = (wave & (sh.wpr - 1)) * kWave + l;
+    step = sh.wpr * kWave * 8;
+    if (kRuns == 1 && sh.lanes < kWave) {
+      slot = wave * (kWave / sh.lanes) + l / sh.lanes;
+      lane = l & (sh.lanes - 1);
+    }
+  }
+};
+
+// The sums of v[0 .. n) over a row's lanes, waves in wave order; every wave
+// of the workgroup calls it.
 template <int n, typename T>
-__device__ __forceinline__ void row_sum(T (&v)[n], T (*lds)[n], int wave, int wpr) {
+__device__ __forceinline__ void row_sum(T (&v)[n], T (*lds)[n], int wave, RowShape sh) {
 #pragma unroll
-  for (int i = 0; i < n; ++i) v[i] = wave_sum(v[i]);
-  if (wpr == 1) return;
+  for (int i = 0; i < n; ++i) v[i] = lanes_sum(v[i], sh.lanes);
+  if (sh.wpr == 1) return;
   __syncthreads();
   if ((threadIdx.x & (kWave - 1)) == 0)
 #pragma unroll
     for (int i = 0; i < n; ++i) lds[wave][i] = v[i];
   __syncthreads();
-  const int first = wave & -wpr;
+  const int first = wave & -sh.wpr;
 #pragma unroll
   for (int i = 0; i < n; ++i) v[i] = lds[first][i];
-  for (int w = 1; w < wpr; ++w)
+  for (int w = 1; w < sh.wpr; ++w)
 #pragma unroll
     for (int i = 0; i < n; ++i) v[i] += lds[first + w][i];
 }
@@ -110,14 +136,12 @@ __device__ __forceinline__ double fused(double a, double b, double c) { return _
 __device__ __forceinline__ double fused(float a, float b, double c) { return fused((double)a, (double)b, c); }
 
 template <int kType, int kOut, int kRuns>
-__global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(NormArgs a, int wpr) {
+__global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(NormArgs a, RowShape sh) {
   using Sum = std::conditional_t<kOut == kNormSame, float, double>;   // block_scale
   __shared__ Sum lds[kNormMaxWaves][1];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int slots = (blockDim.x / kWave) / wpr;   // powers of two
-  const int64_t row = (int64_t)blockIdx.x * slots + wave / wpr;
-  const int lane = (wave & (wpr - 1)) * kWave + (threadIdx.x & (kWave - 1));
-  const int step = wpr * kWave * 8;
+  const Place<kRuns> at_(sh);
+  const int64_t row = (int64_t)blockIdx.x * sh.waves_slots(blockDim.x / kWave) + at_.slot;
+  const int lane = at_.lane, step = at_.step;
   const int width = row < a.rows ? (int)a.width : 0;   // no elements of a row past the last
   const int64_t at = row < a.rows ? row : 0;
   const uint8_t* xr = row_of<kType>(a.x, at, a.x_stride);
@@ -152,7 +176,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
 #pragma unroll
     for (int e = 0; e < 8; ++e) q[0] = fused(s[i][e], s[i][e], q[0]);
   }
-  row_sum(q, lds, wave, wpr);
+  row_sum(q, lds, at_.wave, sh);
   Sum rho;
   if constexpr (kOut == kNormSame) {
     rho = 1.0f / __builtin_sqrtf(q[0] / (float)a.width + a.eps);
@@ -190,28 +214,29 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
   }
 }
 
-// Waves of a row, and runs a lane, for this width: the fewest waves that
-// need at most `most` runs a lane.
-static void row_shape(int64_t width, int most, int* wpr, int* runs) {
+// The shape for this width: the fewest waves that need at most `most` runs
+// a lane; a row that fits half a wave on as few lanes as hold it.
+static RowShape row_shape(int64_t width, int most) {
   const int64_t all = (width + 7) / 8;
-  *wpr = 1;
-  while (*wpr < kNormMaxWaves && all > (int64_t)*wpr * kWave * most) *wpr *= 2;
-  *runs = (int)((all + *wpr * kWave - 1) / (*wpr * kWave));
+  RowShape sh = {1, kWave, 1};
+  while (sh.wpr < kNormMaxWaves && all > (int64_t)sh.wpr * kWave * most) sh.wpr *= 2;
+  sh.runs = (int)((all + sh.wpr * kWave - 1) / (sh.wpr * kWave));
+  while (sh.lanes > 1 && all <= sh.lanes / 2) sh.lanes /= 2;
+  return sh;
 }
 
 template <int kType, int kOut>
 static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
-  int wpr, runs;
-  row_shape(a.width, kNormMaxRuns, &wpr, &runs);
-  const int waves = wpr > 4 ? wpr : 4, slots = waves / wpr;
+  const RowShape sh = row_shape(a.width, kNormMaxRuns);
+  const int waves = sh.wpr > 4 ? sh.wpr : 4, slots = sh.waves_slots(waves);
   const dim3 grid((unsigned)((a.rows + slots - 1) / slots)), block(waves * kWave);
-  switch (runs) {
-    case 1: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 1>, grid, block, stream, a, wpr);
-    case 2: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 2>, grid, block, stream, a, wpr);
-    case 3: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 3>, grid, block, stream, a, wpr);
-    case 4: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 4>, grid, block, stream, a, wpr);
-    case 5: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 5>, grid, block, stream, a, wpr);
-    default: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 6>, grid, block, stream, a, wpr);
+  switch (sh.runs) {
+    case 1: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 1>, grid, block, stream, a, sh);
+    case 2: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 2>, grid, block, stream, a, sh);
+    case 3: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 3>, grid, block, stream, a, sh);
+    case 4: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 4>, grid, block, stream, a, sh);
+    case 5: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 5>, grid, block, stream, a, sh);
+    default: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 6>, grid, block, stream, a, sh);
   }
 }
 
@@ -231,21 +256,23 @@ hipError_t launch_add_rmsnorm(int type, int out, const NormArgs& a, hipStream_t 
 
 // ---- backward -------------------------------------------------------------
 
+// Runs a lane above which a row gets more waves: with these the kernel takes
+// at most 128 registers, and two workgroups share a CU.
+template <int kType>
+constexpr int kBackRuns = kType == SOLFP4_F32 ? 2 : 3;
+
 // ds of every row, and each workgroup's share of dg: a workgroup of eight
-// waves (8 / wpr row slots) takes every `parts`-th run of slots rows of one
-// group, so that the chip reads one window of the operands at a time, and
+// waves takes every `parts`-th run of as many rows as it holds of one group, so that the chip reads one window of the operands at a time, and
 // keeps dg of its columns in registers; at the end the slots' sums are added
 // in slot order and stored as one row of the workspace.  All of a row's loads go out before the first use and stay as
 // they were read (converted again after the reduction: half the registers
 // of FP32 copies, twice the waves).
 template <int kType, int kRuns>
-__global__ __launch_bounds__(kNormMaxWaves * kWave) void rmsnorm_backward_kernel(NormBackArgs a, int wpr) {
+__global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 4 : 2) void rmsnorm_backward_kernel(NormBackArgs a, RowShape sh) {
   __shared__ float lds[kNormMaxWaves][2];
   __shared__ __attribute__((aligned(16))) float fold[kNormMaxWaves * kWave * 8];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int slots = kNormMaxWaves / wpr, slot = wave / wpr;
-  const int lane = (wave & (wpr - 1)) * kWave + (threadIdx.x & (kWave - 1));
-  const int step = wpr * kWave * 8;
+  const Place<kRuns> at_(sh);
+  const int slots = sh.waves_slots(kNormMaxWaves), slot = at_.slot, lane = at_.lane, step = at_.step;
   const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
   const int rows = (int)a.group_rows;
   const int64_t row0 = group * a.group_rows;
@@ -289,7 +316,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void rmsnorm_backward_kernel
         qb[1] = fused(D[e] * v[e], s[e], qb[1]);
       }
     }
-    row_sum(qb, lds, wave, wpr);
+    row_sum(qb, lds, at_.wave, sh);
     const float rho = 1.0f / __builtin_sqrtf(qb[0] / (float)a.width + a.eps);
     const float k = qb[1] / (float)a.width * rho * rho;
     uint8_t* outr = row_of<kType>(a.dx, row, a.dx_stride);
@@ -314,8 +341,8 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void rmsnorm_backward_kernel
   }
   if (!a.partial) return;
   float* part_row = a.partial + (int64_t)blockIdx.x * a.width;
-  // run by run: every slot's sums to LDS, then each thread adds `wpr` columns'
-  const int cols = wpr * kWave * 8;
+  // run by run: every slot's sums to LDS, then each thread adds some columns'
+  const int cols = sh.wpr * sh.lanes * 8;
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
     __syncthreads();
@@ -355,37 +382,38 @@ __global__ __launch_bounds__(kFoldCols * kFoldSlices) void dgain_kernel(const fl
   dgain[group * width + col] = t;
 }
 
-// Runs a lane above which a row gets more waves: with these the kernel takes
-// at most 128 registers, and two workgroups share a CU.
-template <int kType>
-constexpr int kBackRuns = kType == SOLFP4_F32 ? 2 : 3;
-
 // Workgroups a group's rows are dealt to: at most two a compute unit over all
 // groups (one round: with 516 on 256 CUs, 26574 x 2432 took 126 us, with 510
-// 107), but at least kPartMinRows rows each, so that the partial sums stay a
-// small share of the rows' bytes.
-constexpr int64_t kPartMinRows = 8;
+// 107).  Few rows go one round to a workgroup while that makes at most one a
+// CU (a round's loads, reduction and stores take 3 us), else at least eight
+// rows, so that the partial sums stay few (1311 x 3072: 328 of four rows 20.4
+// us, 164 of eight 14.8).  Up to kOnePass rounds stay on one workgroup, which
+// then needs no second launch.  (Rounds by FP32's shape for all types: the
+// workspace does not depend on the type.)
+constexpr int64_t kOnePass = 2;
 
-int64_t rmsnorm_backward_parts(int64_t rows, int64_t groups) {
+int64_t rmsnorm_backward_parts(int64_t rows, int64_t width, int64_t groups) {
   if (rows == 0 || groups == 0) return 0;
-  const int64_t per = rows / groups;
-  const int64_t parts = 2 * (int64_t)device_cu_count() / groups;
-  const int64_t most = (per + kPartMinRows - 1) / kPartMinRows;
+  const int64_t per = rows / groups, cus = device_cu_count();
+  const int64_t slots = row_shape(width, kBackRuns<SOLFP4_F32>).waves_slots(kNormMaxWaves);
+  const int64_t rounds = (per + slots - 1) / slots;
+  if (rounds <= kOnePass) return 1;
+  if (rounds * groups <= cus) return rounds;
+  const int64_t parts = 2 * cus / groups, most = slots >= 8 ? rounds : (per + 7) / 8;
   return parts < 1 ? 1 : parts < most ? parts : most;
 }
 
 template <int kType>
 static hipError_t launch_back(const NormBackArgs& a, int64_t groups, hipStream_t stream) {
-  int wpr, runs;
-  row_shape(a.width, kBackRuns<kType>, &wpr, &runs);
+  const RowShape sh = row_shape(a.width, kBackRuns<kType>);
   const dim3 grid((unsigned)(groups * a.parts)), block(kNormMaxWaves * kWave);
-  switch (runs) {
-    case 1: return launch_kernel(rmsnorm_backward_kernel<kType, 1>, grid, block, stream, a, wpr);
-    case 2: return launch_kernel(rmsnorm_backward_kernel<kType, 2>, grid, block, stream, a, wpr);
-    case 3: return launch_kernel(rmsnorm_backward_kernel<kType, 3>, grid, block, stream, a, wpr);
-    case 4: return launch_kernel(rmsnorm_backward_kernel<kType, 4>, grid, block, stream, a, wpr);
-    case 5: return launch_kernel(rmsnorm_backward_kernel<kType, 5>, grid, block, stream, a, wpr);
-    default: return launch_kernel(rmsnorm_backward_kernel<kType, 6>, grid, block, stream, a, wpr);
+  switch (sh.runs) {
+    case 1: return launch_kernel(rmsnorm_backward_kernel<kType, 1>, grid, block, stream, a, sh);
+    case 2: return launch_kernel(rmsnorm_backward_kernel<kType, 2>, grid, block, stream, a, sh);
+    case 3: return launch_kernel(rmsnorm_backward_kernel<kType, 3>, grid, block, stream, a, sh);
+    case 4: return launch_kernel(rmsnorm_backward_kernel<kType, 4>, grid, block, stream, a, sh);
+    case 5: return launch_kernel(rmsnorm_backward_kernel<kType, 5>, grid, block, stream, a, sh);
+    default: return launch_kernel(rmsnorm_backward_kernel<kType, 6>, grid, block, stream, a, sh);
   }
 }
 
@@ -393,7 +421,8 @@ hipError_t launch_rmsnorm_backward(int type, NormBackArgs a, float* dgain, hipSt
   const int64_t groups = a.groups;
   if (a.width == 0 || groups == 0) return hipSuccess;
   hipError_t e = hipSuccess;
-  const int64_t parts = rmsnorm_backward_parts(a.rows, groups);
+  const int64_t parts = rmsnorm_backward_parts(a.rows, a.width, groups);
+  if (parts == 1 && dgain) a.partial = dgain;   // the one workgroup's sums are the group's
   if (parts) {
     a.group_rows = a.rows / groups;
     a.parts = (int)parts;
@@ -401,7 +430,7 @@ hipError_t launch_rmsnorm_backward(int type, NormBackArgs a, float* dgain, hipSt
     else if (type == SOLFP4_F16) e = launch_back<SOLFP4_F16>(a, groups, stream);
     else e = launch_back<SOLFP4_F32>(a, groups, stream);
   }
-  if (e != hipSuccess || !dgain) return e;
+  if (e != hipSuccess || !dgain || parts == 1) return e;
   const dim3 grid((unsigned)((a.width + kFoldCols - 1) / kFoldCols), (unsigned)groups);
   return launch_kernel(dgain_kernel, grid, dim3(kFoldCols * kFoldSlices), stream, (const float*)a.partial, dgain,
                        a.width, (int)parts);

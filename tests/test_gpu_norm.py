@@ -296,3 +296,39 @@ def test_graph_replay():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, step()))
+
+
+# ---- rows that share a wave -----------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [1, 5, 8, 9, 16, 31, 32, 64, 65, 96, 128, 200, 255, 256, 257])
+@pytest.mark.parametrize("rows", [1, 63, 64, 1030])
+def test_narrow_rows(dtype, width, rows):
+    """As few lanes a row as hold it: every lane count, rows that fill no
+    workgroup, one NaN row among them."""
+    x, r, dy = (draw(width + i, rows, width, dtype) for i in range(3))
+    g = 1 + draw(width + 3, 1, width, dtype, 0.3)[0]
+    s, y = R.add_rmsnorm(f64(x), f64(r), f64(g))
+    out, total = sol.add_rmsnorm(x, r, g)
+    check(out, y, REL, 0.0, dtype, "norm")
+    check(total, s, 0.0, np.abs(s) * 2.0 ** -24, dtype, "sum")
+    check_backward(dy, x, g, r, dtype)
+    check_backward(dy, x, None, None, dtype)
+    if rows > 1:
+        x[rows // 2, width // 2] = float("nan")
+        bad, _ = sol.add_rmsnorm(x, r, g)
+        keep = [i for i in range(rows) if i != rows // 2]
+        assert torch.equal(bad[keep], out[keep]) and torch.all(torch.isnan(bad[rows // 2]))
+    if width % 32 == 0 and rows > 1:
+        c = sol.mxfp8_add_rmsnorm(x[:rows // 2], r[:rows // 2], g)
+        assert np.linalg.norm(R.mxfp8_values(c[0].cpu().numpy(), c[1].cpu().numpy()) - y[:rows // 2]) <= \
+            2.0 ** -4 * np.linalg.norm(y[:rows // 2])
+
+
+@pytest.mark.parametrize("rows,groups,width", [(4, 1, 12000), (33, 1, 4000), (64, 2, 136), (256, 1, 128), (257, 1, 128),
+                                               (8192, 4, 128), (96, 96, 40)])
+def test_backward_one_and_several_workgroups(rows, groups, width):
+    """Around the largest row count that one workgroup takes alone."""
+    for dtype in TYPES:
+        dy, s = draw(rows, rows, width, dtype), draw(rows + 1, rows, width, dtype)
+        check_backward(dy, s, draw(rows + 2, groups, width, dtype), None, dtype)
