@@ -60,7 +60,8 @@ extern "C" {
 #define SOLFP4_EINVAL (-1)     /* null pointer where data is needed, negative size */
 #define SOLFP4_ESHAPE (-2)     /* K not a multiple of the block (16 NVFP4, 32 MXFP4), a size of
                                   2^31 or more, or a GEMM with K of 2^24 or more or N of 2^22
-                                  or more */
+                                  or more; for the operators around the linears, a size beyond
+                                  what the call states */
 #define SOLFP4_EALIGN (-3)     /* a pointer is not 16-byte aligned */
 #define SOLFP4_EWORKSPACE (-4) /* workspace missing or smaller than the *_workspace_bytes query */
 #define SOLFP4_EHIP (-5)       /* a HIP launch reported an error */
@@ -395,7 +396,8 @@ SOLFP4_API int mxfp4_linear(const uint16_t* x, const uint8_t* w_codes, const uin
  *            residual, ignored without one.  May be x or residual (same
  *            address and stride)
  *   out      [rows][width], written; must not overlap the inputs or sum,
- *            except that it may be x
+ *            except that it may be x.  Overlaps that are not allowed are
+ *            refused (SOLFP4_EINVAL)
  *
  * The norm is taken of the FP32 sum, not of its rounded form.  width is at
  * most 24576.  A row with a NaN or an infinity gives NaN; the squares are

@@ -142,7 +142,8 @@ const char* solfp4_strerror(int status) {
     case SOLFP4_EINVAL: return "invalid argument (null pointer or negative size)";
     case SOLFP4_ESHAPE:
       return "unsupported shape (K must be a multiple of 16, or of 32 for MXFP4; sizes below 2^31; "
-             "GEMM K below 2^24 and N below 2^22)";
+             "GEMM K below 2^24 and N below 2^22; norm rows of at most 24576 elements, dealt to groups "
+             "evenly; an even number of rotated elements within the head)";
     case SOLFP4_EALIGN: return "pointer not 16-byte aligned";
     case SOLFP4_EWORKSPACE: return "workspace missing or too small";
     case SOLFP4_EHIP: return "HIP kernel launch failed";

@@ -52,6 +52,12 @@ Extent extent(int type, const void* p, int64_t stride, int64_t rows, int64_t wid
 
 bool overlap(Extent a, Extent b) { return a.lo < b.hi && b.lo < a.hi; }
 
+// Whether the gain lies apart from rows that the call writes.
+bool gain_apart(int type, const void* gain, int64_t gain_stride, int64_t groups, const void* out, int64_t out_stride,
+                int64_t rows, int64_t width) {
+  return !gain || !overlap(extent(type, gain, gain_stride, groups, width), extent(type, out, out_stride, rows, width));
+}
+
 // The two are one operand (each element is read before it is written) or apart.
 bool same_or_apart(int type, const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t rows,
                    int64_t width) {
@@ -76,10 +82,14 @@ int norm_checks(int type, const solfp4::NormArgs& a, int64_t groups, int out) {
       return SOLFP4_EINVAL;
   }
   if (a.gain && (rc = check_rows(type, a.gain, a.gain_stride, groups, a.width, false))) return rc;
+  if (a.residual && !gain_apart(type, a.gain, a.gain_stride, groups, a.sum, a.sum_stride, a.rows, a.width))
+    return SOLFP4_EINVAL;
   if (out == solfp4::kNormSame) {
     if ((rc = check_rows(type, a.out, a.out_stride, a.rows, a.width, true))) return rc;
     const Extent o = extent(type, a.out, a.out_stride, a.rows, a.width);
-    if (!same_or_apart(type, a.x, a.x_stride, a.out, a.out_stride, a.rows, a.width)) return SOLFP4_EINVAL;
+    if (!same_or_apart(type, a.x, a.x_stride, a.out, a.out_stride, a.rows, a.width) ||
+        !gain_apart(type, a.gain, a.gain_stride, groups, a.out, a.out_stride, a.rows, a.width))
+      return SOLFP4_EINVAL;
     if (a.residual && (overlap(o, extent(type, a.residual, a.residual_stride, a.rows, a.width)) ||
                        overlap(o, extent(type, a.sum, a.sum_stride, a.rows, a.width))))
       return SOLFP4_EINVAL;
@@ -221,7 +231,8 @@ int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const v
     if ((rc = check_rows(type, dx, dx_stride, rows, width, true))) return rc;
     if (!same_or_apart(type, dy, dy_stride, dx, dx_stride, rows, width) ||
         !same_or_apart(type, x, x_stride, dx, dx_stride, rows, width) ||
-        (dsum && !same_or_apart(type, dsum, dsum_stride, dx, dx_stride, rows, width)))
+        (dsum && !same_or_apart(type, dsum, dsum_stride, dx, dx_stride, rows, width)) ||
+        !gain_apart(type, gain, gain_stride, groups, dx, dx_stride, rows, width))
       return SOLFP4_EINVAL;
   }
   if (dgain) {

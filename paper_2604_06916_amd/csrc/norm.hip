@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 
   const Place<kRuns> at_(sh);
   const int slots = sh.waves_slots(kNormMaxWaves), slot = at_.slot, lane = at_.lane, step = at_.step;
   const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
-  const int rows = (int)a.group_rows;
+  const uint32_t rows = (uint32_t)a.group_rows;   // a hop past its end still fits 32 bits
   const int64_t row0 = group * a.group_rows;
   Run<kType> g[kRuns];
   const uint8_t* gr = row_of<kType>(a.gain, group, a.gain_stride);
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 
     if (a.gain && n > 0) g[i] = load_run<kType>(gr, col, n);
   }
   float dg[kRuns][8] = {};
-  for (int base = part * slots; base < rows; base += a.parts * slots) {
+  for (uint32_t base = part * slots; base < rows; base += a.parts * slots) {
     const bool in = base + slot < rows;
     const int64_t row = row0 + (in ? base + slot : base);
     const int width = in ? (int)a.width : 0;

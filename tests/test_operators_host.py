@@ -125,6 +125,11 @@ def test_weight_linear_refusals(kind):
         assert call(xs=None) == EINVAL and call(xs=at(4)) == EALIGN
 
 
+def test_gain_over_what_is_written_is_refused():
+    assert norm(g=apart(4)) == EINVAL and norm(g=apart(3)) == EINVAL and back(g=apart(4)) == EINVAL
+    assert norm(g=at((4 << 32) + 2 * 64 * 3)) == EINVAL
+
+
 # ---- the binding ----------------------------------------------------------
 
 class Reached(Exception):
