@@ -8,12 +8,16 @@
 // (y is rounded once, not norm-of-a-rounded-sum), and the stored sum is that
 // sum rounded once.
 //
-// A row belongs to `wpr` waves (1, 2, 4 or 8; as few as hold it in
-// kNormMaxRuns runs of 8 elements a lane), so a row is read once, stays in
-// registers, and for most widths is reduced inside one wave without a
-// barrier.  Rows of at most 256 elements (a head's q or k) share a wave: 4 to
-// 32 lanes a row, or fewer (kRuns == 1).  Bound by memory: 8 bytes an element in BF16 (7.03 with MXFP8
-// output).
+// A row belongs to `wpr` waves (1, 2, 4 or 8; as few as hold it in kNormRuns,
+// at most kNormMaxRuns, runs of 8 elements a lane), so a row is read once and
+// stays in registers between the sum and the output.  Rows of at most 256
+// elements (a head's q or k) share a wave: 32 lanes a row or fewer
+// (kRuns == 1).
+//
+// Bound by memory: 8 bytes an element in BF16 with a residual, 7.03 with MXFP8
+// output.  BF16, 8192 x 2240 in 8 groups 26.1 us, 5.6 TB/s; 18432 x 3072 to MXFP8
+// 71.8 us, 5.5 TB/s (a 1 GB copy moves 5.0, a 0.2 GB one 5.4); one row of 1152
+// 3.2 us, a launch.
 #include "elements.h"
 #include "kernels.h"
 
@@ -214,6 +218,14 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
   }
 }
 
+// Runs a lane above which a row of the forward pass gets more waves.  More of
+// a row a lane costs registers and so waves in flight, more waves a barrier:
+// BF16 8192 x 2240 takes 26.1 us with up to three and 27.6 with six (25.5 with
+// two, but 9000 x 1235 18.7 and 22.6), FP32 9216 x 3072 80.8, 84.7 and 97.1 with
+// one, two and six.
+template <int kType>
+constexpr int kNormRuns = kType == SOLFP4_F32 ? 1 : 3;
+
 // The shape for this width: the fewest waves that need at most `most` runs
 // a lane; a row that fits half a wave on as few lanes as hold it.
 static RowShape row_shape(int64_t width, int most) {
@@ -227,7 +239,7 @@ static RowShape row_shape(int64_t width, int most) {
 
 template <int kType, int kOut>
 static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
-  const RowShape sh = row_shape(a.width, kNormMaxRuns);
+  const RowShape sh = row_shape(a.width, kNormRuns<kType>);
   const int waves = sh.wpr > 4 ? sh.wpr : 4, slots = sh.waves_slots(waves);
   const dim3 grid((unsigned)((a.rows + slots - 1) / slots)), block(waves * kWave);
   switch (sh.runs) {
@@ -262,15 +274,21 @@ template <int kType>
 constexpr int kBackRuns = kType == SOLFP4_F32 ? 2 : 3;
 
 // ds of every row, and each workgroup's share of dg: a workgroup of eight
-// waves takes every `parts`-th run of as many rows as it holds of one group, so that the chip reads one window of the operands at a time, and
-// keeps dg of its columns in registers; at the end the slots' sums are added
-// in slot order and stored as one row of the workspace.  All of a row's loads go out before the first use and stay as
-// they were read (converted again after the reduction: half the registers
-// of FP32 copies, twice the waves).
+// waves takes every `parts`-th run of as many rows as it holds of one group,
+// so that the chip reads one window of the operands at a time (contiguous
+// blocks of rows a workgroup were slower), and keeps dg of its columns in
+// registers; at the end the slots' sums are added in slot order and stored as
+// one row of the workspace.  All of a row's loads go out before the first use
+// and stay as they were read (converted again after the reduction: half the
+// registers of FP32 copies, twice the waves).  Holding the next row's loads
+// beside them was slower, 130 us for 126, by the registers.
+//
+// Bound by memory, 8 bytes an element in BF16 with dsum: 26574 x 2432 in 6
+// groups 108 us with the sums of dg, 4.8 TB/s; FP32 777 x 1235 8.1 + 2.7 us.
 template <int kType, int kRuns>
 __global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 4 : 2) void rmsnorm_backward_kernel(NormBackArgs a, RowShape sh) {
   __shared__ float lds[kNormMaxWaves][2];
-  __shared__ __attribute__((aligned(16))) float fold[kNormMaxWaves * kWave * 8];
+  __shared__ __attribute__((aligned(16))) float fold[kRuns][kNormMaxWaves * kWave * 8];
   const Place<kRuns> at_(sh);
   const int slots = sh.waves_slots(kNormMaxWaves), slot = at_.slot, lane = at_.lane, step = at_.step;
   const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
@@ -341,26 +359,30 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 
   }
   if (!a.partial) return;
   float* part_row = a.partial + (int64_t)blockIdx.x * a.width;
-  // run by run: every slot's sums to LDS, then each thread adds some columns'
+  // every slot's sums to LDS, then each thread adds some columns'
   const int cols = sh.wpr * sh.lanes * 8;
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    __syncthreads();
-    floatx4_t* to = reinterpret_cast<floatx4_t*>(fold + slot * cols + lane * 8);
+    floatx4_t* to = reinterpret_cast<floatx4_t*>(fold[i] + slot * cols + lane * 8);
     to[0] = floatx4_t{dg[i][0], dg[i][1], dg[i][2], dg[i][3]};
     to[1] = floatx4_t{dg[i][4], dg[i][5], dg[i][6], dg[i][7]};
-    __syncthreads();
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
     for (int c = threadIdx.x; c < cols; c += kNormMaxWaves * kWave) {
-      float t = fold[c];
-      for (int z = 1; z < slots; ++z) t += fold[z * cols + c];
+      float t = fold[i][c];
+      for (int z = 1; z < slots; ++z) t += fold[i][z * cols + c];
       if (i * step + c < a.width) part_row[i * step + c] = t;
     }
   }
 }
 
 // dg[group][col] = sum of the group's parts, each of kFoldSlices threads
-// taking every kFoldSlices-th part, their sums added in slice order.
-constexpr int kFoldCols = 64, kFoldSlices = 16;
+// taking every kFoldSlices-th part, their sums added in slice order; a
+// thread's loads go out kFoldDeep at a time, so that up to 256 parts cost one
+// round trip (195 parts of 1235 columns: 2.7 us, 3.2 in a loop of eight).
+constexpr int kFoldCols = 64, kFoldSlices = 16, kFoldDeep = 16;
 
 __global__ __launch_bounds__(kFoldCols * kFoldSlices) void dgain_kernel(const float* __restrict__ partial,
                                                                          float* __restrict__ dgain, int64_t width,
@@ -371,8 +393,13 @@ __global__ __launch_bounds__(kFoldCols * kFoldSlices) void dgain_kernel(const fl
   float t = 0.0f;
   if (col < width) {
     const float* p = partial + group * parts * width + col;
-#pragma unroll 8
-    for (int i = z; i < parts; i += kFoldSlices) t += p[i * width];
+    for (int i = z; i < parts; i += kFoldSlices * kFoldDeep) {
+      float v[kFoldDeep];
+#pragma unroll
+      for (int u = 0; u < kFoldDeep; ++u) v[u] = i + u * kFoldSlices < parts ? p[(i + u * kFoldSlices) * width] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < kFoldDeep; ++u) t += v[u];
+    }
   }
   sums[z][c] = t;
   __syncthreads();
@@ -382,25 +409,23 @@ __global__ __launch_bounds__(kFoldCols * kFoldSlices) void dgain_kernel(const fl
   dgain[group * width + col] = t;
 }
 
-// Workgroups a group's rows are dealt to: at most two a compute unit over all
-// groups (one round: with 516 on 256 CUs, 26574 x 2432 took 126 us, with 510
-// 107).  Few rows go one round to a workgroup while that makes at most one a
-// CU (a round's loads, reduction and stores take 3 us), else at least eight
-// rows, so that the partial sums stay few (1311 x 3072: 328 of four rows 20.4
-// us, 164 of eight 14.8).  Up to kOnePass rounds stay on one workgroup, which
-// then needs no second launch.  (Rounds by FP32's shape for all types: the
-// workspace does not depend on the type.)
-constexpr int64_t kOnePass = 2;
+// Workgroups a group's rows are dealt to: over all groups at most two a
+// compute unit (one round: with 516 on 256 CUs, 26574 x 2432 took 126 us, with
+// 510 107), or one where they then take fewer than kBackDeep rounds of rows
+// each (FP32, one and two a CU: 1311 x 3072 18.7 and 18.5 us, 777 x 9728 36.0 and
+// 40.8, but 2304 x 5600, nine rounds, 47.3 and 43.9).  Up to kOnePass rounds
+// stay on one workgroup, which then needs no second launch.  (Rounds by FP32's
+// shape for all types: the workspace does not depend on the type.)
+constexpr int64_t kOnePass = 2, kBackDeep = 8;
 
 int64_t rmsnorm_backward_parts(int64_t rows, int64_t width, int64_t groups) {
   if (rows == 0 || groups == 0) return 0;
-  const int64_t per = rows / groups, cus = device_cu_count();
+  const int64_t cus = device_cu_count();
   const int64_t slots = row_shape(width, kBackRuns<SOLFP4_F32>).waves_slots(kNormMaxWaves);
-  const int64_t rounds = (per + slots - 1) / slots;
+  const int64_t rounds = (rows / groups + slots - 1) / slots;
   if (rounds <= kOnePass) return 1;
-  if (rounds * groups <= cus) return rounds;
-  const int64_t parts = 2 * cus / groups, most = slots >= 8 ? rounds : (per + 7) / 8;
-  return parts < 1 ? 1 : parts < most ? parts : most;
+  const int64_t parts = (rounds * groups < kBackDeep * cus ? cus : 2 * cus) / groups;
+  return parts < 1 ? 1 : parts < rounds ? parts : rounds;
 }
 
 template <int kType>
