@@ -3,8 +3,10 @@
 //
 //   out[m][n] = bf16(alpha * sum_k x[m][k] (s q)[n][k] + bias[n])
 //
-// Bound by reading the weight once.  A workgroup makes 16 NT outputs of
-// 16 MT tokens; its waves share the reduction: each takes a run of K steps
+// Bound by reading the weight once: 4 x 18432 x 3072 NVFP4 8.9 us, 3.6 TB/s, of
+// which loads, scales and the reduction alone take 7.5 to 8.5; 64 x 9728 x 2432
+// MXFP8 10.4 us, the activations' way through L2 and LDS to 304 tiles of columns.
+// A workgroup makes 16 NT outputs of 16 MT tokens; its waves share the reduction: each takes a run of K steps
 // of 128, and their FP32 partial sums are added in wave order through LDS.
 // So even a narrow layer has enough 16-byte loads in flight, and the result
 // does not depend on timing.
@@ -74,9 +76,16 @@ __device__ __forceinline__ bf16x8_t weights8(uint32_t c, float s) {
 // way.  Here 4 (weights), 16 (BF16) or 8 (MXFP8) neighbouring lanes read one
 // row's 64, 256 or 128 bytes of a step.
 //
-// kWhole: K % 128 == 0, no partial step.  U steps are in flight in registers; the LDS buffer holds one.  Pieces of
-// 16 bytes are stored at their number XOR the row's, so that 16 lanes that
-// read one piece of 16 rows reach all banks.
+// Loads of the activations alone in operand order, 64 bytes of a row by four
+// lanes, were slower still (32 x 9728 x 2432 NVFP4 12.4 us for 9.2): the address
+// path takes them at half its rate.
+//
+// kWhole: K % 128 == 0, no partial step.  One step is in flight in registers
+// and one in the LDS buffer (two or four in registers: slower or the same).
+// Pieces of 16 bytes are stored at their number XOR the row's, so that 16
+// lanes that read one piece of 16 rows reach all banks.  Scales come four
+// steps at a time for each wave by itself (all waves' steps at once by the
+// workgroup: slower, by the barrier).
 template <int kFormat, bool kX8, bool kWhole, int MT, int NT, int XR, int W>
 __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearArgs a, int tiles_m) {
   constexpr bool kNv = kFormat == SOLFP4_FORMAT_NVFP4;
@@ -336,34 +345,54 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
   }
 }
 
-// The tile of a shape: up to 16 tokens 16 x 16 outputs a workgroup; beyond,
-// 32 tokens and 16 or 32 columns (more than 32 tokens a tile won nowhere by
-// more than a tenth, 64 x 9728 x 2432).  Of these, 32 columns halve the
-// activations' way from L2 but also the workgroups; with at most half a
-// workgroup a CU 16 are faster (32 x 2432 x 2432 NVFP4 5.4 against 6.3 us), and
-// past one a CU four waves, three workgroups of which fit a CU, beat eight
-// (64 x 9728 x 2432 13.1 against 17.0; below, eight win: 32 x 4864 x 2432 6.5
-// against 7.1).
+// The tile of a shape (us: NVFP4, MXFP4, MXFP8 x MXFP4).  A step brings 256 bytes a
+// token and 64 a column into a wave's buffer, so wide tiles save the
+// activations' way from L2 and LDS; narrow ones make more workgroups and
+// shorter steps.
+//
+// Up to 16 tokens, 16 columns a workgroup while that is at most one a CU.
+// Past it, 32 columns (16 x 4500 x 12288 16.1, 14.9, 14.7 with 16 columns, 12.9, 10.6,
+// 10.7 with 32), of eight waves up to one workgroup a CU and of four beyond (16 x
+// 8300 x 5600 13.8, 12.2, 12.1 and 13.2, 11.7, 11.7), of which more fit a CU.  So `few`
+// tokens that one load brings (4 in BF16, 8 in MXFP8) keep 16 columns: 16 waves up
+// to one workgroup a CU (4 x 3072 x 12288 8.1, 6.9, 7.7 with 8 and 7.5, 6.2, 6.4
+// with 16), then eight (4 x 4500 x 12288 13.0, 10.6, 11.0 with 16 and 11.8, 9.6,
+// 9.9 with 8), and four once eight would start a second round of workgroups
+// (more than four a CU: 8 x 18000 x 512 5.6, 5.0, 4.8 and 4.2, 3.9, 4.1).
+//
+// Beyond, 32 tokens a workgroup, and 16, 32 or 64 columns.  16 up to half a CU
+// of 32-column workgroups (32 x 2432 x 2432 NVFP4 5.4 us, 6.3 with 32), 32 up to a
+// whole one (64 x 3072 x 12288 17.8, 15.4, 15.8; 23.5, 21.9, 23.2 with 16), 64 while
+// those are at most one a CU (64 x 4500 x 12288 25.9, 20.8, 20.9; 30.7, 26.8, 28.0
+// with 32 and four waves, the best of the others), and past that 32 again, of four
+// waves (64 x 9728 x 2432 12.8, 11.2, 10.4; 16.6, 14.3, 10.6 with eight, 14.9, 11.8,
+// 11.2 with 64 columns).
 struct Tile {
   int mt, nt, waves;
+  int64_t groups(int64_t M, int64_t N) const { return ((M + 16 * mt - 1) / (16 * mt)) * ((N + 16 * nt - 1) / (16 * nt)); }
 };
 
-static Tile tile_of(int64_t M, int64_t N) {
-  if (M <= 16) return {1, 1, 8};
-  const int64_t wide = ((M + 31) / 32) * ((N + 31) / 32), cus = device_cu_count();
+static Tile tile_of(int64_t M, int64_t N, bool few) {
+  const int64_t cus = device_cu_count();
+  if (M <= 16) {
+    const int64_t narrow = Tile{1, 1, 0}.groups(M, N);
+    if (few) return {1, 1, narrow <= cus ? 16 : narrow <= 4 * cus ? 8 : 4};
+    if (narrow <= cus) return {1, 1, 8};
+    return {1, 2, Tile{1, 2, 0}.groups(M, N) <= cus ? 8 : 4};
+  }
+  const int64_t wide = Tile{2, 2, 0}.groups(M, N);
   if (wide <= cus / 2) return {2, 1, 8};
-  return {2, 2, wide <= cus ? 8 : 4};
+  if (wide <= cus) return {2, 2, 8};
+  if (Tile{2, 4, 0}.groups(M, N) <= cus) return {2, 4, 8};
+  return {2, 2, 4};
 }
 
-int64_t weight_linear_groups(int64_t M, int64_t N) {
-  const Tile t = tile_of(M, N);
-  return ((N + 16 * t.nt - 1) / (16 * t.nt)) * ((M + 16 * t.mt - 1) / (16 * t.mt));
-}
+int64_t weight_linear_groups(int64_t M, int64_t N) { return tile_of(M, N, true).groups(M, N); }
 
 template <int kFormat, bool kX8, int MT, int NT, int XR, int W>
 static hipError_t launch_tile(const WeightLinearArgs& a, hipStream_t stream) {
   const int tiles_m = (int)((a.M + 16 * MT - 1) / (16 * MT));
-  const dim3 grid((unsigned)weight_linear_groups(a.M, a.N)), block(W * kWave);
+  const dim3 grid((unsigned)Tile{MT, NT, W}.groups(a.M, a.N)), block(W * kWave);
   if (a.K % kWLStep == 0)
     return launch_kernel(weight_linear_kernel<kFormat, kX8, true, MT, NT, XR, W>, grid, block, stream, a, tiles_m);
   return launch_kernel(weight_linear_kernel<kFormat, kX8, false, MT, NT, XR, W>, grid, block, stream, a, tiles_m);
@@ -372,11 +401,21 @@ static hipError_t launch_tile(const WeightLinearArgs& a, hipStream_t stream) {
 template <int kFormat, bool kX8>
 static hipError_t launch_format(const WeightLinearArgs& a, hipStream_t stream) {
   constexpr int kFull = kX8 ? 2 : 4;   // loads of 16 tokens' step
-  const Tile t = tile_of(a.M, a.N);
   // as few activation rows as one load brings need no more LDS than that
-  if (a.M <= 16 / kFull) return launch_tile<kFormat, kX8, 1, 1, 1, 8>(a, stream);
-  if (t.mt == 1) return launch_tile<kFormat, kX8, 1, 1, kFull, 8>(a, stream);
+  const bool few = a.M <= 16 / kFull;
+  const Tile t = tile_of(a.M, a.N, few);
+  if (few) {
+    if (t.waves == 16) return launch_tile<kFormat, kX8, 1, 1, 1, 16>(a, stream);
+    if (t.waves == 8) return launch_tile<kFormat, kX8, 1, 1, 1, 8>(a, stream);
+    return launch_tile<kFormat, kX8, 1, 1, 1, 4>(a, stream);
+  }
+  if (t.mt == 1) {
+    if (t.nt == 1) return launch_tile<kFormat, kX8, 1, 1, kFull, 8>(a, stream);
+    if (t.waves == 8) return launch_tile<kFormat, kX8, 1, 2, kFull, 8>(a, stream);
+    return launch_tile<kFormat, kX8, 1, 2, kFull, 4>(a, stream);
+  }
   if (t.nt == 1) return launch_tile<kFormat, kX8, 2, 1, 2 * kFull, 8>(a, stream);
+  if (t.nt == 4) return launch_tile<kFormat, kX8, 2, 4, 2 * kFull, 8>(a, stream);
   if (t.waves == 8) return launch_tile<kFormat, kX8, 2, 2, 2 * kFull, 8>(a, stream);
   return launch_tile<kFormat, kX8, 2, 2, 2 * kFull, 4>(a, stream);
 }

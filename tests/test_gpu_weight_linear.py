@@ -86,6 +86,16 @@ def test_layer_sizes(kind, M, N, K):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("M,N,K", [(3, 700, 1056), (3, 4117, 544), (2, 16401, 288), (16, 700, 928), (16, 4117, 1056),
+                                   (9, 8209, 288), (40, 1235, 416), (64, 3001, 672), (64, 4499, 1184), (33, 9001, 288)])
+def test_every_tile(kind, M, N, K):
+    """Ragged shapes on either side of each change of tile (on 256 compute units)."""
+    check(kind, M, N, K, 800 + M)
+    if kind == "nvfp4":
+        check(kind, M, N, K + 16, 900 + M, bias=False)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_empty_sizes(kind):
     for M, N, K in ((0, 16, 32), (3, 0, 32), (0, 0, 0)):
         x, _ = activations(kind, M, K, 1) if K else ((torch.empty(M, 0, dtype=torch.uint8 if kind == "mxfp8" else
