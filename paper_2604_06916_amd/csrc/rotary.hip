@@ -10,8 +10,12 @@
 // A wave takes the heads of one token (or, where they are few, of several):
 // a lane one 16-byte piece of every `slots`-th head, or the piece and its
 // partner R/2 elements further on, so its cosines and sines are read once for
-// all of them, and the loads of kRotaryHeads heads go out together.  Bound by
-// memory: each element is read and written once.
+// all of them, and the loads of kRotaryHeads heads go out together.
+//
+// Bound by memory: each element is read and written once.  BF16, 18432 tokens
+// of 24 + 24 heads of 128, interleaved: 84 us, 5.4 TB/s (a 1 GB copy moves 5.0, a
+// 0.2 GB one 5.4); F16, 1998 tokens of 19 + 19 heads, 80 of 128 turned, positions
+// given: 8.8 us in the caches, 4.5 TB/s; one token 2.4 us, a launch.
 #include "elements.h"
 #include "kernels.h"
 
@@ -86,7 +90,11 @@ __device__ __forceinline__ void store_piece(uint8_t* p, int n, u32x4_t r) {
   }
 }
 
-constexpr int kRotaryHeads = 2;   // heads of a lane at most, all in flight together
+// Heads of a lane at most, all in flight together: more share the turns'
+// loads, fewer leave more waves (18432 tokens of 48 heads of 128, BF16
+// interleaved and 9000 in FP32, 64 turned: 107 and 113 us with one, 86 and 87 with
+// two, 84 and 92 with three, 91 and 128 with four, 155 and 181 with six).
+constexpr int kRotaryHeads = 2;
 
 // n of the kPairs floats at p, the rest zero
 template <int kPairs>
