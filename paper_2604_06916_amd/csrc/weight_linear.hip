@@ -5,7 +5,7 @@
 //
 // Bound by reading the weight once: 4 x 18432 x 3072 NVFP4 8.9 us, 3.6 TB/s, of
 // which loads, scales and the reduction alone take 7.5 to 8.5; 64 x 9728 x 2432
-// MXFP8 10.4 us, the activations' way through L2 and LDS to 304 tiles of columns.
+// MXFP8 9.7 us, the activations' way through L2 and LDS to 304 tiles of columns.
 // A workgroup makes 16 NT outputs of 16 MT tokens; its waves share the reduction: each takes a run of K steps
 // of 128, and their FP32 partial sums are added in wave order through LDS.
 // So even a narrow layer has enough 16-byte loads in flight, and the result
@@ -98,9 +98,11 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);   // uniform: offsets by step stay scalar
   const int r = lane & 15, g = lane >> 4;
-  const int tile_n = tiles_m == 1 ? blockIdx.x : blockIdx.x / tiles_m;
-  const int64_t n0 = (int64_t)tile_n * (16 * NT);
-  const int64_t m0 = (int64_t)(blockIdx.x - tile_n * tiles_m) * (16 * MT);
+  // the tiles of the same columns on one XCD, whose L2 then gets their weights
+  // once (64 x 9728 x 2432 MXFP8 10.4 us and 27 MB read, 9.7 so)
+  int tile_m = 0, tile_n = blockIdx.x;
+  if (tiles_m > 1) tile_coords(tiles_m, gridDim.x / tiles_m, tile_m, tile_n);
+  const int64_t n0 = (int64_t)tile_n * (16 * NT), m0 = (int64_t)tile_m * (16 * MT);
   // rows of this tile inside the operands
   const int rows_n = a.N - n0 < 16 * NT ? (int)(a.N - n0) : 16 * NT;
   const int rows_m = a.M - m0 < 16 * MT ? (int)(a.M - m0) : 16 * MT;
@@ -361,12 +363,12 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
 // (more than four a CU: 8 x 18000 x 512 5.6, 5.0, 4.8 and 4.2, 3.9, 4.1).
 //
 // Beyond, 32 tokens a workgroup, and 16, 32 or 64 columns.  16 up to half a CU
-// of 32-column workgroups (32 x 2432 x 2432 NVFP4 5.4 us, 6.3 with 32), 32 up to a
-// whole one (64 x 3072 x 12288 17.8, 15.4, 15.8; 23.5, 21.9, 23.2 with 16), 64 while
-// those are at most one a CU (64 x 4500 x 12288 25.9, 20.8, 20.9; 30.7, 26.8, 28.0
-// with 32 and four waves, the best of the others), and past that 32 again, of four
-// waves (64 x 9728 x 2432 12.8, 11.2, 10.4; 16.6, 14.3, 10.6 with eight, 14.9, 11.8,
-// 11.2 with 64 columns).
+// of 32-column workgroups (64 x 1235 x 9728 11.4, 10.4, 9.0; 14.5, 12.0, 10.9 with
+// 32), 32 up to a whole one (64 x 3072 x 12288 17.6, 14.5, 14.7; 22.8, 21.2, 22.3
+// with 16), 64 while those are at most one a CU (64 x 4500 x 12288 25.6, 19.8, 19.9;
+// 30.5, 24.5, 25.9 with 32 and four waves, the best of the others), and past that
+// 32 again, of four waves (64 x 9728 x 2432 12.3, 10.6, 9.8; 16.4, 14.1, 10.5 with
+// eight, 13.8, 10.8, 10.2 with 64 columns).
 struct Tile {
   int mt, nt, waves;
   int64_t groups(int64_t M, int64_t N) const { return ((M + 16 * mt - 1) / (16 * mt)) * ((N + 16 * nt - 1) / (16 * nt)); }
