@@ -6,10 +6,10 @@
 // Bound by reading the weight once: 4 x 18432 x 3072 NVFP4 8.9 us, 3.6 TB/s, of
 // which loads, scales and the reduction alone take 7.5 to 8.5; 64 x 9728 x 2432
 // MXFP8 9.7 us, the activations' way through L2 and LDS to 304 tiles of columns.
-// A workgroup makes 16 NT outputs of 16 MT tokens; its waves share the reduction: each takes a run of K steps
-// of 128, and their FP32 partial sums are added in wave order through LDS.
-// So even a narrow layer has enough 16-byte loads in flight, and the result
-// does not depend on timing.
+// A workgroup makes 16 NT outputs of 16 MT tokens; its waves share the
+// reduction: each takes a run of K steps of 128, and their FP32 partial sums
+// are added in wave order through LDS.  So even a narrow layer has enough
+// 16-byte loads in flight, and the result does not depend on timing.
 //
 // A lane holds 32 consecutive weights of one row a step (16 bytes of codes);
 // lane group g of four takes weights 32 g .. 32 g + 31.  For BF16 activations
