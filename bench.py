@@ -85,6 +85,9 @@ KERNEL_SOURCES = {
     "mx_gemm.hip": ("mx_gemm.hip", "device_common.h"),
     "quantize.hip": ("quantize.hip", "device_common.h"),
     "mx_quantize.hip": ("mx_quantize.hip", "device_common.h"),
+    "norm.hip": ("norm.hip", "elements.h", "device_common.h"),
+    "rotary.hip": ("rotary.hip", "elements.h", "device_common.h"),
+    "weight_linear.hip": ("weight_linear.hip", "elements.h", "device_common.h"),
 }
 
 
