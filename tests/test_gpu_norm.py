@@ -332,3 +332,31 @@ def test_backward_one_and_several_workgroups(rows, groups, width):
     for dtype in TYPES:
         dy, s = draw(rows, rows, width, dtype), draw(rows + 1, rows, width, dtype)
         check_backward(dy, s, draw(rows + 2, groups, width, dtype), None, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [1000, 2100, 4101, 9000, 16390, 20480, 22528])
+def test_widths_between(dtype, width):
+    """Widths at which a lane holds one to six runs of a row on one to eight waves."""
+    rows = 9
+    x, r = draw(width, rows, width, dtype), draw(width + 1, rows, width, dtype)
+    g = draw(width + 2, 3, width, dtype)
+    s, y = R.add_rmsnorm(f64(x), f64(r), f64(g))
+    out, total = sol.add_rmsnorm(x, r, g)
+    check(total, s, 0.0, np.abs(s) * 2.0 ** -24, dtype, "sum")
+    check(out, y, REL, 0.0, dtype, "norm")
+    check_backward(x, r, g, total, dtype)
+
+
+@pytest.mark.parametrize("kind", ["mxfp8", "mxfp4"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [992, 4128, 9024, 16416, 20480, 24576])
+def test_quantized_widths_between(kind, dtype, width):
+    test_quantized_output(kind, dtype, width)
+
+
+@pytest.mark.parametrize("rows,groups", [(9000, 1), (12000, 3), (70000, 1), (72000, 6)])
+def test_backward_many_rows(rows, groups):
+    """One round of workgroups a compute unit, and two."""
+    dy, s = draw(rows, rows, 104, torch.bfloat16), draw(rows + 1, rows, 104, torch.bfloat16)
+    check_backward(dy, s, draw(rows + 2, groups, 104, torch.bfloat16), None, torch.bfloat16)
