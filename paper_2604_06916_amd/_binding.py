@@ -707,7 +707,7 @@ def rotary_table(frequencies, positions, axis_pairs=None, magnitude=1.0, device=
         _need(out, torch.float32, (rows, 2 * pairs), "out", dev)
     st = _stream(stream, dev)
     with torch.cuda.stream(st):
-        f = frequencies.to(dev)
+        f = frequencies.to(dev).contiguous()   # the kernel reads them one after another
     if out is None:
         out = _alloc((rows, 2 * pairs), torch.float32, dev, st)
     counts = None if axis_pairs is None else (ctypes.c_int64 * axes)(*axis_pairs)
