@@ -700,6 +700,8 @@ def rotary_table(frequencies, positions, axis_pairs=None, magnitude=1.0, device=
         if rows < 0:
             raise ValueError(f"positions: expected at least 0 rows, got {rows}")
         dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if dev.type != "cuda":
+            raise ValueError(f"device: expected a CUDA device, got {dev}")
     if axes > 1 or axis_pairs is not None:
         if axis_pairs is None or len(axis_pairs) != axes or sum(axis_pairs) != pairs or min(axis_pairs) < 0:
             raise ValueError(f"axis_pairs: expected {axes} counts that add up to {pairs}")

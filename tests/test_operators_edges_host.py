@@ -40,3 +40,16 @@ def test_table_frequencies_of_any_stride(host, monkeypatch, view):
     monkeypatch.setattr(B.lib, "solfp4_rotary_table", table)
     sol.rotary_table(f, torch.arange(3))
     assert seen == f.tolist()
+
+
+# ---- the table's device ---------------------------------------------------
+
+@pytest.mark.parametrize("device", ["cpu", "meta"])
+def test_table_refuses_other_devices(host, monkeypatch, device):
+    """With a stream given nothing else looks at the device: the table would
+    be host memory, which the kernel cannot write."""
+    calls = []
+    monkeypatch.setattr(B.lib, "solfp4_rotary_table", lambda *a: calls.append(a) or OK)
+    with pytest.raises(ValueError):
+        sol.rotary_table(sol.rotary_frequencies(8), 4, device=device, stream=HostStream())
+    assert not calls
