@@ -699,12 +699,14 @@ def rotary_table(frequencies, positions, axis_pairs=None, magnitude=1.0, device=
         rows, at = int(positions), None
         if rows < 0:
             raise ValueError(f"positions: expected at least 0 rows, got {rows}")
-        dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        dev = torch.device("cuda" if device is None else device)
         if dev.type != "cuda":
             raise ValueError(f"device: expected a CUDA device, got {dev}")
     if axes > 1 or axis_pairs is not None:
         if axis_pairs is None or len(axis_pairs) != axes or sum(axis_pairs) != pairs or min(axis_pairs) < 0:
             raise ValueError(f"axis_pairs: expected {axes} counts that add up to {pairs}")
+    if at is None and dev.index is None:
+        dev = torch.device("cuda", torch.cuda.current_device())
     if out is not None:
         _need(out, torch.float32, (rows, 2 * pairs), "out", dev)
     st = _stream(stream, dev)

@@ -53,3 +53,20 @@ def test_table_refuses_other_devices(host, monkeypatch, device):
     with pytest.raises(ValueError):
         sol.rotary_table(sol.rotary_frequencies(8), 4, device=device, stream=HostStream())
     assert not calls
+
+
+def test_table_device_without_an_index_is_the_current_one(host, monkeypatch):
+    """out lives on "cuda:1": "cuda" names the same device while it is the current one."""
+    class Table(torch.Tensor):
+        device = torch.device("cuda", 1)
+
+    class Frequencies(torch.Tensor):
+        def to(self, dev):
+            assert dev == torch.device("cuda", 1)
+            return self
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(B.lib, "solfp4_rotary_table", lambda *a: OK)
+    out = torch.empty(4, 8).as_subclass(Table)
+    f = sol.rotary_frequencies(8).as_subclass(Frequencies)
+    assert sol.rotary_table(f, 4, device="cuda", out=out) is out
+    assert sol.rotary_table(f, 4, out=out) is out
