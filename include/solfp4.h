@@ -491,8 +491,10 @@ SOLFP4_API int solfp4_rotary_table(const int64_t* positions, int64_t rows, const
  * QKV buffer.
  *
  *   q, q_out   [tokens][q_heads][dim], each with its own strides; q_out may
- *              be q (same strides) and must not overlap it otherwise
- *   k, k_out   [tokens][k_heads][dim] likewise; k_heads may be 0
+ *              be q (same strides)
+ *   k, k_out   [tokens][k_heads][dim] likewise; k_heads may be 0.  Otherwise
+ *              an output must not overlap q or k (SOLFP4_EINVAL); side by
+ *              side in one buffer, by tokens or by heads, is apart
  *   rotated    even, at most dim: the first `rotated` elements of a head turn,
  *              the others are copied
  *   layout     SOLFP4_ROTARY_HALF: pairs (i, i + rotated/2);

@@ -3,6 +3,8 @@
 // the first HIP call.
 #include <math.h>
 
+#include <numeric>
+
 #include "solfp4.h"
 #include "kernels.h"
 
@@ -56,6 +58,31 @@ bool overlap(Extent a, Extent b) { return a.lo < b.hi && b.lo < a.hi; }
 bool gain_apart(int type, const void* gain, int64_t gain_stride, int64_t groups, const void* out, int64_t out_stride,
                 int64_t rows, int64_t width) {
   return !gain || !overlap(extent(type, gain, gain_stride, groups, width), extent(type, out, out_stride, rows, width));
+}
+
+// What an operand covers: w bytes at p + i s0 + j s1, i < n0, j < n1.
+struct Region {
+  uintptr_t p;
+  int64_t n0, s0, n1, s1, w;
+  int64_t span0() const { return (n0 - 1) * s0 + w; }
+  int64_t span1() const { return (n1 - 1) * s1 + w; }
+};
+
+// Whether two regions (every count at least 1) share no byte: one ends before
+// the other begins, or they lie side by side as columns or heads of one
+// buffer do, which shows in their offsets modulo the strides' common divisor.
+bool apart(const Region& a, const Region& b) {
+  const int64_t a_len = (a.n0 - 1) * a.s0 + a.span1(), b_len = (b.n0 - 1) * b.s0 + b.span1();
+  if (!a_len || !b_len || a.p + (uint64_t)a_len <= b.p || b.p + (uint64_t)b_len <= a.p) return true;
+  const int64_t d = (int64_t)(b.p - a.p);
+  const auto beside = [d](int64_t g, int64_t wa, int64_t wb) {
+    if (g <= 0) return false;
+    const int64_t r = (d % g + g) % g;
+    return r >= wa && r + wb <= g;
+  };
+  const auto step = [](int64_t n, int64_t s) { return n > 1 ? s : (int64_t)0; };
+  const int64_t g0 = std::gcd(step(a.n0, a.s0), step(b.n0, b.s0)), g1 = std::gcd(step(a.n1, a.s1), step(b.n1, b.s1));
+  return beside(g0, a.span1(), b.span1()) || beside(g1, a.span0(), b.span0()) || beside(std::gcd(g0, g1), a.w, b.w);
 }
 
 // The two are one operand (each element is read before it is written) or apart.
@@ -165,20 +192,9 @@ int rotary_operand(int type, solfp4::RotaryOperand* o, const void* in, int64_t i
   return by_token || by_head ? SOLFP4_OK : SOLFP4_EINVAL;
 }
 
-bool rotary_apart(int type, const solfp4::RotaryOperand& in, const solfp4::RotaryOperand& out, int64_t tokens,
-                  int64_t dim) {
-  if (!in.heads || !out.heads) return true;
-  const int64_t in_span = (tokens - 1) * in.in_token + (in.heads - 1) * in.in_head + dim;
-  const int64_t out_span = (tokens - 1) * out.out_token + (out.heads - 1) * out.out_head + dim;
-  if (!overlap(extent(type, in.in, 0, 1, in_span), extent(type, out.out, 0, 1, out_span))) return true;
-  // two views of one buffer whose heads lie side by side in every token
-  const int64_t s = in.in_token;
-  if (s != out.out_token || s <= 0) return false;
+Region heads_region(int type, const void* p, int64_t token, int64_t head, int64_t heads, int64_t tokens, int64_t dim) {
   const int64_t bytes = type == SOLFP4_F32 ? 4 : 2;
-  const int64_t d = ((const char*)out.out - (const char*)in.in) / bytes;
-  const int64_t iw = (in.heads - 1) * in.in_head + dim, ow = (out.heads - 1) * out.out_head + dim;
-  const int64_t r = ((d % s) + s) % s;   // where the output's heads start in the input's token
-  return r >= iw && r + ow <= s;
+  return {(uintptr_t)p, tokens, token * bytes, heads, head * bytes, dim * bytes};
 }
 
 bool rotary_in_place(const solfp4::RotaryOperand& o, int64_t tokens) {
@@ -301,10 +317,18 @@ int solfp4_rotary(int type, int layout, int inverse, const void* q, int64_t q_to
   if (rotated > 0 && (!table || table_rows == 0)) return SOLFP4_EINVAL;
   if ((uintptr_t)table & 3u) return SOLFP4_EALIGN;
   if (position_bytes && ((uintptr_t)positions & (uintptr_t)(position_bytes - 1))) return SOLFP4_EALIGN;
-  if ((!rotary_in_place(a.q, tokens) && !rotary_apart(type, a.q, a.q, tokens, dim)) ||
-      (!rotary_in_place(a.k, tokens) && !rotary_apart(type, a.k, a.k, tokens, dim)) ||
-      !rotary_apart(type, a.q, a.k, tokens, dim) || !rotary_apart(type, a.k, a.q, tokens, dim))
-    return SOLFP4_EINVAL;
+  // neither output over what the call reads, except in place
+  const solfp4::RotaryOperand* const both[2] = {&a.q, &a.k};
+  for (int i = 0; i < 2; ++i) {
+    const solfp4::RotaryOperand &o = *both[i], &other = *both[1 - i];
+    if (!o.heads) continue;
+    const Region out = heads_region(type, o.out, o.out_token, o.out_head, o.heads, tokens, dim);
+    if (!rotary_in_place(o, tokens) && !apart(out, heads_region(type, o.in, o.in_token, o.in_head, o.heads, tokens, dim)))
+      return SOLFP4_EINVAL;
+    if (other.heads &&
+        !apart(out, heads_region(type, other.in, other.in_token, other.in_head, other.heads, tokens, dim)))
+      return SOLFP4_EINVAL;
+  }
   // waves are numbered in 32 bits
   if (solfp4::rotary_waves(type, layout == SOLFP4_ROTARY_INTERLEAVED, tokens, dim, rotated, q_heads + k_heads) >
       kMaxGroups)

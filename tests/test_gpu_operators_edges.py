@@ -24,3 +24,26 @@ def test_table_of_strided_frequencies(view):
     """A view of device frequencies gives the table of its values."""
     f = view(sol.rotary_frequencies(96).to(device()))
     assert torch.equal(sol.rotary_table(f, 40), sol.rotary_table(f.cpu().clone(), 40))
+
+
+# ---- packed buffers -------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("order", [(0, 2, 1, 3), (0, 1, 2, 3), (1, 0, 2, 3), (2, 1, 0, 3)])
+def test_rotary_in_place_in_packed_buffers(dtype, layout, order):
+    """q, k and v of one buffer in every order of tokens, heads and the three:
+    turned in place as out of place, v untouched."""
+    T, H, D, rotated = 9, 5, 56, 36
+    t = torch.randn(T, 3, H, D, generator=torch.Generator().manual_seed(3)).to(dtype).to(device())
+    # a buffer laid out in this order, seen as [tokens, 3, heads, dim]
+    t = t.permute(order).contiguous().permute([order.index(i) for i in range(4)])
+    q, k, v = (t[:, i] for i in range(3))
+    keep = v.clone()
+    table = sol.rotary_table(sol.rotary_frequencies(rotated), 20)
+    want = sol.rotary(q.contiguous(), k.contiguous(), table, layout=layout)
+    out = torch.empty_like(t)
+    got = sol.rotary(q, k, table, layout=layout, q_out=out[:, 0], k_out=out[:, 1])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    sol.rotary(q, k, table, layout=layout, q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, keep)

@@ -70,3 +70,40 @@ def test_table_device_without_an_index_is_the_current_one(host, monkeypatch):
     f = sol.rotary_frequencies(8).as_subclass(Frequencies)
     assert sol.rotary_table(f, 4, device="cuda", out=out) is out
     assert sol.rotary_table(f, 4, out=out) is out
+
+
+# ---- overlaps -------------------------------------------------------------
+
+def at(n):
+    return ctypes.c_void_p(0x7F0000000000 + n)
+
+
+def apart(i):
+    return at(i << 32)
+
+
+#: what a call that passes every check gives without a GPU: the launch's error
+PASSED = -5
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="a call that passes would launch on addresses that no GPU holds")
+
+
+def rotate(q=apart(0), qo=apart(1), k=apart(2), ko=apart(3), table=apart(8), pos=None, token=4096, head=512, out_token=4096,
+           out_head=512, heads=8, k_heads=8, tokens=6, dim=128, rows=16):
+    """In bytes of FP32 elements."""
+    return sol.lib.solfp4_rotary(2, 0, 0, q, token // 4, head // 4, qo, out_token // 4, out_head // 4, heads, k, token // 4,
+                                 head // 4, ko, out_token // 4, out_head // 4, k_heads, table, rows, pos, 8 if pos else 0,
+                                 tokens, dim, dim, None)
+
+
+@no_gpu
+def test_rotary_side_by_side_is_apart():
+    """q and k of one packed buffer, in place and as outputs: by tokens
+    [tokens, 3, heads, dim], by heads [tokens, heads, 3, dim], heads first
+    [heads, tokens, 3, dim] and [3, heads, tokens, dim]."""
+    for token, head, k_at in ((3 * 4096, 512, 4096), (3 * 4096, 1536, 512), (1536, 6 * 1536, 512), (512, 6 * 512, 8 * 6 * 512)):
+        layout = dict(token=token, head=head, out_token=token, out_head=head)
+        assert rotate(q=at(0), qo=at(0), k=at(k_at), ko=at(k_at), **layout) == PASSED
+        assert rotate(qo=at(0), ko=at(k_at), q=apart(4), k=apart(5), **layout) == PASSED
+        # one element less far apart
+        assert rotate(q=at(0), qo=at(0), k=at(k_at - 4), ko=at(k_at - 4), **layout) == EINVAL
