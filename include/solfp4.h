@@ -492,9 +492,10 @@ SOLFP4_API int solfp4_rotary_table(const int64_t* positions, int64_t rows, const
  *
  *   q, q_out   [tokens][q_heads][dim], each with its own strides; q_out may
  *              be q (same strides)
- *   k, k_out   [tokens][k_heads][dim] likewise; k_heads may be 0.  Otherwise
- *              an output must not overlap q or k (SOLFP4_EINVAL); side by
- *              side in one buffer, by tokens or by heads, is apart
+ *   k, k_out   [tokens][k_heads][dim] likewise; k_heads may be 0.  An output
+ *              must not overlap the other one or anything the call reads
+ *              otherwise (SOLFP4_EINVAL); side by side in one buffer, by
+ *              tokens or by heads, is apart
  *   rotated    even, at most dim: the first `rotated` elements of a head turn,
  *              the others are copied
  *   layout     SOLFP4_ROTARY_HALF: pairs (i, i + rotated/2);

@@ -85,6 +85,8 @@ bool apart(const Region& a, const Region& b) {
   return beside(g0, a.span1(), b.span1()) || beside(g1, a.span0(), b.span0()) || beside(std::gcd(g0, g1), a.w, b.w);
 }
 
+Region block_of(const void* p, int64_t bytes) { return {(uintptr_t)p, 1, 0, 1, 0, bytes}; }
+
 // The two are one operand (each element is read before it is written) or apart.
 bool same_or_apart(int type, const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t rows,
                    int64_t width) {
@@ -315,9 +317,10 @@ int solfp4_rotary(int type, int layout, int inverse, const void* q, int64_t q_to
   if (tokens == 0 || dim == 0 || q_heads + k_heads == 0) return SOLFP4_OK;
   if ((position_bytes != 0) != (positions != nullptr)) return SOLFP4_EINVAL;
   if (rotated > 0 && (!table || table_rows == 0)) return SOLFP4_EINVAL;
+  if (rotated > 0 && table_rows > kMaxSpan / rotated) return SOLFP4_ESHAPE;
   if ((uintptr_t)table & 3u) return SOLFP4_EALIGN;
   if (position_bytes && ((uintptr_t)positions & (uintptr_t)(position_bytes - 1))) return SOLFP4_EALIGN;
-  // neither output over what the call reads, except in place
+  // neither output over what the call reads, except in place, nor over the other
   const solfp4::RotaryOperand* const both[2] = {&a.q, &a.k};
   for (int i = 0; i < 2; ++i) {
     const solfp4::RotaryOperand &o = *both[i], &other = *both[1 - i];
@@ -326,7 +329,11 @@ int solfp4_rotary(int type, int layout, int inverse, const void* q, int64_t q_to
     if (!rotary_in_place(o, tokens) && !apart(out, heads_region(type, o.in, o.in_token, o.in_head, o.heads, tokens, dim)))
       return SOLFP4_EINVAL;
     if (other.heads &&
-        !apart(out, heads_region(type, other.in, other.in_token, other.in_head, other.heads, tokens, dim)))
+        (!apart(out, heads_region(type, other.in, other.in_token, other.in_head, other.heads, tokens, dim)) ||
+         !apart(out, heads_region(type, other.out, other.out_token, other.out_head, other.heads, tokens, dim))))
+      return SOLFP4_EINVAL;
+    if ((rotated && !apart(out, block_of(table, table_rows * rotated * 4))) ||
+        (positions && !apart(out, block_of(positions, tokens * position_bytes))))
       return SOLFP4_EINVAL;
   }
   // waves are numbered in 32 bits

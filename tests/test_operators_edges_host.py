@@ -107,3 +107,21 @@ def test_rotary_side_by_side_is_apart():
         assert rotate(qo=at(0), ko=at(k_at), q=apart(4), k=apart(5), **layout) == PASSED
         # one element less far apart
         assert rotate(q=at(0), qo=at(0), k=at(k_at - 4), ko=at(k_at - 4), **layout) == EINVAL
+        assert rotate(qo=at(0), ko=at(k_at - 4), q=apart(4), k=apart(5), **layout) == EINVAL
+
+
+@no_gpu
+def test_rotary_outputs_over_each_other_are_refused():
+    assert rotate() == PASSED
+    assert rotate(qo=apart(3)) == EINVAL and rotate(ko=at((1 << 32) + 512)) == EINVAL
+    assert rotate(ko=at((1 << 32) + 6 * 4096 - 512)) == EINVAL and rotate(ko=at((1 << 32) + 6 * 4096)) == PASSED
+    # in place, k over q
+    assert rotate(qo=apart(0), ko=apart(0)) == EINVAL and rotate(qo=apart(0), ko=apart(2)) == PASSED
+    assert rotate(qo=apart(2), ko=apart(0)) == EINVAL
+
+
+@no_gpu
+def test_rotary_outputs_over_table_or_positions_are_refused():
+    assert rotate(table=apart(1)) == EINVAL and rotate(table=at((3 << 32) + 6 * 4096 - 4)) == EINVAL
+    assert rotate(pos=apart(3)) == EINVAL and rotate(pos=apart(9)) == PASSED
+    assert rotate(table=at((1 << 32) + 6 * 4096)) == PASSED
