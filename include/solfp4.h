@@ -397,7 +397,7 @@ SOLFP4_API int mxfp4_linear(const uint16_t* x, const uint8_t* w_codes, const uin
  *            address and stride)
  *   out      [rows][width], written; must not overlap the inputs or sum,
  *            except that it may be x.  Overlaps that are not allowed are
- *            refused (SOLFP4_EINVAL)
+ *            refused (SOLFP4_EINVAL); columns of one buffer are apart
  *
  * The norm is taken of the FP32 sum, not of its rounded form.  width is at
  * most 24576.  A row with a NaN or an infinity gives NaN; the squares are

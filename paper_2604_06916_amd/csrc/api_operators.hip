@@ -41,25 +41,6 @@ int check_rows(int type, const void* p, int64_t stride, int64_t rows, int64_t wi
   return SOLFP4_OK;
 }
 
-// [a, a + bytes) of rows x width elements
-struct Extent {
-  uintptr_t lo, hi;
-};
-
-Extent extent(int type, const void* p, int64_t stride, int64_t rows, int64_t width) {
-  const uint64_t bytes = type == SOLFP4_F32 ? 4 : 2;
-  const uintptr_t lo = (uintptr_t)p;
-  return {lo, lo + (uintptr_t)(((uint64_t)(rows - 1) * (uint64_t)stride + (uint64_t)width) * bytes)};
-}
-
-bool overlap(Extent a, Extent b) { return a.lo < b.hi && b.lo < a.hi; }
-
-// Whether the gain lies apart from rows that the call writes.
-bool gain_apart(int type, const void* gain, int64_t gain_stride, int64_t groups, const void* out, int64_t out_stride,
-                int64_t rows, int64_t width) {
-  return !gain || !overlap(extent(type, gain, gain_stride, groups, width), extent(type, out, out_stride, rows, width));
-}
-
 // What an operand covers: w bytes at p + i s0 + j s1, i < n0, j < n1.
 struct Region {
   uintptr_t p;
@@ -87,11 +68,14 @@ bool apart(const Region& a, const Region& b) {
 
 Region block_of(const void* p, int64_t bytes) { return {(uintptr_t)p, 1, 0, 1, 0, bytes}; }
 
+Region rows_region(int type, const void* p, int64_t stride, int64_t rows, int64_t width) {
+  const int64_t bytes = type == SOLFP4_F32 ? 4 : 2;
+  return {(uintptr_t)p, p ? rows : 1, rows > 1 ? stride * bytes : 0, 1, 0, p ? width * bytes : 0};
+}
+
 // The two are one operand (each element is read before it is written) or apart.
-bool same_or_apart(int type, const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t rows,
-                   int64_t width) {
-  if (in == out && (in_stride == out_stride || rows == 1)) return true;
-  return !overlap(extent(type, in, in_stride, rows, width), extent(type, out, out_stride, rows, width));
+bool same_or_apart(const Region& a, const Region& b) {
+  return (a.p == b.p && a.n0 == b.n0 && a.s0 == b.s0 && a.w == b.w) || apart(a, b);
 }
 
 int norm_checks(int type, const solfp4::NormArgs& a, int64_t groups, int out) {
@@ -106,23 +90,18 @@ int norm_checks(int type, const solfp4::NormArgs& a, int64_t groups, int out) {
   if (a.residual) {
     if ((rc = check_rows(type, a.residual, a.residual_stride, a.rows, a.width, false))) return rc;
     if ((rc = check_rows(type, a.sum, a.sum_stride, a.rows, a.width, true))) return rc;
-    if (!same_or_apart(type, a.x, a.x_stride, a.sum, a.sum_stride, a.rows, a.width) ||
-        !same_or_apart(type, a.residual, a.residual_stride, a.sum, a.sum_stride, a.rows, a.width))
-      return SOLFP4_EINVAL;
   }
   if (a.gain && (rc = check_rows(type, a.gain, a.gain_stride, groups, a.width, false))) return rc;
-  if (a.residual && !gain_apart(type, a.gain, a.gain_stride, groups, a.sum, a.sum_stride, a.rows, a.width))
-    return SOLFP4_EINVAL;
+  // what is written over nothing else, except in place
+  const Region x = rows_region(type, a.x, a.x_stride, a.rows, a.width);
+  const Region residual = rows_region(type, a.residual, a.residual_stride, a.rows, a.width);
+  const Region gain = rows_region(type, a.gain, a.gain_stride, groups, a.width);
+  const Region sum = rows_region(type, a.residual ? a.sum : nullptr, a.sum_stride, a.rows, a.width);
+  if (!same_or_apart(x, sum) || !same_or_apart(residual, sum) || !apart(gain, sum)) return SOLFP4_EINVAL;
   if (out == solfp4::kNormSame) {
     if ((rc = check_rows(type, a.out, a.out_stride, a.rows, a.width, true))) return rc;
-    const Extent o = extent(type, a.out, a.out_stride, a.rows, a.width);
-    if (!same_or_apart(type, a.x, a.x_stride, a.out, a.out_stride, a.rows, a.width) ||
-        !gain_apart(type, a.gain, a.gain_stride, groups, a.out, a.out_stride, a.rows, a.width))
-      return SOLFP4_EINVAL;
-    if (a.residual && (overlap(o, extent(type, a.residual, a.residual_stride, a.rows, a.width)) ||
-                       overlap(o, extent(type, a.sum, a.sum_stride, a.rows, a.width))))
-      return SOLFP4_EINVAL;
-    return SOLFP4_OK;
+    const Region o = rows_region(type, a.out, a.out_stride, a.rows, a.width);
+    return same_or_apart(x, o) && apart(residual, o) && apart(gain, o) && apart(sum, o) ? SOLFP4_OK : SOLFP4_EINVAL;
   }
   if (!a.codes || !a.scales) return SOLFP4_EINVAL;
   return aligned16(a.codes) && aligned16(a.scales) ? SOLFP4_OK : SOLFP4_EALIGN;
@@ -196,7 +175,7 @@ int rotary_operand(int type, solfp4::RotaryOperand* o, const void* in, int64_t i
 
 Region heads_region(int type, const void* p, int64_t token, int64_t head, int64_t heads, int64_t tokens, int64_t dim) {
   const int64_t bytes = type == SOLFP4_F32 ? 4 : 2;
-  return {(uintptr_t)p, tokens, token * bytes, heads, head * bytes, dim * bytes};
+  return {(uintptr_t)p, tokens, tokens > 1 ? token * bytes : 0, heads, heads > 1 ? head * bytes : 0, dim * bytes};
 }
 
 bool rotary_in_place(const solfp4::RotaryOperand& o, int64_t tokens) {
@@ -247,10 +226,11 @@ int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const v
     if (gain && (rc = check_rows(type, gain, gain_stride, groups, width, false))) return rc;
     if (dsum && (rc = check_rows(type, dsum, dsum_stride, rows, width, false))) return rc;
     if ((rc = check_rows(type, dx, dx_stride, rows, width, true))) return rc;
-    if (!same_or_apart(type, dy, dy_stride, dx, dx_stride, rows, width) ||
-        !same_or_apart(type, x, x_stride, dx, dx_stride, rows, width) ||
-        (dsum && !same_or_apart(type, dsum, dsum_stride, dx, dx_stride, rows, width)) ||
-        !gain_apart(type, gain, gain_stride, groups, dx, dx_stride, rows, width))
+    const Region out = rows_region(type, dx, dx_stride, rows, width);
+    if (!same_or_apart(rows_region(type, dy, dy_stride, rows, width), out) ||
+        !same_or_apart(rows_region(type, x, x_stride, rows, width), out) ||
+        !same_or_apart(rows_region(type, dsum, dsum_stride, rows, width), out) ||
+        !apart(rows_region(type, gain, gain_stride, groups, width), out))
       return SOLFP4_EINVAL;
   }
   if (dgain) {

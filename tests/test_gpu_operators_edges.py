@@ -47,3 +47,22 @@ def test_rotary_in_place_in_packed_buffers(dtype, layout, order):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     sol.rotary(q, k, table, layout=layout, q_out=q, k_out=k)
     assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, keep)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_in_columns_of_one_buffer(dtype):
+    """Operands and outputs that are columns of one buffer: as with buffers of
+    their own, and the columns beside them untouched."""
+    rows, width = 37, 150
+    g = torch.Generator().manual_seed(4)
+    t = torch.randn(rows, 5, width, generator=g).to(dtype).to(device())
+    x, r, total, out, other = (t[:, i] for i in range(5))
+    gain = torch.randn(1, width, generator=g).to(dtype).to(device())
+    keep = t.clone()
+    y, s = sol.add_rmsnorm(x.contiguous(), r.contiguous(), gain)
+    sol.add_rmsnorm(x, r, gain, out=out, sum_out=total)
+    assert torch.equal(out, y) and torch.equal(total, s)
+    assert torch.equal(x, keep[:, 0]) and torch.equal(r, keep[:, 1]) and torch.equal(other, keep[:, 4])
+    dx, dgain = sol.rmsnorm_backward(x.contiguous(), s, gain, r.contiguous())
+    got, got_gain = sol.rmsnorm_backward(x, total, gain, r, dx=out)
+    assert got is out and torch.equal(out, dx) and torch.equal(got_gain, dgain) and torch.equal(other, keep[:, 4])

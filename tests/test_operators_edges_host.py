@@ -125,3 +125,50 @@ def test_rotary_outputs_over_table_or_positions_are_refused():
     assert rotate(table=apart(1)) == EINVAL and rotate(table=at((3 << 32) + 6 * 4096 - 4)) == EINVAL
     assert rotate(pos=apart(3)) == EINVAL and rotate(pos=apart(9)) == PASSED
     assert rotate(table=at((1 << 32) + 6 * 4096)) == PASSED
+
+
+W = 64   # columns, FP32
+
+
+def norm(x=apart(0), xs=W, r=apart(1), rs=W, g=apart(2), gs=W, groups=2, s=apart(3), ss=W, out=apart(4), os=W, rows=6):
+    return sol.lib.solfp4_add_rmsnorm(2, x, xs, r, rs, g, gs, groups, 1e-6, s, ss, out, os, rows, W, None)
+
+
+def back(dy=apart(0), dys=W, x=apart(1), xs=W, g=apart(2), gs=W, ds=apart(3), dss=W, dx=apart(4), dxs=W, dg=apart(5),
+         ws=apart(6), wsb=1 << 20, rows=6, groups=2):
+    return sol.lib.solfp4_rmsnorm_backward(2, dy, dys, x, xs, g, gs, groups, ds, dss, 1e-6, dx, dxs, dg, ws, wsb, rows, W,
+                                           None)
+
+
+@no_gpu
+def test_norm_columns_of_one_buffer_are_apart():
+    """Operands that are columns of one [rows, 5 W] buffer, gains columns of a [groups, 2 W] one."""
+    at_ = [at(4 * W * i) for i in range(5)]
+    s = dict(xs=5 * W, rs=5 * W, ss=5 * W, os=5 * W)
+    assert norm() == PASSED
+    assert norm(x=at_[0], r=at_[1], s=at_[2], out=at_[3], **s) == PASSED
+    assert norm(x=at_[0], r=at_[1], s=at_[1], out=at_[0], **s) == PASSED
+    assert norm(x=at_[0], r=at_[1], s=at_[2], out=at_[3], g=at_[4], gs=5 * W, **s) == PASSED
+    s = dict(dys=5 * W, xs=5 * W, dss=5 * W, dxs=5 * W)
+    assert back(dy=at_[0], x=at_[1], ds=at_[2], dx=at_[3], **s) == PASSED
+    assert back(dy=at_[0], x=at_[1], ds=at_[2], dx=at_[2], **s) == PASSED
+
+
+@no_gpu
+def test_norm_columns_over_each_other_are_refused():
+    at_ = [at(4 * W * i) for i in range(5)]
+    s = dict(xs=5 * W, rs=5 * W, ss=5 * W, os=5 * W)
+    one = at(4 * W * 3 - 4)
+    assert norm(x=at_[0], r=at_[1], s=at_[2], out=one, **s) == EINVAL
+    assert norm(x=at_[0], r=at_[2], s=at_[4], out=one, **s) == EINVAL
+    assert norm(x=at_[0], r=at_[4], s=one, out=at_[1], g=at_[2], gs=5 * W, **s) == EINVAL
+    assert norm(x=at_[2], r=at_[4], s=one, out=at_[0], **s) == EINVAL
+    # rows of another stride meet sooner or later; a last column reaches into the next row's first
+    assert norm(x=at_[0], out=at_[2], xs=5 * W, os=4 * W) == EINVAL
+    assert norm(x=at_[0], out=at(4 * (4 * W + 1)), xs=5 * W, os=5 * W) == EINVAL
+    # one row: its stride does not matter
+    assert norm(x=at_[0], out=at_[0], xs=5 * W, os=W, rows=1, groups=1) == PASSED
+    s = dict(dys=5 * W, xs=5 * W, dss=5 * W, dxs=5 * W)
+    for d in (dict(dy=at_[2]), dict(x=at_[2]), dict(ds=at_[2])):
+        assert back(**{**dict(dy=apart(0), x=apart(1), ds=apart(3)), **d}, dx=one, **s) == EINVAL
+    assert back(g=at_[2], gs=5 * W, dx=one, dxs=5 * W) == EINVAL
