@@ -421,7 +421,8 @@ SOLFP4_API int solfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, con
  *   mxfp4_add_rmsnorm  codes [rows][width/2] and scales [rows][width/32]
  *                      as mxfp4_quantize writes them (mxfp4_gemm reads them)
  *
- * A NaN keeps its E4M3 code 0x7F or 0xFF; E2M1 has none.
+ * codes and scales must not overlap each other, the inputs or sum
+ * (SOLFP4_EINVAL).  A NaN keeps its E4M3 code 0x7F or 0xFF; E2M1 has none.
  */
 SOLFP4_API int mxfp8_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual,
                    int64_t residual_stride, const void* gain, int64_t gain_stride, int64_t groups,

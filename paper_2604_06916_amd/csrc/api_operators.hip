@@ -104,7 +104,12 @@ int norm_checks(int type, const solfp4::NormArgs& a, int64_t groups, int out) {
     return same_or_apart(x, o) && apart(residual, o) && apart(gain, o) && apart(sum, o) ? SOLFP4_OK : SOLFP4_EINVAL;
   }
   if (!a.codes || !a.scales) return SOLFP4_EINVAL;
-  return aligned16(a.codes) && aligned16(a.scales) ? SOLFP4_OK : SOLFP4_EALIGN;
+  if (!aligned16(a.codes) || !aligned16(a.scales)) return SOLFP4_EALIGN;
+  const Region codes = block_of(a.codes, a.rows * (out == solfp4::kNormMxfp8 ? a.width : a.width / 2));
+  const Region scales = block_of(a.scales, a.rows * (a.width / 32));
+  for (const Region& o : {codes, scales})
+    if (!apart(x, o) || !apart(residual, o) || !apart(gain, o) || !apart(sum, o)) return SOLFP4_EINVAL;
+  return apart(codes, scales) ? SOLFP4_OK : SOLFP4_EINVAL;
 }
 
 int add_rmsnorm(int type, int kind, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,

@@ -172,3 +172,24 @@ def test_norm_columns_over_each_other_are_refused():
     for d in (dict(dy=at_[2]), dict(x=at_[2]), dict(ds=at_[2])):
         assert back(**{**dict(dy=apart(0), x=apart(1), ds=apart(3)), **d}, dx=one, **s) == EINVAL
     assert back(g=at_[2], gs=5 * W, dx=one, dxs=5 * W) == EINVAL
+
+
+@no_gpu
+@pytest.mark.parametrize("pack", [1, 2])
+def test_norm_codes_and_scales_over_operands_are_refused(pack):
+    fn = sol.lib.mxfp8_add_rmsnorm if pack == 1 else sol.lib.mxfp4_add_rmsnorm
+    rows, codes_bytes, scales_bytes = 48, 48 * W // pack, 48 * W // 32
+
+    def call(codes=apart(5), scales=apart(6), x=apart(0), xs=W, r=apart(1), g=apart(2), s=apart(3)):
+        return fn(2, x, xs, r, W, g, W, 2, 1e-6, s, W, codes, scales, rows, W, None)
+    assert call() == PASSED
+    last = 4 * W * rows - 16      # the operands' last 16 bytes
+    for i, n in ((0, last), (1, last), (2, 4 * W * 2 - 16), (3, last)):
+        assert call(codes=apart(i)) == EINVAL and call(scales=apart(i)) == EINVAL
+        assert call(codes=at((i << 32) + n)) == EINVAL and call(codes=at((i << 32) + n + 16)) == PASSED
+        assert call(scales=at((i << 32) + n)) == EINVAL and call(scales=at((i << 32) + n + 16)) == PASSED
+    assert call(scales=apart(5)) == EINVAL and call(scales=at((5 << 32) + codes_bytes - 16)) == EINVAL
+    assert call(scales=at((5 << 32) + codes_bytes)) == PASSED
+    assert call(codes=at((6 << 32) + scales_bytes - 16)) == EINVAL and call(codes=at((6 << 32) + scales_bytes + 16)) == PASSED
+    # without a residual nothing is written to the sum's address, which then does not matter
+    assert fn(2, apart(0), W, None, 0, None, 0, 1, 1e-6, apart(5), W, apart(5), apart(6), rows, W, None) == PASSED
