@@ -449,11 +449,14 @@ SOLFP4_API size_t solfp4_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t 
  *   gain, groups as in the forward call
  *   dsum   [rows][width], what reaches s past the norm; or NULL
  *   dx     [rows][width], written: the gradient of s, which is that of x and
- *          of the residual alike; may be dy or dsum (same address and stride)
+ *          of the residual alike; may be dy, x or dsum (same address and stride)
  *   dgain  [groups][width] FP32 contiguous, written; or NULL (not computed).
  *          Valid without a gain too
  *   workspace  >= solfp4_rmsnorm_backward_workspace_bytes bytes, 16-byte
  *          aligned; ignored when dgain is NULL
+ *
+ * dx, dgain and the workspace must not overlap each other or, but for dx in
+ * place, what the call reads (SOLFP4_EINVAL).
  *
  * Sums over rows are formed in an order that depends on the sizes and the
  * device alone: results are the same on every call.

@@ -231,19 +231,24 @@ int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const v
     if (gain && (rc = check_rows(type, gain, gain_stride, groups, width, false))) return rc;
     if (dsum && (rc = check_rows(type, dsum, dsum_stride, rows, width, false))) return rc;
     if ((rc = check_rows(type, dx, dx_stride, rows, width, true))) return rc;
-    const Region out = rows_region(type, dx, dx_stride, rows, width);
-    if (!same_or_apart(rows_region(type, dy, dy_stride, rows, width), out) ||
-        !same_or_apart(rows_region(type, x, x_stride, rows, width), out) ||
-        !same_or_apart(rows_region(type, dsum, dsum_stride, rows, width), out) ||
-        !apart(rows_region(type, gain, gain_stride, groups, width), out))
-      return SOLFP4_EINVAL;
   }
+  const size_t need = dgain ? back_workspace(rows, width, groups) : 0;
   if (dgain) {
     if ((uintptr_t)dgain & 3u) return SOLFP4_EALIGN;
-    const size_t need = back_workspace(rows, width, groups);
     if (need && !workspace) return SOLFP4_EWORKSPACE;
     if (!aligned16(workspace)) return SOLFP4_EALIGN;
     if (workspace_bytes < need) return SOLFP4_EWORKSPACE;
+  }
+  if (rows > 0) {
+    const Region in[4] = {rows_region(type, dy, dy_stride, rows, width), rows_region(type, x, x_stride, rows, width),
+                          rows_region(type, dsum, dsum_stride, rows, width),
+                          rows_region(type, gain, gain_stride, groups, width)};
+    const Region out = rows_region(type, dx, dx_stride, rows, width);
+    const Region sums = block_of(dgain, dgain ? groups * width * 4 : 0), scratch = block_of(workspace, (int64_t)need);
+    for (int i = 0; i < 4; ++i)
+      if (!(i < 3 ? same_or_apart(in[i], out) : apart(in[i], out)) || !apart(in[i], sums) || !apart(in[i], scratch))
+        return SOLFP4_EINVAL;
+    if (!apart(out, sums) || !apart(out, scratch) || !apart(sums, scratch)) return SOLFP4_EINVAL;
   }
   solfp4::NormBackArgs a = {};
   a.dy = dy, a.dy_stride = dy_stride, a.x = x, a.x_stride = x_stride;

@@ -66,3 +66,13 @@ def test_norm_in_columns_of_one_buffer(dtype):
     dx, dgain = sol.rmsnorm_backward(x.contiguous(), s, gain, r.contiguous())
     got, got_gain = sol.rmsnorm_backward(x, total, gain, r, dx=out)
     assert got is out and torch.equal(out, dx) and torch.equal(got_gain, dgain) and torch.equal(other, keep[:, 4])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [24, 1152, 6151])
+def test_gradient_in_the_place_of_x(dtype, width):
+    g = torch.Generator().manual_seed(width)
+    dy, x, gain = (torch.randn(n, width, generator=g).to(dtype).to(device()) for n in (50, 50, 2))
+    dx, dgain = sol.rmsnorm_backward(dy, x, gain)
+    got, again = sol.rmsnorm_backward(dy, x, gain, dx=x)
+    assert got is x and torch.equal(x, dx) and torch.equal(again, dgain)

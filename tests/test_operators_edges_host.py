@@ -193,3 +193,23 @@ def test_norm_codes_and_scales_over_operands_are_refused(pack):
     assert call(codes=at((6 << 32) + scales_bytes - 16)) == EINVAL and call(codes=at((6 << 32) + scales_bytes + 16)) == PASSED
     # without a residual nothing is written to the sum's address, which then does not matter
     assert fn(2, apart(0), W, None, 0, None, 0, 1, 1e-6, apart(5), W, apart(5), apart(6), rows, W, None) == PASSED
+
+
+@no_gpu
+def test_gradient_outputs_and_workspace_over_operands_are_refused():
+    rows = 6
+    need = sol.rmsnorm_backward_workspace_bytes(rows, W, 2)
+    last = 4 * W * rows - 16
+    assert back() == PASSED and back(dg=None) == PASSED
+    for i, n in ((0, last), (1, last), (2, 4 * W * 2 - 16), (3, last), (4, last)):
+        assert back(dg=apart(i)) == EINVAL and back(ws=apart(i)) == EINVAL
+        assert back(dg=at((i << 32) + n)) == EINVAL and back(dg=at((i << 32) + n + 16)) == PASSED
+        assert back(ws=at((i << 32) + n)) == EINVAL and back(ws=at((i << 32) + n + 16)) == PASSED
+        # the workspace is ignored where there is no gradient of the gain
+        assert back(dg=None, ws=apart(i)) == PASSED
+    assert back(ws=apart(5)) == EINVAL and back(ws=at((5 << 32) + 2 * W * 4 - 16)) == EINVAL
+    assert back(ws=at((5 << 32) + 2 * W * 4)) == PASSED
+    assert back(dg=at((6 << 32) + need - 4)) == EINVAL and back(dg=at((6 << 32) + need)) == PASSED
+    # in place is still in place
+    assert back(dx=apart(0)) == PASSED and back(dx=apart(1)) == PASSED and back(dx=apart(3)) == PASSED
+    assert back(dx=apart(2)) == EINVAL
