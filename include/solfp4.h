@@ -480,7 +480,8 @@ SOLFP4_API int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stri
  *               axis 0, the next with axis 1, ...; they add up to pairs.
  *               NULL with one axis
  *   axes        1 to 4
- *   table       [rows][2 pairs] FP32, written
+ *   table       [rows][2 pairs] FP32, written; must not overlap positions or
+ *               frequencies (SOLFP4_EINVAL)
  *
  * Angles, cosines and sines are formed in 64 bits and rounded once.
  */
@@ -541,7 +542,8 @@ SOLFP4_API int solfp4_rotary(int type, int layout, int inverse,
  * read the weight once (from L2 after the first): from a few hundred tokens
  * on, nvfp4_linear and mxfp4_linear are the faster calls.  M, N or K equal to 0 are valid (K == 0 writes the bias,
  * or zeros).  K must be below 2^24 and N below 2^22.  Packed operands, x, bias
- * and out are contiguous and 16-byte aligned; no workspace.
+ * and out are contiguous and 16-byte aligned, out must not overlap the others
+ * (SOLFP4_EINVAL); no workspace.
  */
 SOLFP4_API int nvfp4_weight_linear(const uint16_t* x, const uint8_t* w_codes, const uint8_t* w_scales,
                    const float* w_global_scale, const uint16_t* bias, uint16_t* out,

@@ -155,6 +155,12 @@ int linear_checks(const void* x, const void* x_scales, bool scaled_x, const void
   if (!aligned16(out) || (bias && !aligned16(bias)) || (has_global && !aligned16(wg))) return SOLFP4_EALIGN;
   if (K > 0 && (!aligned16(x) || !aligned16(wc) || !aligned16(ws) || (scaled_x && !aligned16(x_scales))))
     return SOLFP4_EALIGN;
+  const Region o = block_of(out, M * N * 2);
+  const Region in[6] = {block_of(x, M * K * (scaled_x ? 1 : 2)), block_of(x_scales, scaled_x ? M * (K / 32) : 0),
+                        block_of(wc, N * (K / 2)), block_of(ws, N * (K / block)),
+                        block_of(wg, has_global ? 4 : 0), block_of(bias, bias ? N * 2 : 0)};
+  for (const Region& i : in)
+    if (!apart(i, o)) return SOLFP4_EINVAL;
   return SOLFP4_OK;
 }
 
@@ -281,6 +287,10 @@ int solfp4_rotary_table(const int64_t* positions, int64_t rows, const double* fr
   if (rows == 0 || pairs == 0) return SOLFP4_OK;
   if (!frequencies || !table) return SOLFP4_EINVAL;
   if (((uintptr_t)positions & 7u) || ((uintptr_t)frequencies & 7u) || ((uintptr_t)table & 3u)) return SOLFP4_EALIGN;
+  const Region out = block_of(table, rows * pairs * 8);
+  if (!apart(out, block_of(frequencies, pairs * 8)) ||
+      !apart(out, block_of(positions, positions ? rows * axes * 8 : 0)))
+    return SOLFP4_EINVAL;
   const hipError_t e = solfp4::launch_rotary_table(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
 }

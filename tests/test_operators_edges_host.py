@@ -213,3 +213,36 @@ def test_gradient_outputs_and_workspace_over_operands_are_refused():
     # in place is still in place
     assert back(dx=apart(0)) == PASSED and back(dx=apart(1)) == PASSED and back(dx=apart(3)) == PASSED
     assert back(dx=apart(2)) == EINVAL
+
+
+@no_gpu
+@pytest.mark.parametrize("kind", ["nvfp4", "mxfp4", "mxfp8"])
+def test_linear_output_over_operands_is_refused(kind):
+    M, N, K = 8, 32, 64
+
+    def call(out=apart(6), bias=apart(5)):
+        if kind == "nvfp4":
+            return sol.lib.nvfp4_weight_linear(apart(0), apart(2), apart(3), apart(4), bias, out, M, N, K, None)
+        if kind == "mxfp4":
+            return sol.lib.mxfp4_weight_linear(apart(0), apart(2), apart(3), bias, out, M, N, K, None)
+        return sol.lib.mxfp8_linear(apart(0), apart(1), apart(2), apart(3), bias, out, M, N, K, None)
+    assert call() == PASSED
+    sizes = {0: M * K * (1 if kind == "mxfp8" else 2), 2: N * K // 2, 3: N * K // (16 if kind == "nvfp4" else 32), 5: N * 2}
+    if kind == "mxfp8":
+        sizes[1] = M * K // 32
+    for i, n in sizes.items():
+        assert call(apart(i)) == EINVAL and call(at((i << 32) + n - 16)) == EINVAL and call(at((i << 32) + n)) == PASSED
+        assert call(at((i << 32) - M * N * 2)) == PASSED
+    if kind == "nvfp4":
+        assert call(apart(4)) == EINVAL and call(at((4 << 32) + 16)) == PASSED
+    assert call(apart(5), None) == PASSED
+
+
+@no_gpu
+def test_table_over_positions_or_frequencies_is_refused():
+    def call(out=apart(2), pos=apart(3)):
+        return sol.lib.solfp4_rotary_table(pos, 8, apart(1), 16, None, 1, 1.0, out, None)
+    assert call() == PASSED and call(pos=None) == PASSED
+    for i, n in ((1, 16 * 8), (3, 8 * 8)):
+        assert call(apart(i)) == EINVAL and call(at((i << 32) + n - 4)) == EINVAL and call(at((i << 32) + n)) == PASSED
+    assert call(apart(3), None) == PASSED
