@@ -335,7 +335,8 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 
       }
     }
     row_sum(qb, lds, at_.wave, sh);
-    const float rho = 1.0f / __builtin_sqrtf(qb[0] / (float)a.width + a.eps);
+    // 0 where the slot has no row: with eps = 0 its zeros would add 0 times infinity to dg
+    const float rho = in ? 1.0f / __builtin_sqrtf(qb[0] / (float)a.width + a.eps) : 0.0f;
     const float k = qb[1] / (float)a.width * rho * rho;
     uint8_t* outr = row_of<kType>(a.dx, row, a.dx_stride);
 #pragma unroll

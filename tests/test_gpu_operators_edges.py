@@ -76,3 +76,36 @@ def test_gradient_in_the_place_of_x(dtype, width):
     dx, dgain = sol.rmsnorm_backward(dy, x, gain)
     got, again = sol.rmsnorm_backward(dy, x, gain, dx=x)
     assert got is x and torch.equal(x, dx) and torch.equal(again, dgain)
+
+
+# ---- gradients with eps = 0 -----------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,groups,width", [(1, 1, 1152), (1, 1, 24), (9, 3, 200), (5, 1, 6151), (101, 1, 104),
+                                               (4429, 1, 2432), (8858, 2, 96), (3001, 1, 12000)])
+def test_gradients_without_eps(dtype, rows, groups, width):
+    """eps = 0 and no row of zeros: the slots of a workgroup that have no row
+    add nothing, whether the group's sums are one workgroup's or several's.
+
+    dx: REL 2^-18 of the magnitudes it is formed from, and the type's
+    rounding; dgain: that of its terms and a rounding a row."""
+    g = torch.Generator().manual_seed(rows + width)
+    dy, s, gain = (torch.randn(n, width, generator=g).to(dtype).to(device()) for n in (rows, rows, groups))
+    dx, dgain = sol.rmsnorm_backward(dy, s, gain, eps=0.0)
+    want, want_gain, size, terms = R.rmsnorm_backward(f64(dy), f64(s), f64(gain), None, 0.0)
+    unit = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}[dtype]
+    tiny = {torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24, torch.float32: 2.0 ** -126}[dtype]
+    assert np.all(np.abs(f64(dx) - want) <= np.abs(want) * unit + size * 2.0 ** -18 * (1 + unit) + tiny)
+    assert np.all(np.abs(f64(dgain) - want_gain) <= terms * (2.0 ** -18 + (rows + 64) * 2.0 ** -24) + 1e-30)
+
+
+@pytest.mark.parametrize("rows", [3, 700])
+def test_gradients_of_a_zero_row_without_eps(rows):
+    """0 times infinity is the row's own: its dx and its group's dgain are NaN, no other's."""
+    g = torch.Generator().manual_seed(rows)
+    dy, s, gain = (torch.randn(n, 72, generator=g).to(device()) for n in (2 * rows, 2 * rows, 2))
+    s[1] = 0
+    dx, dgain = sol.rmsnorm_backward(dy, s, gain, eps=0.0)
+    keep = torch.arange(2 * rows, device=device()) != 1
+    assert torch.all(torch.isnan(dx[1])) and torch.all(torch.isfinite(dx[keep]))
+    assert torch.all(torch.isnan(dgain[0])) and torch.all(torch.isfinite(dgain[1]))
