@@ -400,9 +400,12 @@ SOLFP4_API int mxfp4_linear(const uint16_t* x, const uint8_t* w_codes, const uin
  *            refused (SOLFP4_EINVAL); columns of one buffer are apart
  *
  * The norm is taken of the FP32 sum, not of its rounded form.  width is at
- * most 24576.  A row with a NaN or an infinity gives NaN; the squares are
- * FP32, so rows beyond 2^63 overflow.  rows == 0 or width == 0 launches
- * nothing.  Strides of inputs may be 0 (one row for all); output rows must
+ * most 24576.  A row with a NaN is NaN; a row with an infinity has rho = 0,
+ * so it is NaN where it is infinite and 0 elsewhere.  The squares are FP32:
+ * rows beyond 2^63 overflow to rho = 0, and with eps == 0 rows under 2^-63
+ * lose bits and, once their squares are all 0, get an infinite rho, as a row
+ * of zeros does (NaN).  rows == 0 or width == 0 launches nothing.  Strides of
+ * inputs may be 0 (one row for all); output rows must
  * not overlap.
  */
 SOLFP4_API int solfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual,
@@ -412,7 +415,8 @@ SOLFP4_API int solfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, con
 
 /*
  * The same with the output quantized in the same pass, width % 32 == 0, from
- * the FP32 result (no rounding to `type` in between):
+ * the FP32 result (no rounding to `type` in between).  Squares and rho are
+ * formed in 64 bits: rows of a root mean square from 2^-126 to 2^126.
  *
  *   mxfp8_add_rmsnorm  codes [rows][width] uint8, E4M3 (OCP E4M3FN);
  *                      scales [rows][width/32] uint8, E8M0, with
@@ -458,7 +462,9 @@ SOLFP4_API size_t solfp4_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t 
  * dx, dgain and the workspace must not overlap each other or, but for dx in
  * place, what the call reads (SOLFP4_EINVAL).
  *
- * Sums over rows are formed in an order that depends on the sizes and the
+ * A row with a NaN or an infinity, or beyond the range of the forward call's
+ * FP32 squares, spoils its own dx and its group's dgain, no others.  Sums over
+ * rows are formed in an order that depends on the sizes and the
  * device alone: results are the same on every call.
  */
 SOLFP4_API int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const void* x,

@@ -185,12 +185,17 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
   if constexpr (kOut == kNormSame) {
     rho = 1.0f / __builtin_sqrtf(q[0] / (float)a.width + a.eps);
   } else {
-    // an FP32 root and two Newton steps: 2^-22, 2^-43, beyond 2^-50
+    // The FP32 root of v scaled by an even power of two to [1/2, 2), where FP32
+    // holds it whatever v is, and two Newton steps: 2^-22, 2^-43, beyond
+    // 2^-50.  The root of 0, infinity and NaN is what it is.
     const double v = q[0] / (double)a.width + (double)a.eps;
-    rho = 1.0f / __builtin_sqrtf((float)v);
-    if (rho < 0x1p126f)   // else v is 0, a subnormal FP32 or NaN: rho as it is
+    const int half = __builtin_amdgcn_frexp_exp(v) >> 1;
+    const double m = __builtin_ldexp(v, -2 * half);
+    rho = 1.0f / __builtin_sqrtf((float)m);
+    if (rho > 0.0 && rho < __builtin_inf())
 #pragma unroll
-      for (int i = 0; i < 2; ++i) rho = rho * (1.5 - 0.5 * v * rho * rho);
+      for (int i = 0; i < 2; ++i) rho = rho * (1.5 - 0.5 * m * rho * rho);
+    rho = __builtin_ldexp(rho, -half);
   }
   const float rho32 = (float)rho;
   uint8_t* outr = row_of<kType>(a.out, at, a.out_stride);
