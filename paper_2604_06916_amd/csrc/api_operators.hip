@@ -118,7 +118,7 @@ int add_rmsnorm(int type, int kind, const void* x, int64_t x_stride, const void*
                 void* stream) {
   const solfp4::NormArgs a = {x, x_stride, residual, residual_stride, gain, gain_stride,
                               groups > 0 && rows > 0 ? rows / groups : 1, eps, sum, sum_stride, out, out_stride,
-                              codes, scales, rows, width};
+                              codes, scales, rows, width, 0};
   const int rc = norm_checks(type, a, groups, kind);
   if (rc) return rc;
   const hipError_t e = solfp4::launch_add_rmsnorm(type, kind, a, static_cast<hipStream_t>(stream));

@@ -28,6 +28,10 @@ hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_
   return launch_impl(kernel, grid, block, stream, std::index_sequence_for<P...>{}, t);
 }
 
+// Threads that a launch may have along one dimension (HIP's limit); more rows
+// or tokens than they hold take another launch.
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
+
 // First quantize pass: at most this many partial maxima (workspace words).
 constexpr int kMaxPartials = 1024;
 // Encode pass: grid-stride loop over at most this many workgroups (eight
@@ -219,6 +223,7 @@ struct NormArgs {
   int64_t out_stride;
   uint8_t *codes, *scales;   // kNormMxfp8, kNormMxfp4: contiguous
   int64_t rows, width;
+  int64_t first;             // first row of a launch (set by it)
 };
 hipError_t launch_add_rmsnorm(int type, int out, const NormArgs& a, hipStream_t stream);
 

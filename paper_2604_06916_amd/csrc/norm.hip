@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_rmsnorm_kernel(Norm
   using Sum = std::conditional_t<kOut == kNormSame, float, double>;   // block_scale
   __shared__ Sum lds[kNormMaxWaves][1];
   const Place<kRuns> at_(sh);
-  const int64_t row = (int64_t)blockIdx.x * sh.waves_slots(blockDim.x / kWave) + at_.slot;
+  const int64_t row = a.first + (int64_t)blockIdx.x * sh.waves_slots(blockDim.x / kWave) + at_.slot;
   const int lane = at_.lane, step = at_.step;
   const int width = row < a.rows ? (int)a.width : 0;   // no elements of a row past the last
   const int64_t at = row < a.rows ? row : 0;
@@ -243,18 +243,29 @@ static RowShape row_shape(int64_t width, int most) {
 }
 
 template <int kType, int kOut>
-static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
+static auto norm_kernel(int runs) {
+  switch (runs) {
+    case 1: return add_rmsnorm_kernel<kType, kOut, 1>;
+    case 2: return add_rmsnorm_kernel<kType, kOut, 2>;
+    case 3: return add_rmsnorm_kernel<kType, kOut, 3>;
+    case 4: return add_rmsnorm_kernel<kType, kOut, 4>;
+    case 5: return add_rmsnorm_kernel<kType, kOut, 5>;
+    default: return add_rmsnorm_kernel<kType, kOut, 6>;
+  }
+}
+
+template <int kType, int kOut>
+static hipError_t launch_norm(NormArgs a, hipStream_t stream) {
   const RowShape sh = row_shape(a.width, kNormRuns<kType>);
   const int waves = sh.wpr > 4 ? sh.wpr : 4, slots = sh.waves_slots(waves);
-  const dim3 grid((unsigned)((a.rows + slots - 1) / slots)), block(waves * kWave);
-  switch (sh.runs) {
-    case 1: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 1>, grid, block, stream, a, sh);
-    case 2: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 2>, grid, block, stream, a, sh);
-    case 3: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 3>, grid, block, stream, a, sh);
-    case 4: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 4>, grid, block, stream, a, sh);
-    case 5: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 5>, grid, block, stream, a, sh);
-    default: return launch_kernel(add_rmsnorm_kernel<kType, kOut, 6>, grid, block, stream, a, sh);
+  const int64_t most = kMaxThreads / (waves * kWave) * slots;   // rows of one launch
+  for (a.first = 0; a.first < a.rows; a.first += most) {
+    const int64_t rows = a.rows - a.first < most ? a.rows - a.first : most;
+    const hipError_t e = launch_kernel(norm_kernel<kType, kOut>(sh.runs), dim3((unsigned)((rows + slots - 1) / slots)),
+                                       dim3(waves * kWave), stream, a, sh);
+    if (e != hipSuccess) return e;
   }
+  return hipSuccess;
 }
 
 template <int kType>
