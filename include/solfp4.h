@@ -520,7 +520,8 @@ SOLFP4_API int solfp4_rotary_table(const int64_t* positions, int64_t rows, const
  *              follow each other
  *
  * A position outside [0, table_rows) gives NaN in the rotated elements of
- * its token and reads nothing outside the table.
+ * its token and reads nothing outside the table.  dim and each count of heads
+ * are below 2^20, (q_heads + k_heads) dim is below 2^31.
  */
 #define SOLFP4_ROTARY_HALF 0
 #define SOLFP4_ROTARY_INTERLEAVED 1

@@ -314,6 +314,7 @@ int solfp4_rotary(int type, int layout, int inverse, const void* q, int64_t q_to
   if ((rc = rotary_operand(type, &a.k, k, k_token_stride, k_head_stride, k_out, k_out_token_stride, k_out_head_stride,
                            k_heads, tokens, dim)))
     return rc;
+  if ((q_heads + k_heads) * dim >= kMaxDim) return SOLFP4_ESHAPE;
   if (tokens == 0 || dim == 0 || q_heads + k_heads == 0) return SOLFP4_OK;
   if ((position_bytes != 0) != (positions != nullptr)) return SOLFP4_EINVAL;
   if (rotated > 0 && (!table || table_rows == 0)) return SOLFP4_EINVAL;
@@ -336,10 +337,6 @@ int solfp4_rotary(int type, int layout, int inverse, const void* q, int64_t q_to
         (positions && !apart(out, block_of(positions, tokens * position_bytes))))
       return SOLFP4_EINVAL;
   }
-  // waves are numbered in 32 bits
-  if (solfp4::rotary_waves(type, layout == SOLFP4_ROTARY_INTERLEAVED, tokens, dim, rotated, q_heads + k_heads) >
-      kMaxGroups)
-    return SOLFP4_ESHAPE;
   a.table = table, a.table_rows = table_rows > 0 ? table_rows : 1;
   a.positions = positions, a.tokens = tokens, a.dim = (int)dim, a.rotated = (int)rotated;
   const hipError_t e = solfp4::launch_rotary(type, layout == SOLFP4_ROTARY_INTERLEAVED, inverse != 0, position_bytes,

@@ -263,9 +263,8 @@ struct RotaryArgs {
   const void* positions;       // NULL: token % table_rows
   int64_t tokens;
   int dim, rotated;
+  int64_t first;               // first token of a launch (set by it)
 };
-// Waves of the launch (host only; all sizes positive).
-int64_t rotary_waves(int type, bool interleaved, int64_t tokens, int64_t dim, int64_t rotated, int64_t heads);
 hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,
                          hipStream_t stream);
 

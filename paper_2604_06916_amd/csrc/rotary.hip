@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a, Ro
   if (sh.parts > 1) part = unit % sh.parts, unit /= sh.parts;
   const int at_slot = lane / sh.lanes, c = (int)block * sh.lanes + lane - at_slot * sh.lanes;
   const int sub = at_slot / sh.slots;
-  const int64_t token = (int64_t)unit * sh.packed + sub;
+  const int64_t token = a.first + (int64_t)unit * sh.packed + sub;
   if (c >= sh.pieces || sub >= sh.packed || token >= a.tokens) return;
   const int half = a.rotated / 2;
   const bool copies = c >= sh.turning;
@@ -225,9 +225,8 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a, Ro
 // Waves wanted a CU; with fewer tokens their heads are split.
 constexpr int64_t kRotaryWaves = 16;
 
-// The shape of a launch and its waves, for vectors of VE elements.
-static RotaryShape rotary_shape(int VE, bool interleaved, int64_t tokens, int64_t dim, int64_t rotated, int64_t heads,
-                                int64_t* waves) {
+// The shape of a call's launches, for vectors of VE elements.
+static RotaryShape rotary_shape(int VE, bool interleaved, int64_t tokens, int64_t dim, int64_t rotated, int64_t heads) {
   const int64_t span = interleaved ? rotated : rotated / 2;
   RotaryShape sh;
   sh.turning = (int)((span + VE - 1) / VE);
@@ -241,26 +240,29 @@ static RotaryShape rotary_shape(int VE, bool interleaved, int64_t tokens, int64_
   const int64_t least = (rounds + kRotaryHeads - 1) / kRotaryHeads;
   const int64_t wanted = (kRotaryWaves * device_cu_count() + units - 1) / units;
   sh.parts = (int)(wanted < least ? least : wanted < rounds ? wanted : rounds);
-  *waves = units * sh.parts * sh.blocks;
   return sh;
 }
 
-int64_t rotary_waves(int type, bool interleaved, int64_t tokens, int64_t dim, int64_t rotated, int64_t heads) {
-  int64_t waves;
-  rotary_shape(type == SOLFP4_F32 ? 4 : 8, interleaved, tokens, dim, rotated, heads, &waves);
-  return waves;
-}
-
 template <int kType>
-static hipError_t launch_rotary_type(bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,
+static hipError_t launch_rotary_type(bool interleaved, bool inverse, int position_bytes, RotaryArgs a,
                                      hipStream_t stream) {
-  int64_t waves;
   const RotaryShape sh = rotary_shape(16 / kElemBytes<kType>, interleaved, a.tokens, a.dim, a.rotated,
-                                      (int64_t)a.q.heads + a.k.heads, &waves);
-  const dim3 grid((unsigned)((waves + kRotaryThreads / kWave - 1) / (kRotaryThreads / kWave))), block(kRotaryThreads);
+                                      (int64_t)a.q.heads + a.k.heads);
+  constexpr int kWaves = kRotaryThreads / kWave;
+  // waves of `packed` tokens, and so tokens of one launch (heads x dim below
+  // 2^31 are fewer than 2^26 waves)
+  const int64_t each = (int64_t)sh.parts * sh.blocks;
+  const int64_t most = kMaxThreads / kRotaryThreads * kWaves / each * sh.packed;
   const float sign = inverse ? -1.0f : 1.0f;
-  return interleaved ? launch_kernel(rotary_kernel<kType, true>, grid, block, stream, a, sh, position_bytes, sign)
-                     : launch_kernel(rotary_kernel<kType, false>, grid, block, stream, a, sh, position_bytes, sign);
+  for (a.first = 0; a.first < a.tokens; a.first += most) {
+    const int64_t tokens = a.tokens - a.first < most ? a.tokens - a.first : most;
+    const int64_t waves = (tokens + sh.packed - 1) / sh.packed * each;
+    const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves)), block(kRotaryThreads);
+    const hipError_t e = launch_kernel(interleaved ? rotary_kernel<kType, true> : rotary_kernel<kType, false>, grid,
+                                       block, stream, a, sh, position_bytes, sign);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,

@@ -86,3 +86,20 @@ def test_gradients_past_4gib():
     assert dx is dy and torch.equal(dy[at], want)
     # FP32 sums of the kernel's 2^-18 terms in partial sums of at most 2^12 rows, then 2^9 parts
     assert bool(((dgain.double() - sums).abs() <= terms * (2.0 ** -17 + (2 ** 12 + 2 ** 9) * 2.0 ** -24)).all())
+
+
+def test_rotary_past_a_launch():
+    """A head of 33 pieces of 16 bytes takes a wave: 2^26 tokens of one head are 2^32 threads."""
+    tokens, dim = (1 << 26) + 5, 251
+    q = torch.empty((tokens, 1, dim), dtype=torch.bfloat16, device=device())
+    q.normal_(generator=torch.Generator(device=device()).manual_seed(4))
+    table = sol.rotary_table(sol.rotary_frequencies(2), 513)
+    at = sample(tokens, 2 * dim, 1 << 26)
+    kept, want = q[at], sol.rotary(q[at], None, table, at % 513, layout="interleaved")[0]
+    say(f"  {tokens} tokens of a head of {dim} ({q.numel() * 2 / 2**30:.1f} GiB) in place")
+    sol.rotary(q, None, table, layout="interleaved", q_out=q)
+    assert torch.equal(q[at], want)
+    # back again; every token's rotated pair keeps its length
+    sol.rotary(q, None, table, layout="interleaved", inverse=True, q_out=q)
+    assert torch.equal(q[at][..., 2:], kept[..., 2:])
+    assert bool(((q[at] - kept)[..., :2].float().abs() <= 2.0 ** -6 * kept[..., :2].float().abs().amax(-1, True)).all())

@@ -246,3 +246,11 @@ def test_table_over_positions_or_frequencies_is_refused():
     for i, n in ((1, 16 * 8), (3, 8 * 8)):
         assert call(apart(i)) == EINVAL and call(at((i << 32) + n - 4)) == EINVAL and call(at((i << 32) + n)) == PASSED
     assert call(apart(3), None) == PASSED
+
+
+def test_rotary_sizes_beyond_the_stated_ones_are_refused():
+    def call(heads=1, dim=64, tokens=4):
+        return sol.lib.solfp4_rotary(0, 0, 0, apart(0), heads * dim, dim, apart(1 << 8), heads * dim, dim, heads, None, 0, 0,
+                                     None, 0, 0, 0, apart(1 << 10), 16, None, 0, tokens, dim, 64, None)
+    assert call(heads=1 << 20) == ESHAPE and call(dim=1 << 20) == ESHAPE and call(tokens=1 << 31) == ESHAPE
+    assert call(heads=1 << 16, dim=1 << 15) == ESHAPE
