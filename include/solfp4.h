@@ -486,6 +486,7 @@ SOLFP4_API int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stri
  *               axis 0, the next with axis 1, ...; they add up to pairs.
  *               NULL with one axis
  *   axes        1 to 4
+ *   pairs       below 2^20
  *   table       [rows][2 pairs] FP32, written; must not overlap positions or
  *               frequencies (SOLFP4_EINVAL)
  *

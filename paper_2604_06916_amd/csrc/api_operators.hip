@@ -272,8 +272,8 @@ int solfp4_rotary_table(const int64_t* positions, int64_t rows, const double* fr
   int rc = check_dims(rows, pairs);
   if (rc) return rc;
   if (axes < 1 || (axes > 1 && (!axis_pairs || !positions))) return SOLFP4_EINVAL;
-  if (axes > solfp4::kRotaryMaxAxes || pairs >= 1 << 20 || rows * pairs > kMaxGroups * 256) return SOLFP4_ESHAPE;
-  solfp4::RotaryTableArgs a = {positions, frequencies, rows, (int)pairs, axes, {}, magnitude, table};
+  if (axes > solfp4::kRotaryMaxAxes || pairs >= 1 << 20) return SOLFP4_ESHAPE;
+  solfp4::RotaryTableArgs a = {positions, frequencies, rows, (int)pairs, axes, {}, magnitude, table, 0};
   int64_t end = axis_pairs ? 0 : pairs;
   for (int i = 0; i < axes; ++i) {
     if (axis_pairs) {

@@ -277,8 +277,9 @@ struct RotaryTableArgs {
   int axis_end[kRotaryMaxAxes];   // pairs before axis_end[a] and not before axis_end[a - 1] turn with axis a
   double magnitude;
   float* table;
+  int64_t first;               // first row of a launch (set by it)
 };
-hipError_t launch_rotary_table(const RotaryTableArgs& a, hipStream_t stream);
+hipError_t launch_rotary_table(RotaryTableArgs a, hipStream_t stream);
 
 // ---- few tokens with 4-bit weights (weight_linear.hip) --------------------
 struct WeightLinearArgs {

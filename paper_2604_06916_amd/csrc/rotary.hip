@@ -278,7 +278,7 @@ hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_
 // worth of angle already.
 __global__ __launch_bounds__(kRotaryThreads) void rotary_table_kernel(RotaryTableArgs a) {
   const int64_t unit = (int64_t)blockIdx.x * kRotaryThreads + threadIdx.x;
-  const int64_t row = unit / a.pairs;
+  const int64_t row = a.first + unit / a.pairs;
   const int i = (int)(unit % a.pairs);
   if (row >= a.rows) return;
   int axis = 0;
@@ -291,11 +291,18 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_table_kernel(RotaryTabl
   t[a.pairs] = (float)(s * a.magnitude);
 }
 
-hipError_t launch_rotary_table(const RotaryTableArgs& a, hipStream_t stream) {
-  const int64_t units = a.rows * a.pairs;
-  if (units == 0) return hipSuccess;
-  return launch_kernel(rotary_table_kernel, dim3((unsigned)((units + kRotaryThreads - 1) / kRotaryThreads)),
-                       dim3(kRotaryThreads), stream, a);
+hipError_t launch_rotary_table(RotaryTableArgs a, hipStream_t stream) {
+  if (a.rows == 0 || a.pairs == 0) return hipSuccess;
+  const int64_t most = kMaxThreads / kRotaryThreads * kRotaryThreads / a.pairs;   // rows of one launch
+  const int64_t rows = a.rows;
+  for (a.first = 0; a.first < rows; a.first += most) {
+    a.rows = rows - a.first < most ? rows : a.first + most;   // the last workgroup ends with the launch's rows
+    const int64_t units = (a.rows - a.first) * a.pairs;
+    const hipError_t e = launch_kernel(rotary_table_kernel, dim3((unsigned)((units + kRotaryThreads - 1) / kRotaryThreads)),
+                                       dim3(kRotaryThreads), stream, a);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace solfp4

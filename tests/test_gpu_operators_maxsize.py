@@ -103,3 +103,17 @@ def test_rotary_past_a_launch():
     sol.rotary(q, None, table, layout="interleaved", inverse=True, q_out=q)
     assert torch.equal(q[at][..., 2:], kept[..., 2:])
     assert bool(((q[at] - kept)[..., :2].float().abs() <= 2.0 ** -6 * kept[..., :2].float().abs().amax(-1, True)).all())
+
+
+def test_table_past_a_launch():
+    """A pair a thread: 2^26 positions of 64 pairs are 2^32 threads."""
+    rows = (1 << 26) + 5
+    f = sol.rotary_frequencies(128).to(device())
+    say(f"  table of {rows} positions ({rows * 128 * 4 / 2**30:.1f} GiB)")
+    table = sol.rotary_table(f, rows)
+    at = sample(rows, 512, 1 << 26)
+    assert torch.equal(table[at], sol.rotary_table(f, at))
+    # every angle's cosine and sine
+    for i in range(0, rows, 1 << 24):
+        t = table[i:i + (1 << 24)]
+        assert float((t[:, :64].square() + t[:, 64:].square() - 1).abs().max()) < 2.0 ** -21
