@@ -261,7 +261,7 @@ struct RotaryArgs {
   const float* table;          // [table_rows][rotated]: cos of every pair, then sin
   int64_t table_rows;
   const void* positions;       // NULL: token % table_rows
-  int64_t tokens;
+  int64_t tokens;              // in a launch: its last token + 1
   int dim, rotated;
   int64_t first;               // first token of a launch (set by it)
 };
@@ -272,7 +272,7 @@ constexpr int kRotaryMaxAxes = 4;
 struct RotaryTableArgs {
   const int64_t* positions;    // [rows][axes], NULL: the row's index on one axis
   const double* frequencies;   // [pairs]
-  int64_t rows;
+  int64_t rows;                // in a launch: its last row + 1
   int pairs, axes;
   int axis_end[kRotaryMaxAxes];   // pairs before axis_end[a] and not before axis_end[a - 1] turn with axis a
   double magnitude;

@@ -254,9 +254,10 @@ static hipError_t launch_rotary_type(bool interleaved, bool inverse, int positio
   const int64_t each = (int64_t)sh.parts * sh.blocks;
   const int64_t most = kMaxThreads / kRotaryThreads * kWaves / each * sh.packed;
   const float sign = inverse ? -1.0f : 1.0f;
-  for (a.first = 0; a.first < a.tokens; a.first += most) {
-    const int64_t tokens = a.tokens - a.first < most ? a.tokens - a.first : most;
-    const int64_t waves = (tokens + sh.packed - 1) / sh.packed * each;
+  const int64_t tokens = a.tokens;
+  for (a.first = 0; a.first < tokens; a.first += most) {
+    a.tokens = tokens - a.first < most ? tokens : a.first + most;   // the last workgroup ends with the launch's tokens
+    const int64_t waves = (a.tokens - a.first + sh.packed - 1) / sh.packed * each;
     const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves)), block(kRotaryThreads);
     const hipError_t e = launch_kernel(interleaved ? rotary_kernel<kType, true> : rotary_kernel<kType, false>, grid,
                                        block, stream, a, sh, position_bytes, sign);

@@ -117,3 +117,19 @@ def test_table_past_a_launch():
     for i in range(0, rows, 1 << 24):
         t = table[i:i + (1 << 24)]
         assert float((t[:, :64].square() + t[:, 64:].square() - 1).abs().max()) < 2.0 ** -21
+
+
+def test_rotary_past_a_launch_of_odd_waves():
+    """11 waves a token: the workgroups of four that a launch ends with reach
+    into the tokens after it, which must turn once all the same."""
+    per_launch = 4 * ((1 << 24) - 1) // 11
+    tokens, heads, dim = per_launch + 5, 22, 251
+    assert per_launch * 11 % 4
+    q = torch.empty((tokens, heads, dim), dtype=torch.bfloat16, device=device())
+    q.normal_(generator=torch.Generator(device=device()).manual_seed(5))
+    table = sol.rotary_table(sol.rotary_frequencies(2), 513)
+    at = torch.cat((sample(tokens, 2 * heads * dim), torch.arange(per_launch - 5, tokens, device=device())))
+    want = sol.rotary(q[at], None, table, at % 513, layout="interleaved")[0]
+    say(f"  {tokens} tokens of {heads} heads of {dim} ({q.numel() * 2 / 2**30:.1f} GiB) in place")
+    sol.rotary(q, None, table, layout="interleaved", q_out=q)
+    assert torch.equal(q[at], want)
