@@ -12,8 +12,6 @@ namespace {
 
 constexpr int64_t kMaxDim = (int64_t)1 << 31;
 constexpr int64_t kMaxK = (int64_t)1 << 24, kMaxN = (int64_t)1 << 22;
-// a launch has at most 2^31 workgroups
-constexpr int64_t kMaxGroups = kMaxDim - 1;
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
@@ -148,7 +146,6 @@ int linear_checks(const void* x, const void* x_scales, bool scaled_x, const void
   rc = check_dims(K, 0);
   if (rc) return rc;
   if (K % block || K >= kMaxK || N >= kMaxN) return SOLFP4_ESHAPE;
-  if (solfp4::weight_linear_groups(M, N) > kMaxGroups) return SOLFP4_ESHAPE;
   if (M == 0 || N == 0) return SOLFP4_OK;
   if (!out || (has_global && !wg)) return SOLFP4_EINVAL;
   if (K > 0 && (!x || !wc || !ws || (scaled_x && !x_scales))) return SOLFP4_EINVAL;

@@ -292,8 +292,6 @@ struct WeightLinearArgs {
   uint16_t* out;               // [M][N]
   int64_t M, N, K;
 };
-// Workgroups of the launch (host only).
-int64_t weight_linear_groups(int64_t M, int64_t N);
 hipError_t launch_weight_linear(int w_format, bool x_mxfp8, const WeightLinearArgs& a, hipStream_t stream);
 
 }  // namespace solfp4

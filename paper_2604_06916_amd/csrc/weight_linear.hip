@@ -389,15 +389,23 @@ static Tile tile_of(int64_t M, int64_t N, bool few) {
   return {2, 2, 4};
 }
 
-int64_t weight_linear_groups(int64_t M, int64_t N) { return tile_of(M, N, true).groups(M, N); }
-
 template <int kFormat, bool kX8, int MT, int NT, int XR, int W>
 static hipError_t launch_tile(const WeightLinearArgs& a, hipStream_t stream) {
-  const int tiles_m = (int)((a.M + 16 * MT - 1) / (16 * MT));
-  const dim3 grid((unsigned)Tile{MT, NT, W}.groups(a.M, a.N)), block(W * kWave);
-  if (a.K % kWLStep == 0)
-    return launch_kernel(weight_linear_kernel<kFormat, kX8, true, MT, NT, XR, W>, grid, block, stream, a, tiles_m);
-  return launch_kernel(weight_linear_kernel<kFormat, kX8, false, MT, NT, XR, W>, grid, block, stream, a, tiles_m);
+  const auto kernel = a.K % kWLStep == 0 ? weight_linear_kernel<kFormat, kX8, true, MT, NT, XR, W>
+                                         : weight_linear_kernel<kFormat, kX8, false, MT, NT, XR, W>;
+  // tokens of one launch, by whole tiles (N < 2^22 leaves at least one)
+  const int64_t most = kMaxThreads / (W * kWave) / Tile{MT, NT, W}.groups(1, a.N) * (16 * MT);
+  for (int64_t m = 0; m < a.M; m += most) {
+    WeightLinearArgs p = a;
+    p.M = a.M - m < most ? a.M - m : most;
+    p.x = static_cast<const uint8_t*>(a.x) + m * a.K * (kX8 ? 1 : 2);
+    if (kX8) p.x_scales += m * (a.K / 32);
+    p.out += m * a.N;
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)Tile{MT, NT, W}.groups(p.M, p.N)), dim3(W * kWave), stream,
+                                       p, (int)((p.M + 16 * MT - 1) / (16 * MT)));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <int kFormat, bool kX8>

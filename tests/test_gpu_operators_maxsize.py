@@ -133,3 +133,28 @@ def test_rotary_past_a_launch_of_odd_waves():
     say(f"  {tokens} tokens of {heads} heads of {dim} ({q.numel() * 2 / 2**30:.1f} GiB) in place")
     sol.rotary(q, None, table, layout="interleaved", q_out=q)
     assert torch.equal(q[at], want)
+
+
+@pytest.mark.parametrize("kind", ["nvfp4", "mxfp8"])
+def test_linear_past_a_launch(kind):
+    """Tiles of 32 tokens in workgroups of 256 threads: 2^29 tokens are 2^32 threads."""
+    M, N, K = (1 << 29) + 37, 3, 16 if kind == "nvfp4" else 32
+    g = torch.Generator(device=device()).manual_seed(6)
+    u8 = dict(dtype=torch.uint8, device=device())
+    w = [torch.randint(256, (N, K // 2), generator=g, **u8),
+         torch.randint(100, 140, (N, K // 32), generator=g, **u8) if kind == "mxfp8" else
+         torch.randint(8, 120, (N, K // 16), generator=g, **u8)]
+    if kind == "mxfp8":
+        x = [torch.randint(0, 126, (M, K), generator=g, **u8), torch.randint(110, 130, (M, K // 32), generator=g, **u8)]
+        call = sol.mxfp8_linear
+    else:
+        w.append(torch.ones(1, device=device()))
+        x = [torch.empty((M, K), dtype=torch.bfloat16, device=device()).normal_(generator=g)]
+        call = sol.nvfp4_weight_linear
+    bias = torch.randn(N, generator=g, device=device()).bfloat16()
+    say(f"  {kind} {M} x {N} x {K} ({x[0].numel() * x[0].element_size() / 2**30:.1f} GiB of activations)")
+    out = torch.full((M, N), float("nan"), dtype=torch.bfloat16, device=device())
+    call(*x, *w, bias, out)
+    at = torch.cat((sample(M, K * x[0].element_size(), 1 << 29), torch.arange((1 << 29) - 40, M, device=device())))
+    assert torch.equal(out[at], call(*(t[at] for t in x), *w, bias))
+    assert not bool(torch.isnan(out).any())
