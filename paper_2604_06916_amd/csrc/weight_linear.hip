@@ -33,6 +33,15 @@ constexpr int kWLStep = 128;      // K a step
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
+// Between one wave's LDS accesses by some lanes and by others: they keep their
+// order (the hardware runs a wave's LDS instructions in theirs, so no wait is
+// needed).
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // An E8M0 byte as the converters take it (they read the exponent field: 0 is 2^-127).
 __device__ __forceinline__ float e8m0_float(uint32_t b) { return __uint_as_float(b << 23); }
 
@@ -244,6 +253,7 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
   }
 
   for (int s = first; s < last; s += 4) {
+    wave_order();
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i)
       if (i * kWave + lane < NT * 16 * kScalePieces)
@@ -253,6 +263,7 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
     for (int v = 0; v < 4; ++v) {
       if (s + v >= last) break;
       if (s + v == steps - 1) trim(c, s + v);
+      if (v > 0) wave_order();
 #pragma unroll
       for (int t = 0; t < NT; ++t) *reinterpret_cast<u32x4_t*>(w_to + t * 1024) = c.w[t];
 #pragma unroll
@@ -260,6 +271,7 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
         const int row = j * (64 / P) + xr;
         *reinterpret_cast<u32x4_t*>(lx + row * (16 * P) + 16 * (xp ^ (row & (P - 1)))) = c.x[j];
       }
+      wave_order();
       uint32_t sx[MT];
 #pragma unroll
       for (int t = 0; t < MT; ++t) sx[t] = kX8 ? c.xs[t] : 0u;
@@ -305,8 +317,8 @@ __global__ __launch_bounds__(W * kWave) void weight_linear_kernel(WeightLinearAr
     }
   }
 
-  // each wave's sums in place of its buffer (its reads are done: one wave's
-  // LDS operations keep their order)
+  // each wave's sums in place of its buffer, after its reads
+  wave_order();
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
