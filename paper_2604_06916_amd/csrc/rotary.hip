@@ -147,8 +147,8 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a, Ro
   // First element and count of the lane's piece (and of its partner R/2
   // further on).  The last piece of a span that it does not fill starts early
   // instead: a whole vector that repeats elements of the lane before.  Both
-  // lanes have read them before either writes (one wave, one instruction), and
-  // write the same values.
+  // lanes have read them before either writes (in place they are the same
+  // memory: one wave, one load, and the fence below), and write the same values.
   const int span = copies ? a.dim - a.rotated : kInterleaved ? a.rotated : half;
   int at = (copies ? c - sh.turning : c) * VE;
   if (sh.blocks == 1 && span >= VE) at = min(at, span - VE);
@@ -191,6 +191,9 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a, Ro
     pu[j] = load_piece<kType, VE>(in, n);
     if (!kInterleaved && !copies) pv[j] = load_piece<kType, VE>(in + apart, n);
   }
+  // no lane's store before another's load
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int j = 0; j < kRotaryHeads; ++j) {
     if (h0 + j * hop >= heads) continue;
