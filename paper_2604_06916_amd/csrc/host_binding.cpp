@@ -17,7 +17,10 @@
 // with a kept output and workspace, in MXFP4, 14.5 -> 8.2.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/Context.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <ATen/ops/empty.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
 
 #include "solfp4.h"
 
@@ -47,8 +50,14 @@ void need_tensor(const Tensor& t, at::ScalarType type, at::IntArrayRef shape, co
 
 void need_matrix(const Tensor& t) { need(t.layout() == at::kStrided && t.dim() == 2); }
 
-// The device's allocation itself, without the dispatcher's way to it.
+// The device's allocation itself, without the dispatcher's way to it (0.3 us
+// an output), unless a dispatch mode looks on or torch is asked to fill fresh
+// memory.
 Tensor make(at::IntArrayRef shape, at::ScalarType type, const at::Device& dev) {
+  const at::Context& context = at::globalContext();
+  if (c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::Python) ||
+      (context.deterministicAlgorithms() && context.deterministicFillUninitializedMemory()))
+    return at::empty(shape, at::TensorOptions().dtype(type).device(dev));
   return at::detail::empty_cuda(shape, type, dev, std::nullopt);
 }
 

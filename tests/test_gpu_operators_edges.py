@@ -163,3 +163,56 @@ def test_quantized_norm_of_large_and_small_rows(kind, dtype, size):
     unit = np.repeat(np.exp2(scales - 127.0), 32, axis=1)
     v = np.clip(want / unit, -most, most)
     assert np.all(np.abs(got / unit - v) <= np.abs(v) * (step + d) + least)
+
+
+# ---- allocations ----------------------------------------------------------
+
+def allocating_calls():
+    x = torch.randn(32, 64, generator=torch.Generator().manual_seed(1)).bfloat16().to(device())
+    w = sol.nvfp4_quantize(x)
+    m = sol.mxfp4_quantize(x)
+    table = sol.rotary_table(sol.rotary_frequencies(16), 32)
+    heads = x.view(32, 4, 16)
+    m8 = sol.mxfp8_add_rmsnorm(x)[:2]
+    return {"nvfp4_quantize": lambda: sol.nvfp4_quantize(x), "mxfp4_quantize": lambda: sol.mxfp4_quantize(x),
+            "nvfp4_gemm": lambda: sol.nvfp4_gemm(*w, *w), "mxfp4_gemm": lambda: sol.mxfp4_gemm(*m, *m),
+            "nvfp4_linear": lambda: sol.nvfp4_linear(x, *w), "mxfp4_linear": lambda: sol.mxfp4_linear(x, *m),
+            "add_rmsnorm": lambda: sol.add_rmsnorm(x, x), "mxfp4_add_rmsnorm": lambda: sol.mxfp4_add_rmsnorm(x),
+            "rmsnorm_backward": lambda: sol.rmsnorm_backward(x, x, x[0]), "rotary": lambda: sol.rotary(heads, heads, table),
+            "nvfp4_weight_linear": lambda: sol.nvfp4_weight_linear(x, *w),
+            "mxfp8_linear": lambda: sol.mxfp8_linear(*m8, *m)}
+
+
+def test_allocations_are_seen_by_dispatch_modes():
+    """Outputs and workspaces that a call allocates go through torch's
+    dispatcher while a mode looks on, and hold the same results."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Seen(TorchDispatchMode):
+        def __init__(self):
+            super().__init__()
+            self.empties = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            self.empties += "empty" in str(func)
+            return func(*args, **(kwargs or {}))
+    for name, call in allocating_calls().items():
+        want = call()
+        with Seen() as seen:
+            got = call()
+        assert seen.empties > 0, name
+        pairs = zip(want, got) if isinstance(want, tuple) else [(want, got)]
+        assert all((a is None and b is None) or torch.equal(a, b) for a, b in pairs), name
+
+
+def test_results_with_deterministic_algorithms():
+    calls = allocating_calls()
+    want = {name: call() for name, call in calls.items()}
+    torch.use_deterministic_algorithms(True)
+    try:
+        got = {name: call() for name, call in calls.items()}
+    finally:
+        torch.use_deterministic_algorithms(False)
+    for name in calls:
+        pairs = zip(want[name], got[name]) if isinstance(want[name], tuple) else [(want[name], got[name])]
+        assert all((a is None and b is None) or torch.equal(a, b) for a, b in pairs), name
