@@ -171,12 +171,12 @@ class Runner:
         H, D = cfg.hidden, cfg.mlp
         self.buf = {n: torch.empty((M, c), dtype=torch.bfloat16, device=device)
                     for n, c in [("qkv", 3 * H), ("o", H), ("u", D), ("d", H)]}
-        if cfg.conditioned:
-            self._prepare_condition(model)
         self.linear_events = None
         self.op_events = None    # dict: op kind -> [(start, end)] of HIP events, when timing
         self.trace = None        # list: (stage name, tensor copy) of every block stage
         self.step_trace = None   # list: {"y": blocks output, "x": latents after} per Euler step
+        if cfg.conditioned:
+            self._prepare_condition(model)
 
     def _prepare_condition(self, model):
         """The modulations' weights, the condition's buffers, the residual
@@ -206,30 +206,36 @@ class Runner:
         blocks that run from here on (a captured step replays with the
         condition set last)."""
         time = self.time[step: step + 1].expand(self.cfg.rollouts, -1)
+        ev = self._op("condition")
         if self.backend == "mxfp4":
             sol.mxfp8_add_rmsnorm(time, self.text, None, EPS, *self.c)
         else:
             sol.add_rmsnorm(time, self.text, None, EPS, *self.c)
+        _end(ev)
 
     def _modulate(self, layer):
         """The two gains [rollouts, hidden] of one block."""
         q, b = layer
         H = self.cfg.hidden
+        ev = self._op("modulation")
         if self.backend == "mxfp4":
             sol.mxfp8_linear(*self.c, *q, b, self.gains)
         elif self.backend == "nvfp4":
             sol.nvfp4_weight_linear(*self.c, *q, b, self.gains)
         else:
             torch.addmm(b, *self.c, *q, out=self.gains)
+        _end(ev)
         return self.gains[:, :H], self.gains[:, H:]
 
     def _norm(self, x, residual, gain):
         """(x + residual, its norm as the linears take it)."""
         total = None if residual is None else self.buf["x"]
+        ev = self._op("norm")
         if self.backend == "mxfp4":
             sol.mxfp4_add_rmsnorm(x, residual, gain, EPS, *self.h, total)
         else:
             sol.add_rmsnorm(x, residual, gain, EPS, *self.h, total)
+        _end(ev)
         return x if residual is None else total
 
     def _trace_norm(self, name):
@@ -240,7 +246,10 @@ class Runner:
         if self.backend != "mxfp4":
             return self.linear(self.h[0], layer, out)
         q, b, _, _ = layer
-        return sol.mxfp4_gemm(*self.h, *q, b, out)
+        ev = self._linear_event()
+        sol.mxfp4_gemm(*self.h, *q, b, out)
+        _end(ev)
+        return out
 
     def _conditioned_blocks(self, x):
         cfg, B = self.cfg, self.buf
@@ -254,23 +263,36 @@ class Runner:
             qkv = self._linear_of_norm(L["qkv"], B["qkv"])
             self._t("qkv", qkv)
             heads = qkv.view(R * T, 3, Hh, hd)
+            ev = self._op("rotary")
             sol.rotary(heads[:, 0], heads[:, 1], self.table, layout="interleaved", q_out=heads[:, 0], k_out=heads[:, 1])
+            _end(ev)
             self._t("rotated", qkv)
             q, k, v = (qkv.view(R, T, 3, Hh, hd)[:, :, i].transpose(1, 2) for i in range(3))
+            ev = self._op("attention")
             with sdpa_kernel([SDPBackend.FLASH_ATTENTION, SDPBackend.EFFICIENT_ATTENTION]):
                 a = F.scaled_dot_product_attention(q, k, v)
+            _end(ev)
+            ev = self._op("copy")
             a = self._t("a", a.transpose(1, 2).reshape(R * T, cfg.hidden))
+            _end(ev)
             o = self._t("o", self.linear(a, L["out"], B["o"]))
             x = self._t("x2", self._norm(o, x, g2))
             self._trace_norm("h2")
             u = self._t("up", self._linear_of_norm(L["up"], B["u"]))
             fused = self.backend == "nvfp4"
+            ev = self._op("gelu+amax" if fused else "gelu")
             if fused:
                 sol.nvfp4_gelu_amax(u, self.down_amax)
             else:
                 torch.ops.aten.gelu_(u, approximate="tanh")
+            _end(ev)
             d = self._t("d", self.linear(B["u"], L["down"], B["d"], fused))
-        return x if d is None else self._t("x3", x + d)
+        if d is None:
+            return x
+        ev = self._op("residual")
+        x = self._t("x3", x + d)
+        _end(ev)
+        return x
 
     def _down_views(self, cfg):
         """The regions of the workspace that the down layer's quantizer and
@@ -304,14 +326,20 @@ class Runner:
             self.trace.append((name, t.clone()))
         return t
 
+    def _linear_event(self):
+        """A (start, end) event pair for one linear, or None."""
+        if self.linear_events is None:
+            return None
+        ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True))
+        ev[0].record()
+        self.linear_events.append(ev)
+        return ev
+
     def linear(self, x, layer, out, have_amax=False):
         """One linear; have_amax: x's partial maxima are in down_amax already
         (NVFP4 down layer)."""
         q, b, N, K = layer
-        ev = None
-        if self.linear_events is not None:
-            ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True))
-            ev[0].record()
+        ev = self._linear_event()
         if have_amax:
             a = sol.nvfp4_quantize_encode(x, *self.down_q, self.down_amax)
             sol.nvfp4_gemm(*a, *q, b, out, self.down_ws)
@@ -321,9 +349,7 @@ class Runner:
             sol.mxfp4_linear(x, q[0], q[1], b, out, self.ws)
         else:
             torch.addmm(b, x, q[0], out=out)
-        if ev is not None:
-            ev[1].record()
-            self.linear_events.append(ev)
+        _end(ev)
         return out
 
     def blocks(self, x):
@@ -331,33 +357,29 @@ class Runner:
             return self._conditioned_blocks(x)
         cfg, B = self.cfg, self.buf
         R, T, Hh, hd = cfg.rollouts, cfg.tokens, cfg.heads, cfg.head_dim
-        def end(ev):
-            if ev is not None:
-                ev[1].record()
-
         for L in self.layers:
             self._t("x", x)
             ev = self._op("norm")
             h = self._t("h1", _rmsnorm(x))
-            end(ev)
+            _end(ev)
             qkv = self._t("qkv", self.linear(h, L["qkv"], B["qkv"])).view(R, T, 3, Hh, hd)
             q, k, v = (qkv[:, :, i].transpose(1, 2) for i in range(3))   # [R, heads, T, hd] views
             ev = self._op("attention")
             with sdpa_kernel([SDPBackend.FLASH_ATTENTION, SDPBackend.EFFICIENT_ATTENTION]):
                 a = F.scaled_dot_product_attention(q, k, v)
-            end(ev)
+            _end(ev)
             # the fused attention lays its result out token by token, so this is
             # a view (a copy only if a backend lays it out by heads)
             ev = self._op("copy")
             a = self._t("a", a.transpose(1, 2).reshape(R * T, cfg.hidden))
-            end(ev)
+            _end(ev)
             o = self._t("o", self.linear(a, L["out"], B["o"]))
             ev = self._op("residual")
             x = self._t("x2", x + o)
-            end(ev)
+            _end(ev)
             ev = self._op("norm")
             h = self._t("h2", _rmsnorm(x))
-            end(ev)
+            _end(ev)
             u = self._t("up", self.linear(h, L["up"], B["u"]))
             fused = self.backend == "nvfp4"
             ev = self._op("gelu+amax" if fused else "gelu")
@@ -369,12 +391,12 @@ class Runner:
                 sol.nvfp4_gelu_amax(u, self.down_amax)
             else:
                 torch.ops.aten.gelu_(u, approximate="tanh")
-            end(ev)
+            _end(ev)
             self._t("g", B["u"])
             d = self._t("d", self.linear(B["u"], L["down"], B["d"], fused))
             ev = self._op("residual")
             x = self._t("x3", x + d)
-            end(ev)
+            _end(ev)
         return x
 
     def rollout(self, x0):
@@ -387,8 +409,7 @@ class Runner:
             y = self.blocks(x)
             ev = self._op("euler")
             x = (x.float() + dt * (y.float() - x.float())).to(torch.bfloat16)
-            if ev is not None:
-                ev[1].record()
+            _end(ev)
             if self.step_trace is not None:
                 self.step_trace.append({"y": y.clone(), "x": x.clone()})
         return x
@@ -415,6 +436,12 @@ class Runner:
         with torch.cuda.graph(g):
             self.euler_step_(x_static)
         return g
+
+
+def _end(ev):
+    """The end of an event pair, or nothing without one."""
+    if ev is not None:
+        ev[1].record()
 
 
 def _rmsnorm(x):
