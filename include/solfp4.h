@@ -450,7 +450,7 @@ SOLFP4_API size_t solfp4_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t 
  *   dy     [rows][width], the output's gradient
  *   x      [rows][width], s (the forward call's sum, or its x without a
  *          residual)
- *   gain, groups as in the forward call
+ *   gain, groups as in the forward call, with at most 65535 groups
  *   dsum   [rows][width], what reaches s past the norm; or NULL
  *   dx     [rows][width], written: the gradient of s, which is that of x and
  *          of the residual alike; may be dy, x or dsum (same address and stride)
@@ -545,11 +545,13 @@ SOLFP4_API int solfp4_rotary(int type, int layout, int inverse,
  *   mxfp8_linear         x_codes [M][K] E4M3, x_scales [M][K/32] E8M0 as
  *                        mxfp8_add_rmsnorm writes them; MXFP4 weight
  *
- * Products are exact and sums FP32 in a fixed order; decoded weights,
- * products or sums outside the FP32 range are unspecified.  Every 32 tokens
- * read the weight once (from L2 after the first): from a few hundred tokens
- * on, nvfp4_linear and mxfp4_linear are the faster calls.  M, N or K equal to 0 are valid (K == 0 writes the bias,
- * or zeros).  K must be below 2^24 and N below 2^22.  Packed operands, x, bias
+ * Products are exact and sums FP32 in a fixed order; decoded weights or
+ * activations, products or sums outside FP32's normal range are unspecified.
+ * Every 32 tokens read the weight once (from L2 after the first), so with more
+ * of them the linears that quantize the activations become the faster calls:
+ * mxfp4_linear from 32 tokens (18432 x 3072), 64 (9728 x 2432) or more than
+ * 512 (1152 x 1152), nvfp4_linear from about 100 and 200 (the first two).
+ * M, N or K equal to 0 are valid (K == 0 writes the bias, or zeros).  K must be below 2^24 and N below 2^22.  Packed operands, x, bias
  * and out are contiguous and 16-byte aligned, out must not overlap the others
  * (SOLFP4_EINVAL); no workspace.
  */

@@ -529,7 +529,8 @@ def add_rmsnorm(x, residual=None, gain=None, eps=1e-6, out=None, sum_out=None, s
     ([width], or [groups, width] with the rows dealt to the groups in order)
     -> (out, sum); sum, x + residual rounded to x's type, is None without a
     residual.  x [rows, width] BF16, FP16 or FP32, rows of any stride; sum_out
-    may be x or residual."""
+    may be x or residual.  Nothing is recorded for autograd here or in the other
+    calls: gradients are rmsnorm_backward's and rotary's with inverse=True."""
     if stream is None:
         r = _host.add_rmsnorm(x, residual, gain, eps, out, sum_out)
         if r is not None:

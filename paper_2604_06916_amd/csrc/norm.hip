@@ -11,7 +11,7 @@
 // A row belongs to `wpr` waves (1, 2, 4 or 8; as few as hold it in kNormRuns,
 // at most kNormMaxRuns, runs of 8 elements a lane), so a row is read once and
 // stays in registers between the sum and the output.  Rows of at most 256
-// elements (a head's q or k) share a wave: 32 lanes a row or fewer
+// elements (contiguous heads of q or k) share a wave: 32 lanes a row or fewer
 // (kRuns == 1).
 //
 // Bound by memory: 8 bytes an element in BF16 with a residual, 7.03 with MXFP8
@@ -35,8 +35,8 @@ __device__ __forceinline__ uint32_t quad_max_bits(uint32_t v) {
 // gives the largest scale and stays a NaN where the elements have one.
 //
 // An FP32 amax next to a power of two may lie on the wrong side of it, which
-// would double or halve the scale: within 4 units (y is within 2) the
-// comparison is made in 64 bits.  That takes a rho of more than 32 bits, for
+// would double or halve the scale: within 4 units (y is within 3, the
+// roundings of rho and the two products) the comparison is made in 64 bits.  That takes a rho of more than 32 bits, for
 // which the row's squares are summed in 64.
 template <int kEmax>
 __device__ __forceinline__ uint32_t block_scale(const float (&y)[8], const float (&s)[8], const float (&g)[8],

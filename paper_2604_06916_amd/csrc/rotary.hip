@@ -278,8 +278,8 @@ hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_
 }
 
 // The angle and its cosine and sine in 64 bits, each rounded once: an FP32
-// product of a position of 10^5 and its frequency is off by up to 2^-8 turns'
-// worth of angle already.
+// product of a position of 10^5 and its frequency is off by up to 2^-8 radians
+// already.
 __global__ __launch_bounds__(kRotaryThreads) void rotary_table_kernel(RotaryTableArgs a) {
   const int64_t unit = (int64_t)blockIdx.x * kRotaryThreads + threadIdx.x;
   const int64_t row = a.first + unit / a.pairs;

@@ -426,7 +426,8 @@ class Runner:
         """One Euler step on the static buffer x_static, captured as a HIP
         graph (warmed up once on a side stream first, which advances
         x_static by a step); replaying it T times from the initial latents
-        is the rollout without any host launch cost."""
+        is the rollout without any host launch cost.  Conditioned blocks take
+        the condition set last: set_step(t) before the replay of step t."""
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
