@@ -405,8 +405,7 @@ SOLFP4_API int mxfp4_linear(const uint16_t* x, const uint8_t* w_codes, const uin
  * rows beyond 2^63 overflow to rho = 0, and with eps == 0 rows under 2^-63
  * lose bits and, once their squares are all 0, get an infinite rho, as a row
  * of zeros does (NaN).  rows == 0 or width == 0 launches nothing.  Strides of
- * inputs may be 0 (one row for all); output rows must
- * not overlap.
+ * inputs may be 0 (one row for all); output rows must not overlap.
  */
 SOLFP4_API int solfp4_add_rmsnorm(int type, const void* x, int64_t x_stride, const void* residual,
                    int64_t residual_stride, const void* gain, int64_t gain_stride, int64_t groups,
@@ -464,8 +463,8 @@ SOLFP4_API size_t solfp4_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t 
  *
  * A row with a NaN or an infinity, or beyond the range of the forward call's
  * FP32 squares, spoils its own dx and its group's dgain, no others.  Sums over
- * rows are formed in an order that depends on the sizes and the
- * device alone: results are the same on every call.
+ * rows are formed in an order that depends on the sizes and the device alone:
+ * results are the same on every call.
  */
 SOLFP4_API int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const void* x,
                    int64_t x_stride, const void* gain, int64_t gain_stride, int64_t groups,
@@ -551,8 +550,9 @@ SOLFP4_API int solfp4_rotary(int type, int layout, int inverse,
  * of them the linears that quantize the activations become the faster calls:
  * mxfp4_linear from 32 tokens (18432 x 3072), 64 (9728 x 2432) or more than
  * 512 (1152 x 1152), nvfp4_linear from about 100 and 200 (the first two).
- * M, N or K equal to 0 are valid (K == 0 writes the bias, or zeros).  K must be below 2^24 and N below 2^22.  Packed operands, x, bias
- * and out are contiguous and 16-byte aligned, out must not overlap the others
+ * M, N or K equal to 0 are valid (K == 0 writes the bias, or zeros).  K must
+ * be below 2^24 and N below 2^22.  Packed operands, x, bias and out are
+ * contiguous and 16-byte aligned, out must not overlap the others
  * (SOLFP4_EINVAL); no workspace.
  */
 SOLFP4_API int nvfp4_weight_linear(const uint16_t* x, const uint8_t* w_codes, const uint8_t* w_scales,

@@ -36,8 +36,9 @@ __device__ __forceinline__ uint32_t quad_max_bits(uint32_t v) {
 //
 // An FP32 amax next to a power of two may lie on the wrong side of it, which
 // would double or halve the scale: within 4 units (y is within 3, the
-// roundings of rho and the two products) the comparison is made in 64 bits.  That takes a rho of more than 32 bits, for
-// which the row's squares are summed in 64.
+// roundings of rho and the two products) the comparison is made in 64 bits.
+// That takes a rho of more than 32 bits, for which the row's squares are
+// summed in 64.
 template <int kEmax>
 __device__ __forceinline__ uint32_t block_scale(const float (&y)[8], const float (&s)[8], const float (&g)[8],
                                                 double rho) {

@@ -17,10 +17,10 @@
 // activations of a token (a permutation of K, alike on both sides).  Weights
 // become BF16 exactly: s q has at most 6 significant bits (E4M3 times E2M1),
 // or 2 and a power of two.  So do MXFP8 activations (4 bits and a power of
-// two) from 2^-133, BF16's smallest, on.  The scaled matrix instruction would take E2M1 against E4M3 as they
-// are, but adds its 128 products with fewer bits than FP32: with 20-fold
-// outliers among the activations its result was off by up to 1.4 times what
-// any order of FP32 sums can be, at K = 160.
+// two) from 2^-133, BF16's smallest, on.  The scaled matrix instruction would
+// take E2M1 against E4M3 as they are, but adds its 128 products with fewer
+// bits than FP32: with 20-fold outliers among the activations its result was
+// off by up to 1.4 times what any order of FP32 sums can be, at K = 160.
 //
 // Tokens are the columns of the matrix instruction, so up to 16 cost what
 // one does; columns past M hold anything and are not stored.
