@@ -262,8 +262,8 @@ struct RotaryArgs {
   int64_t table_rows;
   const void* positions;       // NULL: token % table_rows
   int64_t tokens;              // in a launch: its last token + 1
-  int dim, rotated;
   int64_t first;               // first token of a launch (set by it)
+  int dim, rotated;
 };
 hipError_t launch_rotary(int type, bool interleaved, bool inverse, int position_bytes, const RotaryArgs& a,
                          hipStream_t stream);
