@@ -473,6 +473,73 @@ SOLFP4_API int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stri
                    int64_t width, void* stream);
 
 /*
+ * Layer norm with the residual's addition:
+ *
+ *   s = x + residual,  m = mean(s),  rho = (mean((s - m)^2) + eps)^(-1/2)
+ *   out = (s - m) rho gain + shift
+ *
+ * Operands, strides, overlaps and limits as solfp4_add_rmsnorm's, and
+ *   shift    [groups][width], groups shift_stride apart; or NULL (all 0).
+ *            The gain's groups: row i takes gain and shift row
+ *            i / (rows / groups)
+ *
+ * The norm is taken of the FP32 sum.  Differences from the mean are formed
+ * from the mean in more than FP32, so rows far from zero keep their bits.  A
+ * row with a NaN or an infinity is NaN; rows whose sums leave FP32's range do
+ * not keep their values, rows whose squared differences do (beyond 2^63) get
+ * rho = 0, so the shift.  With eps == 0 a row of equal elements has no norm:
+ * what is written for it is unspecified.
+ */
+SOLFP4_API int solfp4_add_layernorm(int type, const void* x, int64_t x_stride, const void* residual,
+                   int64_t residual_stride, const void* gain, int64_t gain_stride, const void* shift,
+                   int64_t shift_stride, int64_t groups, float eps, void* sum, int64_t sum_stride,
+                   void* out, int64_t out_stride, int64_t rows, int64_t width, void* stream);
+
+/*
+ * The same with the output quantized in the same pass, width % 32 == 0, codes
+ * and scales as mxfp8_add_rmsnorm and mxfp4_add_rmsnorm write them, from the
+ * FP32 result.  Squares, rho and a scale that the FP32 result does not decide
+ * are formed in 64 bits.
+ */
+SOLFP4_API int mxfp8_add_layernorm(int type, const void* x, int64_t x_stride, const void* residual,
+                   int64_t residual_stride, const void* gain, int64_t gain_stride, const void* shift,
+                   int64_t shift_stride, int64_t groups, float eps, void* sum, int64_t sum_stride,
+                   uint8_t* codes, uint8_t* scales, int64_t rows, int64_t width, void* stream);
+SOLFP4_API int mxfp4_add_layernorm(int type, const void* x, int64_t x_stride, const void* residual,
+                   int64_t residual_stride, const void* gain, int64_t gain_stride, const void* shift,
+                   int64_t shift_stride, int64_t groups, float eps, void* sum, int64_t sum_stride,
+                   uint8_t* codes, uint8_t* scales, int64_t rows, int64_t width, void* stream);
+
+/* Device workspace of solfp4_layernorm_backward with both dgain and dshift
+ * (with one of them, half of it is enough).  Host only; 0 for invalid sizes. */
+SOLFP4_API size_t solfp4_layernorm_backward_workspace_bytes(int64_t rows, int64_t width, int64_t groups);
+
+/*
+ * Backward pass of solfp4_add_layernorm, with n = (x - mean(x)) rho:
+ *
+ *   G      = dy gain
+ *   dx     = rho (G - mean(G) - n mean(G n)) + dsum
+ *   dgain  = sum over the group's rows of dy n
+ *   dshift = sum over the group's rows of dy
+ *
+ * x is the sum of the forward call (its x without a residual); operands as
+ * solfp4_rmsnorm_backward's, and
+ *   dshift [groups][width] FP32, written; or NULL (not wanted; the shift
+ *          itself is not needed)
+ *   workspace  at least solfp4_layernorm_backward_workspace_bytes bytes, 16-byte
+ *          aligned; ignored when dgain and dshift are NULL
+ *
+ * dx, dgain, dshift and the workspace must not overlap each other or, but for
+ * dx in place, what the call reads (SOLFP4_EINVAL).  dgain may be wanted without
+ * a gain (all 1).  Results are the same on every call.
+ */
+SOLFP4_API int solfp4_layernorm_backward(int type, const void* dy, int64_t dy_stride, const void* x,
+                   int64_t x_stride, const void* gain, int64_t gain_stride, int64_t groups,
+                   const void* dsum, int64_t dsum_stride, float eps, void* dx, int64_t dx_stride,
+                   float* dgain, float* dshift, void* workspace, size_t workspace_bytes, int64_t rows,
+                   int64_t width, void* stream);
+
+/*
  * Table of cosines and sines for solfp4_rotary:
  *
  *   table[p][i]         = magnitude cos(position frequency_i)

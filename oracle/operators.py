@@ -1,5 +1,5 @@
 """Float64 definitions of the operators around the linears: the norm with the
-residual's addition and its gradients, rotary positions, products with 4-bit
+residual's addition and its gradients, the layer norm and its, rotary positions, products with 4-bit
 weights, the MXFP8 encoding.  Plain and slow; no code of the GPU path."""
 from __future__ import annotations
 
@@ -36,6 +36,40 @@ def rmsnorm_backward(dy, s, gain=None, dsum=None, eps=1e-6):
         ds = ds + dsum
     n = (dy * s * rho).reshape(groups, rows // groups, width)
     return ds, n.sum(1), size, np.abs(n).sum(1)
+
+
+def add_layernorm(x, residual=None, gain=None, shift=None, eps=1e-6):
+    """(sum, layer norm of the sum, and for every element the magnitude that
+    an FP32 evaluation's error goes by, in units of its rounding)."""
+    s = np.asarray(x, np.float64) + (0.0 if residual is None else np.asarray(residual, np.float64))
+    rows, width = s.shape
+    c = s - s.mean(axis=1, keepdims=True)
+    rho = 1.0 / np.sqrt(np.mean(c * c, axis=1, keepdims=True) + eps)
+    n, g = c * rho, _gain(gain, rows, width)
+    t = np.zeros_like(s) if shift is None else _gain(shift, rows, width)
+    far = rho * np.sqrt(np.mean(s * s, axis=1, keepdims=True))
+    size = np.abs(g) * (rho * np.abs(s) + far + np.abs(n) * (40 + 2 * far) + 68) + 2 * (np.abs(n * g) + np.abs(t))
+    return s, n * g + t, size
+
+
+def layernorm_backward(dy, s, gain=None, groups=1, dsum=None, eps=1e-6):
+    """(ds, dgain, dshift [groups, width]; magnitudes that the FP32 evaluation's
+    error goes by: of ds per element, of dgain's and of dshift's summands; and
+    the normalised rows' own)."""
+    dy, s = np.asarray(dy, np.float64), np.asarray(s, np.float64)
+    rows, width = s.shape
+    c = s - s.mean(axis=1, keepdims=True)
+    q = np.mean(c * c, axis=1, keepdims=True)
+    rho = 1.0 / np.sqrt(q + eps)
+    G = dy * _gain(gain, rows, width)
+    mean = lambda v: np.mean(v, axis=1, keepdims=True)
+    ds = rho * (G - mean(G) - c * rho ** 2 * mean(G * c))
+    size = rho * (np.abs(G) + mean(np.abs(G)) + (np.abs(c) + np.sqrt(q)) * rho ** 2 *
+                  (mean(np.abs(G * c)) + np.sqrt(q) * mean(np.abs(G))))
+    if dsum is not None:
+        ds = ds + dsum
+    split = lambda v: v.reshape(groups, rows // groups, width).sum(1)
+    return ds, split(dy * c * rho), split(dy), size, split(np.abs(dy * c * rho)), split(np.abs(dy))
 
 
 def rotate(t, table, positions, layout, inverse=False):

@@ -12,7 +12,8 @@ _NAMES = ("EXPORTED", "LIB_PATH", "Solfp4Error", "lib", "gemm_plan", "FORMAT_NVF
           "nvfp4_gemm_workspace_bytes", "nvfp4_linear", "nvfp4_linear_workspace_bytes",
           "nvfp4_quantize", "nvfp4_gelu_amax", "nvfp4_quantize_amax", "nvfp4_quantize_encode", "nvfp4_quantize_noalloc", "nvfp4_quantize_workspace_bytes", "mxfp4_gemm", "mxfp4_linear", "mxfp4_linear_workspace_bytes", "mxfp4_quantize",
           "add_rmsnorm", "mxfp8_add_rmsnorm", "mxfp4_add_rmsnorm", "rmsnorm_backward",
-          "rmsnorm_backward_workspace_bytes", "rotary", "rotary_frequencies", "rotary_table",
+          "rmsnorm_backward_workspace_bytes", "add_layernorm", "mxfp8_add_layernorm",
+          "mxfp4_add_layernorm", "layernorm_backward", "layernorm_backward_workspace_bytes", "rotary", "rotary_frequencies", "rotary_table",
           "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear")
 __all__ = list(_NAMES)
 

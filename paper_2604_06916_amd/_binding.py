@@ -83,6 +83,18 @@ lib.solfp4_rmsnorm_backward_workspace_bytes.argtypes = [_i64, _i64, _i64]
 lib.solfp4_rmsnorm_backward.restype = _int
 lib.solfp4_rmsnorm_backward.argtypes = [_int, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i64, _f32, _p, _i64, _p, _p,
                                         _sz, _i64, _i64, _p]
+_layernorm_in = [_int, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i64, _f32, _p, _i64]
+lib.solfp4_add_layernorm.restype = _int
+lib.solfp4_add_layernorm.argtypes = [*_layernorm_in, _p, _i64, _i64, _i64, _p]
+lib.mxfp8_add_layernorm.restype = _int
+lib.mxfp8_add_layernorm.argtypes = [*_layernorm_in, _p, _p, _i64, _i64, _p]
+lib.mxfp4_add_layernorm.restype = _int
+lib.mxfp4_add_layernorm.argtypes = [*_layernorm_in, _p, _p, _i64, _i64, _p]
+lib.solfp4_layernorm_backward_workspace_bytes.restype = _sz
+lib.solfp4_layernorm_backward_workspace_bytes.argtypes = [_i64, _i64, _i64]
+lib.solfp4_layernorm_backward.restype = _int
+lib.solfp4_layernorm_backward.argtypes = [_int, _p, _i64, _p, _i64, _p, _i64, _i64, _p, _i64, _f32, _p, _i64, _p, _p, _p,
+                                          _sz, _i64, _i64, _p]
 lib.solfp4_rotary_table.restype = _int
 lib.solfp4_rotary_table.argtypes = [_p, _i64, _p, _i64, _p, _int, _f64, _p, _p]
 lib.solfp4_rotary.restype = _int
@@ -103,6 +115,8 @@ EXPORTED = ["solfp4_strerror", "solfp4_version", "solfp4_gemm_plan",
             "mxfp4_quantize", "mxfp4_gemm", "mxfp4_linear_workspace_bytes", "mxfp4_linear",
             "solfp4_add_rmsnorm", "mxfp8_add_rmsnorm", "mxfp4_add_rmsnorm",
             "solfp4_rmsnorm_backward_workspace_bytes", "solfp4_rmsnorm_backward",
+            "solfp4_add_layernorm", "mxfp8_add_layernorm", "mxfp4_add_layernorm",
+            "solfp4_layernorm_backward_workspace_bytes", "solfp4_layernorm_backward",
             "solfp4_rotary_table", "solfp4_rotary",
             "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear"]
 
@@ -636,6 +650,140 @@ def rmsnorm_backward(dy, x, gain=None, dsum=None, eps=1e-6, dx=None, dgain=None,
                                        0 if workspace is None else workspace.numel(), rows, width,
                                        ctypes.c_void_p(st.cuda_stream)))
     return dx, dgain
+
+
+def _shift(shift, gain, x, rows, width, dev):
+    """Checked with the gain: (groups, gain stride, shift stride)."""
+    groups, gain_stride = _gain(gain, x, rows, width, dev)
+    if shift is None:
+        return groups, gain_stride, 0
+    if not isinstance(shift, torch.Tensor) or shift.dim() not in (1, 2):
+        raise ValueError("shift: expected a tensor [width] or [groups, width]")
+    if gain is not None and shift.shape != gain.shape:
+        raise ValueError(f"shift: expected the gain's shape {tuple(gain.shape)}, got {tuple(shift.shape)}")
+    shift_groups = 1 if shift.dim() == 1 else shift.shape[0]
+    _need_strided(shift, x.dtype, (width,) if shift.dim() == 1 else (shift_groups, width), "shift", dev)
+    if shift_groups < 1 or rows % shift_groups:
+        raise ValueError(f"shift: {rows} rows cannot be dealt to {shift_groups} groups evenly")
+    return shift_groups, gain_stride, 0 if shift.dim() == 1 else shift.stride(0)
+
+
+def add_layernorm(x, residual=None, gain=None, shift=None, eps=1e-6, out=None, sum_out=None, stream=None):
+    """Layer norm of the rows of x + residual, times gain, plus shift (each
+    [width], or both [groups, width] with the rows dealt to the groups in
+    order) -> (out, sum), as add_rmsnorm's."""
+    if stream is None:
+        r = _host.add_layernorm(x, residual, gain, shift, eps, out, sum_out)
+        if r is not None:
+            return _native(r)
+    kind, rows, width, dev, _, _ = _norm_operands(x, residual, gain, eps, sum_out)
+    groups, gain_stride, shift_stride = _shift(shift, gain, x, rows, width, dev)
+    if out is not None:
+        _need_strided(out, x.dtype, (rows, width), "out", dev)
+    st = _stream(stream, dev)
+    if out is None:
+        out = _alloc((rows, width), x.dtype, dev, st)
+    if residual is not None and sum_out is None:
+        sum_out = _alloc((rows, width), x.dtype, dev, st)
+    _check(lib.solfp4_add_layernorm(kind, *_rows_of(x), *_rows_of(residual), _ptr(gain), gain_stride, _ptr(shift),
+                                    shift_stride, groups, eps, *_rows_of(sum_out), *_rows_of(out), rows, width,
+                                    ctypes.c_void_p(st.cuda_stream)))
+    return out, sum_out
+
+
+def _quantized_add_layernorm(fn, native, pack, x, residual, gain, shift, eps, codes, scales, sum_out, stream):
+    if stream is None:
+        r = native(x, residual, gain, shift, eps, codes, scales, sum_out)
+        if r is not None:
+            return _native(r)
+    kind, rows, width, dev, _, _ = _norm_operands(x, residual, gain, eps, sum_out)
+    groups, gain_stride, shift_stride = _shift(shift, gain, x, rows, width, dev)
+    if width % 32:
+        raise ValueError(f"x: width {width} is not a multiple of 32")
+    if codes is not None:
+        _need(codes, torch.uint8, (rows, width // pack), "codes", dev)
+    if scales is not None:
+        _need(scales, torch.uint8, (rows, width // 32), "scales", dev)
+    st = _stream(stream, dev)
+    if codes is None:
+        codes = _alloc((rows, width // pack), torch.uint8, dev, st)
+    if scales is None:
+        scales = _alloc((rows, width // 32), torch.uint8, dev, st)
+    if residual is not None and sum_out is None:
+        sum_out = _alloc((rows, width), x.dtype, dev, st)
+    _check(fn(kind, *_rows_of(x), *_rows_of(residual), _ptr(gain), gain_stride, _ptr(shift), shift_stride, groups, eps,
+              *_rows_of(sum_out), _ptr(codes), _ptr(scales), rows, width, ctypes.c_void_p(st.cuda_stream)))
+    return codes, scales, sum_out
+
+
+def mxfp8_add_layernorm(x, residual=None, gain=None, shift=None, eps=1e-6, codes=None, scales=None, sum_out=None,
+                        stream=None):
+    """add_layernorm with its output in MXFP8, as mxfp8_add_rmsnorm's."""
+    return _quantized_add_layernorm(lib.mxfp8_add_layernorm, _host.mxfp8_add_layernorm, 1, x, residual, gain, shift, eps,
+                                    codes, scales, sum_out, stream)
+
+
+def mxfp4_add_layernorm(x, residual=None, gain=None, shift=None, eps=1e-6, codes=None, scales=None, sum_out=None,
+                        stream=None):
+    """add_layernorm with its output in MXFP4, as mxfp4_add_rmsnorm's."""
+    return _quantized_add_layernorm(lib.mxfp4_add_layernorm, _host.mxfp4_add_layernorm, 2, x, residual, gain, shift, eps,
+                                    codes, scales, sum_out, stream)
+
+
+def layernorm_backward_workspace_bytes(rows: int, width: int, groups: int = 1) -> int:
+    return lib.solfp4_layernorm_backward_workspace_bytes(rows, width, groups)
+
+
+def layernorm_backward(dy, x, gain=None, shift=None, dsum=None, eps=1e-6, dx=None, dgain=None, dshift=None,
+                       workspace=None, stream=None):
+    """Backward pass of add_layernorm: dy, the output's gradient; x, the sum
+    (or the x of a call without a residual); dsum, what reaches the sum past
+    the norm -> (dx, dgain, dshift).  dx is the gradient of x and of the residual
+    alike; dgain and dshift are FP32 in the gain's and the shift's shape, None
+    without one (of the shift only the shape is used)."""
+    if stream is None:
+        r = _host.layernorm_backward(dy, x, gain, shift, dsum, eps, dx, dgain, dshift, workspace)
+        if r is not None:
+            return _native(r)
+    kind = _type(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: expected a 2-D tensor")
+    rows, width = x.shape
+    dev = x.device
+    _need_strided(x, x.dtype, (rows, width), "x", dev)
+    _need_strided(dy, x.dtype, (rows, width), "dy", dev)
+    if dsum is not None:
+        _need_strided(dsum, x.dtype, (rows, width), "dsum", dev)
+    if dx is not None:
+        _need_strided(dx, x.dtype, (rows, width), "dx", dev)
+    groups, gain_stride, _ = _shift(shift, gain, x, rows, width, dev)
+    if not eps >= 0:
+        raise ValueError(f"eps: expected a number of at least 0, got {eps}")
+    for given, of, name in ((dgain, gain, "gain"), (dshift, shift, "shift")):
+        if given is not None:
+            if of is None:
+                raise ValueError(f"d{name}: given without a {name}")
+            _need(given, torch.float32, tuple(of.shape), f"d{name}", dev)
+    sums = gain is not None or shift is not None
+    need = 0
+    if sums:
+        need = layernorm_backward_workspace_bytes(rows, width, groups)
+        if workspace is not None:
+            _need_workspace(workspace, need, "workspace", dev)
+    st = _stream(stream, dev)
+    if dx is None:
+        dx = _alloc((rows, width), x.dtype, dev, st)
+    if gain is not None and dgain is None:
+        dgain = _alloc(tuple(gain.shape), torch.float32, dev, st)
+    if shift is not None and dshift is None:
+        dshift = _alloc(tuple(shift.shape), torch.float32, dev, st)
+    if sums and workspace is None:
+        workspace = _alloc((max(need, 256),), torch.uint8, dev, st)
+    _check(lib.solfp4_layernorm_backward(kind, *_rows_of(dy), *_rows_of(x), _ptr(gain), gain_stride, groups,
+                                         *_rows_of(dsum), eps, *_rows_of(dx), _ptr(dgain), _ptr(dshift),
+                                         _ptr(workspace), 0 if workspace is None else workspace.numel(), rows, width,
+                                         ctypes.c_void_p(st.cuda_stream)))
+    return dx, dgain, dshift
 
 
 def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,

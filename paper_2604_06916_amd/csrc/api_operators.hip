@@ -3,80 +3,17 @@
 // the first HIP call.
 #include <math.h>
 
-#include <numeric>
-
 #include "solfp4.h"
 #include "kernels.h"
+#include "operand_checks.h"
 
 namespace {
 
-constexpr int64_t kMaxDim = (int64_t)1 << 31;
 constexpr int64_t kMaxK = (int64_t)1 << 24, kMaxN = (int64_t)1 << 22;
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+using namespace solfp4::checks;
 
-bool type_ok(int type) { return type == SOLFP4_BF16 || type == SOLFP4_F16 || type == SOLFP4_F32; }
-
-bool element_aligned(int type, const void* p) { return ((uintptr_t)p & (type == SOLFP4_F32 ? 3u : 1u)) == 0; }
-
-int check_dims(int64_t a, int64_t b) {
-  if (a < 0 || b < 0) return SOLFP4_EINVAL;
-  if (a >= kMaxDim || b >= kMaxDim) return SOLFP4_ESHAPE;
-  return SOLFP4_OK;
-}
-
-// Whether an operand of this many rows stays within kMaxSpan elements.
-constexpr int64_t kMaxSpan = (int64_t)1 << 46;
-bool span_ok(int64_t stride, int64_t rows) { return stride == 0 || rows - 1 <= kMaxSpan / stride; }
-
-// Rows of an operand that the call reads or, with `written`, writes (whose
-// rows must not overlap).
-int check_rows(int type, const void* p, int64_t stride, int64_t rows, int64_t width, bool written) {
-  if (!p || stride < 0) return SOLFP4_EINVAL;
-  if (!span_ok(stride, rows)) return SOLFP4_ESHAPE;
-  if (!element_aligned(type, p)) return SOLFP4_EALIGN;
-  if (written && rows > 1 && stride < width) return SOLFP4_EINVAL;
-  return SOLFP4_OK;
-}
-
-// What an operand covers: w bytes at p + i s0 + j s1, i < n0, j < n1.
-struct Region {
-  uintptr_t p;
-  int64_t n0, s0, n1, s1, w;
-  int64_t span0() const { return (n0 - 1) * s0 + w; }
-  int64_t span1() const { return (n1 - 1) * s1 + w; }
-};
-
-// Whether two regions (every count at least 1) share no byte: one ends before
-// the other begins, or they lie side by side as columns or heads of one
-// buffer do, which shows in their offsets modulo the strides' common divisor.
-bool apart(const Region& a, const Region& b) {
-  const int64_t a_len = (a.n0 - 1) * a.s0 + a.span1(), b_len = (b.n0 - 1) * b.s0 + b.span1();
-  if (!a_len || !b_len || a.p + (uint64_t)a_len <= b.p || b.p + (uint64_t)b_len <= a.p) return true;
-  const int64_t d = (int64_t)(b.p - a.p);
-  const auto beside = [d](int64_t g, int64_t wa, int64_t wb) {
-    if (g <= 0) return false;
-    const int64_t r = (d % g + g) % g;
-    return r >= wa && r + wb <= g;
-  };
-  const auto step = [](int64_t n, int64_t s) { return n > 1 ? s : (int64_t)0; };
-  const int64_t g0 = std::gcd(step(a.n0, a.s0), step(b.n0, b.s0)), g1 = std::gcd(step(a.n1, a.s1), step(b.n1, b.s1));
-  return beside(g0, a.span1(), b.span1()) || beside(g1, a.span0(), b.span0()) || beside(std::gcd(g0, g1), a.w, b.w);
-}
-
-Region block_of(const void* p, int64_t bytes) { return {(uintptr_t)p, 1, 0, 1, 0, bytes}; }
-
-Region rows_region(int type, const void* p, int64_t stride, int64_t rows, int64_t width) {
-  const int64_t bytes = type == SOLFP4_F32 ? 4 : 2;
-  return {(uintptr_t)p, p ? rows : 1, rows > 1 ? stride * bytes : 0, 1, 0, p ? width * bytes : 0};
-}
-
-// The two are one operand (each element is read before it is written) or apart.
-bool same_or_apart(const Region& a, const Region& b) {
-  return (a.p == b.p && a.n0 == b.n0 && a.s0 == b.s0 && a.w == b.w) || apart(a, b);
-}
-
-int norm_checks(int type, const solfp4::NormArgs& a, int64_t groups, int out) {
+int norm_checks(int type, const solfp4::NormArgs& a, const void* shift_rows, int64_t shift_stride, int64_t groups, int out) {
   if (!type_ok(type)) return SOLFP4_EINVAL;
   int rc = check_dims(a.rows, a.width);
   if (rc) return rc;
@@ -90,23 +27,28 @@ int norm_checks(int type, const solfp4::NormArgs& a, int64_t groups, int out) {
     if ((rc = check_rows(type, a.sum, a.sum_stride, a.rows, a.width, true))) return rc;
   }
   if (a.gain && (rc = check_rows(type, a.gain, a.gain_stride, groups, a.width, false))) return rc;
+  if (shift_rows && (rc = check_rows(type, shift_rows, shift_stride, groups, a.width, false))) return rc;
   // what is written over nothing else, except in place
   const Region x = rows_region(type, a.x, a.x_stride, a.rows, a.width);
   const Region residual = rows_region(type, a.residual, a.residual_stride, a.rows, a.width);
   const Region gain = rows_region(type, a.gain, a.gain_stride, groups, a.width);
+  const Region shift = rows_region(type, shift_rows, shift_stride, groups, a.width);
   const Region sum = rows_region(type, a.residual ? a.sum : nullptr, a.sum_stride, a.rows, a.width);
-  if (!same_or_apart(x, sum) || !same_or_apart(residual, sum) || !apart(gain, sum)) return SOLFP4_EINVAL;
+  if (!same_or_apart(x, sum) || !same_or_apart(residual, sum) || !apart(gain, sum) || !apart(shift, sum))
+    return SOLFP4_EINVAL;
   if (out == solfp4::kNormSame) {
     if ((rc = check_rows(type, a.out, a.out_stride, a.rows, a.width, true))) return rc;
     const Region o = rows_region(type, a.out, a.out_stride, a.rows, a.width);
-    return same_or_apart(x, o) && apart(residual, o) && apart(gain, o) && apart(sum, o) ? SOLFP4_OK : SOLFP4_EINVAL;
+    return same_or_apart(x, o) && apart(residual, o) && apart(gain, o) && apart(shift, o) && apart(sum, o)
+               ? SOLFP4_OK : SOLFP4_EINVAL;
   }
   if (!a.codes || !a.scales) return SOLFP4_EINVAL;
   if (!aligned16(a.codes) || !aligned16(a.scales)) return SOLFP4_EALIGN;
   const Region codes = block_of(a.codes, a.rows * (out == solfp4::kNormMxfp8 ? a.width : a.width / 2));
   const Region scales = block_of(a.scales, a.rows * (a.width / 32));
   for (const Region& o : {codes, scales})
-    if (!apart(x, o) || !apart(residual, o) || !apart(gain, o) || !apart(sum, o)) return SOLFP4_EINVAL;
+    if (!apart(x, o) || !apart(residual, o) || !apart(gain, o) || !apart(shift, o) || !apart(sum, o))
+      return SOLFP4_EINVAL;
   return apart(codes, scales) ? SOLFP4_OK : SOLFP4_EINVAL;
 }
 
@@ -117,9 +59,22 @@ int add_rmsnorm(int type, int kind, const void* x, int64_t x_stride, const void*
   const solfp4::NormArgs a = {x, x_stride, residual, residual_stride, gain, gain_stride,
                               groups > 0 && rows > 0 ? rows / groups : 1, eps, sum, sum_stride, out, out_stride,
                               codes, scales, rows, width, 0};
-  const int rc = norm_checks(type, a, groups, kind);
+  const int rc = norm_checks(type, a, nullptr, 0, groups, kind);
   if (rc) return rc;
   const hipError_t e = solfp4::launch_add_rmsnorm(type, kind, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
+int add_layernorm(int type, int kind, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                  const void* gain, int64_t gain_stride, const void* shift, int64_t shift_stride, int64_t groups,
+                  float eps, void* sum, int64_t sum_stride, void* out, int64_t out_stride, uint8_t* codes,
+                  uint8_t* scales, int64_t rows, int64_t width, void* stream) {
+  const solfp4::LayerNormArgs a = {{x, x_stride, residual, residual_stride, gain, gain_stride,
+                                    groups > 0 && rows > 0 ? rows / groups : 1, eps, sum, sum_stride, out, out_stride,
+                                    codes, scales, rows, width, 0}, shift, shift_stride};
+  const int rc = norm_checks(type, a.n, shift, shift_stride, groups, kind);
+  if (rc) return rc;
+  const hipError_t e = solfp4::launch_add_layernorm(type, kind, a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
 }
 
@@ -261,6 +216,86 @@ int solfp4_rmsnorm_backward(int type, const void* dy, int64_t dy_stride, const v
   a.partial = dgain ? static_cast<float*>(workspace) : nullptr;
   a.rows = rows, a.width = width;
   const hipError_t e = solfp4::launch_rmsnorm_backward(type, a, dgain, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
+int solfp4_add_layernorm(int type, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                         const void* gain, int64_t gain_stride, const void* shift, int64_t shift_stride,
+                         int64_t groups, float eps, void* sum, int64_t sum_stride, void* out, int64_t out_stride,
+                         int64_t rows, int64_t width, void* stream) {
+  return add_layernorm(type, solfp4::kNormSame, x, x_stride, residual, residual_stride, gain, gain_stride, shift,
+                       shift_stride, groups, eps, sum, sum_stride, out, out_stride, nullptr, nullptr, rows, width, stream);
+}
+
+int mxfp8_add_layernorm(int type, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                        const void* gain, int64_t gain_stride, const void* shift, int64_t shift_stride, int64_t groups,
+                        float eps, void* sum, int64_t sum_stride, uint8_t* codes, uint8_t* scales, int64_t rows,
+                        int64_t width, void* stream) {
+  return add_layernorm(type, solfp4::kNormMxfp8, x, x_stride, residual, residual_stride, gain, gain_stride, shift,
+                       shift_stride, groups, eps, sum, sum_stride, nullptr, 0, codes, scales, rows, width, stream);
+}
+
+int mxfp4_add_layernorm(int type, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                        const void* gain, int64_t gain_stride, const void* shift, int64_t shift_stride, int64_t groups,
+                        float eps, void* sum, int64_t sum_stride, uint8_t* codes, uint8_t* scales, int64_t rows,
+                        int64_t width, void* stream) {
+  return add_layernorm(type, solfp4::kNormMxfp4, x, x_stride, residual, residual_stride, gain, gain_stride, shift,
+                       shift_stride, groups, eps, sum, sum_stride, nullptr, 0, codes, scales, rows, width, stream);
+}
+
+size_t solfp4_layernorm_backward_workspace_bytes(int64_t rows, int64_t width, int64_t groups) {
+  return back_dims(rows, width, groups) ? 0 : 2 * back_workspace(rows, width, groups);
+}
+
+int solfp4_layernorm_backward(int type, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                              const void* gain, int64_t gain_stride, int64_t groups, const void* dsum,
+                              int64_t dsum_stride, float eps, void* dx, int64_t dx_stride, float* dgain, float* dshift,
+                              void* workspace, size_t workspace_bytes, int64_t rows, int64_t width, void* stream) {
+  if (!type_ok(type)) return SOLFP4_EINVAL;
+  int rc = back_dims(rows, width, groups);
+  if (rc) return rc;
+  if (!(eps >= 0.0f)) return SOLFP4_EINVAL;
+  if (width == 0) return SOLFP4_OK;
+  if (rows > 0) {
+    if ((rc = check_rows(type, dy, dy_stride, rows, width, false))) return rc;
+    if ((rc = check_rows(type, x, x_stride, rows, width, false))) return rc;
+    if (gain && (rc = check_rows(type, gain, gain_stride, groups, width, false))) return rc;
+    if (dsum && (rc = check_rows(type, dsum, dsum_stride, rows, width, false))) return rc;
+    if ((rc = check_rows(type, dx, dx_stride, rows, width, true))) return rc;
+  }
+  // the gain's shares first, then the shift's
+  const size_t half = back_workspace(rows, width, groups), gain_bytes = dgain ? half : 0;
+  const size_t need = gain_bytes + (dshift ? half : 0);
+  if (dgain || dshift) {
+    if (((uintptr_t)dgain & 3u) || ((uintptr_t)dshift & 3u)) return SOLFP4_EALIGN;
+    if (need && !workspace) return SOLFP4_EWORKSPACE;
+    if (!aligned16(workspace)) return SOLFP4_EALIGN;
+    if (workspace_bytes < need) return SOLFP4_EWORKSPACE;
+  }
+  const Region sums[2] = {block_of(dgain, dgain ? groups * width * 4 : 0), block_of(dshift, dshift ? groups * width * 4 : 0)};
+  if (!apart(sums[0], sums[1])) return SOLFP4_EINVAL;
+  if (rows > 0) {
+    const Region in[4] = {rows_region(type, dy, dy_stride, rows, width), rows_region(type, x, x_stride, rows, width),
+                          rows_region(type, dsum, dsum_stride, rows, width),
+                          rows_region(type, gain, gain_stride, groups, width)};
+    const Region out = rows_region(type, dx, dx_stride, rows, width), scratch = block_of(workspace, (int64_t)need);
+    for (int i = 0; i < 4; ++i)
+      if (!(i < 3 ? same_or_apart(in[i], out) : apart(in[i], out)) || !apart(in[i], sums[0]) ||
+          !apart(in[i], sums[1]) || !apart(in[i], scratch))
+        return SOLFP4_EINVAL;
+    if (!apart(out, sums[0]) || !apart(out, sums[1]) || !apart(out, scratch) || !apart(sums[0], scratch) ||
+        !apart(sums[1], scratch))
+      return SOLFP4_EINVAL;
+  }
+  solfp4::LayerNormBackArgs a = {};
+  a.n.dy = dy, a.n.dy_stride = dy_stride, a.n.x = x, a.n.x_stride = x_stride;
+  a.n.gain = gain, a.n.gain_stride = gain_stride, a.n.groups = groups;
+  a.n.dsum = dsum, a.n.dsum_stride = dsum_stride, a.n.eps = eps;
+  a.n.dx = dx, a.n.dx_stride = dx_stride;
+  a.n.partial = dgain ? static_cast<float*>(workspace) : nullptr;
+  a.shift_partial = dshift ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + gain_bytes) : nullptr;
+  a.n.rows = rows, a.n.width = width;
+  const hipError_t e = solfp4::launch_layernorm_backward(type, a, dgain, dshift, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
 }
 

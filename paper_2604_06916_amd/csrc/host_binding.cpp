@@ -350,6 +350,14 @@ struct Gain {
   }
 };
 
+// The shift beside the gain: its shape where there is one.
+struct Shift : Gain {
+  Shift(PyObject* o, const Gain& gain, const Tensor& x, int64_t rows, int64_t width) : Gain(o, x, rows, width) {
+    need(!t.defined() || !gain.t.defined() || t.sizes() == gain.t.sizes());
+    if (!t.defined()) groups = gain.groups;
+  }
+};
+
 const Tensor& matrix_operand(PyObject* o) {
   const Tensor& x = tensor(o);
   need_matrix(x);
@@ -445,6 +453,107 @@ PyObject* rmsnorm_backward_(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (rc) return failed(rc);
     if (g.t.defined()) return Py_BuildValue("(NN)", dx.object(), dgain.object());
     return Py_BuildValue("(NO)", dx.object(), Py_None);
+  });
+}
+
+// (x, residual, gain, shift, eps, out, sum_out) -> (out, sum)
+PyObject* add_layernorm_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 7, [&]() -> PyObject* {
+    const Tensor& x = matrix_operand(a[0]);
+    const int64_t rows = x.size(0), width = x.size(1);
+    Strided r(a[1], x, {rows, width}), out(a[5], x, {rows, width}), sum(a[6], x, {rows, width});
+    Gain g(a[2], x, rows, width);
+    Shift t(a[3], g, x, rows, width);
+    const double eps = number(a[4]);
+    need(eps >= 0);
+    need(r.given || !sum.given);
+    void* stream = stream_of(x.device());
+    out.allocate(x, {rows, width});
+    if (r.given) sum.allocate(x, {rows, width});
+    const int rc = call([&] {
+      return solfp4_add_layernorm(type_of(x), ptr(x), x.stride(0), ptr(r.t), r.stride(0), ptr(g.t), g.stride, ptr(t.t),
+                                  t.stride, t.groups, (float)eps, ptr(sum.t), sum.stride(0), ptr(out.t), out.stride(0),
+                                  rows, width, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NN)", out.object(), sum.object());
+  });
+}
+
+// (x, residual, gain, shift, eps, codes, scales, sum_out) -> (codes, scales, sum)
+template <typename F>
+PyObject* quantized_layernorm(PyObject* const* a, Py_ssize_t n, int pack, F f) {
+  return entry(n, 8, [&]() -> PyObject* {
+    const Tensor& x = matrix_operand(a[0]);
+    const int64_t rows = x.size(0), width = x.size(1);
+    need(width % 32 == 0);
+    const at::Device dev = x.device();
+    Strided r(a[1], x, {rows, width}), sum(a[7], x, {rows, width});
+    Gain g(a[2], x, rows, width);
+    Shift t(a[3], g, x, rows, width);
+    const double eps = number(a[4]);
+    need(eps >= 0);
+    Operand codes(a[5], at::kByte, {rows, width / pack}, dev), scales(a[6], at::kByte, {rows, width / 32}, dev);
+    need(r.given || !sum.given);
+    void* stream = stream_of(dev);
+    codes.allocate(at::kByte, {rows, width / pack}, dev);
+    scales.allocate(at::kByte, {rows, width / 32}, dev);
+    if (r.given) sum.allocate(x, {rows, width});
+    const int rc = call([&] {
+      return f(type_of(x), ptr(x), x.stride(0), ptr(r.t), r.stride(0), ptr(g.t), g.stride, ptr(t.t), t.stride, t.groups,
+               (float)eps, ptr(sum.t), sum.stride(0), u8(codes.t), u8(scales.t), rows, width, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NNN)", codes.object(), scales.object(), sum.object());
+  });
+}
+
+PyObject* mxfp8_add_layernorm_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return quantized_layernorm(a, n, 1, mxfp8_add_layernorm);
+}
+PyObject* mxfp4_add_layernorm_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return quantized_layernorm(a, n, 2, mxfp4_add_layernorm);
+}
+
+// An output that the call has or has not; None where it has not.
+PyObject* object_or_none(const Operand& o) {
+  if (o.t.defined()) return o.object();
+  Py_RETURN_NONE;
+}
+
+// (dy, x, gain, shift, dsum, eps, dx, dgain, dshift, workspace) -> (dx, dgain, dshift)
+PyObject* layernorm_backward_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 10, [&]() -> PyObject* {
+    const Tensor& x = matrix_operand(a[1]);
+    const int64_t rows = x.size(0), width = x.size(1);
+    const Tensor& dy = tensor(a[0]);
+    need_strided(dy, x, {rows, width});
+    Gain g(a[2], x, rows, width);
+    Shift t(a[3], g, x, rows, width);
+    Strided dsum(a[4], x, {rows, width}), dx(a[6], x, {rows, width});
+    const double eps = number(a[5]);
+    need(eps >= 0);
+    const at::Device dev = x.device();
+    need((g.t.defined() || a[7] == Py_None) && (t.t.defined() || a[8] == Py_None));
+    const at::IntArrayRef gain_shape = g.t.defined() ? g.t.sizes() : at::IntArrayRef();
+    const at::IntArrayRef shift_shape = t.t.defined() ? t.t.sizes() : at::IntArrayRef();
+    Operand dgain(a[7], at::kFloat, gain_shape, dev), dshift(a[8], at::kFloat, shift_shape, dev);
+    const bool sums = g.t.defined() || t.t.defined();
+    const size_t bytes = sums ? solfp4_layernorm_backward_workspace_bytes(rows, width, t.groups) : 0;
+    Tensor ws = sums ? workspace_arg(a[9], bytes, dev) : Tensor();
+    void* stream = stream_of(dev);
+    dx.allocate(x, {rows, width});
+    if (g.t.defined()) dgain.allocate(at::kFloat, gain_shape, dev);
+    if (t.t.defined()) dshift.allocate(at::kFloat, shift_shape, dev);
+    if (sums && !ws.defined()) ws = make({(int64_t)std::max<size_t>(bytes, 256)}, at::kByte, dev);
+    const int rc = call([&] {
+      return solfp4_layernorm_backward(type_of(x), ptr(dy), dy.stride(0), ptr(x), x.stride(0), ptr(g.t), g.stride,
+                                       t.groups, ptr(dsum.t), dsum.stride(0), (float)eps, ptr(dx.t), dx.stride(0),
+                                       f32(dgain.t), f32(dshift.t), ptr(ws), ws.defined() ? (size_t)ws.numel() : 0, rows,
+                                       width, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NNN)", dx.object(), object_or_none(dgain), object_or_none(dshift));
   });
 }
 
@@ -577,6 +686,10 @@ PyMethodDef methods[] = {
     {"mxfp8_add_rmsnorm", (PyCFunction)(void*)mxfp8_add_rmsnorm_, METH_FASTCALL, nullptr},
     {"mxfp4_add_rmsnorm", (PyCFunction)(void*)mxfp4_add_rmsnorm_, METH_FASTCALL, nullptr},
     {"rmsnorm_backward", (PyCFunction)(void*)rmsnorm_backward_, METH_FASTCALL, nullptr},
+    {"add_layernorm", (PyCFunction)(void*)add_layernorm_, METH_FASTCALL, nullptr},
+    {"mxfp8_add_layernorm", (PyCFunction)(void*)mxfp8_add_layernorm_, METH_FASTCALL, nullptr},
+    {"mxfp4_add_layernorm", (PyCFunction)(void*)mxfp4_add_layernorm_, METH_FASTCALL, nullptr},
+    {"layernorm_backward", (PyCFunction)(void*)layernorm_backward_, METH_FASTCALL, nullptr},
     {"rotary", (PyCFunction)(void*)rotary_, METH_FASTCALL, nullptr},
     {"nvfp4_weight_linear", (PyCFunction)(void*)nvfp4_weight_linear_, METH_FASTCALL, nullptr},
     {"mxfp4_weight_linear", (PyCFunction)(void*)mxfp4_weight_linear_, METH_FASTCALL, nullptr},

@@ -248,6 +248,21 @@ struct NormBackArgs {
 int64_t rmsnorm_backward_parts(int64_t rows, int64_t width, int64_t groups);
 hipError_t launch_rmsnorm_backward(int type, NormBackArgs a, float* dgain, hipStream_t stream);
 
+// ---- layer norm (layer_norm.hip) ------------------------------------------
+struct LayerNormArgs {
+  NormArgs n;
+  const void* shift;      // NULL: 0; the gain's groups
+  int64_t shift_stride;
+};
+hipError_t launch_add_layernorm(int type, int out, const LayerNormArgs& a, hipStream_t stream);
+
+// Its rows are dealt to rmsnorm_backward_parts workgroups a group.
+struct LayerNormBackArgs {
+  NormBackArgs n;
+  float* shift_partial;   // like n.partial, NULL: no shift gradient
+};
+hipError_t launch_layernorm_backward(int type, LayerNormBackArgs a, float* dgain, float* dshift, hipStream_t stream);
+
 // ---- rotary positions (rotary.hip) ----------------------------------------
 struct RotaryOperand {
   const void* in;

@@ -1,0 +1,364 @@
+// Layer norm of rows with a gain and a shift, with the residual's addition
+// and an output in the rows' type, in MXFP8 or in MXFP4; and its backward pass.
+//
+//   s = x + r,  m = mean(s),  rho = (mean((s - m)^2) + eps)^-1/2
+//   n = (s - m) rho,  y = n g + t
+//   G = dy g,  ds = rho (G - mean(G) - n mean(G n)) + dsum
+//   dg = sum over rows of dy n,  dt = sum over rows of dy
+//
+// Rows lie on waves as in the root-mean-square norm and are read once.  The
+// statistics take two sums over the registers: the mean, then the differences
+// d = s - m and their squares.  The second sum of d corrects the first: m is
+// rounded to FP32, so a row far from zero (1000 +- 1) would keep an error of
+// 2^-24 of its mean in every element; with d's own mean taken off, elements
+// are right to 2^-24 of themselves, and mean(d^2) - mean(d)^2 loses nothing,
+// since mean(d) is 2^-24 of m.
+//
+// Bound by memory: 8 bytes an element in BF16 with a residual, 7.03 with MXFP8
+// output.
+#include "norm_common.h"
+
+namespace solfp4 {
+
+// The E8M0 byte of a 32-element block held by a lane quad, 8 values y = n g + t
+// a lane, as the root-mean-square norm's: floor(log2(amax)) - kEmax + 127, at
+// least 0.  Where y is the difference of two larger numbers its error goes by
+// those: `size` is the lane's largest |n g| + |t|, and y is within 5 roundings
+// of 2^-24 of it (d, its correction, rho, and the product and sum).  An amax
+// within 2^-21 size of a power of two is formed in 64 bits.
+template <int kEmax, typename F>
+__device__ __forceinline__ uint32_t block_scale(const float (&y)[8], float size, F y64) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(y[e]) & 0x7FFFFFFFu);
+  m = quad_max_bits(m);
+  const float near = __uint_as_float(quad_max_bits(__float_as_uint(size))) * 0x1p-21f, amax = __uint_as_float(m);
+  const float below = amax > near ? amax - near : 0.0f;
+  uint32_t f = m >> 23;
+  if (__float_as_uint(below) >> 23 != __float_as_uint(amax + near) >> 23 && f < 255u) {   // alike in the quad
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double v = __builtin_fabs(y64(e));
+      const int b = v > 0.0 ? __builtin_amdgcn_frexp_exp(v) - 1 + 127 : 0;
+      top = max(top, (uint32_t)max(b, 0));
+    }
+    f = quad_max_bits(top);
+  }
+  return f > kEmax ? f - kEmax : 0u;
+}
+
+// A variance that its rounding took below 0 (a row of equal elements); NaN stays NaN
+template <typename T>
+__device__ __forceinline__ T not_negative(T v) { return v < 0 ? 0 : v; }
+
+template <int kType, int kOut, int kRuns>
+__global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(LayerNormArgs p, RowShape sh) {
+  using Sum = std::conditional_t<kOut == kNormSame, float, double>;   // block_scale
+  __shared__ Sum lds[kNormMaxWaves][2];
+  __shared__ float lds_mean[kNormMaxWaves][1];
+  const NormArgs& a = p.n;
+  const Place<kRuns> at_(sh);
+  const int64_t row = a.first + (int64_t)blockIdx.x * sh.waves_slots(blockDim.x / kWave) + at_.slot;
+  const int lane = at_.lane, step = at_.step;
+  const int width = row < a.rows ? (int)a.width : 0;   // no elements of a row past the last
+  const int64_t at = row < a.rows ? row : 0;
+  const int64_t group = (uint32_t)at / (uint32_t)a.group_rows;
+  const uint8_t* xr = row_of<kType>(a.x, at, a.x_stride);
+  const uint8_t* rr = row_of<kType>(a.residual, at, a.residual_stride);
+  const uint8_t* gr = row_of<kType>(a.gain, group, a.gain_stride);
+  const uint8_t* tr = row_of<kType>(p.shift, group, p.shift_stride);
+  Run<kType> x[kRuns], r[kRuns], g[kRuns], t[kRuns];
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
+    const int col = i * step + lane * 8, n = width - col;
+    x[i] = r[i] = t[i] = zero_run<kType>();
+    g[i] = one_run<kType>();
+    if (n > 0) {
+      x[i] = load_run<kType>(xr, col, n);
+      if (a.residual) r[i] = load_run<kType>(rr, col, n);
+      if (a.gain) g[i] = load_run<kType>(gr, col, n);
+      if (p.shift) t[i] = load_run<kType>(tr, col, n);
+    }
+  }
+  float s[kRuns][8];
+  float mean[1] = {0.0f};
+  uint8_t* sr = row_of<kType>(a.sum, at, a.sum_stride);
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
+    const int col = i * step + lane * 8, n = width - col;
+    to_f32<kType>(x[i], s[i]);
+    if (a.residual) {
+      float v[8];
+      to_f32<kType>(r[i], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[i][e] += v[e];
+      if (n > 0) store_run<kType>(sr, col, n, from_f32<kType>(s[i]));
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mean[0] += s[i][e];
+  }
+  row_sum(mean, lds_mean, at_.wave, sh);
+  const float m = mean[0] / (float)a.width;
+  Sum q[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
+    const int n = width - (i * step + lane * 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[i][e] = e < n ? s[i][e] - m : 0.0f;
+      q[0] += s[i][e];
+      q[1] = fused(s[i][e], s[i][e], q[1]);
+    }
+  }
+  row_sum(q, lds, at_.wave, sh);
+  const Sum off = q[0] / (Sum)a.width, var = not_negative(q[1] / (Sum)a.width - off * off);
+  Sum rho;
+  if constexpr (kOut == kNormSame) rho = 1.0f / __builtin_sqrtf(var + a.eps);
+  else rho = inverse_root(var + (double)a.eps);
+  const float rho32 = (float)rho, off32 = (float)off;
+  uint8_t* outr = row_of<kType>(a.out, at, a.out_stride);
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
+    const int col = i * step + lane * 8, n = width - col;
+    float v[8], w[8], y[8];
+    forget(g[i]);
+    forget(t[i]);
+    to_f32<kType>(g[i], v);
+    to_f32<kType>(t[i], w);
+    float size = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float ng = (s[i][e] - off32) * rho32 * v[e];
+      y[e] = ng + w[e];
+      size = __builtin_fmaxf(size, __builtin_fabsf(ng) + __builtin_fabsf(w[e]));
+    }
+    if (n <= 0) continue;
+    if constexpr (kOut == kNormSame) {
+      store_run<kType>(outr, col, n, from_f32<kType>(y));
+    } else {
+      // the four lanes of a block are inside the row or outside it together
+      const uint32_t sc = block_scale<(kOut == kNormMxfp8 ? 8 : 2)>(y, size, [&](int e) {
+        float d = s[i][e];
+        asm volatile("" : "+v"(d));   // converted here, where it is rarely needed, and not kept in 64 bits
+        return ((double)d - off) * rho * (double)v[e] + (double)w[e];
+      });
+      const float inv = inverse_scale(sc);
+      if constexpr (kOut == kNormMxfp8)
+        *reinterpret_cast<u32x2_t*>(a.codes + at * a.width + col) = e4m3_codes(y, inv);
+      else
+        *reinterpret_cast<uint32_t*>(a.codes + (at * a.width + col) / 2) = e2m1_codes(y, inv);
+      if ((threadIdx.x & 3) == 0) a.scales[(at * a.width + col) / 32] = (uint8_t)sc;
+    }
+  }
+}
+
+template <int kType, int kOut>
+static auto norm_kernel(int runs) {
+  switch (runs) {
+    case 1: return add_layernorm_kernel<kType, kOut, 1>;
+    case 2: return add_layernorm_kernel<kType, kOut, 2>;
+    case 3: return add_layernorm_kernel<kType, kOut, 3>;
+    case 4: return add_layernorm_kernel<kType, kOut, 4>;
+    case 5: return add_layernorm_kernel<kType, kOut, 5>;
+    default: return add_layernorm_kernel<kType, kOut, 6>;
+  }
+}
+
+template <int kType, int kOut>
+static hipError_t launch_norm(LayerNormArgs a, hipStream_t stream) {
+  const RowShape sh = row_shape(a.n.width, kNormRuns<kType>);
+  const int waves = sh.wpr > 4 ? sh.wpr : 4, slots = sh.waves_slots(waves);
+  const int64_t most = kMaxThreads / (waves * kWave) * slots;   // rows of one launch
+  for (a.n.first = 0; a.n.first < a.n.rows; a.n.first += most) {
+    const int64_t rows = a.n.rows - a.n.first < most ? a.n.rows - a.n.first : most;
+    const hipError_t e = launch_kernel(norm_kernel<kType, kOut>(sh.runs), dim3((unsigned)((rows + slots - 1) / slots)),
+                                       dim3(waves * kWave), stream, a, sh);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <int kType>
+static hipError_t launch_norm_type(const LayerNormArgs& a, int out, hipStream_t stream) {
+  if (out == kNormSame) return launch_norm<kType, kNormSame>(a, stream);
+  if (out == kNormMxfp8) return launch_norm<kType, kNormMxfp8>(a, stream);
+  return launch_norm<kType, kNormMxfp4>(a, stream);
+}
+
+hipError_t launch_add_layernorm(int type, int out, const LayerNormArgs& a, hipStream_t stream) {
+  if (a.n.rows == 0 || a.n.width == 0) return hipSuccess;
+  if (type == SOLFP4_BF16) return launch_norm_type<SOLFP4_BF16>(a, out, stream);
+  if (type == SOLFP4_F16) return launch_norm_type<SOLFP4_F16>(a, out, stream);
+  return launch_norm_type<SOLFP4_F32>(a, out, stream);
+}
+
+// ---- backward -------------------------------------------------------------
+
+// ds of every row, and each workgroup's share of dg and dt: rows are dealt to
+// the workgroups as in the root-mean-square norm's backward pass, all of a
+// row's loads go out before the first use and stay as they were read.
+template <int kType, int kRuns>
+__global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 4 : 2) void layernorm_backward_kernel(LayerNormBackArgs p, RowShape sh) {
+  __shared__ float lds[kNormMaxWaves][4], lds_mean[kNormMaxWaves][1];
+  __shared__ __attribute__((aligned(16))) float fold[kRuns][kNormMaxWaves * kWave * 8];
+  const NormBackArgs& a = p.n;
+  const Place<kRuns> at_(sh);
+  const int slots = sh.waves_slots(kNormMaxWaves), slot = at_.slot, lane = at_.lane, step = at_.step;
+  const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
+  const uint32_t rows = (uint32_t)a.group_rows;   // a hop past its end still fits 32 bits
+  const int64_t row0 = group * a.group_rows;
+  Run<kType> g[kRuns];
+  const uint8_t* gr = row_of<kType>(a.gain, group, a.gain_stride);
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
+    const int col = i * step + lane * 8, n = (int)a.width - col;
+    g[i] = one_run<kType>();
+    if (a.gain && n > 0) g[i] = load_run<kType>(gr, col, n);
+  }
+  float dg[kRuns][8] = {}, dt[kRuns][8] = {};
+  for (uint32_t base = part * slots; base < rows; base += a.parts * slots) {
+    const bool in = base + slot < rows;
+    const int64_t row = row0 + (in ? base + slot : base);
+    const int width = in ? (int)a.width : 0;
+    const uint8_t* xr = row_of<kType>(a.x, row, a.x_stride);
+    const uint8_t* dr = row_of<kType>(a.dy, row, a.dy_stride);
+    const uint8_t* er = row_of<kType>(a.dsum, row, a.dsum_stride);
+    Run<kType> x[kRuns], d[kRuns], ex[kRuns];
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const int col = i * step + lane * 8, n = width - col;
+      x[i] = d[i] = ex[i] = zero_run<kType>();
+      if (n > 0) {
+        x[i] = load_run<kType>(xr, col, n);
+        d[i] = load_run<kType>(dr, col, n);
+        if (a.dsum) ex[i] = load_run<kType>(er, col, n);
+      }
+    }
+    float mean[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      float s[8];
+      to_f32<kType>(x[i], s);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mean[0] += s[e];
+    }
+    row_sum(mean, lds_mean, at_.wave, sh);
+    const float m = mean[0] / (float)a.width;
+    float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // d, d^2, G, G d
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const int n = width - (i * step + lane * 8);
+      float s[8], D[8], v[8];
+      forget(x[i]);
+      to_f32<kType>(x[i], s);
+      to_f32<kType>(d[i], D);
+      to_f32<kType>(g[i], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float c = e < n ? s[e] - m : 0.0f, G = D[e] * v[e];
+        q[0] += c;
+        q[1] = fused(c, c, q[1]);
+        q[2] += G;
+        q[3] = fused(G, c, q[3]);
+      }
+    }
+    row_sum(q, lds, at_.wave, sh);
+    const float off = q[0] / (float)a.width;
+    // 0 where the slot has no row: with eps = 0 its zeros would add 0 times infinity to dg
+    const float rho = in ? 1.0f / __builtin_sqrtf(not_negative(q[1] / (float)a.width - off * off) + a.eps) : 0.0f;
+    const float mg = q[2] / (float)a.width;
+    const float k = fused(-off, q[2], q[3]) / (float)a.width * rho * rho;
+    uint8_t* outr = row_of<kType>(a.dx, row, a.dx_stride);
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const int col = i * step + lane * 8, n = width - col;
+      float s[8], D[8], v[8], out[8];
+      forget(x[i]);
+      forget(d[i]);
+      forget(g[i]);
+      to_f32<kType>(x[i], s);
+      to_f32<kType>(d[i], D);
+      to_f32<kType>(g[i], v);
+      to_f32<kType>(ex[i], out);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float c = (s[e] - m) - off;
+        dt[i][e] += D[e];
+        dg[i][e] = fused(D[e], c * rho, dg[i][e]);
+        out[e] = fused(rho, fused(c, -k, fused(D[e], v[e], -mg)), out[e]);
+      }
+      if (n > 0) store_run<kType>(outr, col, n, from_f32<kType>(out));
+    }
+  }
+  // every slot's sums to LDS, then each thread adds some columns'
+  const int cols = sh.wpr * sh.lanes * 8;
+  const auto share = [&](const float (&v)[kRuns][8], float* partial) {
+    float* part_row = partial + (int64_t)blockIdx.x * a.width;
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      floatx4_t* to = reinterpret_cast<floatx4_t*>(fold[i] + slot * cols + lane * 8);
+      to[0] = floatx4_t{v[i][0], v[i][1], v[i][2], v[i][3]};
+      to[1] = floatx4_t{v[i][4], v[i][5], v[i][6], v[i][7]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      for (int c = threadIdx.x; c < cols; c += kNormMaxWaves * kWave) {
+        float t = fold[i][c];
+        for (int z = 1; z < slots; ++z) t += fold[i][z * cols + c];
+        if (i * step + c < a.width) part_row[i * step + c] = t;
+      }
+    }
+  };
+  if (a.partial) share(dg, a.partial);
+  if (a.partial && p.shift_partial) __syncthreads();
+  if (p.shift_partial) share(dt, p.shift_partial);
+}
+
+// dg and dt from the workgroups' shares, one a slice of the grid.
+__global__ __launch_bounds__(kFoldCols * kFoldSlices) void layernorm_sums_kernel(const float* __restrict__ partial,
+                                                                                  float* __restrict__ dgain,
+                                                                                  const float* __restrict__ shift_partial,
+                                                                                  float* __restrict__ dshift,
+                                                                                  int64_t width, int parts) {
+  const bool shift = blockIdx.z || !dgain;
+  fold_parts(shift ? shift_partial : partial, shift ? dshift : dgain, width, parts);
+}
+
+template <int kType>
+static hipError_t launch_back(const LayerNormBackArgs& a, hipStream_t stream) {
+  const RowShape sh = row_shape(a.n.width, kBackRuns<kType>);
+  const dim3 grid((unsigned)(a.n.groups * a.n.parts)), block(kNormMaxWaves * kWave);
+  switch (sh.runs) {
+    case 1: return launch_kernel(layernorm_backward_kernel<kType, 1>, grid, block, stream, a, sh);
+    case 2: return launch_kernel(layernorm_backward_kernel<kType, 2>, grid, block, stream, a, sh);
+    case 3: return launch_kernel(layernorm_backward_kernel<kType, 3>, grid, block, stream, a, sh);
+    case 4: return launch_kernel(layernorm_backward_kernel<kType, 4>, grid, block, stream, a, sh);
+    case 5: return launch_kernel(layernorm_backward_kernel<kType, 5>, grid, block, stream, a, sh);
+    default: return launch_kernel(layernorm_backward_kernel<kType, 6>, grid, block, stream, a, sh);
+  }
+}
+
+hipError_t launch_layernorm_backward(int type, LayerNormBackArgs a, float* dgain, float* dshift, hipStream_t stream) {
+  NormBackArgs& n = a.n;
+  if (n.width == 0 || n.groups == 0) return hipSuccess;
+  hipError_t e = hipSuccess;
+  const int64_t parts = rmsnorm_backward_parts(n.rows, n.width, n.groups);
+  if (parts == 1) n.partial = dgain, a.shift_partial = dshift;   // the one workgroup's sums are the group's
+  if (parts) {
+    n.group_rows = n.rows / n.groups;
+    n.parts = (int)parts;
+    if (type == SOLFP4_BF16) e = launch_back<SOLFP4_BF16>(a, stream);
+    else if (type == SOLFP4_F16) e = launch_back<SOLFP4_F16>(a, stream);
+    else e = launch_back<SOLFP4_F32>(a, stream);
+  }
+  const unsigned sums = (dgain ? 1 : 0) + (dshift ? 1 : 0);
+  if (e != hipSuccess || !sums || parts == 1) return e;
+  const dim3 grid((unsigned)((n.width + kFoldCols - 1) / kFoldCols), (unsigned)n.groups, sums);
+  return launch_kernel(layernorm_sums_kernel, grid, dim3(kFoldCols * kFoldSlices), stream,
+                       dgain ? (const float*)n.partial : nullptr, dgain, (const float*)a.shift_partial, dshift, n.width,
+                       (int)parts);
+}
+
+}  // namespace solfp4
