@@ -98,6 +98,16 @@ __device__ __forceinline__ void to_f32(const Run<kType>& r, float (&v)[8]) {
   }
 }
 
+// sum + the run's values, in FP32
+template <int kType>
+__device__ __forceinline__ float add_run(const Run<kType>& r, float sum) {
+  float v[8];
+  to_f32<kType>(r, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum += v[e];
+  return sum;
+}
+
 // Each value rounded once (nearest, ties to even).
 template <int kType>
 __device__ __forceinline__ Run<kType> from_f32(const float (&v)[8]) {
@@ -138,6 +148,66 @@ __device__ __forceinline__ void store_run(uint8_t* base, uint32_t at, int n, con
     }
   }
 }
+
+// A row as a buffer, its base uniform over the wave: whole runs of 8 are one
+// range-checked load or store a piece with no branch and no 64-bit address a
+// lane (kept over a loop those were spilled, and each reload waited for all
+// loads before it); the row's last width % 8 elements (kWhole: there are none)
+// go one by one.
+template <int kType, bool kWhole>
+struct BufferRow {
+  __amdgpu_buffer_rsrc_t runs, all;
+  __device__ __forceinline__ BufferRow(const uint8_t* row, int width) {
+    runs = uniform_rsrc(row, (width & -8) * kElemBytes<kType>);
+    all = uniform_rsrc(row, width * kElemBytes<kType>);
+  }
+  // The run at column `col`, of which n elements exist (n <= 0: zeros).
+  __device__ __forceinline__ Run<kType> load(uint32_t col, int n) const {
+    const uint32_t off = col * kElemBytes<kType>;
+    Run<kType> r;
+#pragma unroll
+    for (int i = 0; i < kRunPieces<kType>; ++i)
+      r.p[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(runs, off + 16 * i, 0, 0));
+    if (!kWhole && n > 0 && n < 8) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e) {
+        if constexpr (kType == SOLFP4_F32)
+          r.p[e / 4][e % 4] = __builtin_amdgcn_raw_buffer_load_b32(all, off + 4 * e, 0, 0);
+        else
+          r.p[0][e / 2] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(all, off + 2 * e, 0, 0) << (16 * (e & 1));
+      }
+    }
+    return r;
+  }
+  __device__ __forceinline__ void store(uint32_t col, int n, const Run<kType>& r) const {
+    const uint32_t off = col * kElemBytes<kType>;
+#pragma unroll
+    for (int i = 0; i < kRunPieces<kType>; ++i)
+      __builtin_amdgcn_raw_buffer_store_b128(r.p[i], runs, off + 16 * i, 0, 0);
+    if (!kWhole && n > 0 && n < 8) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e) {
+        if constexpr (kType == SOLFP4_F32)
+          __builtin_amdgcn_raw_buffer_store_b32(r.p[e / 4][e % 4], all, off + 4 * e, 0, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r.p[0][e / 2] >> (16 * (e & 1))), all, off + 2 * e, 0, 0);
+      }
+    }
+  }
+};
+
+// The same interface for rows whose base differs between a wave's lanes.
+template <int kType>
+struct LaneRow {
+  const uint8_t* row;
+  __device__ __forceinline__ LaneRow(const uint8_t* row, int) : row(row) {}
+  __device__ __forceinline__ Run<kType> load(uint32_t col, int n) const {
+    return n > 0 ? load_run<kType>(row, col, n) : zero_run<kType>();
+  }
+  __device__ __forceinline__ void store(uint32_t col, int n, const Run<kType>& r) const {
+    if (n > 0) store_run<kType>(const_cast<uint8_t*>(row), col, n, r);
+  }
+};
 
 // Hides that the run is as it was, so that its conversion is made again
 // where it is used again and no FP32 copy is kept in between.

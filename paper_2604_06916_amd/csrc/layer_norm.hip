@@ -52,6 +52,16 @@ __device__ __forceinline__ uint32_t block_scale(const float (&y)[8], float size,
 template <typename T>
 __device__ __forceinline__ T not_negative(T v) { return v < 0 ? 0 : v; }
 
+// s - m of a lane's run, 0 where the row has no elements (the first n of the run exist)
+__device__ __forceinline__ void differences(float (&s)[8], float m, int n, bool whole) {
+  const float from = n > 0 ? m : 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[e] -= from;
+  if (!whole)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = e < n ? s[e] : 0.0f;
+}
+
 template <int kType, int kOut, int kRuns>
 __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(LayerNormArgs p, RowShape sh) {
   using Sum = std::conditional_t<kOut == kNormSame, float, double>;   // block_scale
@@ -98,20 +108,19 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(La
 #pragma unroll
     for (int e = 0; e < 8; ++e) mean[0] += s[i][e];
   }
-  row_sum(mean, lds_mean, at_.wave, sh);
+  row_sum<false>(mean, lds_mean, at_.wave, sh);
   const float m = mean[0] / (float)a.width;
   Sum q[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    const int n = width - (i * step + lane * 8);
+    differences(s[i], m, width - (i * step + lane * 8), (a.width & 7) == 0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      s[i][e] = e < n ? s[i][e] - m : 0.0f;
       q[0] += s[i][e];
       q[1] = fused(s[i][e], s[i][e], q[1]);
     }
   }
-  row_sum(q, lds, at_.wave, sh);
+  row_sum<false>(q, lds, at_.wave, sh);
   const Sum off = q[0] / (Sum)a.width, var = not_negative(q[1] / (Sum)a.width - off * off);
   Sum rho;
   if constexpr (kOut == kNormSame) rho = 1.0f / __builtin_sqrtf(var + a.eps);
@@ -195,11 +204,27 @@ hipError_t launch_add_layernorm(int type, int out, const LayerNormArgs& a, hipSt
 
 // ---- backward -------------------------------------------------------------
 
+// Runs a lane above which a row gets more waves.  A row needs two exchanges
+// between its waves, so in 16 bits one wave with all of the row in up to 256
+// registers, two waves a SIMD, is faster than two to four waves with 128 (BF16
+// with up to six and two runs: 26574 x 2432 121 and 143 us, 6000 x 9728 125 and
+// 141, 30000 x 1152 67 and 78; 10000 x 5600 122 and 119).  FP32 rows would spill
+// (12000 x 2432 102 us with two, 108 with three).
+template <int kType>
+constexpr int kLayerBackRuns = kType == SOLFP4_F32 ? 2 : 6;
+
 // ds of every row, and each workgroup's share of dg and dt: rows are dealt to
 // the workgroups as in the root-mean-square norm's backward pass, all of a
-// row's loads go out before the first use and stay as they were read.
-template <int kType, int kRuns>
-__global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 4 : 2) void layernorm_backward_kernel(LayerNormBackArgs p, RowShape sh) {
+// row's loads go out before the first use and stay as they were read.  dt is
+// summed in LDS and the gain kept there, each lane's in places of its own: with
+// all of it in registers the kernel spilled (26574 x 2432 BF16 371 us).
+//
+// Bound by memory, 8 bytes an element in BF16 with dsum, and by how few waves
+// hold it in flight: 26574 x 2432 in 6 groups 121 us, 4.3 TB/s; FP32 1009 x 1283
+// 13.4 us.
+// kWhole: the width is a multiple of 8.
+template <int kType, int kRuns, bool kWhole>
+__global__ __launch_bounds__(kNormMaxWaves * kWave, 2) void layernorm_backward_kernel(LayerNormBackArgs p, RowShape sh) {
   __shared__ float lds[kNormMaxWaves][4], lds_mean[kNormMaxWaves][1];
   __shared__ __attribute__((aligned(16))) float fold[kRuns][kNormMaxWaves * kWave * 8];
   const NormBackArgs& a = p.n;
@@ -208,99 +233,115 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 
   const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
   const uint32_t rows = (uint32_t)a.group_rows;   // a hop past its end still fits 32 bits
   const int64_t row0 = group * a.group_rows;
-  Run<kType> g[kRuns];
+  // the gain, each lane's in places of its own
+  constexpr bool kGainInLds = kRuns <= kLayerBackRuns<kType>;
+  __shared__ u32x4_t gains[kGainInLds ? kRuns * kRunPieces<kType> : 1][kNormMaxWaves * kWave];
+  Run<kType> g[kGainInLds ? 1 : kRuns];
   const uint8_t* gr = row_of<kType>(a.gain, group, a.gain_stride);
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
     const int col = i * step + lane * 8, n = (int)a.width - col;
-    g[i] = one_run<kType>();
-    if (a.gain && n > 0) g[i] = load_run<kType>(gr, col, n);
+    Run<kType> v = one_run<kType>();
+    if (a.gain && n > 0) v = load_run<kType>(gr, col, n);
+    if constexpr (kGainInLds) {
+#pragma unroll
+      for (int k = 0; k < kRunPieces<kType>; ++k) gains[i * kRunPieces<kType> + k][threadIdx.x] = v.p[k];
+    } else {
+      g[i] = v;
+    }
   }
-  float dg[kRuns][8] = {}, dt[kRuns][8] = {};
+  const auto gain_run = [&](int i) {
+    if constexpr (kGainInLds) {
+      Run<kType> v;
+      asm volatile("" ::: "memory");   // read again where it is used again
+#pragma unroll
+      for (int k = 0; k < kRunPieces<kType>; ++k) v.p[k] = gains[i * kRunPieces<kType> + k][threadIdx.x];
+      return v;
+    } else {
+      forget(g[i]);
+      return g[i];
+    }
+  };
+  const int cols = sh.wpr * sh.lanes * 8;
+  float dg[kRuns][8] = {};
+  floatx4_t* const mine = reinterpret_cast<floatx4_t*>(fold[0] + slot * cols + lane * 8);
+  constexpr int kNext = kNormMaxWaves * kWave * 2;   // from a run's place to the next's, in fours
+  if (p.shift_partial)
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) mine[i * kNext] = mine[i * kNext + 1] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
   for (uint32_t base = part * slots; base < rows; base += a.parts * slots) {
     const bool in = base + slot < rows;
     const int64_t row = row0 + (in ? base + slot : base);
     const int width = in ? (int)a.width : 0;
-    const uint8_t* xr = row_of<kType>(a.x, row, a.x_stride);
-    const uint8_t* dr = row_of<kType>(a.dy, row, a.dy_stride);
-    const uint8_t* er = row_of<kType>(a.dsum, row, a.dsum_stride);
+    using Row = std::conditional_t<(kRuns > 1), BufferRow<kType, kWhole>, LaneRow<kType>>;
+    const Row xr(row_of<kType>(a.x, row, a.x_stride), width), dr(row_of<kType>(a.dy, row, a.dy_stride), width);
+    const Row er(row_of<kType>(a.dsum, row, a.dsum_stride), a.dsum ? width : 0);
     Run<kType> x[kRuns], d[kRuns], ex[kRuns];
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
       const int col = i * step + lane * 8, n = width - col;
-      x[i] = d[i] = ex[i] = zero_run<kType>();
-      if (n > 0) {
-        x[i] = load_run<kType>(xr, col, n);
-        d[i] = load_run<kType>(dr, col, n);
-        if (a.dsum) ex[i] = load_run<kType>(er, col, n);
-      }
+      x[i] = xr.load(col, n);
+      d[i] = dr.load(col, n);
+      ex[i] = er.load(col, a.dsum ? n : 0);
     }
     float mean[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i) {
-      float s[8];
-      to_f32<kType>(x[i], s);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mean[0] += s[e];
-    }
-    row_sum(mean, lds_mean, at_.wave, sh);
+    for (int i = 0; i < kRuns; ++i) mean[0] = add_run<kType>(x[i], mean[0]);
+    row_sum<false>(mean, lds_mean, at_.wave, sh);
     const float m = mean[0] / (float)a.width;
     float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // d, d^2, G, G d
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const int n = width - (i * step + lane * 8);
       float s[8], D[8], v[8];
       forget(x[i]);
       to_f32<kType>(x[i], s);
+      differences(s, m, width - (i * step + lane * 8), kWhole);
       to_f32<kType>(d[i], D);
-      to_f32<kType>(g[i], v);
+      to_f32<kType>(gain_run(i), v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float c = e < n ? s[e] - m : 0.0f, G = D[e] * v[e];
-        q[0] += c;
-        q[1] = fused(c, c, q[1]);
+        const float G = D[e] * v[e];
+        q[0] += s[e];
+        q[1] = fused(s[e], s[e], q[1]);
         q[2] += G;
-        q[3] = fused(G, c, q[3]);
+        q[3] = fused(G, s[e], q[3]);
       }
     }
-    row_sum(q, lds, at_.wave, sh);
+    row_sum<false>(q, lds, at_.wave, sh);
     const float off = q[0] / (float)a.width;
     // 0 where the slot has no row: with eps = 0 its zeros would add 0 times infinity to dg
     const float rho = in ? 1.0f / __builtin_sqrtf(not_negative(q[1] / (float)a.width - off * off) + a.eps) : 0.0f;
     const float mg = q[2] / (float)a.width;
-    const float k = fused(-off, q[2], q[3]) / (float)a.width * rho * rho;
-    uint8_t* outr = row_of<kType>(a.dx, row, a.dx_stride);
+    const float k = fused(-off, q[2], q[3]) / (float)a.width * rho;   // mean(G n)
+    const float away = -off * rho;
+    const Row outr(row_of<kType>(a.dx, row, a.dx_stride), width);
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
       const int col = i * step + lane * 8, n = width - col;
       float s[8], D[8], v[8], out[8];
       forget(x[i]);
       forget(d[i]);
-      forget(g[i]);
       to_f32<kType>(x[i], s);
       to_f32<kType>(d[i], D);
-      to_f32<kType>(g[i], v);
+      to_f32<kType>(gain_run(i), v);
       to_f32<kType>(ex[i], out);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float c = (s[e] - m) - off;
-        dt[i][e] += D[e];
-        dg[i][e] = fused(D[e], c * rho, dg[i][e]);
-        out[e] = fused(rho, fused(c, -k, fused(D[e], v[e], -mg)), out[e]);
+        const float nrm = fused(s[e] - m, rho, away);
+        dg[i][e] = fused(D[e], nrm, dg[i][e]);
+        out[e] = fused(rho, fused(nrm, -k, fused(D[e], v[e], -mg)), out[e]);
       }
-      if (n > 0) store_run<kType>(outr, col, n, from_f32<kType>(out));
+      outr.store(col, n, from_f32<kType>(out));
+      if (p.shift_partial) {
+        mine[i * kNext] += floatx4_t{D[0], D[1], D[2], D[3]};
+        mine[i * kNext + 1] += floatx4_t{D[4], D[5], D[6], D[7]};
+      }
+      __builtin_amdgcn_sched_barrier(0);   // one run's values at a time in registers
     }
   }
-  // every slot's sums to LDS, then each thread adds some columns'
-  const int cols = sh.wpr * sh.lanes * 8;
-  const auto share = [&](const float (&v)[kRuns][8], float* partial) {
+  // every slot's sums in LDS: each thread adds some columns'
+  const auto share = [&](float* partial) {
     float* part_row = partial + (int64_t)blockIdx.x * a.width;
-#pragma unroll
-    for (int i = 0; i < kRuns; ++i) {
-      floatx4_t* to = reinterpret_cast<floatx4_t*>(fold[i] + slot * cols + lane * 8);
-      to[0] = floatx4_t{v[i][0], v[i][1], v[i][2], v[i][3]};
-      to[1] = floatx4_t{v[i][4], v[i][5], v[i][6], v[i][7]};
-    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
@@ -311,9 +352,17 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave, kRuns <= kBackRuns<kType> ? 
       }
     }
   };
-  if (a.partial) share(dg, a.partial);
-  if (a.partial && p.shift_partial) __syncthreads();
-  if (p.shift_partial) share(dt, p.shift_partial);
+  if (p.shift_partial) {
+    share(p.shift_partial);
+    __syncthreads();
+  }
+  if (!a.partial) return;
+#pragma unroll
+  for (int i = 0; i < kRuns; ++i) {
+    mine[i * kNext] = floatx4_t{dg[i][0], dg[i][1], dg[i][2], dg[i][3]};
+    mine[i * kNext + 1] = floatx4_t{dg[i][4], dg[i][5], dg[i][6], dg[i][7]};
+  }
+  share(a.partial);
 }
 
 // dg and dt from the workgroups' shares, one a slice of the grid.
@@ -326,18 +375,23 @@ __global__ __launch_bounds__(kFoldCols * kFoldSlices) void layernorm_sums_kernel
   fold_parts(shift ? shift_partial : partial, shift ? dshift : dgain, width, parts);
 }
 
+template <int kType, bool kWhole>
+static auto back_kernel(int runs) {
+  switch (runs) {
+    case 1: return layernorm_backward_kernel<kType, 1, kWhole>;
+    case 2: return layernorm_backward_kernel<kType, 2, kWhole>;
+    case 3: return layernorm_backward_kernel<kType, 3, kWhole>;
+    case 4: return layernorm_backward_kernel<kType, 4, kWhole>;
+    case 5: return layernorm_backward_kernel<kType, 5, kWhole>;
+    default: return layernorm_backward_kernel<kType, 6, kWhole>;
+  }
+}
+
 template <int kType>
 static hipError_t launch_back(const LayerNormBackArgs& a, hipStream_t stream) {
-  const RowShape sh = row_shape(a.n.width, kBackRuns<kType>);
-  const dim3 grid((unsigned)(a.n.groups * a.n.parts)), block(kNormMaxWaves * kWave);
-  switch (sh.runs) {
-    case 1: return launch_kernel(layernorm_backward_kernel<kType, 1>, grid, block, stream, a, sh);
-    case 2: return launch_kernel(layernorm_backward_kernel<kType, 2>, grid, block, stream, a, sh);
-    case 3: return launch_kernel(layernorm_backward_kernel<kType, 3>, grid, block, stream, a, sh);
-    case 4: return launch_kernel(layernorm_backward_kernel<kType, 4>, grid, block, stream, a, sh);
-    case 5: return launch_kernel(layernorm_backward_kernel<kType, 5>, grid, block, stream, a, sh);
-    default: return launch_kernel(layernorm_backward_kernel<kType, 6>, grid, block, stream, a, sh);
-  }
+  const RowShape sh = row_shape(a.n.width, kLayerBackRuns<kType>);
+  return launch_kernel(a.n.width % 8 ? back_kernel<kType, false>(sh.runs) : back_kernel<kType, true>(sh.runs),
+                       dim3((unsigned)(a.n.groups * a.n.parts)), dim3(kNormMaxWaves * kWave), stream, a, sh);
 }
 
 hipError_t launch_layernorm_backward(int type, LayerNormBackArgs a, float* dgain, float* dshift, hipStream_t stream) {

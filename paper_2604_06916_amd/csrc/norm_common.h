@@ -68,13 +68,15 @@ struct Place {
 };
 
 // The sums of v[0 .. n) over a row's lanes, waves in wave order; every wave
-// of the workgroup calls it.
-template <int n, typename T>
+// of the workgroup calls it.  kAgain: the waves may still read what an earlier
+// call left in this lds (callers that alternate between two need no wait: a
+// wave is past its reads of one when it reaches the other's).
+template <bool kAgain = true, int n, typename T>
 __device__ __forceinline__ void row_sum(T (&v)[n], T (*lds)[n], int wave, RowShape sh) {
 #pragma unroll
   for (int i = 0; i < n; ++i) v[i] = lanes_sum(v[i], sh.lanes);
   if (sh.wpr == 1) return;
-  __syncthreads();
+  if (kAgain) __syncthreads();
   if ((threadIdx.x & (kWave - 1)) == 0)
 #pragma unroll
     for (int i = 0; i < n; ++i) lds[wave][i] = v[i];
@@ -82,6 +84,7 @@ __device__ __forceinline__ void row_sum(T (&v)[n], T (*lds)[n], int wave, RowSha
   const int first = wave & -sh.wpr;
 #pragma unroll
   for (int i = 0; i < n; ++i) v[i] = lds[first][i];
+#pragma unroll 1
   for (int w = 1; w < sh.wpr; ++w)
 #pragma unroll
     for (int i = 0; i < n; ++i) v[i] += lds[first + w][i];
