@@ -540,6 +540,50 @@ SOLFP4_API int solfp4_layernorm_backward(int type, const void* dy, int64_t dy_st
                    int64_t width, void* stream);
 
 /*
+ * Low-rank adapters beside a linear, many at once (requests of several
+ * adapters, rollouts of several policies, over one set of quantized weights):
+ *
+ *   h_t   = a_e x_t
+ *   out_t = y_t + scale_e b_e h_t        e = index[t], the adapter of token t
+ *
+ * y is the linear's output.  The plan brings the tokens of an adapter together;
+ * it is made from the index once for all layers and passes over these tokens,
+ * in a buffer of the caller's of solfp4_adapter_plan_bytes bytes (host only; 0
+ * for invalid sizes), 16-byte aligned, and read only by the calls that take it.
+ *
+ *   index   [tokens] int32 or int64 (index_bytes 4 or 8), in any order.
+ *           Negative: no adapter, the token's out is its y.  adapters or more:
+ *           the token's out (and dx) is NaN and it has no part in the gradients
+ *
+ * tokens below 2^27, at most 65536 adapters.  tokens == 0 is valid.
+ */
+SOLFP4_API size_t solfp4_adapter_plan_bytes(int64_t tokens, int64_t adapters);
+SOLFP4_API int solfp4_adapter_plan(const void* index, int index_bytes, int64_t tokens, int64_t adapters,
+                   void* plan, size_t plan_bytes, void* stream);
+
+/*
+ *   y       [tokens][N] BF16, rows y_stride apart
+ *   x       [tokens][K] BF16, rows x_stride apart: the linear's input
+ *   a       [adapters][rank][K] BF16, contiguous
+ *   b       [adapters][N][rank] BF16, contiguous
+ *   scales  [adapters] FP32; or NULL (all 1)
+ *   plan    for these tokens and adapters; or NULL: every token takes the one
+ *           adapter (adapters must be 1)
+ *   out     [tokens][N] BF16, rows out_stride apart, written; may be y
+ *   hidden  [tokens][rank] FP32, written with h (0 for tokens without an
+ *           adapter), what the backward pass needs; or NULL
+ *
+ * rank from 1 to 128 (adapters of fewer ranks: pad with zeros), N and K below
+ * 2^22.  Sums are FP32; h enters the second product with 16 bits and out is
+ * rounded once.  Rows and columns that lie between those of out are left as
+ * they were.  Overlaps other than out == y are refused (SOLFP4_EINVAL).
+ */
+SOLFP4_API int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const uint16_t* x,
+                   int64_t x_stride, const uint16_t* a, const uint16_t* b, const float* scales,
+                   int64_t adapters, const void* plan, uint16_t* out, int64_t out_stride,
+                   float* hidden, int64_t tokens, int64_t N, int64_t K, int64_t rank, void* stream);
+
+/*
  * Table of cosines and sines for solfp4_rotary:
  *
  *   table[p][i]         = magnitude cos(position frequency_i)

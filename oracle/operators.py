@@ -113,3 +113,19 @@ def mxfp8_values(codes, scales):
     rows, K = codes.shape
     v = O.e4m3_decode(codes & 127) * np.where(codes & 128, -1.0, 1.0)
     return (v.reshape(rows, K // 32, 32) * O.e8m0_decode(scales)[..., None]).reshape(rows, K)
+
+
+def add_adapters(y, x, a, b, scales, index):
+    """(out, hidden, and the magnitudes that their FP32 evaluation's errors go
+    by: sum of |a x| per hidden value, of |scale b| (|a| |x|) per output) of
+    adapters a [E, rank, K], b [E, N, rank] on tokens with these indices."""
+    out, hid = np.array(y, np.float64), np.zeros((x.shape[0], a.shape[1]))
+    size, hid_size = np.zeros_like(out), np.zeros_like(hid)
+    for e in range(a.shape[0]):
+        t = np.flatnonzero(index == e)
+        hid[t], hid_size[t] = x[t] @ a[e].T, np.abs(x[t]) @ np.abs(a[e]).T
+        out[t] += scales[e] * (hid[t] @ b[e].T)
+        size[t] = abs(scales[e]) * (hid_size[t] @ np.abs(b[e]).T)
+    bad = index >= a.shape[0]
+    out[bad] = hid[bad] = np.nan
+    return out, hid, size, hid_size

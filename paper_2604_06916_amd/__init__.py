@@ -14,7 +14,8 @@ _NAMES = ("EXPORTED", "LIB_PATH", "Solfp4Error", "lib", "gemm_plan", "FORMAT_NVF
           "add_rmsnorm", "mxfp8_add_rmsnorm", "mxfp4_add_rmsnorm", "rmsnorm_backward",
           "rmsnorm_backward_workspace_bytes", "add_layernorm", "mxfp8_add_layernorm",
           "mxfp4_add_layernorm", "layernorm_backward", "layernorm_backward_workspace_bytes", "rotary", "rotary_frequencies", "rotary_table",
-          "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear")
+          "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear",
+          "AdapterPlan", "adapter_plan", "adapter_plan_bytes", "add_adapters")
 __all__ = list(_NAMES)
 
 

@@ -100,6 +100,12 @@ lib.solfp4_rotary_table.argtypes = [_p, _i64, _p, _i64, _p, _int, _f64, _p, _p]
 lib.solfp4_rotary.restype = _int
 lib.solfp4_rotary.argtypes = [_int, _int, _int, *2 * [_p, _i64, _i64, _p, _i64, _i64, _i64], _p, _i64, _p, _int, _i64,
                               _i64, _i64, _p]
+lib.solfp4_adapter_plan_bytes.restype = _sz
+lib.solfp4_adapter_plan_bytes.argtypes = [_i64, _i64]
+lib.solfp4_adapter_plan.restype = _int
+lib.solfp4_adapter_plan.argtypes = [_p, _int, _i64, _i64, _p, _sz, _p]
+lib.solfp4_add_adapters.restype = _int
+lib.solfp4_add_adapters.argtypes = [_p, _i64, _p, _i64, _p, _p, _p, _i64, _p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p]
 lib.nvfp4_weight_linear.restype = _int
 lib.nvfp4_weight_linear.argtypes = [*6 * [_p], _i64, _i64, _i64, _p]
 lib.mxfp4_weight_linear.restype = _int
@@ -118,6 +124,7 @@ EXPORTED = ["solfp4_strerror", "solfp4_version", "solfp4_gemm_plan",
             "solfp4_add_layernorm", "mxfp8_add_layernorm", "mxfp4_add_layernorm",
             "solfp4_layernorm_backward_workspace_bytes", "solfp4_layernorm_backward",
             "solfp4_rotary_table", "solfp4_rotary",
+            "solfp4_adapter_plan_bytes", "solfp4_adapter_plan", "solfp4_add_adapters",
             "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear"]
 
 FORMAT_NVFP4, FORMAT_MXFP4 = 0, 1
@@ -999,3 +1006,106 @@ def mxfp8_linear(x_codes, x_scales, w_codes, w_scales, bias=None, out=None, stre
     _check(lib.mxfp8_linear(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(out),
                             M, N, K, ctypes.c_void_p(st.cuda_stream)))
     return out
+
+
+# ---- low-rank adapters ----------------------------------------------------
+
+class AdapterPlan:
+    """Tokens by adapter, from adapter_plan: `tokens`, `adapters`, and the
+    library's own layout of them in `buffer` (int32, on the GPU)."""
+    __slots__ = ("tokens", "adapters", "buffer")
+
+    def __init__(self, tokens, adapters, buffer):
+        self.tokens, self.adapters, self.buffer = tokens, adapters, buffer
+
+
+def adapter_plan_bytes(tokens: int, adapters: int) -> int:
+    return lib.solfp4_adapter_plan_bytes(tokens, adapters)
+
+
+def adapter_plan(index, adapters: int, plan=None, stream=None):
+    """The plan that add_adapters and adapters_backward take for tokens with
+    these adapters: index int32 or int64 [tokens], in any order, negative for
+    none.  Made once for all layers and passes; plan: one of the same sizes to
+    write again (in a captured graph, say) instead of a new one."""
+    if not isinstance(index, torch.Tensor) or index.dim() != 1 or index.dtype not in (torch.int32, torch.int64):
+        raise ValueError("index: expected a 1-D int32 or int64 tensor")
+    tokens, dev = index.numel(), index.device
+    _need(index, index.dtype, (tokens,), "index")
+    need = adapter_plan_bytes(tokens, adapters)
+    if not need:
+        raise ValueError(f"adapter_plan: {tokens} tokens of {adapters} adapters are not supported")
+    if plan is not None:
+        if not isinstance(plan, AdapterPlan) or plan.tokens != tokens or plan.adapters != adapters:
+            raise ValueError(f"plan: expected an AdapterPlan of {tokens} tokens and {adapters} adapters")
+        _need(plan.buffer, torch.int32, (need // 4,), "plan.buffer", dev)
+    st = _stream(stream, dev)
+    if plan is None:
+        plan = AdapterPlan(tokens, adapters, _alloc((need // 4,), torch.int32, dev, st))
+    _check(lib.solfp4_adapter_plan(_ptr(index), index.element_size(), tokens, adapters, _ptr(plan.buffer), need,
+                                   ctypes.c_void_p(st.cuda_stream)))
+    return plan
+
+
+def _adapter_operands(t, x, a, b, scales, plan, name):
+    """Checked: (tokens, N, K, rank, adapters, device) of t [tokens, N] (the
+    operand called `name`), x [tokens, K] and the adapters."""
+    for v, n, d in ((t, name, 2), (x, "x", 2), (a, "a", 3), (b, "b", 3)):
+        if not isinstance(v, torch.Tensor) or v.dim() != d:
+            raise ValueError(f"{n}: expected a {d}-D tensor")
+    tokens, N = t.shape
+    K = x.shape[1]
+    adapters, rank = a.shape[0], a.shape[1]
+    dev = x.device
+    _need_strided(t, torch.bfloat16, (tokens, N), name, dev)
+    _need_strided(x, torch.bfloat16, (tokens, K), "x", dev)
+    _need(a, torch.bfloat16, (adapters, rank, K), "a", dev)
+    _need(b, torch.bfloat16, (adapters, N, rank), "b", dev)
+    if scales is not None:
+        _need(scales, torch.float32, (adapters,), "scales", dev)
+    if not 1 <= rank <= 128:
+        raise ValueError(f"a: rank {rank}, expected 1 to 128")
+    if plan is None:
+        if adapters != 1:
+            raise ValueError(f"plan: needed for {adapters} adapters")
+    else:
+        if not isinstance(plan, AdapterPlan) or plan.tokens != tokens or plan.adapters != adapters:
+            raise ValueError(f"plan: expected an AdapterPlan of {tokens} tokens and {adapters} adapters")
+        _need(plan.buffer, torch.int32, (adapter_plan_bytes(tokens, adapters) // 4,), "plan.buffer", dev)
+    return tokens, N, K, rank, adapters, dev
+
+
+def add_adapters(y, x, a, b, scales=None, plan=None, hidden=False, out=None, stream=None):
+    """Low-rank adapters beside a linear: y [tokens, N], the linear's output, plus
+    scales[e] b[e] (a[e] x[t]) for every token t of adapter e -> (out, hidden).
+
+    x: BF16 [tokens, K], the linear's input; a: BF16 [adapters, rank, K]; b: BF16
+    [adapters, N, rank]; scales: FP32 [adapters] or None (1).  plan: from
+    adapter_plan, None where all tokens take the one adapter.  y and out may
+    have rows of any stride (columns of a packed QKV buffer), out may be y.
+    hidden: True or FP32 [tokens, rank] to keep a[e] x[t] for
+    adapters_backward; None is returned without it."""
+    keep = None if hidden is False or hidden is None else hidden
+    if stream is None:
+        if plan is None:
+            r = _host.add_adapters(y, x, a, b, scales, None, 0, 0, keep, out)
+        elif type(plan) is AdapterPlan:
+            r = _host.add_adapters(y, x, a, b, scales, plan.buffer, plan.tokens, plan.adapters, keep, out)
+        else:
+            r = None
+        if r is not None:
+            return _native(r)
+    tokens, N, K, rank, adapters, dev = _adapter_operands(y, x, a, b, scales, plan, "y")
+    if out is not None:
+        _need_strided(out, torch.bfloat16, (tokens, N), "out", dev)
+    if keep is not None and keep is not True:
+        _need(keep, torch.float32, (tokens, rank), "hidden", dev)
+    st = _stream(stream, dev)
+    if out is None:
+        out = _alloc((tokens, N), torch.bfloat16, dev, st)
+    if keep is True:
+        keep = _alloc((tokens, rank), torch.float32, dev, st)
+    _check(lib.solfp4_add_adapters(*_rows_of(y), *_rows_of(x), _ptr(a), _ptr(b), _ptr(scales), adapters,
+                                   _ptr(None if plan is None else plan.buffer), *_rows_of(out), _ptr(keep), tokens, N, K,
+                                   rank, ctypes.c_void_p(st.cuda_stream)))
+    return out, keep

@@ -20,8 +20,9 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsolfp4.so")
 HOST_LIB = os.path.join(PKG, "_host.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "gemm_small.hip", "gemm_wavek.hip", "mx_quantize.hip",
-           "mx_gemm.hip", "api_operators.hip", "norm.hip", "layer_norm.hip", "rotary.hip", "weight_linear.hip"]
-HEADERS = ["device_common.h", "elements.h", "kernels.h", "norm_common.h", "nvfp4_gemm_common.h",
+           "mx_gemm.hip", "api_operators.hip", "norm.hip", "layer_norm.hip", "rotary.hip", "weight_linear.hip",
+           "api_adapters.hip", "adapters.hip"]
+HEADERS = ["adapters.h", "device_common.h", "elements.h", "kernels.h", "norm_common.h", "nvfp4_gemm_common.h",
            "operand_checks.h"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

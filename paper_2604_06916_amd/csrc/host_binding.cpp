@@ -675,6 +675,65 @@ PyObject* mxfp8_linear_(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- low-rank adapters ----------------------------------------------------
+
+// The operands that both passes have: t [tokens][N], x, a, b, scales, and the
+// plan (buffer, tokens, adapters).
+struct Adapters {
+  const Tensor &t, &x, &a, &b;
+  Tensor scales, plan;
+  int64_t tokens, N, K, rank, adapters;
+  at::Device dev;
+  static const Tensor& of(PyObject* o, int64_t dims) {
+    const Tensor& v = tensor(o);
+    need(v.layout() == at::kStrided && v.dim() == dims);
+    return v;
+  }
+  Adapters(PyObject* t_, PyObject* x_, PyObject* a_, PyObject* b_, PyObject* scales_, PyObject* plan_,
+           PyObject* plan_tokens, PyObject* plan_adapters)
+      : t(of(t_, 2)), x(of(x_, 2)), a(of(a_, 3)), b(of(b_, 3)), tokens(t.size(0)), N(t.size(1)), K(x.size(1)),
+        rank(a.size(1)), adapters(a.size(0)), dev(x.device()) {
+    need(x.scalar_type() == at::kBFloat16);
+    need_strided(x, x, {tokens, K});
+    need_strided(t, x, {tokens, N});
+    need_tensor(a, at::kBFloat16, {adapters, rank, K}, &dev);
+    need_tensor(b, at::kBFloat16, {adapters, N, rank}, &dev);
+    if (scales_ != Py_None) {
+      scales = tensor(scales_);
+      need_tensor(scales, at::kFloat, {adapters}, &dev);
+    }
+    need(rank >= 1 && rank <= 128);
+    if (plan_ == Py_None) {
+      need(adapters == 1);
+    } else {
+      plan = tensor(plan_);
+      need(PyLong_CheckExact(plan_tokens) && PyLong_CheckExact(plan_adapters));
+      need(PyLong_AsLongLong(plan_tokens) == tokens && PyLong_AsLongLong(plan_adapters) == adapters);
+      need_tensor(plan, at::kInt, {(int64_t)solfp4_adapter_plan_bytes(tokens, adapters) / 4}, &dev);
+    }
+  }
+};
+
+// (y, x, a, b, scales, plan, plan_tokens, plan_adapters, hidden, out) -> (out, hidden)
+PyObject* add_adapters_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 10, [&]() -> PyObject* {
+    const Adapters o(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]);
+    const bool fresh = a[8] == Py_True;
+    Operand hidden(fresh ? Py_None : a[8], at::kFloat, {o.tokens, o.rank}, o.dev);
+    Strided out(a[9], o.x, {o.tokens, o.N});
+    void* stream = stream_of(o.dev);
+    out.allocate(o.x, {o.tokens, o.N});
+    if (fresh) hidden.allocate(at::kFloat, {o.tokens, o.rank}, o.dev);
+    const int rc = call([&] {
+      return solfp4_add_adapters(u16(o.t), o.t.stride(0), u16(o.x), o.x.stride(0), u16(o.a), u16(o.b), f32(o.scales),
+                                 o.adapters, ptr(o.plan), u16(out.t), out.stride(0), f32(hidden.t), o.tokens, o.N, o.K,
+                                 o.rank, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NN)", out.object(), object_or_none(hidden));
+  });
+}
+
 PyMethodDef methods[] = {
     {"nvfp4_quantize", (PyCFunction)(void*)nvfp4_quantize_, METH_FASTCALL, nullptr},
     {"mxfp4_quantize", (PyCFunction)(void*)mxfp4_quantize_, METH_FASTCALL, nullptr},
@@ -694,6 +753,7 @@ PyMethodDef methods[] = {
     {"nvfp4_weight_linear", (PyCFunction)(void*)nvfp4_weight_linear_, METH_FASTCALL, nullptr},
     {"mxfp4_weight_linear", (PyCFunction)(void*)mxfp4_weight_linear_, METH_FASTCALL, nullptr},
     {"mxfp8_linear", (PyCFunction)(void*)mxfp8_linear_, METH_FASTCALL, nullptr},
+    {"add_adapters", (PyCFunction)(void*)add_adapters_, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "Native checks, allocation and calls of the binding.",

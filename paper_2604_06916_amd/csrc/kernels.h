@@ -309,4 +309,44 @@ struct WeightLinearArgs {
 };
 hipError_t launch_weight_linear(int w_format, bool x_mxfp8, const WeightLinearArgs& a, hipStream_t stream);
 
+// ---- low-rank adapters (adapters.hip, adapters_back.hip) ------------------
+constexpr int kAdapterTile = 32;            // tokens of a tile
+constexpr int kAdapterMaxRank = 128;
+constexpr int64_t kAdapterMaxAdapters = 65536;
+constexpr int64_t kAdapterMaxTokens = (int64_t)1 << 27;   // a launch holds their tiles
+constexpr int64_t kAdapterMaxFeatures = (int64_t)1 << 22;
+
+// The plan, in 4-byte words: first tile of every group, first place of every
+// group, the tokens group by group (in their own order inside a group), and
+// the tiles (group, first place, count, 0; count 0 past the last).  Groups:
+// the adapters, then tokens without one, then tokens whose index is past the
+// last adapter.
+struct AdapterTokens {
+  const int* plan;       // NULL: all tokens take the one adapter
+  int64_t tokens;
+  int adapters;
+  int64_t places_at, order_at, tiles_at;   // words
+  int64_t max_tiles;
+};
+AdapterTokens adapter_tokens(const void* plan, int64_t tokens, int64_t adapters);
+size_t adapter_plan_bytes(int64_t tokens, int64_t adapters);
+hipError_t launch_adapter_plan(const void* index, int index_bytes, int64_t tokens, int64_t adapters, void* plan,
+                               hipStream_t stream);
+
+struct AdapterArgs {
+  AdapterTokens t;
+  const uint16_t* y;
+  int64_t y_stride;
+  const uint16_t* x;
+  int64_t x_stride;
+  const uint16_t *a, *b;  // [adapters][rank][K], [adapters][N][rank]
+  const float* scales;    // [adapters], NULL: 1
+  uint16_t* out;
+  int64_t out_stride;
+  float* hidden;          // [tokens][rank], NULL: not wanted
+  int N, K, rank;
+  int splits, split_cols;   // set by the launch
+};
+hipError_t launch_add_adapters(const AdapterArgs& a, hipStream_t stream);
+
 }  // namespace solfp4
