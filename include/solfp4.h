@@ -583,6 +583,44 @@ SOLFP4_API int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const ui
                    int64_t adapters, const void* plan, uint16_t* out, int64_t out_stride,
                    float* hidden, int64_t tokens, int64_t N, int64_t K, int64_t rank, void* stream);
 
+/* Device workspace of solfp4_adapters_backward (planned: nonzero with a plan).
+ * Host only; 0 for invalid sizes. */
+SOLFP4_API size_t solfp4_adapters_backward_workspace_bytes(int64_t tokens, int64_t adapters, int planned,
+                   int64_t N, int64_t K, int64_t rank);
+
+/*
+ * Backward pass of solfp4_add_adapters (the gradient of y is dy itself):
+ *
+ *   g_t  = scale_e b_e^T dy_t
+ *   dx_t = past_t + a_e^T g_t          past_t for tokens without an adapter
+ *   da_e = sum over e's tokens of g_t x_t^T
+ *   db_e = scale_e * sum over e's tokens of dy_t h_t^T
+ *
+ *   dy      [tokens][N] BF16, rows dy_stride apart
+ *   x       [tokens][K] BF16, rows x_stride apart
+ *   hidden  [tokens][rank] FP32, as the forward call wrote it
+ *   a, b, scales, plan  the forward call's
+ *   past    [tokens][K] BF16, rows past_stride apart: the gradient that reaches
+ *           x past the adapters (through the linear); or NULL (0)
+ *   dx      [tokens][K] BF16, rows dx_stride apart, written; may be past
+ *   da      [adapters][rank][K] FP32, written (0 for adapters without tokens)
+ *   db      [adapters][N][rank] FP32, written
+ *   workspace  at least solfp4_adapters_backward_workspace_bytes bytes,
+ *           16-byte aligned
+ *
+ * Sums are FP32, in an order that depends on the sizes, the plan and the
+ * device alone: results are the same on every call.  g and h enter the products
+ * for da and db with all their bits, g that for dx with 16.  A row with an
+ * infinity or a NaN spoils its own dx and its adapter's da and db (infinite or
+ * NaN), no others.  Overlaps other than dx == past are refused (SOLFP4_EINVAL).
+ */
+SOLFP4_API int solfp4_adapters_backward(const uint16_t* dy, int64_t dy_stride, const uint16_t* x,
+                   int64_t x_stride, const float* hidden, const uint16_t* a, const uint16_t* b,
+                   const float* scales, int64_t adapters, const void* plan, const uint16_t* past,
+                   int64_t past_stride, uint16_t* dx, int64_t dx_stride, float* da, float* db,
+                   void* workspace, size_t workspace_bytes, int64_t tokens, int64_t N, int64_t K,
+                   int64_t rank, void* stream);
+
 /*
  * Table of cosines and sines for solfp4_rotary:
  *

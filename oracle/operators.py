@@ -129,3 +129,20 @@ def add_adapters(y, x, a, b, scales, index):
     bad = index >= a.shape[0]
     out[bad] = hid[bad] = np.nan
     return out, hid, size, hid_size
+
+
+def adapters_backward(dy, x, hidden, a, b, scales, index, past=None):
+    """(dx, da, db, and of each the sum of the magnitudes that it is formed
+    from: |a| (|scale b| |dy|) for dx, over the tokens for da and db)."""
+    dx = np.zeros_like(x, dtype=np.float64) if past is None else np.array(past, np.float64)
+    da, db = np.zeros(a.shape), np.zeros(b.shape)
+    sizes = [np.zeros_like(v) for v in (dx, da, db)]
+    for e in range(a.shape[0]):
+        t, c = np.flatnonzero(index == e), scales[e]
+        g, g_size = c * (dy[t] @ b[e]), abs(c) * (np.abs(dy[t]) @ np.abs(b[e]))
+        dx[t] += g @ a[e]
+        da[e], db[e] = g.T @ x[t], c * (dy[t].T @ hidden[t])
+        sizes[0][t] = g_size @ np.abs(a[e])
+        sizes[1][e], sizes[2][e] = g_size.T @ np.abs(x[t]), abs(c) * (np.abs(dy[t]).T @ np.abs(hidden[t]))
+    dx[index >= a.shape[0]] = np.nan
+    return (dx, da, db, *sizes)

@@ -106,6 +106,11 @@ lib.solfp4_adapter_plan.restype = _int
 lib.solfp4_adapter_plan.argtypes = [_p, _int, _i64, _i64, _p, _sz, _p]
 lib.solfp4_add_adapters.restype = _int
 lib.solfp4_add_adapters.argtypes = [_p, _i64, _p, _i64, _p, _p, _p, _i64, _p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p]
+lib.solfp4_adapters_backward_workspace_bytes.restype = _sz
+lib.solfp4_adapters_backward_workspace_bytes.argtypes = [_i64, _i64, _int, _i64, _i64, _i64]
+lib.solfp4_adapters_backward.restype = _int
+lib.solfp4_adapters_backward.argtypes = [_p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _p, _p, _i64, _p, _i64, _p, _p, _p, _sz,
+                                         _i64, _i64, _i64, _i64, _p]
 lib.nvfp4_weight_linear.restype = _int
 lib.nvfp4_weight_linear.argtypes = [*6 * [_p], _i64, _i64, _i64, _p]
 lib.mxfp4_weight_linear.restype = _int
@@ -125,6 +130,7 @@ EXPORTED = ["solfp4_strerror", "solfp4_version", "solfp4_gemm_plan",
             "solfp4_layernorm_backward_workspace_bytes", "solfp4_layernorm_backward",
             "solfp4_rotary_table", "solfp4_rotary",
             "solfp4_adapter_plan_bytes", "solfp4_adapter_plan", "solfp4_add_adapters",
+            "solfp4_adapters_backward_workspace_bytes", "solfp4_adapters_backward",
             "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear"]
 
 FORMAT_NVFP4, FORMAT_MXFP4 = 0, 1
@@ -1109,3 +1115,53 @@ def add_adapters(y, x, a, b, scales=None, plan=None, hidden=False, out=None, str
                                    _ptr(None if plan is None else plan.buffer), *_rows_of(out), _ptr(keep), tokens, N, K,
                                    rank, ctypes.c_void_p(st.cuda_stream)))
     return out, keep
+
+
+def adapters_backward_workspace_bytes(tokens: int, adapters: int, planned: bool, N: int, K: int, rank: int) -> int:
+    return lib.solfp4_adapters_backward_workspace_bytes(tokens, adapters, int(planned), N, K, rank)
+
+
+def adapters_backward(dy, x, hidden, a, b, scales=None, plan=None, past=None, dx=None, da=None, db=None, workspace=None,
+                      stream=None):
+    """Backward pass of add_adapters: dy [tokens, N], the gradient of its output
+    (and so of y); x, a, b, scales and plan as there; hidden, what it kept ->
+    (dx, da, db).  past: BF16 [tokens, K], the gradient that reaches x through the
+    linear, added to dx (which may be past).  da and db are FP32 in the shapes of
+    a and b."""
+    if stream is None:
+        if plan is None:
+            r = _host.adapters_backward(dy, x, hidden, a, b, scales, None, 0, 0, past, dx, da, db, workspace)
+        elif type(plan) is AdapterPlan:
+            r = _host.adapters_backward(dy, x, hidden, a, b, scales, plan.buffer, plan.tokens, plan.adapters, past, dx,
+                                        da, db, workspace)
+        else:
+            r = None
+        if r is not None:
+            return _native(r)
+    tokens, N, K, rank, adapters, dev = _adapter_operands(dy, x, a, b, scales, plan, "dy")
+    _need(hidden, torch.float32, (tokens, rank), "hidden", dev)
+    if past is not None:
+        _need_strided(past, torch.bfloat16, (tokens, K), "past", dev)
+    if dx is not None:
+        _need_strided(dx, torch.bfloat16, (tokens, K), "dx", dev)
+    if da is not None:
+        _need(da, torch.float32, (adapters, rank, K), "da", dev)
+    if db is not None:
+        _need(db, torch.float32, (adapters, N, rank), "db", dev)
+    need = adapters_backward_workspace_bytes(tokens, adapters, plan is not None, N, K, rank)
+    if workspace is not None:
+        _need_workspace(workspace, need, "workspace", dev)
+    st = _stream(stream, dev)
+    if dx is None:
+        dx = _alloc((tokens, K), torch.bfloat16, dev, st)
+    if da is None:
+        da = _alloc((adapters, rank, K), torch.float32, dev, st)
+    if db is None:
+        db = _alloc((adapters, N, rank), torch.float32, dev, st)
+    if workspace is None:
+        workspace = _alloc((max(need, 256),), torch.uint8, dev, st)
+    _check(lib.solfp4_adapters_backward(*_rows_of(dy), *_rows_of(x), _ptr(hidden), _ptr(a), _ptr(b), _ptr(scales),
+                                        adapters, _ptr(None if plan is None else plan.buffer), *_rows_of(past),
+                                        *_rows_of(dx), _ptr(da), _ptr(db), _ptr(workspace), workspace.numel(), tokens, N,
+                                        K, rank, ctypes.c_void_p(st.cuda_stream)))
+    return dx, da, db

@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "libsolfp4.so")
 HOST_LIB = os.path.join(PKG, "_host.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "gemm_small.hip", "gemm_wavek.hip", "mx_quantize.hip",
            "mx_gemm.hip", "api_operators.hip", "norm.hip", "layer_norm.hip", "rotary.hip", "weight_linear.hip",
-           "api_adapters.hip", "adapters.hip"]
+           "api_adapters.hip", "adapters.hip", "adapters_back.hip"]
 HEADERS = ["adapters.h", "device_common.h", "elements.h", "kernels.h", "norm_common.h", "nvfp4_gemm_common.h",
            "operand_checks.h"]
 

@@ -52,14 +52,19 @@ struct Tile {
   int group, first, count;
 };
 
-__device__ __forceinline__ Tile tile_of(const AdapterTokens& t, int i) {
+// As read, without waiting for it: made uniform where it is used.
+__device__ __forceinline__ Tile load_tile(const AdapterTokens& t, int i) {
   if (t.plan) {
     const int* p = t.plan + t.tiles_at + 4 * (int64_t)i;
-    return {__builtin_amdgcn_readfirstlane(p[0]), __builtin_amdgcn_readfirstlane(p[1]),
-            __builtin_amdgcn_readfirstlane(p[2])};
+    return {p[0], p[1], p[2]};
   }
   const int64_t first = (int64_t)i * kAdapterTile, left = t.tokens - first;
   return {0, (int)first, (int)(left < kAdapterTile ? left : kAdapterTile)};
+}
+
+__device__ __forceinline__ Tile uniform(Tile t) {
+  return {__builtin_amdgcn_readfirstlane(t.group), __builtin_amdgcn_readfirstlane(t.first),
+          __builtin_amdgcn_readfirstlane(t.count)};
 }
 
 // The token at place `at` of the order.

@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kWaves * kWave) void add_adapters_kernel(AdapterArg
   const int64_t index = (int64_t)(at / p.splits) * kXcds + id % kXcds;
   const int split = at % p.splits;
   if (index >= p.t.max_tiles) return;
-  const Tile tile = tile_of(p.t, (int)index);
+  const Tile tile = uniform(load_tile(p.t, (int)index));
   if (tile.count == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int m = lane % 16, g = lane / 16;

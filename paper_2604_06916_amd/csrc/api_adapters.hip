@@ -89,4 +89,58 @@ int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const uint16_t* x, 
   return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
 }
 
+size_t solfp4_adapters_backward_workspace_bytes(int64_t tokens, int64_t adapters, int planned, int64_t N, int64_t K,
+                                                int64_t rank) {
+  if (adapter_dims(tokens, adapters) || N < 0 || K < 0 || rank < 1 || N >= solfp4::kAdapterMaxFeatures ||
+      K >= solfp4::kAdapterMaxFeatures || rank > solfp4::kAdapterMaxRank)
+    return 0;
+  // without a plan tiles start at every 32nd token, with one every adapter starts a tile
+  const int any = 0;
+  return solfp4::adapters_backward_bytes(solfp4::adapter_tokens(planned ? &any : nullptr, tokens, adapters), N, K, rank);
+}
+
+int solfp4_adapters_backward(const uint16_t* dy, int64_t dy_stride, const uint16_t* x, int64_t x_stride,
+                             const float* hidden, const uint16_t* a, const uint16_t* b, const float* scales,
+                             int64_t adapters, const void* plan, const uint16_t* past, int64_t past_stride,
+                             uint16_t* dx, int64_t dx_stride, float* da, float* db, void* workspace,
+                             size_t workspace_bytes, int64_t tokens, int64_t N, int64_t K, int64_t rank, void* stream) {
+  const Weights w = {a, b, scales, plan, adapters, tokens, N, K, rank};
+  int rc = w.check();
+  if (rc) return rc;
+  if ((K > 0 && !da) || (N > 0 && !db) || (tokens > 0 && !hidden)) return SOLFP4_EINVAL;
+  if (((uintptr_t)da & 3u) || ((uintptr_t)db & 3u) || ((uintptr_t)hidden & 3u)) return SOLFP4_EALIGN;
+  if (tokens > 0) {
+    if (N > 0 && (rc = check_rows(SOLFP4_BF16, dy, dy_stride, tokens, N, false))) return rc;
+    if (K > 0) {
+      if ((rc = check_rows(SOLFP4_BF16, x, x_stride, tokens, K, false))) return rc;
+      if (past && (rc = check_rows(SOLFP4_BF16, past, past_stride, tokens, K, false))) return rc;
+      if ((rc = check_rows(SOLFP4_BF16, dx, dx_stride, tokens, K, true))) return rc;
+    }
+  }
+  const solfp4::AdapterTokens t = solfp4::adapter_tokens(plan, tokens, adapters);
+  const size_t need = solfp4::adapters_backward_bytes(t, N, K, rank);
+  if (need && !workspace) return SOLFP4_EWORKSPACE;
+  if (!aligned16(workspace)) return SOLFP4_EALIGN;
+  if (workspace_bytes < need) return SOLFP4_EWORKSPACE;
+  const bool n = tokens > 0 && N > 0, k = tokens > 0 && K > 0;
+  const Region in[4] = {rows_region(SOLFP4_BF16, n ? dy : nullptr, dy_stride, tokens, N),
+                        rows_region(SOLFP4_BF16, k ? x : nullptr, x_stride, tokens, K),
+                        block_of(hidden, tokens > 0 ? tokens * rank * 4 : 0),
+                        rows_region(SOLFP4_BF16, k ? past : nullptr, past_stride, tokens, K)};
+  const Region out[4] = {rows_region(SOLFP4_BF16, k ? dx : nullptr, dx_stride, tokens, K),
+                         block_of(da, K > 0 ? adapters * rank * K * 4 : 0),
+                         block_of(db, N > 0 ? adapters * N * rank * 4 : 0), block_of(workspace, (int64_t)need)};
+  for (int o = 0; o < 4; ++o) {
+    for (int i = 0; i < 4; ++i)   // dx in the place of past alone
+      if (!(o == 0 && i == 3 ? same_or_apart(in[i], out[o]) : apart(in[i], out[o]))) return SOLFP4_EINVAL;
+    for (int i = 0; i < o; ++i)
+      if (!apart(out[i], out[o])) return SOLFP4_EINVAL;
+    if (!w.apart_from(out[o])) return SOLFP4_EINVAL;
+  }
+  const solfp4::AdapterBackArgs args = {t, dy, dy_stride, x, x_stride, hidden, a, b, scales, past, past_stride, dx,
+                                        dx_stride, da, db, (int)N, (int)K, (int)rank};
+  const hipError_t e = solfp4::launch_adapters_backward(args, workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
+}
+
 }  // extern "C"

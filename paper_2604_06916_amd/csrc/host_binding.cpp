@@ -734,6 +734,33 @@ PyObject* add_adapters_(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (dy, x, hidden, a, b, scales, plan, plan_tokens, plan_adapters, past, dx, da, db, workspace) -> (dx, da, db)
+PyObject* adapters_backward_(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 14, [&]() -> PyObject* {
+    const Adapters o(a[0], a[1], a[3], a[4], a[5], a[6], a[7], a[8]);
+    const Tensor& hidden = tensor(a[2]);
+    need_tensor(hidden, at::kFloat, {o.tokens, o.rank}, &o.dev);
+    Strided past(a[9], o.x, {o.tokens, o.K}), dx(a[10], o.x, {o.tokens, o.K});
+    Operand da(a[11], at::kFloat, o.a.sizes(), o.dev), db(a[12], at::kFloat, o.b.sizes(), o.dev);
+    const size_t bytes =
+        solfp4_adapters_backward_workspace_bytes(o.tokens, o.adapters, o.plan.defined(), o.N, o.K, o.rank);
+    Tensor ws = workspace_arg(a[13], bytes, o.dev);
+    void* stream = stream_of(o.dev);
+    dx.allocate(o.x, {o.tokens, o.K});
+    da.allocate(at::kFloat, o.a.sizes(), o.dev);
+    db.allocate(at::kFloat, o.b.sizes(), o.dev);
+    if (!ws.defined()) ws = make({(int64_t)std::max<size_t>(bytes, 256)}, at::kByte, o.dev);
+    const int rc = call([&] {
+      return solfp4_adapters_backward(u16(o.t), o.t.stride(0), u16(o.x), o.x.stride(0), f32(hidden), u16(o.a), u16(o.b),
+                                      f32(o.scales), o.adapters, ptr(o.plan), u16(past.t), past.stride(0), u16(dx.t),
+                                      dx.stride(0), f32(da.t), f32(db.t), ptr(ws), (size_t)ws.numel(), o.tokens, o.N,
+                                      o.K, o.rank, stream);
+    });
+    if (rc) return failed(rc);
+    return Py_BuildValue("(NNN)", dx.object(), da.object(), db.object());
+  });
+}
+
 PyMethodDef methods[] = {
     {"nvfp4_quantize", (PyCFunction)(void*)nvfp4_quantize_, METH_FASTCALL, nullptr},
     {"mxfp4_quantize", (PyCFunction)(void*)mxfp4_quantize_, METH_FASTCALL, nullptr},
@@ -753,6 +780,7 @@ PyMethodDef methods[] = {
     {"nvfp4_weight_linear", (PyCFunction)(void*)nvfp4_weight_linear_, METH_FASTCALL, nullptr},
     {"mxfp4_weight_linear", (PyCFunction)(void*)mxfp4_weight_linear_, METH_FASTCALL, nullptr},
     {"mxfp8_linear", (PyCFunction)(void*)mxfp8_linear_, METH_FASTCALL, nullptr},
+    {"adapters_backward", (PyCFunction)(void*)adapters_backward_, METH_FASTCALL, nullptr},
     {"add_adapters", (PyCFunction)(void*)add_adapters_, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -349,4 +349,24 @@ struct AdapterArgs {
 };
 hipError_t launch_add_adapters(const AdapterArgs& a, hipStream_t stream);
 
+struct AdapterBackArgs {
+  AdapterTokens t;
+  const uint16_t* dy;
+  int64_t dy_stride;
+  const uint16_t* x;
+  int64_t x_stride;
+  const float* hidden;
+  const uint16_t *a, *b;
+  const float* scales;
+  const uint16_t* past;   // NULL: 0
+  int64_t past_stride;
+  uint16_t* dx;
+  int64_t dx_stride;
+  float *da, *db;
+  int N, K, rank;
+};
+// Device workspace, in bytes.
+size_t adapters_backward_bytes(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank);
+hipError_t launch_adapters_backward(const AdapterBackArgs& a, void* workspace, hipStream_t stream);
+
 }  // namespace solfp4
