@@ -11,9 +11,10 @@
 // them together) and a range of N: its waves share K, add their shares of h in
 // LDS in wave order, and share the columns.  Tokens are the columns of the
 // matrix instructions; the rows, r in the first product and n in the second,
-// are dealt so that a lane's results are consecutive: row 4 g + i of block j is
-// r = 8 g + 4 j + i (so h is the second product's operand as it stands) and
-// n = 16 g + 4 j + i (so a lane reads and writes 32 bytes of a token's row).
+// are dealt so that a lane's results are consecutive: row 4 g + i of blocks 2 u
+// and 2 u + 1 is element 32 u + 8 g + i and four further on.  So h is the second
+// product's operand as it stands, and a wave reads and writes 64 bytes of each
+// token's row an instruction.
 //
 // Bound by memory: x once, y once in and once out; a and b come from L2, as
 // often as there are tiles.
@@ -174,6 +175,7 @@ constexpr int kStepK = 64, kStepN = 64;   // of a wave's step
 template <int kChunks, int kWaves, bool kWholeRank>
 __global__ __launch_bounds__(kWaves * kWave) void add_adapters_kernel(AdapterArgs p) {
   constexpr int kBlocks = 2 * kChunks;   // 16s of the rank
+  constexpr bool kAhead = kChunks < 4;   // the next step's loads go out before this one's products
   __shared__ floatx4_t share[kWaves][2 * kBlocks][kWave];
   // the column ranges of a tile run on one XCD, where its rows are then in L2
   const int id = blockIdx.x, at = id / kXcds;
@@ -204,33 +206,37 @@ __global__ __launch_bounds__(kWaves * kWave) void add_adapters_kernel(AdapterArg
 #pragma unroll
     for (int r = 0; r < kBlocks; ++r)   // rows past the rank: any, their results are set to 0
       ar[r] = a + (int64_t)min(r / 2 * 32 + m / 4 * 8 + r % 2 * 4 + m % 4, p.rank - 1) * p.K;
-    for (int k0 = wave * kStepK; k0 < p.K; k0 += kWaves * kStepK) {
-      bf16x8_t xv[2][2], av[kBlocks][2];
+    struct Step {
+      bf16x8_t x[2][2], a[kBlocks][2];
+    };
+    const auto load = [&](int k0, Step& v) {
       const int k = k0 + 8 * g;
-      if (k0 + kStepK <= p.K) {
+      const bool whole = k0 + kStepK <= p.K;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          xv[0][s] = operand8(xr[0] + k + 32 * s);
-          if (two) xv[1][s] = operand8(xr[1] + k + 32 * s);
+      for (int s = 0; s < 2; ++s) {
+        const int at = k + 32 * s, n = p.K - at;
 #pragma unroll
-          for (int r = 0; r < kBlocks; ++r) av[r][s] = operand8(ar[r] + k + 32 * s);
-        }
-      } else {
+        for (int j = 0; j < 2; ++j)
+          if (j == 0 || two) v.x[j][s] = whole ? operand8(xr[j] + at) : operand8(xr[j], at, n);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          xv[0][s] = operand8(xr[0], k + 32 * s, p.K - (k + 32 * s));
-          if (two) xv[1][s] = operand8(xr[1], k + 32 * s, p.K - (k + 32 * s));
-#pragma unroll
-          for (int r = 0; r < kBlocks; ++r) av[r][s] = operand8(ar[r], k + 32 * s, p.K - (k + 32 * s));
-        }
+        for (int r = 0; r < kBlocks; ++r) v.a[r][s] = whole ? operand8(ar[r] + at) : operand8(ar[r], at, n);
       }
+    };
+    Step now, next;
+    int k0 = wave * kStepK;
+    if (k0 < p.K) load(k0, now);
+    for (; k0 < p.K; k0 += kWaves * kStepK) {
+      const int k1 = k0 + kWaves * kStepK;
+      if (kAhead && k1 < p.K) load(k1, next);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int r = 0; r < kBlocks; ++r) {
-          acc[0][r] = mfma(av[r][s], xv[0][s], acc[0][r]);
-          if (two) acc[1][r] = mfma(av[r][s], xv[1][s], acc[1][r]);
+          acc[0][r] = mfma(now.a[r][s], now.x[0][s], acc[0][r]);
+          if (two) acc[1][r] = mfma(now.a[r][s], now.x[1][s], acc[1][r]);
         }
+      if (!kAhead && k1 < p.K) load(k1, now);
+      if (kAhead) now = next;
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -269,61 +275,77 @@ __global__ __launch_bounds__(kWaves * kWave) void add_adapters_kernel(AdapterArg
   const float scale = !real ? 0.0f : p.scales ? p.scales[tile.group] : 1.0f;
   const uint16_t* b = p.b + (real ? (int64_t)tile.group * p.N * p.rank : 0);
   const int end = min(p.N, (split + 1) * p.split_cols);
-  for (int n0 = split * p.split_cols + wave * kStepN; n0 < end; n0 += kWaves * kStepN) {
-    const int col = n0 + 16 * g;
+  struct Step {
     Run<SOLFP4_BF16> y[2][2];
+    bf16x8_t b[4][kChunks];
+  };
+  const auto load = [&](int n0, Step& v) {
+    const bool whole = n0 + kStepN <= p.N;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if (j == 1 && !two) continue;
-      const uint8_t* yr = reinterpret_cast<const uint8_t*>(p.y + token[j] * p.y_stride);
+      const uint16_t* yr = p.y + token[j] * p.y_stride;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        y[j][u] = zero_run<SOLFP4_BF16>();
-        if (end - (col + 8 * u) > 0) y[j][u] = load_run<SOLFP4_BF16>(yr, col + 8 * u, end - (col + 8 * u));
+        const int col = n0 + 32 * u + 8 * g;
+        v.y[j][u].p[0] = __builtin_bit_cast(u32x4_t, whole ? operand8(yr + col) : operand8(yr, col, p.N - col));
       }
     }
+    if (!real) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int n = min(n0 + q / 2 * 32 + m / 4 * 8 + q % 2 * 4 + m % 4, p.N - 1);   // past the last column: any, not stored
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        // past the rank: any of the row, times an h of 0
+        const int r0 = 32 * c + 8 * g;
+        if constexpr (kWholeRank) v.b[q][c] = operand8(b + (int64_t)n * p.rank + min(r0, p.rank - 8));
+        else v.b[q][c] = operand8(b + (int64_t)n * p.rank, r0, p.rank - r0);
+      }
+    }
+  };
+  Step now, next;
+  int n0 = split * p.split_cols + wave * kStepN;
+  if (n0 < end) load(n0, now);
+  for (; n0 < end; n0 += kWaves * kStepN) {
+    const int n1 = n0 + kWaves * kStepN;
+    if (kAhead && n1 < end) load(n1, next);
     floatx4_t acc[2][4];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) acc[j][q] = floatx4_t{0, 0, 0, 0};
-    if (real) {
+    if (real)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int n = min(n0 + m / 4 * 16 + q * 4 + m % 4, p.N - 1);   // past the last column: any, not stored
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-          const int r0 = 32 * c + 8 * g;
-          bf16x8_t bv;
-          if constexpr (kWholeRank)
-            bv = r0 < p.rank ? operand8(b + (int64_t)n * p.rank + r0) : __builtin_bit_cast(bf16x8_t, u32x4_t{0, 0, 0, 0});
-          else
-            bv = operand8(b + (int64_t)n * p.rank, r0, p.rank - r0);
+        for (int c = 0; c < kChunks; ++c)
 #pragma unroll
           for (int s = 1; s >= 0; --s) {
-            acc[0][q] = mfma(bv, h[0][c][s], acc[0][q]);
-            if (two) acc[1][q] = mfma(bv, h[1][c][s], acc[1][q]);
+            acc[0][q] = mfma(now.b[q][c], h[0][c][s], acc[0][q]);
+            if (two) acc[1][q] = mfma(now.b[q][c], h[1][c][s], acc[1][q]);
           }
-        }
-      }
-    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if (m + 16 * j >= tile.count) continue;
       uint8_t* o = reinterpret_cast<uint8_t*>(p.out + token[j] * p.out_stride);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        if (end - (col + 8 * u) <= 0) continue;
+        const int col = n0 + 32 * u + 8 * g;
         float v[8];
-        to_f32<SOLFP4_BF16>(y[j][u], v);
+        to_f32<SOLFP4_BF16>(now.y[j][u], v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           v[e] = real ? __builtin_fmaf(scale, acc[j][2 * u + e / 4][e % 4], v[e]) : v[e];
           if (tile.group > p.t.adapters) v[e] = __builtin_nanf("");
         }
-        store_run<SOLFP4_BF16>(o, col + 8 * u, end - (col + 8 * u), from_f32<SOLFP4_BF16>(v));
+        const Run<SOLFP4_BF16> r = from_f32<SOLFP4_BF16>(v);
+        if (n0 + kStepN <= p.N) store_run<SOLFP4_BF16>(o, col, 8, r);
+        else if (col < p.N) store_run<SOLFP4_BF16>(o, col, p.N - col, r);
       }
     }
+    if (!kAhead && n1 < end) load(n1, now);
+    if (kAhead) now = next;
   }
 }
 
@@ -346,8 +368,12 @@ static hipError_t launch_rank(AdapterArgs a, hipStream_t stream) {
   a.split_cols = (int)(each * kStepN);
   a.splits = (int)((steps + each - 1) / each);
   const dim3 grid((unsigned)((tiles + kXcds - 1) / kXcds * kXcds * a.splits));
+#ifndef FW
+#define FW 4
+#endif
   if constexpr (kChunks < 4)   // more shares than LDS holds twice
     if (tiles < 3 * cus) return launch_forward<kChunks, 8>(a, grid, stream);
+  if constexpr (kChunks == 1) return launch_forward<kChunks, FW>(a, grid, stream);
   return launch_forward<kChunks, 4>(a, grid, stream);
 }
 
