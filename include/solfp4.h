@@ -561,6 +561,11 @@ SOLFP4_API size_t solfp4_adapter_plan_bytes(int64_t tokens, int64_t adapters);
 SOLFP4_API int solfp4_adapter_plan(const void* index, int index_bytes, int64_t tokens, int64_t adapters,
                    void* plan, size_t plan_bytes, void* stream);
 
+/* Device workspace of solfp4_add_adapters (planned: nonzero with a plan).  Host
+ * only; 0 where none is needed, and for invalid sizes. */
+SOLFP4_API size_t solfp4_add_adapters_workspace_bytes(int64_t tokens, int64_t adapters, int planned,
+                   int64_t N, int64_t K, int64_t rank);
+
 /*
  *   y       [tokens][N] BF16, rows y_stride apart
  *   x       [tokens][K] BF16, rows x_stride apart: the linear's input
@@ -572,6 +577,8 @@ SOLFP4_API int solfp4_adapter_plan(const void* index, int index_bytes, int64_t t
  *   out     [tokens][N] BF16, rows out_stride apart, written; may be y
  *   hidden  [tokens][rank] FP32, written with h (0 for tokens without an
  *           adapter), what the backward pass needs; or NULL
+ *   workspace  at least solfp4_add_adapters_workspace_bytes bytes, 16-byte
+ *           aligned (NULL where that is 0)
  *
  * rank from 1 to 128 (adapters of fewer ranks: pad with zeros), N and K below
  * 2^22.  Sums are FP32; h enters the second product with 16 bits and out is
@@ -581,7 +588,8 @@ SOLFP4_API int solfp4_adapter_plan(const void* index, int index_bytes, int64_t t
 SOLFP4_API int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const uint16_t* x,
                    int64_t x_stride, const uint16_t* a, const uint16_t* b, const float* scales,
                    int64_t adapters, const void* plan, uint16_t* out, int64_t out_stride,
-                   float* hidden, int64_t tokens, int64_t N, int64_t K, int64_t rank, void* stream);
+                   float* hidden, void* workspace, size_t workspace_bytes, int64_t tokens, int64_t N,
+                   int64_t K, int64_t rank, void* stream);
 
 /* Device workspace of solfp4_adapters_backward (planned: nonzero with a plan).
  * Host only; 0 for invalid sizes. */

@@ -16,7 +16,7 @@ _NAMES = ("EXPORTED", "LIB_PATH", "Solfp4Error", "lib", "gemm_plan", "FORMAT_NVF
           "mxfp4_add_layernorm", "layernorm_backward", "layernorm_backward_workspace_bytes", "rotary", "rotary_frequencies", "rotary_table",
           "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear",
           "AdapterPlan", "adapter_plan", "adapter_plan_bytes", "add_adapters",
-          "adapters_backward", "adapters_backward_workspace_bytes")
+          "add_adapters_workspace_bytes", "adapters_backward", "adapters_backward_workspace_bytes")
 __all__ = list(_NAMES)
 
 

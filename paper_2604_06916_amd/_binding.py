@@ -105,7 +105,10 @@ lib.solfp4_adapter_plan_bytes.argtypes = [_i64, _i64]
 lib.solfp4_adapter_plan.restype = _int
 lib.solfp4_adapter_plan.argtypes = [_p, _int, _i64, _i64, _p, _sz, _p]
 lib.solfp4_add_adapters.restype = _int
-lib.solfp4_add_adapters.argtypes = [_p, _i64, _p, _i64, _p, _p, _p, _i64, _p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p]
+lib.solfp4_add_adapters.argtypes = [_p, _i64, _p, _i64, _p, _p, _p, _i64, _p, _p, _i64, _p, _p, _sz, _i64, _i64, _i64,
+                                    _i64, _p]
+lib.solfp4_add_adapters_workspace_bytes.restype = _sz
+lib.solfp4_add_adapters_workspace_bytes.argtypes = [_i64, _i64, _int, _i64, _i64, _i64]
 lib.solfp4_adapters_backward_workspace_bytes.restype = _sz
 lib.solfp4_adapters_backward_workspace_bytes.argtypes = [_i64, _i64, _int, _i64, _i64, _i64]
 lib.solfp4_adapters_backward.restype = _int
@@ -130,6 +133,7 @@ EXPORTED = ["solfp4_strerror", "solfp4_version", "solfp4_gemm_plan",
             "solfp4_layernorm_backward_workspace_bytes", "solfp4_layernorm_backward",
             "solfp4_rotary_table", "solfp4_rotary",
             "solfp4_adapter_plan_bytes", "solfp4_adapter_plan", "solfp4_add_adapters",
+            "solfp4_add_adapters_workspace_bytes",
             "solfp4_adapters_backward_workspace_bytes", "solfp4_adapters_backward",
             "nvfp4_weight_linear", "mxfp4_weight_linear", "mxfp8_linear"]
 
@@ -1081,7 +1085,11 @@ def _adapter_operands(t, x, a, b, scales, plan, name):
     return tokens, N, K, rank, adapters, dev
 
 
-def add_adapters(y, x, a, b, scales=None, plan=None, hidden=False, out=None, stream=None):
+def add_adapters_workspace_bytes(tokens: int, adapters: int, planned: bool, N: int, K: int, rank: int) -> int:
+    return lib.solfp4_add_adapters_workspace_bytes(tokens, adapters, int(planned), N, K, rank)
+
+
+def add_adapters(y, x, a, b, scales=None, plan=None, hidden=False, out=None, workspace=None, stream=None):
     """Low-rank adapters beside a linear: y [tokens, N], the linear's output, plus
     scales[e] b[e] (a[e] x[t]) for every token t of adapter e -> (out, hidden).
 
@@ -1094,9 +1102,10 @@ def add_adapters(y, x, a, b, scales=None, plan=None, hidden=False, out=None, str
     keep = None if hidden is False or hidden is None else hidden
     if stream is None:
         if plan is None:
-            r = _host.add_adapters(y, x, a, b, scales, None, 0, 0, keep, out)
+            r = _host.add_adapters(y, x, a, b, scales, None, 0, 0, keep, out, workspace)
         elif type(plan) is AdapterPlan:
-            r = _host.add_adapters(y, x, a, b, scales, plan.buffer, plan.tokens, plan.adapters, keep, out)
+            r = _host.add_adapters(y, x, a, b, scales, plan.buffer, plan.tokens, plan.adapters, keep, out,
+                                   workspace)
         else:
             r = None
         if r is not None:
@@ -1106,14 +1115,20 @@ def add_adapters(y, x, a, b, scales=None, plan=None, hidden=False, out=None, str
         _need_strided(out, torch.bfloat16, (tokens, N), "out", dev)
     if keep is not None and keep is not True:
         _need(keep, torch.float32, (tokens, rank), "hidden", dev)
+    need = add_adapters_workspace_bytes(tokens, adapters, plan is not None, N, K, rank)
+    if workspace is not None:
+        _need_workspace(workspace, need, "workspace", dev)
     st = _stream(stream, dev)
     if out is None:
         out = _alloc((tokens, N), torch.bfloat16, dev, st)
     if keep is True:
         keep = _alloc((tokens, rank), torch.float32, dev, st)
+    if workspace is None and need:
+        workspace = _alloc((need,), torch.uint8, dev, st)
     _check(lib.solfp4_add_adapters(*_rows_of(y), *_rows_of(x), _ptr(a), _ptr(b), _ptr(scales), adapters,
-                                   _ptr(None if plan is None else plan.buffer), *_rows_of(out), _ptr(keep), tokens, N, K,
-                                   rank, ctypes.c_void_p(st.cuda_stream)))
+                                   _ptr(None if plan is None else plan.buffer), *_rows_of(out), _ptr(keep),
+                                   _ptr(workspace), 0 if workspace is None else workspace.numel(), tokens, N, K, rank,
+                                   ctypes.c_void_p(st.cuda_stream)))
     return out, keep
 
 

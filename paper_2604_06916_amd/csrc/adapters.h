@@ -8,15 +8,74 @@ namespace solfp4 {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-// 8 consecutive BF16 values of `row` from element `at`, of which n exist (zeros after them).
-__device__ __forceinline__ bf16x8_t operand8(const uint16_t* row, uint32_t at, int n) {
-  if (n <= 0) return __builtin_bit_cast(bf16x8_t, u32x4_t{0, 0, 0, 0});
-  return __builtin_bit_cast(bf16x8_t, load_run<SOLFP4_BF16>(reinterpret_cast<const uint8_t*>(row), at, n).p[0]);
+// 8 consecutive BF16 values of `row` from element `at`; zeros from element `end`
+// (uniform), the row's end, on.  One load without a branch: near the end of the
+// row's last 8 values, moved down (element by element, each with a branch and a
+// wait, 1371 x 1235 x 1111 took 25 us).
+__device__ __forceinline__ bf16x8_t operand8(const uint16_t* row, uint32_t at, uint32_t end) {
+  u32x4_t v = {0, 0, 0, 0};
+  if (end < 8) {
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (at + e < end) v[e / 2] |= (uint32_t)row[at + e] << (16 * (e & 1));
+    return __builtin_bit_cast(bf16x8_t, v);
+  }
+  const uint32_t from = min(at, end - 8), by = at - from;
+  v = *reinterpret_cast<const u32x4_at2*>(row + from);
+  if (by & 4) v = u32x4_t{v.z, v.w, 0, 0};
+  if (by & 2) v = u32x4_t{v.y, v.z, v.w, 0};
+  if (by & 1)
+    v = u32x4_t{__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16),
+                __builtin_amdgcn_alignbit(v.w, v.z, 16), v.w >> 16};
+  if (by >= 8) v = u32x4_t{0, 0, 0, 0};
+  return __builtin_bit_cast(bf16x8_t, v);
 }
 
 // The same where all 8 exist.
 __device__ __forceinline__ bf16x8_t operand8(const uint16_t* at) {
   return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_at2*>(at));
+}
+
+// A lane's kCols (8 or 4) consecutive columns of a row.
+template <int kCols>
+struct LaneRun {
+  typedef uint32_t words_t __attribute__((ext_vector_type(kCols / 2)));
+  typedef words_t words_at2_t __attribute__((aligned(2)));
+  words_t w;
+  // Columns col and up, where all of them exist, or zeros from column `end` on.
+  __device__ __forceinline__ void load(const uint16_t* row, uint32_t col, uint32_t end, bool whole) {
+    if (whole) {
+      w = *reinterpret_cast<const words_at2_t*>(row + col);
+    } else {
+      const u32x4_t v = __builtin_bit_cast(u32x4_t, operand8(row, col, end));
+#pragma unroll
+      for (int i = 0; i < kCols / 2; ++i) w[i] = v[i];
+    }
+  }
+  __device__ __forceinline__ float value(int e) const {
+    return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+  }
+  __device__ __forceinline__ void set(const float (&v)[kCols]) {
+#pragma unroll
+    for (int e = 0; e < kCols; e += 2) w[e / 2] = pack_bf16(v[e], v[e + 1]);
+  }
+  __device__ __forceinline__ void store(uint16_t* row, uint32_t col, uint32_t end, bool whole) const {
+    if (whole) {
+      *reinterpret_cast<words_at2_t*>(row + col) = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < kCols; ++e)
+        if (col + e < end) row[col + e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+    }
+  }
+};
+
+// Between one wave's LDS writes by some lanes and reads by others: the hardware
+// keeps a wave's LDS instructions in order, the compiler is told to.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
 // FP32 values as a sum of BF16 pieces, each the rest rounded to nearest: two

@@ -9,15 +9,17 @@
 //
 // A workgroup takes a tile of up to 32 tokens of one adapter (the plan brings
 // them together) and a range of N: its waves share K, add their shares of h in
-// LDS in wave order, and share the columns.  Tokens are the columns of the
-// matrix instructions; the rows, r in the first product and n in the second,
-// are dealt so that a lane's results are consecutive: row 4 g + i of blocks 2 u
-// and 2 u + 1 is element 32 u + 8 g + i and four further on.  So h is the second
-// product's operand as it stands, and a wave reads and writes 64 bytes of each
-// token's row an instruction.
+// LDS in wave order, and share the columns.
 //
 // Bound by memory: x once, y once in and once out; a and b come from L2, as
-// often as there are tiles.
+// often as there are tiles.  So every access to a token's row covers whole
+// lines: 16 lanes read 256 bytes of it (with 64 bytes a row an instruction, as a
+// matrix operand lies, a copy of 26574 x 7296 takes 210 us, with 128 or more
+// 165).  x goes through LDS into operand order.  In the second product tokens
+// are the result's rows and a lane holds 8 consecutive columns of four of them:
+// column m of block q is n = 8 m + q.  In the first, tokens are the columns, and
+// row 4 g + i of blocks 2 c and 2 c + 1 is rank element 32 c + 8 g + i and four
+// further on, so h is the second product's operand as it stands.
 #include "adapters.h"
 
 namespace solfp4 {
@@ -169,88 +171,129 @@ hipError_t launch_adapter_plan(const void* index, int index_bytes, int64_t token
 
 // ---- forward --------------------------------------------------------------
 
-constexpr int kStepK = 64, kStepN = 64;   // of a wave's step
+constexpr int kStepK = 128;   // of a wave's step
 
-// kChunks: 32s of the rank; kWholeRank: the rank is a multiple of 8.
-template <int kChunks, int kWaves, bool kWholeRank>
-__global__ __launch_bounds__(kWaves * kWave) void add_adapters_kernel(AdapterArgs p) {
+// kChunks: 32s of the rank; kLane: columns of a lane a step (8, or 4 where b
+// takes too many registers or there are few tiles: b then comes a step ahead);
+// kWholeRank: the rank is a multiple of 8.  kPart: both products, or h's shares
+// of a range of K alone, or the second product from such shares.
+enum { kBoth, kShares, kFromShares };
+template <int kChunks, int kLane, int kWaves, bool kWholeRank, int kPart>
+__global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(AdapterArgs p) {
   constexpr int kBlocks = 2 * kChunks;   // 16s of the rank
-  constexpr bool kAhead = kChunks < 4;   // the next step's loads go out before this one's products
-  __shared__ floatx4_t share[kWaves][2 * kBlocks][kWave];
-  // the column ranges of a tile run on one XCD, where its rows are then in L2
-  const int id = blockIdx.x, at = id / kXcds;
-  const int64_t index = (int64_t)(at / p.splits) * kXcds + id % kXcds;
-  const int split = at % p.splits;
+  constexpr int kStepN = 16 * kLane;
+  constexpr bool kAhead = kLane == 4 && kChunks < 4;
+  constexpr int kRow = kStepK * 2 + 16;  // a row of x in LDS: 16 rows at one column lie in all banks
+  constexpr int kAStep = 4 / kChunks;    // 32s of K whose rows of a are held at once
+  constexpr int kPlaces = 2 * kBlocks * kWave;   // of four values of h
+  constexpr int kXBytes = kPart == kFromShares ? 0 : kWaves * kAdapterTile * kRow;
+  constexpr int kShareBytes = (kPart == kFromShares ? 1 : kWaves) * kPlaces * 16;
+  // the waves' tiles of x, then their shares of h
+  __shared__ __attribute__((aligned(16))) uint8_t room[kXBytes > kShareBytes ? kXBytes : kShareBytes];
+  floatx4_t(*const share)[2 * kBlocks][kWave] = reinterpret_cast<floatx4_t(*)[2 * kBlocks][kWave]>(room);
+  // with 8 tiles or more a tile's ranges run on one XCD, whose L2 then has its rows
+  const int ranges = kPart == kShares ? p.k_splits : p.splits, at = blockIdx.x / p.xcds;
+  const int index = at / ranges * p.xcds + blockIdx.x % p.xcds, split = at % ranges;
   if (index >= p.t.max_tiles) return;
-  const Tile tile = uniform(load_tile(p.t, (int)index));
+  const Tile tile = uniform(load_tile(p.t, index));
   if (tile.count == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int m = lane % 16, g = lane / 16;
   const bool two = tile.count > 16;          // tokens in both blocks of 16
   const bool real = tile.group < p.t.adapters;
-  int64_t token[2];
+  // a lane reads and writes rows g + 4 i of the tile; the last row again past its end
+  uint32_t token[8];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) token[j] = token_at(p.t, tile.first + min(m + 16 * j, tile.count - 1));
+  for (int i = 0; i < 8; ++i) token[i] = (uint32_t)token_at(p.t, tile.first + min(g + 4 * i, tile.count - 1));
+  // as an operand's row or column, m is row 4 (m % 4) + m / 4 of its block, so that results are of rows g + 4 i
+  const int row = m % 4 * 4 + m / 4;
 
   bf16x8_t h[2][kChunks][2];   // two pieces of h of this lane's tokens
-  if (real) {
+  if (kPart == kFromShares && real) {
+    const floatx4_t* from = static_cast<const floatx4_t*>(p.shares) + (int64_t)index * p.k_splits * kPlaces;
+    for (int i = threadIdx.x; i < (two ? kPlaces : kPlaces / 2); i += kWaves * kWave) {
+      floatx4_t v = from[i];
+      for (int k = 1; k < p.k_splits; ++k) v += from[k * kPlaces + i];
+      share[0][i / kWave][i % kWave] = v;
+    }
+  } else if (real) {
     floatx4_t acc[2][kBlocks];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int r = 0; r < kBlocks; ++r) acc[j][r] = floatx4_t{0, 0, 0, 0};
     const uint16_t* a = p.a + (int64_t)tile.group * p.rank * p.K;
-    const uint16_t *xr[2], *ar[kBlocks];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) xr[j] = p.x + token[j] * p.x_stride;
+    const uint16_t* ar[kBlocks];
 #pragma unroll
     for (int r = 0; r < kBlocks; ++r)   // rows past the rank: any, their results are set to 0
       ar[r] = a + (int64_t)min(r / 2 * 32 + m / 4 * 8 + r % 2 * 4 + m % 4, p.rank - 1) * p.K;
-    struct Step {
-      bf16x8_t x[2][2], a[kBlocks][2];
-    };
-    const auto load = [&](int k0, Step& v) {
-      const int k = k0 + 8 * g;
-      const bool whole = k0 + kStepK <= p.K;
+    uint8_t* const xs = room + wave * kAdapterTile * kRow;
+    bf16x8_t x[8];
+    const auto load = [&](int k0) {
+      const int k = k0 + 8 * m;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int at = k + 32 * s, n = p.K - at;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          if (j == 0 || two) v.x[j][s] = whole ? operand8(xr[j] + at) : operand8(xr[j], at, n);
-#pragma unroll
-        for (int r = 0; r < kBlocks; ++r) v.a[r][s] = whole ? operand8(ar[r] + at) : operand8(ar[r], at, n);
+      for (int i = 0; i < 8; ++i) {
+        if (4 * i >= tile.count) continue;
+        const uint16_t* xr = p.x + token[i] * p.x_stride;
+        x[i] = k0 + kStepK <= p.K ? operand8(xr + k) : operand8(xr, k, p.K);
       }
     };
-    Step now, next;
-    int k0 = wave * kStepK;
-    if (k0 < p.K) load(k0, now);
-    for (; k0 < p.K; k0 += kWaves * kStepK) {
+    const int first = kPart == kShares ? split * p.k_cols : 0, last = kPart == kShares ? min(p.K, first + p.k_cols) : p.K;
+    int k0 = first + wave * kStepK;
+    if (k0 < last) load(k0);
+    for (; k0 < last; k0 += kWaves * kStepK) {
       const int k1 = k0 + kWaves * kStepK;
-      if (kAhead && k1 < p.K) load(k1, next);
+      bf16x8_t av[kBlocks][kAStep];
+      const auto load_a = [&](int s0) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < kAStep; ++s)
 #pragma unroll
-        for (int r = 0; r < kBlocks; ++r) {
-          acc[0][r] = mfma(now.a[r][s], now.x[0][s], acc[0][r]);
-          if (two) acc[1][r] = mfma(now.a[r][s], now.x[1][s], acc[1][r]);
-        }
-      if (!kAhead && k1 < p.K) load(k1, now);
-      if (kAhead) now = next;
+          for (int r = 0; r < kBlocks; ++r) {
+            const int k = k0 + 32 * (s0 + s) + 8 * g;
+            av[r][s] = k0 + kStepK <= p.K ? operand8(ar[r] + k) : operand8(ar[r], k, p.K);
+          }
+      };
+      load_a(0);
+      wave_order();
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (4 * i < tile.count)
+          *reinterpret_cast<u32x4_t*>(xs + (g + 4 * i) * kRow + 16 * m) = __builtin_bit_cast(u32x4_t, x[i]);
+      if (k1 < last) load(k1);
+      wave_order();
+#pragma unroll
+      for (int s0 = 0; s0 < 4; s0 += kAStep) {
+        if (s0) load_a(s0);
+#pragma unroll
+        for (int s = 0; s < kAStep; ++s)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if (j && !two) continue;
+            const bf16x8_t xv = __builtin_bit_cast(
+                bf16x8_t, *reinterpret_cast<const u32x4_t*>(xs + (row + 16 * j) * kRow + 64 * (s0 + s) + 16 * g));
+#pragma unroll
+            for (int r = 0; r < kBlocks; ++r) acc[j][r] = mfma(av[r][s], xv, acc[j][r]);
+          }
+      }
     }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int r = 0; r < kBlocks; ++r) share[wave][j * kBlocks + r][lane] = acc[j][r];
     __syncthreads();
     // each thread adds some places' shares, in wave order, into the first
-    for (int i = threadIdx.x; i < 2 * kBlocks * kWave; i += kWaves * kWave) {
+    for (int i = threadIdx.x; i < kPlaces; i += kWaves * kWave) {
       floatx4_t* const s = &share[0][i / kWave][i % kWave];
       floatx4_t v = *s;
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) v += share[w][i / kWave][i % kWave];
-      *s = v;
+      if (kPart == kShares) static_cast<floatx4_t*>(p.shares)[((int64_t)index * p.k_splits + split) * kPlaces + i] = v;
+      else *s = v;
     }
+  }
+  if (kPart == kShares) return;
+  if (real) {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -261,9 +304,10 @@ __global__ __launch_bounds__(kWaves * kWave) void add_adapters_kernel(AdapterArg
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = r0 + e < p.rank ? (e < 4 ? lo[e % 4] : hi[e % 4]) : 0.0f;
-        if (p.hidden && split == 0 && wave == 0 && m + 16 * j < tile.count)
-          store_run<SOLFP4_F32>(reinterpret_cast<uint8_t*>(p.hidden + token[j] * p.rank), r0, p.rank - r0,
-                                from_f32<SOLFP4_F32>(v));
+        if (p.hidden && split == 0 && wave == 0 && row + 16 * j < tile.count && r0 < p.rank)
+          store_run<SOLFP4_F32>(
+              reinterpret_cast<uint8_t*>(p.hidden + token_at(p.t, tile.first + row + 16 * j) * p.rank), r0, p.rank - r0,
+              from_f32<SOLFP4_F32>(v));
         split_bf16(v, h[j][c]);
       }
   } else if (p.hidden && split == 0) {
@@ -275,109 +319,143 @@ __global__ __launch_bounds__(kWaves * kWave) void add_adapters_kernel(AdapterArg
   const float scale = !real ? 0.0f : p.scales ? p.scales[tile.group] : 1.0f;
   const uint16_t* b = p.b + (real ? (int64_t)tile.group * p.N * p.rank : 0);
   const int end = min(p.N, (split + 1) * p.split_cols);
-  struct Step {
-    Run<SOLFP4_BF16> y[2][2];
-    bf16x8_t b[4][kChunks];
-  };
-  const auto load = [&](int n0, Step& v) {
-    const bool whole = n0 + kStepN <= p.N;
+  LaneRun<kLane> y[8];
+  const auto load = [&](int n0) {
+    const int col = n0 + kLane * m;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (j == 1 && !two) continue;
-      const uint16_t* yr = p.y + token[j] * p.y_stride;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int col = n0 + 32 * u + 8 * g;
-        v.y[j][u].p[0] = __builtin_bit_cast(u32x4_t, whole ? operand8(yr + col) : operand8(yr, col, p.N - col));
-      }
+    for (int i = 0; i < 8; ++i) {
+      if (4 * i >= tile.count) continue;
+      const uint16_t* yr = p.y + token[i] * p.y_stride;
+      y[i].load(yr, col, p.N, n0 + kStepN <= p.N);
     }
+  };
+  bf16x8_t bv[kLane][kChunks];
+  const auto load_b = [&](int n0) {
     if (!real) return;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int n = min(n0 + q / 2 * 32 + m / 4 * 8 + q % 2 * 4 + m % 4, p.N - 1);   // past the last column: any, not stored
+    for (int q = 0; q < kLane; ++q) {
+      const int n = min(n0 + kLane * m + q, p.N - 1);   // past the last column: any, not stored
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
         // past the rank: any of the row, times an h of 0
         const int r0 = 32 * c + 8 * g;
-        if constexpr (kWholeRank) v.b[q][c] = operand8(b + (int64_t)n * p.rank + min(r0, p.rank - 8));
-        else v.b[q][c] = operand8(b + (int64_t)n * p.rank, r0, p.rank - r0);
+        if constexpr (kWholeRank) bv[q][c] = operand8(b + (int64_t)n * p.rank + min(r0, p.rank - 8));
+        else bv[q][c] = operand8(b + (int64_t)n * p.rank, r0, p.rank);
       }
     }
   };
-  Step now, next;
   int n0 = split * p.split_cols + wave * kStepN;
-  if (n0 < end) load(n0, now);
+  if (n0 < end) load(n0);
+  if (kAhead && n0 < end) load_b(n0);
   for (; n0 < end; n0 += kWaves * kStepN) {
-    const int n1 = n0 + kWaves * kStepN;
-    if (kAhead && n1 < end) load(n1, next);
-    floatx4_t acc[2][4];
+    const int n1 = n0 + kWaves * kStepN, col = n0 + kLane * m;
+    bf16x8_t now_b[kLane][kChunks];
+    if (!kAhead) load_b(n0);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int q = 0; q < kLane; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc[j][q] = floatx4_t{0, 0, 0, 0};
-    if (real)
+      for (int c = 0; c < kChunks; ++c) now_b[q][c] = bv[q][c];
+    if (kAhead && n1 < end) load_b(n1);
+    LaneRun<kLane> now[8];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+    for (int i = 0; i < 8; ++i) now[i] = y[i];
+    if (n1 < end) load(n1);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (j && !two) continue;
+      floatx4_t acc[kLane];
+#pragma unroll
+      for (int q = 0; q < kLane; ++q) acc[q] = floatx4_t{0, 0, 0, 0};
+      if (real)
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-          for (int s = 1; s >= 0; --s) {
-            acc[0][q] = mfma(now.b[q][c], h[0][c][s], acc[0][q]);
-            if (two) acc[1][q] = mfma(now.b[q][c], h[1][c][s], acc[1][q]);
-          }
+          for (int s = 1; s >= 0; --s)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (m + 16 * j >= tile.count) continue;
-      uint8_t* o = reinterpret_cast<uint8_t*>(p.out + token[j] * p.out_stride);
+            for (int q = 0; q < kLane; ++q) acc[q] = mfma(h[j][c][s], now_b[q][c], acc[q]);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int col = n0 + 32 * u + 8 * g;
-        float v[8];
-        to_f32<SOLFP4_BF16>(now.y[j][u], v);
+      for (int i = 0; i < 4; ++i) {
+        if (g + 4 * i + 16 * j >= tile.count) continue;
+        float v[kLane];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] = real ? __builtin_fmaf(scale, acc[j][2 * u + e / 4][e % 4], v[e]) : v[e];
-          if (tile.group > p.t.adapters) v[e] = __builtin_nanf("");
+        for (int q = 0; q < kLane; ++q) {
+          v[q] = now[4 * j + i].value(q);
+          if (real) v[q] = __builtin_fmaf(scale, acc[q][i], v[q]);
+          if (tile.group > p.t.adapters) v[q] = __builtin_nanf("");
         }
-        const Run<SOLFP4_BF16> r = from_f32<SOLFP4_BF16>(v);
-        if (n0 + kStepN <= p.N) store_run<SOLFP4_BF16>(o, col, 8, r);
-        else if (col < p.N) store_run<SOLFP4_BF16>(o, col, p.N - col, r);
+        now[4 * j + i].set(v);
+        now[4 * j + i].store(p.out + token[4 * j + i] * p.out_stride, col, p.N, n0 + kStepN <= p.N);
       }
     }
-    if (!kAhead && n1 < end) load(n1, now);
-    if (kAhead) now = next;
   }
 }
 
-template <int kChunks, int kWaves>
-static hipError_t launch_forward(const AdapterArgs& a, dim3 grid, hipStream_t stream) {
-  const dim3 block(kWaves * kWave);
-  if (a.rank % 8 == 0) return launch_kernel(add_adapters_kernel<kChunks, kWaves, true>, grid, block, stream, a);
-  return launch_kernel(add_adapters_kernel<kChunks, kWaves, false>, grid, block, stream, a);
+template <int kChunks, int kLane, int kWaves, int kPart>
+static hipError_t launch_part(const AdapterArgs& a, hipStream_t stream) {
+  const int64_t tiles = (a.t.max_tiles + a.xcds - 1) / a.xcds * a.xcds;
+  const dim3 grid((unsigned)(tiles * (kPart == kShares ? a.k_splits : a.splits))), block(kWaves * kWave);
+  if (a.rank % 8 == 0) return launch_kernel(add_adapters_kernel<kChunks, kLane, kWaves, true, kPart>, grid, block, stream, a);
+  return launch_kernel(add_adapters_kernel<kChunks, kLane, kWaves, false, kPart>, grid, block, stream, a);
 }
 
+// Ranges of at least one step that a tile's `size` is cut to, at most `want`; their width.
+static int cut(int64_t size, int64_t step, int64_t want, int* width) {
+  const int64_t steps = size > step ? (size + step - 1) / step : 1;
+  const int64_t ranges = want < 1 ? 1 : want < steps ? want : steps, each = (steps + ranges - 1) / ranges;
+  *width = (int)(each * step);
+  return (int)((steps + each - 1) / each);
+}
+
+// h in a launch of its own, its K shared by several workgroups, and the second
+// product in another: where a tile's ranges would each go through a large a
+// again (1 token 9728 -> 9728, rank 64: 39.5 us in one launch and 13.6 in two;
+// 2048 tokens 2240 -> 2240, rank 64 25.5 and 23.8; 64 tokens of 48 adapters 2432 -> 7296,
+// rank 32 12.7 and 12.9; 1 token 1152 -> 1152, rank 16 5.8 and 8.0).
+constexpr int64_t kTwoLaunches = (int64_t)1 << 18;   // elements of one adapter's a
+constexpr int kHWaves = 4, kOutWaves = 8;
+
+static bool two_launches(const AdapterTokens& t, int64_t K, int64_t rank) {
+  return t.max_tiles > 0 && t.max_tiles < device_cu_count() && rank * K >= kTwoLaunches;
+}
+static int h_ranges(const AdapterTokens& t, int64_t K, int* width) {
+  return cut(K, kStepK * kHWaves, 2 * device_cu_count() / t.max_tiles, width);
+}
+
+size_t add_adapters_bytes(const AdapterTokens& t, int64_t K, int64_t rank) {
+  if (!two_launches(t, K, rank)) return 0;
+  int width;
+  const int chunks = rank <= 32 ? 1 : rank <= 64 ? 2 : 4;
+  return (size_t)(t.max_tiles * h_ranges(t, K, &width)) * 4 * chunks * kWave * sizeof(floatx4_t);
+}
+
+// A workgroup a tile where there are more than 1.25 tiles a CU, else ranges of a
+// tile's columns, with more waves and shorter steps (8192 tokens 2240 -> 2240, 266
+// tiles, 30 us so and 37 the other way; 12000 tokens 2432 -> 7296, 377 tiles, 112
+// and 110).
 template <int kChunks>
 static hipError_t launch_rank(AdapterArgs a, hipStream_t stream) {
-  const int64_t tiles = a.t.max_tiles, steps = a.N > kStepN ? (a.N + kStepN - 1) / kStepN : 1;
-  const int64_t cus = device_cu_count();
-  // column ranges a tile, so that there is a workgroup a CU
-  int64_t splits = tiles < cus ? cus / tiles : 1;
-  splits = splits < steps ? splits : steps;
-  splits = splits < 1 ? 1 : splits;
-  const int64_t each = (steps + splits - 1) / splits;
-  a.split_cols = (int)(each * kStepN);
-  a.splits = (int)((steps + each - 1) / each);
-  const dim3 grid((unsigned)((tiles + kXcds - 1) / kXcds * kXcds * a.splits));
-#ifndef FW
-#define FW 4
-#endif
-  if constexpr (kChunks < 4)   // more shares than LDS holds twice
-    if (tiles < 3 * cus) return launch_forward<kChunks, 8>(a, grid, stream);
-  if constexpr (kChunks == 1) return launch_forward<kChunks, FW>(a, grid, stream);
-  return launch_forward<kChunks, 4>(a, grid, stream);
+  const int64_t tiles = a.t.max_tiles, cus = device_cu_count();
+  a.xcds = (int)(tiles < kXcds ? tiles : kXcds);
+  if (a.shares) {
+    a.k_splits = h_ranges(a.t, a.K, &a.k_cols);
+    a.splits = cut(a.N, 64, cus / tiles, &a.split_cols);
+    const hipError_t e = launch_part<kChunks, 4, kHWaves, kShares>(a, stream);
+    return e != hipSuccess ? e : launch_part<kChunks, 4, kOutWaves, kFromShares>(a, stream);
+  }
+  if constexpr (kChunks == 4) {   // LDS holds four waves' shares of h
+    a.splits = cut(a.N, 64, cus / tiles, &a.split_cols);
+    return launch_part<4, 4, 4, kBoth>(a, stream);
+  } else if (4 * tiles < 5 * cus) {
+    a.splits = cut(a.N, 64, cus / tiles, &a.split_cols);
+    return launch_part<kChunks, 4, 8, kBoth>(a, stream);
+  } else {
+    a.splits = cut(a.N, 128, 1, &a.split_cols);
+    return launch_part<kChunks, 8, 4, kBoth>(a, stream);
+  }
 }
 
-hipError_t launch_add_adapters(const AdapterArgs& a, hipStream_t stream) {
+hipError_t launch_add_adapters(AdapterArgs a, void* workspace, hipStream_t stream) {
+  a.shares = two_launches(a.t, a.K, a.rank) ? workspace : nullptr;
   if (a.t.tokens == 0 || (a.N == 0 && !a.hidden)) return hipSuccess;
   if (a.rank <= 32) return launch_rank<1>(a, stream);
   if (a.rank <= 64) return launch_rank<2>(a, stream);

@@ -109,14 +109,6 @@ struct TileLds {
   }
 };
 
-// Between one wave's LDS writes by some lanes and reads by others: the hardware
-// keeps a wave's LDS instructions in order, the compiler is told to.
-__device__ __forceinline__ void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-}
-
 // The two tokens of a lane in a tile, m and m + 16 (the last one where the tile ends before).
 struct Pair {
   int64_t token[2];
@@ -140,7 +132,7 @@ struct Rows {
 #pragma unroll
       for (int s = 0; s < kCols / 2; ++s) {
         const int c = col0 + 32 * s + 8 * g;
-        v[j][s] = col0 + 16 * kCols <= cols ? operand8(row + c) : operand8(row, c, cols - c);
+        v[j][s] = col0 + 16 * kCols <= cols ? operand8(row + c) : operand8(row, c, cols);
       }
     }
   }

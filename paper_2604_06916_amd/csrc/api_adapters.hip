@@ -40,6 +40,14 @@ struct Weights {
   }
 };
 
+// Sizes of a call: its tokens, or false.  Without a plan tiles start at every
+// 32nd token, with one every adapter starts a tile.
+bool sized(int64_t tokens, int64_t adapters, int planned, int64_t N, int64_t K, int64_t rank, solfp4::AdapterTokens* t) {
+  if (adapter_dims(tokens, adapters) || rank < 1 || rank > solfp4::kAdapterMaxRank || N < 0 || K < 0 || N >= solfp4::kAdapterMaxFeatures || K >= solfp4::kAdapterMaxFeatures) return false;
+  *t = solfp4::adapter_tokens(planned ? t : nullptr, tokens, adapters);
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -63,10 +71,16 @@ int solfp4_adapter_plan(const void* index, int index_bytes, int64_t tokens, int6
   return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
 }
 
+size_t solfp4_add_adapters_workspace_bytes(int64_t tokens, int64_t adapters, int planned, int64_t N, int64_t K,
+                                           int64_t rank) {
+  solfp4::AdapterTokens t;
+  return sized(tokens, adapters, planned, N, K, rank, &t) ? solfp4::add_adapters_bytes(t, K, rank) : 0;
+}
+
 int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const uint16_t* x, int64_t x_stride, const uint16_t* a,
                         const uint16_t* b, const float* scales, int64_t adapters, const void* plan, uint16_t* out,
-                        int64_t out_stride, float* hidden, int64_t tokens, int64_t N, int64_t K, int64_t rank,
-                        void* stream) {
+                        int64_t out_stride, float* hidden, void* workspace, size_t workspace_bytes, int64_t tokens,
+                        int64_t N, int64_t K, int64_t rank, void* stream) {
   const Weights w = {a, b, scales, plan, adapters, tokens, N, K, rank};
   int rc = w.check();
   if (rc) return rc;
@@ -83,20 +97,25 @@ int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const uint16_t* x, 
   const Region h = block_of(hidden, hidden ? tokens * rank * 4 : 0);
   if (!same_or_apart(ry, o) || !apart(rx, o) || !w.apart_from(o)) return SOLFP4_EINVAL;
   if (!apart(ry, h) || !apart(rx, h) || !apart(o, h) || !w.apart_from(h)) return SOLFP4_EINVAL;
-  const solfp4::AdapterArgs args = {solfp4::adapter_tokens(plan, tokens, adapters), y, y_stride, x, x_stride, a, b,
-                                    scales, out, out_stride, hidden, (int)N, (int)K, (int)rank, 0, 0};
-  const hipError_t e = solfp4::launch_add_adapters(args, static_cast<hipStream_t>(stream));
+  const solfp4::AdapterTokens t = solfp4::adapter_tokens(plan, tokens, adapters);
+  const size_t need = solfp4::add_adapters_bytes(t, K, rank);
+  if (need && !workspace) return SOLFP4_EWORKSPACE;
+  if (!aligned16(workspace)) return SOLFP4_EALIGN;
+  if (workspace_bytes < need) return SOLFP4_EWORKSPACE;
+  const Region s = block_of(workspace, (int64_t)need);
+  if (!apart(ry, s) || !apart(rx, s) || !apart(o, s) || !apart(h, s) || !w.apart_from(s)) return SOLFP4_EINVAL;
+  solfp4::AdapterArgs args = {};
+  args.t = t, args.y = y, args.y_stride = y_stride, args.x = x, args.x_stride = x_stride;
+  args.a = a, args.b = b, args.scales = scales, args.out = out, args.out_stride = out_stride, args.hidden = hidden;
+  args.N = (int)N, args.K = (int)K, args.rank = (int)rank;
+  const hipError_t e = solfp4::launch_add_adapters(args, workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SOLFP4_OK : SOLFP4_EHIP;
 }
 
 size_t solfp4_adapters_backward_workspace_bytes(int64_t tokens, int64_t adapters, int planned, int64_t N, int64_t K,
                                                 int64_t rank) {
-  if (adapter_dims(tokens, adapters) || N < 0 || K < 0 || rank < 1 || N >= solfp4::kAdapterMaxFeatures ||
-      K >= solfp4::kAdapterMaxFeatures || rank > solfp4::kAdapterMaxRank)
-    return 0;
-  // without a plan tiles start at every 32nd token, with one every adapter starts a tile
-  const int any = 0;
-  return solfp4::adapters_backward_bytes(solfp4::adapter_tokens(planned ? &any : nullptr, tokens, adapters), N, K, rank);
+  solfp4::AdapterTokens t;
+  return sized(tokens, adapters, planned, N, K, rank, &t) ? solfp4::adapters_backward_bytes(t, N, K, rank) : 0;
 }
 
 int solfp4_adapters_backward(const uint16_t* dy, int64_t dy_stride, const uint16_t* x, int64_t x_stride,

@@ -714,20 +714,23 @@ struct Adapters {
   }
 };
 
-// (y, x, a, b, scales, plan, plan_tokens, plan_adapters, hidden, out) -> (out, hidden)
+// (y, x, a, b, scales, plan, plan_tokens, plan_adapters, hidden, out, workspace) -> (out, hidden)
 PyObject* add_adapters_(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return entry(n, 10, [&]() -> PyObject* {
+  return entry(n, 11, [&]() -> PyObject* {
     const Adapters o(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]);
     const bool fresh = a[8] == Py_True;
     Operand hidden(fresh ? Py_None : a[8], at::kFloat, {o.tokens, o.rank}, o.dev);
     Strided out(a[9], o.x, {o.tokens, o.N});
+    const size_t bytes = solfp4_add_adapters_workspace_bytes(o.tokens, o.adapters, o.plan.defined(), o.N, o.K, o.rank);
+    Tensor ws = workspace_arg(a[10], bytes, o.dev);
     void* stream = stream_of(o.dev);
     out.allocate(o.x, {o.tokens, o.N});
     if (fresh) hidden.allocate(at::kFloat, {o.tokens, o.rank}, o.dev);
+    if (!ws.defined() && bytes) ws = make({(int64_t)bytes}, at::kByte, o.dev);
     const int rc = call([&] {
       return solfp4_add_adapters(u16(o.t), o.t.stride(0), u16(o.x), o.x.stride(0), u16(o.a), u16(o.b), f32(o.scales),
-                                 o.adapters, ptr(o.plan), u16(out.t), out.stride(0), f32(hidden.t), o.tokens, o.N, o.K,
-                                 o.rank, stream);
+                                 o.adapters, ptr(o.plan), u16(out.t), out.stride(0), f32(hidden.t), ptr(ws),
+                                 ws.defined() ? (size_t)ws.numel() : 0, o.tokens, o.N, o.K, o.rank, stream);
     });
     if (rc) return failed(rc);
     return Py_BuildValue("(NN)", out.object(), object_or_none(hidden));

@@ -345,9 +345,13 @@ struct AdapterArgs {
   int64_t out_stride;
   float* hidden;          // [tokens][rank], NULL: not wanted
   int N, K, rank;
-  int splits, split_cols;   // set by the launch
+  // set by the launch: ranges of a tile's columns and of K, their widths, tiles that take turns
+  int splits, split_cols, k_splits, k_cols, xcds;
+  void* shares;        // of h, NULL: one launch
 };
-hipError_t launch_add_adapters(const AdapterArgs& a, hipStream_t stream);
+// Device workspace, in bytes (0: none needed).
+size_t add_adapters_bytes(const AdapterTokens& t, int64_t K, int64_t rank);
+hipError_t launch_add_adapters(AdapterArgs a, void* workspace, hipStream_t stream);
 
 struct AdapterBackArgs {
   AdapterTokens t;

@@ -26,8 +26,8 @@ def test_plan_refusals():
 
 
 def forward(y=apart(0), ys=64, x=apart(1), xs=32, a=apart(2), b=apart(3), c=apart(4), E=3, p=apart(5), out=apart(6),
-            os=64, h=apart(7), tokens=40, N=64, K=32, rank=8):
-    return sol.lib.solfp4_add_adapters(y, ys, x, xs, a, b, c, E, p, out, os, h, tokens, N, K, rank, None)
+            os=64, h=apart(7), ws=apart(8), wsb=1 << 30, tokens=40, N=64, K=32, rank=8):
+    return sol.lib.solfp4_add_adapters(y, ys, x, xs, a, b, c, E, p, out, os, h, ws, wsb, tokens, N, K, rank, None)
 
 
 def test_forward_refusals():
@@ -45,6 +45,15 @@ def test_forward_refusals():
     for over in range(0, 7):
         assert forward(h=apart(over)) == EINVAL
     assert forward(out=at(2)) == EINVAL and forward(out=apart(0), os=65) == EINVAL
+    size = sol.add_adapters_workspace_bytes
+    assert size(40, 3, True, 64, 32, 8) == 0 == size(40, 3, True, 64, 32, 129) == size(100000, 3, True, 64, 9728, 64)
+    big = dict(K=9728, rank=64, xs=9728)
+    need = size(40, 3, True, 64, 9728, 64)
+    assert need > 0 and forward(ws=None, wsb=0, x=None) == EINVAL
+    assert forward(ws=None, **big) == EWORKSPACE and forward(wsb=need - 1, **big) == EWORKSPACE
+    assert forward(ws=at(8), **big) == EALIGN
+    for over in range(0, 8):
+        assert forward(ws=apart(over), **big) == EINVAL
     assert forward(tokens=0, x=None, y=None, out=None) == OK and forward(N=0, K=0, h=None, a=None, b=None) == OK
 
 

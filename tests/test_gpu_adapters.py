@@ -143,6 +143,21 @@ def test_an_adapter_a_token(tokens, adapters, K, N):
     check_forward(draw(1, tokens, N), draw(2, tokens, K), a, b, c, index, sol.adapter_plan(index, adapters))
 
 
+@pytest.mark.parametrize("tokens,K,N,rank", [(1, 9728, 640, 64), (70, 9001, 130, 33), (40, 2432, 200, 128),
+                                             (300, 4000, 64, 100), (9, 100000, 40, 24)])
+def test_wide_adapters(tokens, K, N, rank):
+    """a of 2^18 elements or more: h is formed by several workgroups in a launch of its own."""
+    adapters = 3
+    a, b, c = weights(tokens, adapters, rank, K, N)
+    index = index_of(tokens, tokens, adapters, "any")
+    plan = sol.adapter_plan(index, adapters)
+    x, y = draw(1, tokens, K), draw(2, tokens, N)
+    out, _ = check_forward(y, x, a, b, c, index, plan)
+    need = sol.add_adapters_workspace_bytes(tokens, adapters, True, N, K, rank)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device=device())
+    assert need and torch.equal(sol.add_adapters(y, x, a, b, c, plan, workspace=ws)[0].nan_to_num(7.0), out.nan_to_num(7.0))
+
+
 @pytest.mark.parametrize("offset", [0, 1, 3])
 def test_strides_in_place_and_what_lies_between(offset):
     """The k part of a packed QKV buffer, in place, from columns of a wider x."""
