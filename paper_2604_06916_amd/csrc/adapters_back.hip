@@ -93,65 +93,119 @@ template <int kCols>
 struct TileLds {
   static constexpr int kRow = kCols * 32 + 32;
   uint8_t* base;
-  __device__ __forceinline__ void put(int token, int col, bf16x8_t v) const {
-    *reinterpret_cast<u32x4_t*>(base + token * kRow + col * 2) = __builtin_bit_cast(u32x4_t, v);
+  __device__ __forceinline__ void put(int row, int m, const LaneRun<kCols>& v) const {
+    *reinterpret_cast<typename LaneRun<kCols>::words_t*>(base + row * kRow + m * kCols * 2) = v.w;
   }
-  // Block c with the columns as lanes: element j of lane (m, g) is column 16 c + m of token 16 (j / 4) + 4 g + j % 4.
-  __device__ __forceinline__ bf16x8_t transposed(int c, int lane) const {
+  // Its columns apart: column kCols m + c in the place of column 16 c + m.
+  __device__ __forceinline__ void spread(int row, int m, const LaneRun<kCols>& v) const {
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+      *reinterpret_cast<uint16_t*>(base + row * kRow + (16 * c + m) * 2) = (uint16_t)(v.w[c / 2] >> (16 * (c & 1)));
+  }
+  // As it lies: element j of lane (m, g) is column 32 s + 16 (j / 4) + 4 g + j % 4 of row `row`.
+  __device__ __forceinline__ bf16x8_t plain(int row, int s, int g) const {
+    const uint8_t* at = base + row * kRow + 64 * s + 8 * g;
+    const u32x2_t lo = *reinterpret_cast<const u32x2_t*>(at), hi = *reinterpret_cast<const u32x2_t*>(at + 32);
+    return __builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y});
+  }
+  // With columns as lanes: element j of lane (m, g) is row 16 (j / 4) + 4 g + j % 4
+  // of column first + hop (m / 4) + m % 4.
+  __device__ __forceinline__ bf16x8_t transposed(int first, int hop, int lane) const {
     const int i = lane % 16, g = lane / 16;
     short4_t v[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint8_t* at = base + (16 * h + 4 * g + i / 4) * kRow + (16 * c + i % 4 * 4) * 2;
+      uint8_t* at = base + (16 * h + 4 * g + i / 4) * kRow + (first + i % 4 * hop) * 2;
       v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)at);
     }
     return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
 
-// The two tokens of a lane in a tile, m and m + 16 (the last one where the tile ends before).
-struct Pair {
-  int64_t token[2];
+// A tile's tokens, one a lane (twice; the last again past the tile's end), so
+// that rows' addresses wait for no load of their own.
+struct Tokens {
+  int mine;
+  __device__ __forceinline__ void load(const AdapterTokens& t, const Tile& tile, int lane) {
+    mine = (int)token_at(t, tile.first + min(lane % kAdapterTile, tile.count - 1));
+  }
+  __device__ __forceinline__ int64_t row(int i) const { return (uint32_t)__shfl(mine, i, kWave); }
 };
-__device__ __forceinline__ Pair pair_of(const AdapterTokens& t, const Tile& tile, int m) {
-  Pair p;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) p.token[j] = token_at(t, tile.first + min(m + 16 * j, tile.count - 1));
-  return p;
-}
 
-// A tile's rows as they lie: element k of [j][s] is column col0 + 32 s + 8 g + k of token m + 16 j.
+// The tiles of a slice, looked up ahead of their use: at work on tile i, the
+// tokens of i + 1 are there, those of i + 2 on their way and tile i + 3 is read.
+// Loads come back in order, so a look-up that waited would wait for the rows
+// before it.
+struct Tiles {
+  const AdapterTokens& t;
+  int end, lane;
+  Tile tile, next, later, raw;
+  Tokens tokens, tokens_next, tokens_later;
+  __device__ __forceinline__ Tile at(int i) const { return i < end ? load_tile(t, i) : Tile{0, 0, 0}; }
+  __device__ __forceinline__ Tiles(const AdapterTokens& t, int first, int end, int lane) : t(t), end(end), lane(lane) {
+    tile = uniform(at(first)), next = uniform(at(first + 1)), raw = at(first + 2);
+    if (tile.count) tokens.load(t, tile, lane);
+    if (next.count) tokens_next.load(t, next, lane);
+  }
+  __device__ __forceinline__ void look(int i) {   // at work on tile i
+    later = uniform(raw);
+    if (later.count) tokens_later.load(t, later, lane);
+    raw = at(i + 3);
+  }
+  __device__ __forceinline__ void advance() {
+    tile = next, tokens = tokens_next;
+    next = later, tokens_next = tokens_later;
+  }
+};
+
+// A tile's rows: 16 lanes read kCols columns each of one row, whole lines where
+// the rank lets a wave have 64 columns or more; a lane has rows g + 4 i.
 template <int kCols>
 struct Rows {
-  bf16x8_t v[2][kCols / 2];
-  __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, const Pair& pair, int col0, int cols,
-                                       int g) {
+  LaneRun<kCols> v[8];
+  __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, const Tokens& tokens, int col0, int cols,
+                                       int m, int g) {
+    if (col0 + 16 * kCols <= cols) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint16_t* row = base + pair.token[j] * stride;
+      for (int i = 0; i < 8; ++i) v[i].load(base + tokens.row(g + 4 * i) * stride, col0 + kCols * m, cols, true);
+    } else {
 #pragma unroll
-      for (int s = 0; s < kCols / 2; ++s) {
-        const int c = col0 + 32 * s + 8 * g;
-        v[j][s] = col0 + 16 * kCols <= cols ? operand8(row + c) : operand8(row, c, cols);
-      }
+      for (int i = 0; i < 8; ++i) v[i].load(base + tokens.row(g + 4 * i) * stride, col0 + kCols * m, cols, false);
     }
   }
-  // zeros in the place of tokens past the tile's end
-  __device__ __forceinline__ void clear(int count, int m) {
-    if (count == kAdapterTile) return;
+  // to LDS, with zeros in the place of tokens past the tile's end
+  __device__ __forceinline__ void put(const TileLds<kCols>& lds, int count, int m, int g) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int s = 0; s < kCols / 2; ++s)
-        if (m + 16 * j >= count) v[j][s] = none8();
+    for (int i = 0; i < 8; ++i) {
+      if (count < kAdapterTile && g + 4 * i >= count) v[i].w = typename LaneRun<kCols>::words_t{};
+      lds.put(g + 4 * i, m, v[i]);
+    }
   }
 };
+
+// acc += factor^T tile, the tile's columns as lanes; factor(r, s) is piece s of block r.
+template <int kCols, int kBlocks, typename F>
+__device__ __forceinline__ void add_products(floatx4_t (&acc)[kCols][kBlocks], const TileLds<kCols>& lds, int lane,
+                                             F factor) {
+  bf16x8_t z[kCols];
+#pragma unroll
+  for (int c = 0; c < kCols; ++c) z[c] = lds.transposed(16 * c, 4, lane);
+#pragma unroll
+  for (int r = 0; r < kBlocks; ++r)
+#pragma unroll
+    for (int s = 2; s >= 0; --s) {
+      const bf16x8_t f = factor(r, s);
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) acc[c][r] = mfma(f, z[c], acc[c][r]);
+    }
+}
 
 // ---- the pass over dy -----------------------------------------------------
 
 template <int kChunks>
 __global__ __launch_bounds__(kWaves * kWave, 2) void adapters_back_y_kernel(BackArgs q) {
   constexpr int kBlocks = 2 * kChunks, kCols = cols_of(kChunks);
+  constexpr int kHBlocks = (kBlocks + kWaves - 1) / kWaves;   // blocks of h that a wave makes an operand
   constexpr int kRounds = kChunks == 4 ? 2 : 1, kShared = 2 * kBlocks / kRounds;   // LDS holds all shares of a round
   __shared__ floatx4_t share[kWaves][kShared][kWave];
   __shared__ bf16x8_t factor[3][kBlocks][kWave];
@@ -186,51 +240,78 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void adapters_back_y_kernel(Back
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
       for (int r = 0; r < kBlocks; ++r) acc[c][r] = floatx4_t{0, 0, 0, 0};
-    // b^T: row 4 g + i of block r is rank element 32 (r / 2) + 8 g + 4 (r % 2) + i
-    const uint16_t* b = p.b + (int64_t)e * p.N * p.rank;
+    // b^T through LDS, 32 columns at a time: row 4 g + i of block r is rank element
+    // 32 (r / 2) + 8 g + 4 (r % 2) + i
+    if (!works) return;
+    int rank = p.rank, row = g;
+    asm volatile("" : "+s"(rank), "+v"(row));   // rows' places made here and not kept over the tiles
+    const uint16_t* b = p.b + (int64_t)e * p.N * rank;
+    constexpr int kFit = kCols < kBlocks ? kCols : kBlocks;   // blocks of the rank that the tile holds
 #pragma unroll
-    for (int r = 0; r < kBlocks; ++r) {
-      const int at = 32 * (r / 2) + m / 4 * 8 + r % 2 * 4 + m % 4;
+    for (int s = 0; s < kCols / 2; ++s)
 #pragma unroll
-      for (int s = 0; s < kCols / 2; ++s) {
-        u32x4_t w = {0, 0, 0, 0};
+      for (int h = 0; h < kBlocks / kFit; ++h) {
+        LaneRun<kCols> v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int n = col0 + 32 * s + 8 * g + k;
-          if (works && n < p.N && at < p.rank) w[k / 2] |= (uint32_t)b[(int64_t)n * p.rank + at] << (16 * (k & 1));
+        for (int i = 0; i < 8; ++i) {
+          const int n = col0 + 32 * s + row + 4 * i;
+          v[i].load(b + (int64_t)min(n, p.N - 1) * rank, 16 * kFit * h + kCols * m, rank,
+                    16 * kFit * h + 16 * kCols <= rank);
+          if (n >= p.N) v[i].w = typename LaneRun<kCols>::words_t{};
         }
-        bt[r][s] = __builtin_bit_cast(bf16x8_t, w);
+        wave_order();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds.put(g + 4 * i, m, v[i]);
+        wave_order();
+#pragma unroll
+        for (int r = 0; r < kFit; ++r) bt[kFit * h + r][s] = lds.transposed(r / 2 * 32 + r % 2 * 4, 8, lane);
+        wave_order();
+        __builtin_amdgcn_sched_barrier(0);   // one step's loads at a time in registers
       }
-    }
   };
 
   const int first = slice * q.d.each_n, end = min(first + q.d.each_n, (int)q.d.tiles);
-  for (int i = first; i < end; ++i) {
-    const Tile tile = uniform(load_tile(p.t, i));
-    if (tile.count == 0 || tile.group >= p.t.adapters) break;   // adapters' tiles come first
-    const Pair pair = pair_of(p.t, tile, m);
-    Rows<kCols> dy;
-    if (works) {
-      dy.load(p.dy, p.dy_stride, pair, col0, p.N, g);
-      dy.clear(tile.count, m);
-    }
-    if (tile.group != group) {
-      flush();
-      begin(tile.group);
-    }
-    // h as an operand, its tokens in the transposed tile's order
-    for (int r = wave; r < kBlocks; r += kWaves) {
-      float v[8];
+  // the next tile's rows and its h come while a tile is worked on
+  Tiles tiles_(p.t, first, end, lane);
+  Tile& tile = tiles_.tile;
+  Tokens& tokens = tiles_.tokens;
+  Rows<kCols> dy;
+  float hv[kHBlocks][8];
+  const auto is_real = [&] { return tile.count && tile.group < p.t.adapters; };   // adapters' tiles come first
+  const auto fetch = [&] {
+#pragma unroll
+    for (int u = 0; u < kHBlocks; ++u) {
+      const int r = wave + u * kWaves;
+      if (r >= kBlocks) continue;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int t = 16 * (k / 4) + 4 * g + k % 4, at = 16 * r + m;
-        v[k] = t < tile.count && at < p.rank ? p.hidden[token_at(p.t, tile.first + t) * p.rank + at] : 0.0f;
+        const int64_t token = tokens.row(t);
+        hv[u][k] = t < tile.count && at < p.rank ? p.hidden[token * p.rank + at] : 0.0f;
       }
+    }
+    if (works) dy.load(p.dy, p.dy_stride, tokens, col0, p.N, m, g);
+  };
+  int i = first;
+  while (is_real()) {
+   begin(tile.group);
+   fetch();
+   for (bool more = true; more; ++i) {
+    tiles_.look(i);
+    if (works) dy.put(lds, tile.count, m, g);
+    // h as an operand, its tokens in the transposed tile's order
+#pragma unroll
+    for (int u = 0; u < kHBlocks; ++u) {
+      const int r = wave + u * kWaves;
+      if (r >= kBlocks) continue;
       bf16x8_t piece[3];
-      split_bf16(v, piece);
+      split_bf16(hv[u], piece);
 #pragma unroll
       for (int s = 0; s < 3; ++s) factor[s][r][lane] = piece[s];
     }
+    tiles_.advance();
+    more = is_real() && tile.group == group;
+    if (more) fetch();
     __syncthreads();
     floatx4_t part[2][kBlocks];
 #pragma unroll
@@ -239,27 +320,14 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void adapters_back_y_kernel(Back
       for (int r = 0; r < kBlocks; ++r) part[j][r] = floatx4_t{0, 0, 0, 0};
     if (works) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int s = 0; s < kCols / 2; ++s) lds.put(m + 16 * j, 32 * s + 8 * g, dy.v[j][s]);
-      wave_order();
-#pragma unroll
       for (int s = 0; s < kCols / 2; ++s)
 #pragma unroll
-        for (int r = 0; r < kBlocks; ++r)
+        for (int j = 0; j < 2; ++j) {
+          const bf16x8_t v = lds.plain(m + 16 * j, s, g);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) part[j][r] = mfma(bt[r][s], dy.v[j][s], part[j][r]);
-      bf16x8_t z[kCols];
-#pragma unroll
-      for (int c = 0; c < kCols; ++c) z[c] = lds.transposed(c, lane);
-#pragma unroll
-      for (int r = 0; r < kBlocks; ++r)
-#pragma unroll
-        for (int s = 2; s >= 0; --s) {
-          const bf16x8_t f = factor[s][r][lane];
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) acc[c][r] = mfma(f, z[c], acc[c][r]);
+          for (int r = 0; r < kBlocks; ++r) part[j][r] = mfma(bt[r][s], v, part[j][r]);
         }
+      add_products<kCols, kBlocks>(acc, lds, lane, [&](int r, int s) { return factor[s][r][lane]; });
       wave_order();
     }
 #pragma unroll
@@ -279,8 +347,9 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void adapters_back_y_kernel(Back
         to_[k] = v;
       }
     }
+   }
+   flush();
   }
-  flush();
 }
 
 // ---- g from its shares ----------------------------------------------------
@@ -305,12 +374,17 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
       lo += from[n * hop + at];
       hi += from[n * hop + at + kWave];
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      gs[lane % 16 + 16 * j][32 * c + lane / 16 * 8 + e] = scale * (e < 4 ? lo[e % 4] : hi[e % 4]);
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < kBlocks * kWave; k += 256) {
+    // row 4 g + i of the result is row g + 4 i of the tile, as in the forward pass
+    const int lane = k % kWave, m = lane % 16, jc = k / kWave, j = jc / kChunks, c = jc % kChunks;
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = scale * (e < 4 ? lo[e % 4] : hi[e % 4]);
-      gs[lane % 16 + 16 * j][32 * c + lane / 16 * 8 + e] = v[e];
-    }
+    for (int e = 0; e < 8; ++e) v[e] = gs[m % 4 * 4 + m / 4 + 16 * j][32 * c + e / 4 * 16 + lane / 16 * 4 + e % 4];
     bf16x8_t piece[2];
     split_bf16(v, piece);
 #pragma unroll
@@ -318,7 +392,6 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
       q.ws[q.d.pieces2 + (((int64_t)i * kChunks + c) * 2 + j) * 2 * kWave + s * kWave + lane] =
           __builtin_bit_cast(floatx4_t, piece[s]);
   }
-  __syncthreads();
   for (int k = threadIdx.x; k < kBlocks * kWave; k += 256) {
     const int lane = k % kWave, r = k / kWave, g = lane / 16;
     float v[8];
@@ -338,7 +411,6 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
 template <int kChunks>
 __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(BackArgs q) {
   constexpr int kBlocks = 2 * kChunks, kCols = cols_of(kChunks);
-  constexpr int kRun = kCols < 4 ? kCols : 4, kRuns = kCols / kRun;   // blocks whose columns a lane holds in a row
   __shared__ __attribute__((aligned(16))) uint8_t tiles[kXWaves][kAdapterTile * TileLds<kCols>::kRow];
   const AdapterBackArgs& p = q.p;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -367,101 +439,111 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
       for (int r = 0; r < kBlocks; ++r) acc[c][r] = floatx4_t{0, 0, 0, 0};
-    // a^T: row 4 g + i of block c is column 16 kRun (c / kRun) + 4 kRun g + 4 (c % kRun) + i
-    const uint16_t* a = p.a + (int64_t)e * p.rank * p.K;
+    // a^T through LDS: column m of block c is column kCols m + c, so that a lane's
+    // results follow each other
+    int K = p.K, row = g;
+    asm volatile("" : "+s"(K), "+v"(row));   // rows' places made here and not kept over the tiles
+    const uint16_t* a = p.a + (int64_t)e * p.rank * K;
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-      const int col = col0 + c / kRun * 16 * kRun + m / 4 * 4 * kRun + c % kRun * 4 + m % 4;
+    for (int h = 0; h < kChunks; ++h) {
+      LaneRun<kCols> v[8];
 #pragma unroll
-      for (int h = 0; h < kChunks; ++h) {
-        u32x4_t w = {0, 0, 0, 0};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int r = 32 * h + 8 * g + k;
-          if (col < p.K && r < p.rank) w[k / 2] |= (uint32_t)a[(int64_t)r * p.K + col] << (16 * (k & 1));
-        }
-        at[c][h] = __builtin_bit_cast(bf16x8_t, w);
+      for (int i = 0; i < 8; ++i) {
+        const int r = 32 * h + row + 4 * i;
+        v[i].load(a + (int64_t)min(r, p.rank - 1) * K, col0 + kCols * m, K, col0 + 16 * kCols <= K);
+        if (r >= p.rank) v[i].w = typename LaneRun<kCols>::words_t{};
       }
+      wave_order();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lds.spread(g + 4 * i, m, v[i]);
+      wave_order();
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) at[c][h] = lds.transposed(16 * c, 4, lane);
+      wave_order();
+      __builtin_amdgcn_sched_barrier(0);   // one step's loads at a time in registers
     }
   };
 
   const int first = slice * q.d.each_x, end = min(first + q.d.each_x, (int)q.d.tiles);
-  for (int i = first; i < end; ++i) {
-    const Tile tile = uniform(load_tile(p.t, i));
-    if (tile.count == 0) break;
-    const bool real = tile.group < p.t.adapters;
-    const Pair pair = pair_of(p.t, tile, m);
-    if (tile.group != group) {
-      flush();
-      begin(tile.group);
+  // x ahead as in the pass over dy; past of the tile itself, needed last
+  Tiles tiles_(p.t, first, end, lane);
+  Tile& tile = tiles_.tile;
+  Tokens& tokens = tiles_.tokens;
+  Rows<kCols> x;
+  int i = first;
+  while (tile.count) {
+   begin(tile.group);
+   const bool real = group < p.t.adapters;
+   if (real) x.load(p.x, p.x_stride, tokens, col0, p.K, m, g);
+   for (bool more = true; more; ++i) {
+    tiles_.look(i);
+    const Tile now = tile;
+    const Tokens of_now = tokens;
+    Rows<kCols> add;
+    if (p.past) {
+      add.load(p.past, p.past_stride, of_now, col0, p.K, m, g);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) add.v[k].w = typename LaneRun<kCols>::words_t{};
     }
-    bf16x8_t two[kChunks][2][2];
+    bf16x8_t two[2][kChunks][2];
     if (real) {
-      Rows<kCols> x;
-      x.load(p.x, p.x_stride, pair, col0, p.K, g);
-      x.clear(tile.count, m);
 #pragma unroll
       for (int h = 0; h < kChunks; ++h)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int s = 0; s < 2; ++s)
-            two[h][j][s] = __builtin_bit_cast(
+            two[j][h][s] = __builtin_bit_cast(
                 bf16x8_t, q.ws[q.d.pieces2 + (((int64_t)i * kChunks + h) * 2 + j) * 2 * kWave + s * kWave + lane]);
       wave_order();
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int s = 0; s < kCols / 2; ++s) lds.put(m + 16 * j, 32 * s + 8 * g, x.v[j][s]);
+      x.put(lds, now.count, m, g);
       wave_order();
-      bf16x8_t z[kCols];
-#pragma unroll
-      for (int c = 0; c < kCols; ++c) z[c] = lds.transposed(c, lane);
-#pragma unroll
-      for (int r = 0; r < kBlocks; ++r)
-#pragma unroll
-        for (int s = 2; s >= 0; --s) {
-          const bf16x8_t f = __builtin_bit_cast(
-              bf16x8_t, q.ws[q.d.pieces3 + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane]);
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) acc[c][r] = mfma(f, z[c], acc[c][r]);
-        }
+    }
+    tiles_.advance();
+    more = tile.count && tile.group == group;
+    if (more && real) x.load(p.x, p.x_stride, tokens, col0, p.K, m, g);
+    if (real) {
+      add_products<kCols, kBlocks>(acc, lds, lane, [&](int r, int s) {
+        return __builtin_bit_cast(
+            bf16x8_t, q.ws[q.d.pieces3 + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane]);
+      });
     }
 #pragma unroll
-    for (int u = 0; u < kRuns; ++u) {
+    for (int j = 0; j < 2; ++j) {
+      if (real) {
+        // two columns of a lane's rows at a time
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int col = col0 + u * 16 * kRun + g * 4 * kRun;
-        floatx4_t d[kRun];
+        for (int c = 0; c < kCols; c += 2) {
+          floatx4_t d[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-        for (int c = 0; c < kRun; ++c) d[c] = floatx4_t{0, 0, 0, 0};
-        if (real)
+          for (int h = 0; h < kChunks; ++h)
 #pragma unroll
-          for (int c = 0; c < kRun; ++c)
+            for (int s = 1; s >= 0; --s)
 #pragma unroll
-            for (int h = 0; h < kChunks; ++h)
+              for (int u = 0; u < 2; ++u) d[u] = mfma(two[j][h][s], at[c + u][h], d[u]);
 #pragma unroll
-              for (int s = 1; s >= 0; --s) d[c] = mfma(at[u * kRun + c][h], two[h][j][s], d[c]);
-        if (m + 16 * j >= tile.count) continue;
-        const uint8_t* pr = reinterpret_cast<const uint8_t*>(p.past + pair.token[j] * p.past_stride);
-        uint8_t* o = reinterpret_cast<uint8_t*>(p.dx + pair.token[j] * p.dx_stride);
-#pragma unroll
-        for (int w = 0; w < kRun / 2; ++w) {
-          const int c0 = col + 8 * w, n = p.K - c0;
-          if (n <= 0) continue;
-          float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-          if (p.past) to_f32<SOLFP4_BF16>(load_run<SOLFP4_BF16>(pr, c0, n), v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (real) v[e] += d[2 * w + e / 4][e % 4];
-            if (tile.group > p.t.adapters) v[e] = __builtin_nanf("");
+          for (int k = 0; k < 4; ++k) {
+            LaneRun<kCols>& o = add.v[4 * j + k];
+            o.w[c / 2] = pack_bf16(o.value(c) + d[0][k], o.value(c + 1) + d[1][k]);
           }
-          store_run<SOLFP4_BF16>(o, c0, n, from_f32<SOLFP4_BF16>(v));
         }
+      } else if (now.group > p.t.adapters) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int c = 0; c < kCols / 2; ++c) add.v[4 * j + k].w[c] = 0x7FC07FC0u;   // NaN
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t token = of_now.row(g + 4 * k + 16 * j);
+        if (g + 4 * k + 16 * j < now.count)
+          add.v[4 * j + k].store(p.dx + token * p.dx_stride, col0 + kCols * m, p.K, col0 + 16 * kCols <= p.K);
       }
     }
+   }
+   flush();
   }
-  flush();
 }
 
 // ---- da and db from the slices' sums --------------------------------------
