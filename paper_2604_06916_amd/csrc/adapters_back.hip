@@ -28,7 +28,11 @@ namespace solfp4 {
 
 namespace {
 
-constexpr int kWaves = 8;        // of a workgroup of the first pass
+// Waves of a workgroup of the first pass: two workgroups a CU that wait for each
+// other's waves less, but more shares of g through the workspace, four times as
+// many values with a rank of 128 (26574 tokens 2432 -> 7296, rank 32: 258 us with 4,
+// 280 with 8; 13000 tokens, rank 64 212 and 201; 6600 tokens, rank 128 392 and 302).
+constexpr int y_waves(int chunks) { return chunks == 1 ? 4 : 8; }
 constexpr int kXWaves = 4;       // of the second, whose waves go by themselves
 
 typedef short short4_t __attribute__((ext_vector_type(4)));
@@ -59,13 +63,14 @@ Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
   d.tiles = t.max_tiles;
   d.units_n = (int)((N + cols - 1) / cols);
   d.units_x = (int)((K + cols - 1) / cols);
-  d.chunks_n = (d.units_n + kWaves - 1) / kWaves;
+  const int waves = y_waves(chunks);
+  d.chunks_n = (d.units_n + waves - 1) / waves;
   const auto slices = [&](int64_t want, int* each) {
     want = want < 1 ? 1 : want < d.tiles ? want : d.tiles;
     *each = (int)(want > 0 ? (d.tiles + want - 1) / want : 1);
     return (int)((d.tiles + *each - 1) / *each);
   };
-  d.slices_n = slices(d.chunks_n ? cus / d.chunks_n : 1, &d.each_n);
+  d.slices_n = slices(d.chunks_n ? 8 * cus / (waves * d.chunks_n) : 1, &d.each_n);
   d.slices_x = slices(d.units_x ? 8 * cus / d.units_x : 1, &d.each_x);
   d.slots_n = d.slices_n + t.adapters;
   d.slots_x = d.slices_x + t.adapters;
@@ -86,6 +91,18 @@ Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
 }
 
 __device__ __forceinline__ bf16x8_t none8() { return __builtin_bit_cast(bf16x8_t, u32x4_t{0, 0, 0, 0}); }
+
+// Columns as lanes of a matrix in LDS whose rows lie `stride` bytes apart: element j
+// of lane (m, g) is row 16 (j / 4) + 4 g + j % 4 of column first + hop (m / 4) + m % 4.
+__device__ __forceinline__ bf16x8_t transposed_read(uint8_t* base, int stride, int first, int hop, int lane) {
+  const int i = lane % 16, g = lane / 16;
+  short4_t v[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_short4_t)(base + (16 * h + 4 * g + i / 4) * stride + (first + i % 4 * hop) * 2));
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
 
 // One wave's tile in LDS, [token][column]; rows 32 bytes apart beyond their
 // columns, so that the eight rows that half a wave reads lie in different banks.
@@ -108,17 +125,9 @@ struct TileLds {
     const u32x2_t lo = *reinterpret_cast<const u32x2_t*>(at), hi = *reinterpret_cast<const u32x2_t*>(at + 32);
     return __builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y});
   }
-  // With columns as lanes: element j of lane (m, g) is row 16 (j / 4) + 4 g + j % 4
-  // of column first + hop (m / 4) + m % 4.
-  __device__ __forceinline__ bf16x8_t transposed(int first, int hop, int lane) const {
-    const int i = lane % 16, g = lane / 16;
-    short4_t v[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint8_t* at = base + (16 * h + 4 * g + i / 4) * kRow + (first + i % 4 * hop) * 2;
-      v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)at);
-    }
-    return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  // Block c with the columns as lanes.
+  __device__ __forceinline__ bf16x8_t transposed(int c, int lane) const {
+    return transposed_read(base, kRow, 16 * c, 4, lane);
   }
 };
 
@@ -189,7 +198,7 @@ __device__ __forceinline__ void add_products(floatx4_t (&acc)[kCols][kBlocks], c
                                              F factor) {
   bf16x8_t z[kCols];
 #pragma unroll
-  for (int c = 0; c < kCols; ++c) z[c] = lds.transposed(16 * c, 4, lane);
+  for (int c = 0; c < kCols; ++c) z[c] = lds.transposed(c, lane);
 #pragma unroll
   for (int r = 0; r < kBlocks; ++r)
 #pragma unroll
@@ -203,8 +212,8 @@ __device__ __forceinline__ void add_products(floatx4_t (&acc)[kCols][kBlocks], c
 // ---- the pass over dy -----------------------------------------------------
 
 template <int kChunks>
-__global__ __launch_bounds__(kWaves * kWave, 2) void adapters_back_y_kernel(BackArgs q) {
-  constexpr int kBlocks = 2 * kChunks, kCols = cols_of(kChunks);
+__global__ __launch_bounds__(y_waves(kChunks) * kWave, 2) void adapters_back_y_kernel(BackArgs q) {
+  constexpr int kWaves = y_waves(kChunks), kBlocks = 2 * kChunks, kCols = cols_of(kChunks);
   constexpr int kHBlocks = (kBlocks + kWaves - 1) / kWaves;   // blocks of h that a wave makes an operand
   constexpr int kRounds = kChunks == 4 ? 2 : 1, kShared = 2 * kBlocks / kRounds;   // LDS holds all shares of a round
   __shared__ floatx4_t share[kWaves][kShared][kWave];
@@ -240,34 +249,46 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void adapters_back_y_kernel(Back
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
       for (int r = 0; r < kBlocks; ++r) acc[c][r] = floatx4_t{0, 0, 0, 0};
-    // b^T through LDS, 32 columns at a time: row 4 g + i of block r is rank element
-    // 32 (r / 2) + 8 g + 4 (r % 2) + i
+    // b^T through LDS: row 4 g + i of block r is rank element 32 (r / 2) + 8 g + 4 (r % 2) + i.
+    // All of the wave's columns, 8 KB, are loaded at once, and pass through LDS in
+    // squares of 32 columns and 32 rank elements, as many at a time as fit.
     if (!works) return;
-    int rank = p.rank, row = g;
+    int rank = p.rank, row = lane / (2 * kBlocks);
     asm volatile("" : "+s"(rank), "+v"(row));   // rows' places made here and not kept over the tiles
     const uint16_t* b = p.b + (int64_t)e * p.N * rank;
-    constexpr int kFit = kCols < kBlocks ? kCols : kBlocks;   // blocks of the rank that the tile holds
+    constexpr int kFit = 4 / kChunks, kSquareRow = 72, kSquare = 32 * kSquareRow;
+    static_assert(kFit * kSquare <= kAdapterTile * TileLds<kCols>::kRow, "the squares' place");
+    const int piece = lane % (2 * kBlocks);
+    u32x4_t v[8];
 #pragma unroll
-    for (int s = 0; s < kCols / 2; ++s)
+    for (int i = 0; i < 8; ++i) {
+      const int n = col0 + row + i * (32 / kBlocks);
+      const uint16_t* br = b + (int64_t)min(n, p.N - 1) * rank;
+      v[i] = __builtin_bit_cast(u32x4_t, rank == 16 * kBlocks ? operand8(br + 8 * piece) : operand8(br, 8 * piece, rank));
+      if (n >= p.N) v[i] = u32x4_t{0, 0, 0, 0};
+    }
 #pragma unroll
-      for (int h = 0; h < kBlocks / kFit; ++h) {
-        LaneRun<kCols> v[8];
+    for (int round = 0; round < 4 / kFit; ++round) {
+      wave_order();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int n = col0 + 32 * s + row + 4 * i;
-          v[i].load(b + (int64_t)min(n, p.N - 1) * rank, 16 * kFit * h + kCols * m, rank,
-                    16 * kFit * h + 16 * kCols <= rank);
-          if (n >= p.N) v[i].w = typename LaneRun<kCols>::words_t{};
-        }
-        wave_order();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) lds.put(g + 4 * i, m, v[i]);
-        wave_order();
-#pragma unroll
-        for (int r = 0; r < kFit; ++r) bt[kFit * h + r][s] = lds.transposed(r / 2 * 32 + r % 2 * 4, 8, lane);
-        wave_order();
-        __builtin_amdgcn_sched_barrier(0);   // one step's loads at a time in registers
+      for (int i = 0; i < 8; ++i) {
+        const int at = row + i * (32 / kBlocks), square = at / 32 * kChunks + piece / 4;
+        if (square / kFit != round) continue;
+        u32x2_t* to_ = reinterpret_cast<u32x2_t*>(lds.base + square % kFit * kSquare + at % 32 * kSquareRow + piece % 4 * 16);
+        to_[0] = u32x2_t{v[i].x, v[i].y};
+        to_[1] = u32x2_t{v[i].z, v[i].w};
       }
+      wave_order();
+#pragma unroll
+      for (int f = 0; f < kFit; ++f)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int square = round * kFit + f;
+          bt[square % kChunks * 2 + r][square / kChunks] =
+              transposed_read(lds.base + f * kSquare, kSquareRow, 4 * r, 8, lane);
+        }
+    }
+    wave_order();
   };
 
   const int first = slice * q.d.each_n, end = min(first + q.d.each_n, (int)q.d.tiles);
@@ -458,7 +479,7 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
       for (int i = 0; i < 8; ++i) lds.spread(g + 4 * i, m, v[i]);
       wave_order();
 #pragma unroll
-      for (int c = 0; c < kCols; ++c) at[c][h] = lds.transposed(16 * c, 4, lane);
+      for (int c = 0; c < kCols; ++c) at[c][h] = lds.transposed(c, lane);
       wave_order();
       __builtin_amdgcn_sched_barrier(0);   // one step's loads at a time in registers
     }
@@ -566,7 +587,15 @@ __global__ __launch_bounds__(256) void adapters_back_sums_kernel(BackArgs q) {
     if (begin < end) {
       const int each = is_db ? q.d.each_n : q.d.each_x;
       const floatx4_t* from = q.ws + (is_db ? q.d.db : q.d.da) + place;
-      for (int s = begin / each; s <= (end - 1) / each; ++s) v += from[(s + e) * per];
+      // in order, eight loads at a time
+      const int s1 = (end - 1) / each;
+      for (int s = begin / each; s <= s1; s += 8) {
+        floatx4_t u[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[k] = s + k <= s1 ? from[(s + k + e) * per] : floatx4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += u[k];
+      }
     }
     const int lane = (int)(place % kWave), r = (int)(place / kWave % kBlocks);
     const int64_t col = place / kWave / kBlocks * 16 + lane % 16;
@@ -594,7 +623,7 @@ hipError_t launch_back(const BackArgs& q, hipStream_t stream) {
   if (q.d.tiles > 0) {
     if (q.d.chunks_n > 0)
       e = launch_kernel(adapters_back_y_kernel<kChunks>, dim3((unsigned)(q.d.chunks_n * q.d.slices_n)),
-                        dim3(kWaves * kWave), stream, q);
+                        dim3(y_waves(kChunks) * kWave), stream, q);
     if (e == hipSuccess && q.d.units_x > 0)
       e = launch_kernel(adapters_back_g_kernel<kChunks>, dim3((unsigned)q.d.tiles), dim3(256), stream, q);
     const int64_t waves = (int64_t)q.d.units_x * q.d.slices_x;
