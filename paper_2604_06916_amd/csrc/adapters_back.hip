@@ -38,8 +38,12 @@ constexpr int kXWaves = 4;       // of the second, whose waves go by themselves
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t* lds_short4_t;
 
-// Blocks of 16 columns of a wave, so that the sums take 64 registers.
+// Blocks of 16 columns of a wave, so that the sums take 64 registers; in the
+// second pass, which holds x, past and g's pieces beside them, 32 where rows stay
+// whole lines (26574 tokens 2432 -> 7296, rank 32: 229 us with four blocks, 252 with
+// eight, whose registers spill).
 constexpr int cols_of(int chunks) { return 8 / chunks; }
+constexpr int x_cols(int chunks) { return chunks == 1 ? 4 : cols_of(chunks); }
 
 // How the work is dealt and where everything lies in the workspace.
 struct Deal {
@@ -57,12 +61,13 @@ struct BackArgs {
 };
 
 Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
-  const int chunks = rank <= 32 ? 1 : rank <= 64 ? 2 : 4, cols = 16 * cols_of(chunks), blocks = 2 * chunks;
+  const int chunks = rank <= 32 ? 1 : rank <= 64 ? 2 : 4, blocks = 2 * chunks;
+  const int cols = 16 * cols_of(chunks), x_wide = 16 * x_cols(chunks);
   const int64_t cus = device_cu_count();
   Deal d = {};
   d.tiles = t.max_tiles;
   d.units_n = (int)((N + cols - 1) / cols);
-  d.units_x = (int)((K + cols - 1) / cols);
+  d.units_x = (int)((K + x_wide - 1) / x_wide);
   const int waves = y_waves(chunks);
   d.chunks_n = (d.units_n + waves - 1) / waves;
   const auto slices = [&](int64_t want, int* each) {
@@ -85,7 +90,7 @@ Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
   d.pieces2 = take(d.tiles * chunks * 2 * 2 * kWave);
   d.pieces3 = take(d.tiles * 3 * frag);
   d.db = take(d.slots_n * d.units_n * cols_of(chunks) * frag);
-  d.da = take(d.slots_x * d.units_x * cols_of(chunks) * frag);
+  d.da = take(d.slots_x * d.units_x * x_cols(chunks) * frag);
   d.bytes = at * 16;
   return d;
 }
@@ -192,21 +197,33 @@ struct Rows {
   }
 };
 
-// acc += factor^T tile, the tile's columns as lanes; factor(r, s) is piece s of block r.
-template <int kCols, int kBlocks, typename F>
+// acc += factor^T tile, the tile's columns as lanes; factor(r, s) is piece s of
+// block r.  kHeld: the factors are in registers, and a block of columns is at a time.
+template <int kCols, int kBlocks, bool kHeld, typename F>
 __device__ __forceinline__ void add_products(floatx4_t (&acc)[kCols][kBlocks], const TileLds<kCols>& lds, int lane,
                                              F factor) {
-  bf16x8_t z[kCols];
+  if constexpr (kHeld) {
 #pragma unroll
-  for (int c = 0; c < kCols; ++c) z[c] = lds.transposed(c, lane);
+    for (int c = 0; c < kCols; ++c) {
+      const bf16x8_t z = lds.transposed(c, lane);
 #pragma unroll
-  for (int r = 0; r < kBlocks; ++r)
+      for (int s = 2; s >= 0; --s)
 #pragma unroll
-    for (int s = 2; s >= 0; --s) {
-      const bf16x8_t f = factor(r, s);
-#pragma unroll
-      for (int c = 0; c < kCols; ++c) acc[c][r] = mfma(f, z[c], acc[c][r]);
+        for (int r = 0; r < kBlocks; ++r) acc[c][r] = mfma(factor(r, s), z, acc[c][r]);
     }
+  } else {
+    bf16x8_t z[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) z[c] = lds.transposed(c, lane);
+#pragma unroll
+    for (int r = 0; r < kBlocks; ++r)
+#pragma unroll
+      for (int s = 2; s >= 0; --s) {
+        const bf16x8_t f = factor(r, s);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) acc[c][r] = mfma(f, z[c], acc[c][r]);
+      }
+  }
 }
 
 // ---- the pass over dy -----------------------------------------------------
@@ -315,61 +332,61 @@ __global__ __launch_bounds__(y_waves(kChunks) * kWave, 2) void adapters_back_y_k
   };
   int i = first;
   while (is_real()) {
-   begin(tile.group);
-   fetch();
-   for (bool more = true; more; ++i) {
-    tiles_.look(i);
-    if (works) dy.put(lds, tile.count, m, g);
-    // h as an operand, its tokens in the transposed tile's order
+    begin(tile.group);
+    fetch();
+    for (bool more = true; more; ++i) {
+      tiles_.look(i);
+      if (works) dy.put(lds, tile.count, m, g);
+      // h as an operand, its tokens in the transposed tile's order
 #pragma unroll
-    for (int u = 0; u < kHBlocks; ++u) {
-      const int r = wave + u * kWaves;
-      if (r >= kBlocks) continue;
-      bf16x8_t piece[3];
-      split_bf16(hv[u], piece);
+      for (int u = 0; u < kHBlocks; ++u) {
+        const int r = wave + u * kWaves;
+        if (r >= kBlocks) continue;
+        bf16x8_t piece[3];
+        split_bf16(hv[u], piece);
 #pragma unroll
-      for (int s = 0; s < 3; ++s) factor[s][r][lane] = piece[s];
-    }
-    tiles_.advance();
-    more = is_real() && tile.group == group;
-    if (more) fetch();
-    __syncthreads();
-    floatx4_t part[2][kBlocks];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < kBlocks; ++r) part[j][r] = floatx4_t{0, 0, 0, 0};
-    if (works) {
-#pragma unroll
-      for (int s = 0; s < kCols / 2; ++s)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const bf16x8_t v = lds.plain(m + 16 * j, s, g);
-#pragma unroll
-          for (int r = 0; r < kBlocks; ++r) part[j][r] = mfma(bt[r][s], v, part[j][r]);
-        }
-      add_products<kCols, kBlocks>(acc, lds, lane, [&](int r, int s) { return factor[s][r][lane]; });
-      wave_order();
-    }
-#pragma unroll
-    for (int round = 0; round < kRounds; ++round) {
-      if (round) __syncthreads();
-#pragma unroll
-      for (int v = 0; v < kShared; ++v) {
-        const int at = round * kShared + v;
-        share[wave][v][lane] = part[at / kBlocks][at % kBlocks];
+        for (int s = 0; s < 3; ++s) factor[s][r][lane] = piece[s];
       }
+      tiles_.advance();
+      more = is_real() && tile.group == group;
+      if (more) fetch();
       __syncthreads();
-      floatx4_t* to_ = q.ws + q.d.share + (((int64_t)chunk * q.d.tiles + i) * kRounds + round) * kShared * kWave;
-      for (int k = threadIdx.x; k < kShared * kWave; k += kWaves * kWave) {
-        floatx4_t v = share[0][k / kWave][k % kWave];
+      floatx4_t part[2][kBlocks];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += share[w][k / kWave][k % kWave];
-        to_[k] = v;
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < kBlocks; ++r) part[j][r] = floatx4_t{0, 0, 0, 0};
+      if (works) {
+#pragma unroll
+        for (int s = 0; s < kCols / 2; ++s)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const bf16x8_t v = lds.plain(m + 16 * j, s, g);
+#pragma unroll
+            for (int r = 0; r < kBlocks; ++r) part[j][r] = mfma(bt[r][s], v, part[j][r]);
+          }
+        add_products<kCols, kBlocks, false>(acc, lds, lane, [&](int r, int s) { return factor[s][r][lane]; });
+        wave_order();
+      }
+#pragma unroll
+      for (int round = 0; round < kRounds; ++round) {
+        if (round) __syncthreads();
+#pragma unroll
+        for (int v = 0; v < kShared; ++v) {
+          const int at = round * kShared + v;
+          share[wave][v][lane] = part[at / kBlocks][at % kBlocks];
+        }
+        __syncthreads();
+        floatx4_t* to_ = q.ws + q.d.share + (((int64_t)chunk * q.d.tiles + i) * kRounds + round) * kShared * kWave;
+        for (int k = threadIdx.x; k < kShared * kWave; k += kWaves * kWave) {
+          floatx4_t v = share[0][k / kWave][k % kWave];
+#pragma unroll
+          for (int w = 1; w < kWaves; ++w) v += share[w][k / kWave][k % kWave];
+          to_[k] = v;
+        }
       }
     }
-   }
-   flush();
+    flush();
   }
 }
 
@@ -431,7 +448,8 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
 
 template <int kChunks>
 __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(BackArgs q) {
-  constexpr int kBlocks = 2 * kChunks, kCols = cols_of(kChunks);
+  constexpr int kBlocks = 2 * kChunks, kCols = x_cols(kChunks);
+  constexpr bool kHeld = kChunks == 1;   // g's pieces fit in registers
   __shared__ __attribute__((aligned(16))) uint8_t tiles[kXWaves][kAdapterTile * TileLds<kCols>::kRow];
   const AdapterBackArgs& p = q.p;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -491,79 +509,87 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
   Tile& tile = tiles_.tile;
   Tokens& tokens = tiles_.tokens;
   Rows<kCols> x;
+  const auto piece3 = [&](int i, int r, int s) {
+    return __builtin_bit_cast(bf16x8_t, q.ws[q.d.pieces3 + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane]);
+  };
   int i = first;
   while (tile.count) {
-   begin(tile.group);
-   const bool real = group < p.t.adapters;
-   if (real) x.load(p.x, p.x_stride, tokens, col0, p.K, m, g);
-   for (bool more = true; more; ++i) {
-    tiles_.look(i);
-    const Tile now = tile;
-    const Tokens of_now = tokens;
-    Rows<kCols> add;
-    if (p.past) {
-      add.load(p.past, p.past_stride, of_now, col0, p.K, m, g);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) add.v[k].w = typename LaneRun<kCols>::words_t{};
-    }
-    bf16x8_t two[2][kChunks][2];
-    if (real) {
-#pragma unroll
-      for (int h = 0; h < kChunks; ++h)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-            two[j][h][s] = __builtin_bit_cast(
-                bf16x8_t, q.ws[q.d.pieces2 + (((int64_t)i * kChunks + h) * 2 + j) * 2 * kWave + s * kWave + lane]);
-      wave_order();
-      x.put(lds, now.count, m, g);
-      wave_order();
-    }
-    tiles_.advance();
-    more = tile.count && tile.group == group;
-    if (more && real) x.load(p.x, p.x_stride, tokens, col0, p.K, m, g);
-    if (real) {
-      add_products<kCols, kBlocks>(acc, lds, lane, [&](int r, int s) {
-        return __builtin_bit_cast(
-            bf16x8_t, q.ws[q.d.pieces3 + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane]);
-      });
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    begin(tile.group);
+    const bool real = group < p.t.adapters;
+    if (real) x.load(p.x, p.x_stride, tokens, col0, p.K, m, g);
+    for (bool more = true; more; ++i) {
+      tiles_.look(i);
+      const Tile now = tile;
+      const Tokens of_now = tokens;
+      // g's operands first, past after them: loads come back in order
+      bf16x8_t two[2][kChunks][2], three[kHeld ? kBlocks : 1][3];
       if (real) {
-        // two columns of a lane's rows at a time
 #pragma unroll
-        for (int c = 0; c < kCols; c += 2) {
-          floatx4_t d[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        for (int r = 0; r < (kHeld ? kBlocks : 0); ++r)
 #pragma unroll
-          for (int h = 0; h < kChunks; ++h)
+          for (int s = 0; s < 3; ++s) three[r][s] = piece3(i, r, s);
 #pragma unroll
-            for (int s = 1; s >= 0; --s)
+        for (int h = 0; h < kChunks; ++h)
 #pragma unroll
-              for (int u = 0; u < 2; ++u) d[u] = mfma(two[j][h][s], at[c + u][h], d[u]);
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            LaneRun<kCols>& o = add.v[4 * j + k];
-            o.w[c / 2] = pack_bf16(o.value(c) + d[0][k], o.value(c + 1) + d[1][k]);
-          }
-        }
-      } else if (now.group > p.t.adapters) {
+            for (int s = 0; s < 2; ++s)
+              two[j][h][s] = __builtin_bit_cast(
+                  bf16x8_t, q.ws[q.d.pieces2 + (((int64_t)i * kChunks + h) * 2 + j) * 2 * kWave + s * kWave + lane]);
+        wave_order();
+        x.put(lds, now.count, m, g);
+        wave_order();
+      }
+      Rows<kCols> add;
+      if (p.past) {
+        add.load(p.past, p.past_stride, of_now, col0, p.K, m, g);
+      } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int c = 0; c < kCols / 2; ++c) add.v[4 * j + k].w[c] = 0x7FC07FC0u;   // NaN
+        for (int k = 0; k < 8; ++k) add.v[k].w = typename LaneRun<kCols>::words_t{};
+      }
+      tiles_.advance();
+      more = tile.count && tile.group == group;
+      if (more && real) x.load(p.x, p.x_stride, tokens, col0, p.K, m, g);
+      if (real) {
+        add_products<kCols, kBlocks, kHeld>(acc, lds, lane, [&](int r, int s) {
+          if constexpr (kHeld) return three[r][s];
+          else return piece3(i, r, s);
+        });
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int64_t token = of_now.row(g + 4 * k + 16 * j);
-        if (g + 4 * k + 16 * j < now.count)
-          add.v[4 * j + k].store(p.dx + token * p.dx_stride, col0 + kCols * m, p.K, col0 + 16 * kCols <= p.K);
+      for (int j = 0; j < 2; ++j) {
+        if (real) {
+          // two columns of a lane's rows at a time
+#pragma unroll
+          for (int c = 0; c < kCols; c += 2) {
+            floatx4_t d[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+            for (int h = 0; h < kChunks; ++h)
+#pragma unroll
+              for (int s = 1; s >= 0; --s)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) d[u] = mfma(two[j][h][s], at[c + u][h], d[u]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              LaneRun<kCols>& o = add.v[4 * j + k];
+              o.w[c / 2] = pack_bf16(o.value(c) + d[0][k], o.value(c + 1) + d[1][k]);
+            }
+          }
+        } else if (now.group > p.t.adapters) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int c = 0; c < kCols / 2; ++c) add.v[4 * j + k].w[c] = 0x7FC07FC0u;   // NaN
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t token = of_now.row(g + 4 * k + 16 * j);
+          if (g + 4 * k + 16 * j < now.count)
+            add.v[4 * j + k].store(p.dx + token * p.dx_stride, col0 + kCols * m, p.K, col0 + 16 * kCols <= p.K);
+        }
       }
     }
-   }
-   flush();
+    flush();
   }
 }
 
@@ -572,9 +598,10 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
 // One thread a place of four rank elements of a column; db first, then da.
 template <int kChunks>
 __global__ __launch_bounds__(256) void adapters_back_sums_kernel(BackArgs q) {
-  constexpr int kBlocks = 2 * kChunks, kCols = cols_of(kChunks);
+  constexpr int kBlocks = 2 * kChunks;
   const AdapterBackArgs& p = q.p;
-  const int64_t per_n = (int64_t)q.d.units_n * kCols * kBlocks * kWave, per_x = (int64_t)q.d.units_x * kCols * kBlocks * kWave;
+  const int64_t per_n = (int64_t)q.d.units_n * cols_of(kChunks) * kBlocks * kWave;
+  const int64_t per_x = (int64_t)q.d.units_x * x_cols(kChunks) * kBlocks * kWave;
   const int64_t all = p.t.adapters * (per_n + per_x);
   for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
     const bool is_db = id < p.t.adapters * per_n;
@@ -632,7 +659,8 @@ hipError_t launch_back(const BackArgs& q, hipStream_t stream) {
                         dim3(kXWaves * kWave), stream, q);
   }
   if (e != hipSuccess) return e;
-  const int64_t places = (int64_t)q.p.t.adapters * (q.d.units_n + q.d.units_x) * cols_of(kChunks) * 2 * kChunks * kWave;
+  const int64_t columns = (int64_t)q.d.units_n * cols_of(kChunks) + (int64_t)q.d.units_x * x_cols(kChunks);   // 16s
+  const int64_t places = q.p.t.adapters * columns * 2 * kChunks * kWave;
   if (places == 0) return hipSuccess;
   const int64_t wgs = (places + 255) / 256, most = 1 << 20;
   return launch_kernel(adapters_back_sums_kernel<kChunks>, dim3((unsigned)(wgs < most ? wgs : most)), dim3(256), stream, q);

@@ -40,10 +40,11 @@ struct Weights {
   }
 };
 
-// Sizes of a call: its tokens, or false.  Without a plan tiles start at every
-// 32nd token, with one every adapter starts a tile.
+// Sizes of a call, and its tokens.  Without a plan tiles start at every 32nd
+// token, with one every adapter starts a tile.
 bool sized(int64_t tokens, int64_t adapters, int planned, int64_t N, int64_t K, int64_t rank, solfp4::AdapterTokens* t) {
-  if (adapter_dims(tokens, adapters) || rank < 1 || rank > solfp4::kAdapterMaxRank || N < 0 || K < 0 || N >= solfp4::kAdapterMaxFeatures || K >= solfp4::kAdapterMaxFeatures) return false;
+  if (adapter_dims(tokens, adapters) || rank < 1 || rank > solfp4::kAdapterMaxRank) return false;
+  if (N < 0 || K < 0 || N >= solfp4::kAdapterMaxFeatures || K >= solfp4::kAdapterMaxFeatures) return false;
   *t = solfp4::adapter_tokens(planned ? t : nullptr, tokens, adapters);
   return true;
 }

@@ -29,6 +29,12 @@ and the attention runs in the library:
     q, k rotated in place, interleaved pairs at positions 0 .. tokens - 1
     x, h = add_rmsnorm(x, linear(a), g2); d = linear(gelu_tanh(linear(h)))
 "mxfp4" norms write the linears' codes (no quantizer pass of their own).
+layer_norm=True takes add_layernorm instead, with a shift beside each gain (the
+modulation makes four vectors a rollout); adapters=n puts low-rank adapters of n
+policies beside the QKV and output linears, rollout i taking those of policy
+i % n over the same quantized weights (the norm before the QKV linear then
+writes BF16, which the adapters read too):
+    qkv = linear(h) + scale b (a h);  o = linear(a) + scale b (a a)
 
 Euler step with T steps: x <- x + (1/T) * (blocks(x) - x).
 Reward of rollout i: mean over its tokens of <x_final[token], u> for a fixed
@@ -47,6 +53,7 @@ from . import _binding as sol
 
 BACKENDS = ("bf16", "nvfp4", "mxfp4")
 EPS = 1e-6
+ADAPTER_ALPHA = 64.0
 
 
 @dataclass(frozen=True)
@@ -62,6 +69,9 @@ class Stage1Config:
     w_sigma: float = 0.015
     seed: int = 5000
     conditioned: bool = False   # norms modulated per rollout and step, rotary positions
+    layer_norm: bool = False    # conditioned: layer norms with a shift, not root-mean-square ones
+    adapters: int = 0           # conditioned: policies whose low-rank adapters the rollouts take in turn
+    rank: int = 32              # of the adapters, scaled by ADAPTER_ALPHA / rank
 
     @property
     def head_dim(self):
@@ -75,8 +85,14 @@ def layer_shapes(cfg):
 
 
 def condition_shape(cfg):
-    """(N, K) of a conditioned block's modulation: two gains from the condition."""
-    return 2 * cfg.hidden, cfg.hidden
+    """(N, K) of a conditioned block's modulation: two gains from the
+    condition, and with layer norms two shifts."""
+    return (4 if cfg.layer_norm else 2) * cfg.hidden, cfg.hidden
+
+
+def adapter_shapes(cfg):
+    """(name, N, K) of the linears with adapters beside them."""
+    return [(name, N, K) for name, N, K in layer_shapes(cfg) if name in ("qkv", "out")]
 
 
 def linear_flops(cfg):
@@ -120,8 +136,14 @@ def make_weights(cfg, device):
         if cfg.conditioned:
             N, K = condition_shape(cfg)
             w = _bf16_dev(draw_weights(N, K, cfg.w_sigma, cfg.seed + 100 * b + 90), device)
-            # gains around 1
-            blk["mod"] = (w, 1 + _bf16_dev(draw_bias(N, cfg.w_sigma, cfg.seed + 100 * b + 91), device))
+            # gains around 1, shifts around 0
+            bias = _bf16_dev(draw_bias(N, cfg.w_sigma, cfg.seed + 100 * b + 91), device)
+            bias[: 2 * cfg.hidden] += 1
+            blk["mod"] = (w, bias)
+            for j, (name, N, K) in enumerate(adapter_shapes(cfg) if cfg.adapters else ()):
+                seed, n, r = cfg.seed + 100 * b + 92 + 2 * j, cfg.adapters, cfg.rank
+                a, up = draw_weights(n * r, K, K ** -0.5, seed), draw_weights(n * N, r, cfg.w_sigma, seed + 1)
+                blk[name + " adapters"] = (_bf16_dev(a, device).view(n, r, K), _bf16_dev(up, device).view(n, N, r))
         model.append(blk)
     return model
 
@@ -145,6 +167,8 @@ class Runner:
     def __init__(self, cfg, model, backend, device):
         if backend not in BACKENDS:
             raise ValueError(backend)
+        if (cfg.layer_norm or cfg.adapters) and not cfg.conditioned:
+            raise ValueError("layer_norm and adapters: for conditioned blocks only")
         self.cfg, self.backend, self.device = cfg, backend, device
         M = cfg.rollouts * cfg.tokens
         self.M = M
@@ -189,8 +213,9 @@ class Runner:
                     "bf16": lambda w: (w.t().contiguous(),)}[self.backend]
         for L, blk in zip(self.layers, model):
             L["mod"] = (quantize(blk["mod"][0]), blk["mod"][1])
+            L.update({name: blk[name] for name in blk if name.endswith(" adapters")})
         self.time, self.text = make_condition(cfg, dev)
-        self.gains = torch.empty((R, 2 * H), **bf16)
+        self.gains = torch.empty((R, condition_shape(cfg)[0]), **bf16)
         self.buf["x"] = torch.empty((self.M, H), **bf16)
         if self.backend == "mxfp4":
             self.c = (torch.empty((R, H), **u8), torch.empty((R, H // 32), **u8))
@@ -198,6 +223,13 @@ class Runner:
         else:
             self.c = (torch.empty((R, H), **bf16),)
             self.h = (torch.empty((self.M, H), **bf16),)
+        self.h16 = self.h                # the QKV linear's input
+        if cfg.adapters:
+            if self.backend == "mxfp4":
+                self.h16 = (torch.empty((self.M, H), **bf16),)
+            policy = torch.arange(R, dtype=torch.int32, device=dev) % cfg.adapters
+            self.plan = sol.adapter_plan(policy.repeat_interleave(cfg.tokens), cfg.adapters)
+            self.scales = torch.full((cfg.adapters,), ADAPTER_ALPHA / cfg.rank, device=dev)
         self.table = sol.rotary_table(sol.rotary_frequencies(cfg.head_dim), cfg.tokens, device=dev)
         self.set_step(0)
 
@@ -214,7 +246,8 @@ class Runner:
         _end(ev)
 
     def _modulate(self, layer):
-        """The two gains [rollouts, hidden] of one block."""
+        """(gain, shift) [rollouts, hidden] of one block's two norms; no
+        shift without layer norms."""
         q, b = layer
         H = self.cfg.hidden
         ev = self._op("modulation")
@@ -225,42 +258,54 @@ class Runner:
         else:
             torch.addmm(b, *self.c, *q, out=self.gains)
         _end(ev)
-        return self.gains[:, :H], self.gains[:, H:]
+        v = [self.gains[:, i * H: (i + 1) * H] for i in range(self.gains.shape[1] // H)]
+        return ((v[0], v[2]), (v[1], v[3])) if self.cfg.layer_norm else ((v[0],), (v[1],))
 
-    def _norm(self, x, residual, gain):
-        """(x + residual, its norm as the linears take it)."""
+    def _norm(self, x, residual, modulation, out):
+        """x + residual, its norm in `out` (BF16, or MXFP4 codes and scales)."""
         total = None if residual is None else self.buf["x"]
         ev = self._op("norm")
-        if self.backend == "mxfp4":
-            sol.mxfp4_add_rmsnorm(x, residual, gain, EPS, *self.h, total)
+        if self.cfg.layer_norm:
+            norm = sol.mxfp4_add_layernorm if len(out) == 2 else sol.add_layernorm
         else:
-            sol.add_rmsnorm(x, residual, gain, EPS, *self.h, total)
+            norm = sol.mxfp4_add_rmsnorm if len(out) == 2 else sol.add_rmsnorm
+        norm(x, residual, *modulation, EPS, *out, sum_out=total)
         _end(ev)
         return x if residual is None else total
 
-    def _trace_norm(self, name):
-        for t, part in zip(self.h, ("", " scales")):
+    def _trace_norm(self, name, h):
+        for t, part in zip(h, ("", " scales")):
             self._t(name + part, t)
 
-    def _linear_of_norm(self, layer, out):
-        if self.backend != "mxfp4":
-            return self.linear(self.h[0], layer, out)
+    def _linear_of_norm(self, h, layer, out):
+        if len(h) == 1:
+            return self.linear(h[0], layer, out)
         q, b, _, _ = layer
         ev = self._linear_event()
-        sol.mxfp4_gemm(*self.h, *q, b, out)
+        sol.mxfp4_gemm(*h, *q, b, out)
         _end(ev)
         return out
+
+    def _adapted(self, name, L, x, y):
+        """y and, in its place, what the adapters beside this linear add for x."""
+        if self.cfg.adapters:
+            self._t(name + " linear", y)
+            ev = self._op("adapters")
+            sol.add_adapters(y, x, *L[name + " adapters"], self.scales, self.plan, out=y)
+            _end(ev)
+        return y
 
     def _conditioned_blocks(self, x):
         cfg, B = self.cfg, self.buf
         R, T, Hh, hd = cfg.rollouts, cfg.tokens, cfg.heads, cfg.head_dim
         d = None
         for L in self.layers:
-            g1, g2 = self._modulate(L["mod"])
+            m1, m2 = self._modulate(L["mod"])
             self._t("gains", self.gains)
-            x = self._t("x", self._norm(x, None, g1) if d is None else self._norm(d, x, g1))
-            self._trace_norm("h1")
-            qkv = self._linear_of_norm(L["qkv"], B["qkv"])
+            h = self.h16
+            x = self._t("x", self._norm(x, None, m1, h) if d is None else self._norm(d, x, m1, h))
+            self._trace_norm("h1", h)
+            qkv = self._adapted("qkv", L, h[0], self._linear_of_norm(h, L["qkv"], B["qkv"]))
             self._t("qkv", qkv)
             heads = qkv.view(R * T, 3, Hh, hd)
             ev = self._op("rotary")
@@ -275,10 +320,10 @@ class Runner:
             ev = self._op("copy")
             a = self._t("a", a.transpose(1, 2).reshape(R * T, cfg.hidden))
             _end(ev)
-            o = self._t("o", self.linear(a, L["out"], B["o"]))
-            x = self._t("x2", self._norm(o, x, g2))
-            self._trace_norm("h2")
-            u = self._t("up", self._linear_of_norm(L["up"], B["u"]))
+            o = self._t("o", self._adapted("out", L, a, self.linear(a, L["out"], B["o"])))
+            x = self._t("x2", self._norm(o, x, m2, self.h))
+            self._trace_norm("h2", self.h)
+            u = self._t("up", self._linear_of_norm(self.h, L["up"], B["u"]))
             fused = self.backend == "nvfp4"
             ev = self._op("gelu+amax" if fused else "gelu")
             if fused:
