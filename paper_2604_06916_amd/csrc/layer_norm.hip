@@ -340,14 +340,31 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave, 2) void layernorm_backward_k
     }
   }
   // every slot's sums in LDS: each thread adds some columns'
+  const bool narrow = kRuns == 1 && sh.lanes < kWave;   // several slots a wave
+  const int parts_of = narrow ? kNormMaxWaves : slots;
   const auto share = [&](float* partial) {
     float* part_row = partial + (int64_t)blockIdx.x * a.width;
+    if (narrow) {
+      // a wave's slots first, by lane exchange: up to 512 slots one after another took 7 us
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = mine[e / 4][e % 4];
+        for (int hop = sh.lanes; hop < kWave; hop *= 2) v[e] += __shfl_xor(v[e], hop, kWave);
+      }
+      __syncthreads();
+      floatx4_t* to = reinterpret_cast<floatx4_t*>(fold[0] + at_.wave * cols + lane * 8);
+      if ((threadIdx.x & (kWave - 1)) < sh.lanes) {
+        to[0] = floatx4_t{v[0], v[1], v[2], v[3]};
+        to[1] = floatx4_t{v[4], v[5], v[6], v[7]};
+      }
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
       for (int c = threadIdx.x; c < cols; c += kNormMaxWaves * kWave) {
         float t = fold[i][c];
-        for (int z = 1; z < slots; ++z) t += fold[i][z * cols + c];
+        for (int z = 1; z < parts_of; ++z) t += fold[i][z * cols + c];
         if (i * step + c < a.width) part_row[i * step + c] = t;
       }
     }
