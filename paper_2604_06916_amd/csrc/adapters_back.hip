@@ -408,9 +408,17 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
     const int lane = k % kWave, jc = k / kWave, j = jc / kChunks, c = jc % kChunks;
     const int at = (j * kBlocks + 2 * c) * kWave + lane;
     floatx4_t lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-    for (int n = 0; n < q.d.chunks_n; ++n) {
-      lo += from[n * hop + at];
-      hi += from[n * hop + at + kWave];
+    // in order, eight workgroups' loads at a time (one by one each waits for the one before)
+    for (int n = 0; n < q.d.chunks_n; n += 8) {
+      floatx4_t u[2][8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool has = n + i < q.d.chunks_n;
+        u[0][i] = has ? from[(n + i) * hop + at] : floatx4_t{0, 0, 0, 0};
+        u[1][i] = has ? from[(n + i) * hop + at + kWave] : floatx4_t{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lo += u[0][i], hi += u[1][i];
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
