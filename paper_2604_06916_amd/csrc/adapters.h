@@ -111,7 +111,8 @@ struct Tile {
   int group, first, count;
 };
 
-// As read, without waiting for it: made uniform where it is used.
+// As read, without waiting for it: made uniform, and within the plan's bounds,
+// where it is used.
 __device__ __forceinline__ Tile load_tile(const AdapterTokens& t, int i) {
   if (t.plan) {
     const int* p = t.plan + t.tiles_at + 4 * (int64_t)i;
@@ -121,14 +122,20 @@ __device__ __forceinline__ Tile load_tile(const AdapterTokens& t, int i) {
   return {0, (int)first, (int)(left < kAdapterTile ? left : kAdapterTile)};
 }
 
-__device__ __forceinline__ Tile uniform(Tile t) {
-  return {__builtin_amdgcn_readfirstlane(t.group), __builtin_amdgcn_readfirstlane(t.first),
-          __builtin_amdgcn_readfirstlane(t.count)};
+// A plan's memory that no call has written yet (a captured one before its first
+// replay) may hold anything: wrong results, but no access outside the operands.
+__device__ __forceinline__ Tile uniform(const AdapterTokens& t, Tile tile) {
+  const uint32_t group = (uint32_t)__builtin_amdgcn_readfirstlane(tile.group);
+  const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane(tile.first);
+  const uint32_t count = (uint32_t)__builtin_amdgcn_readfirstlane(tile.count);
+  const uint32_t place = min(first, (uint32_t)t.tokens - 1u);
+  return {(int)min(group, (uint32_t)t.adapters + 1u), (int)place,
+          (int)min(min(count, (uint32_t)kAdapterTile), (uint32_t)t.tokens - place)};
 }
 
 // The token at place `at` of the order.
 __device__ __forceinline__ int64_t token_at(const AdapterTokens& t, int at) {
-  return t.plan ? t.plan[t.order_at + at] : at;
+  return t.plan ? min((uint32_t)t.plan[t.order_at + at], (uint32_t)t.tokens - 1u) : (uint32_t)at;
 }
 
 }  // namespace solfp4

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(Adapter
   const int ranges = kPart == kShares ? p.k_splits : p.splits, at = blockIdx.x / p.xcds;
   const int index = at / ranges * p.xcds + blockIdx.x % p.xcds, split = at % ranges;
   if (index >= p.t.max_tiles) return;
-  const Tile tile = uniform(load_tile(p.t, index));
+  const Tile tile = uniform(p.t, load_tile(p.t, index));
   if (tile.count == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int m = lane % 16, g = lane / 16;

@@ -157,12 +157,12 @@ struct Tiles {
   Tokens tokens, tokens_next, tokens_later;
   __device__ __forceinline__ Tile at(int i) const { return i < end ? load_tile(t, i) : Tile{0, 0, 0}; }
   __device__ __forceinline__ Tiles(const AdapterTokens& t, int first, int end, int lane) : t(t), end(end), lane(lane) {
-    tile = uniform(at(first)), next = uniform(at(first + 1)), raw = at(first + 2);
+    tile = uniform(t, at(first)), next = uniform(t, at(first + 1)), raw = at(first + 2);
     if (tile.count) tokens.load(t, tile, lane);
     if (next.count) tokens_next.load(t, next, lane);
   }
   __device__ __forceinline__ void look(int i) {   // at work on tile i
-    later = uniform(raw);
+    later = uniform(t, raw);
     if (later.count) tokens_later.load(t, later, lane);
     raw = at(i + 3);
   }
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
   __shared__ float gs[kAdapterTile][kRow];
   const AdapterBackArgs& p = q.p;
   const int i = blockIdx.x;
-  const Tile tile = uniform(load_tile(p.t, i));
+  const Tile tile = uniform(p.t, load_tile(p.t, i));
   if (tile.count == 0 || tile.group >= p.t.adapters) return;
   const float scale = p.scales ? p.scales[tile.group] : 1.0f;
   const floatx4_t* from = q.ws + q.d.share + (int64_t)i * 2 * kBlocks * kWave;
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256) void adapters_back_sums_kernel(BackArgs q) {
     const int e = (int)(k / per);
     const int64_t place = k - e * per;
     int begin = 0, end = (int)q.d.tiles;   // the adapter's tiles
-    if (p.t.plan) begin = p.t.plan[e], end = p.t.plan[e + 1];
+    if (p.t.plan) begin = max(p.t.plan[e], 0), end = min(p.t.plan[e + 1], end);
     floatx4_t v = {0, 0, 0, 0};
     if (begin < end) {
       const int each = is_db ? q.d.each_n : q.d.each_x;

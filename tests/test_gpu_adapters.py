@@ -273,3 +273,29 @@ def test_graph_replay_with_a_plan_written_again():
         want = sol.add_adapters(y, x, a, b, c, sol.adapter_plan(index, adapters), hidden=True)
         torch.cuda.synchronize()
         assert all(torch.equal(p.nan_to_num(7.0), q.nan_to_num(7.0)) for p, q in zip(held, want))
+
+
+@pytest.mark.parametrize("fill", ["zeros", "any"])
+def test_plan_that_is_not_written_yet(fill):
+    """The memory of a plan that only a graph has written so far may hold anything: what the calls give is
+    undefined, but nothing outside their outputs is written and every kernel ends."""
+    tokens, adapters, K, N, rank = 300, 5, 200, 130, 16
+    x, y, dy = draw(1, tokens, K), draw(2, tokens, N), draw(3, tokens, N)
+    a, b, c = weights(4, adapters, rank, K, N)
+    plan = sol.adapter_plan(index_of(6, tokens, adapters, "any"), adapters)
+    g = torch.Generator().manual_seed(7)
+    n = plan.buffer.numel()
+    plan.buffer.copy_(torch.randint(-2 ** 31, 2 ** 31, (n,), generator=g) if fill == "any" else torch.zeros(n))
+    room, dx_room = (torch.full((tokens + 2, w + 8), 3.0, dtype=BF16, device=device()) for w in (N, K))
+    out, dx = room[1:-1, 4:-4], dx_room[1:-1, 4:-4]
+    say(f"  plan of {fill}")
+    _, hidden = sol.add_adapters(y, x, a, b, c, plan, hidden=True, out=out)
+    hidden.zero_()
+    _, da, db = sol.adapters_backward(dy, x, hidden, a, b, c, plan, dx=dx)
+    torch.cuda.synchronize()
+    for whole in (room, dx_room):
+        edges = whole.clone()
+        edges[1:-1, 4:-4] = 3.0
+        assert bool((edges == 3.0).all())
+    if fill == "zeros":   # no token has a tile
+        assert bool((out == 3.0).all()) and bool((dx == 3.0).all()) and not da.any() and not db.any()
