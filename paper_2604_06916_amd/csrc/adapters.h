@@ -133,9 +133,13 @@ __device__ __forceinline__ Tile uniform(const AdapterTokens& t, Tile tile) {
           (int)min(min(count, (uint32_t)kAdapterTile), (uint32_t)t.tokens - place)};
 }
 
-// The token at place `at` of the order.
-__device__ __forceinline__ int64_t token_at(const AdapterTokens& t, int at) {
-  return t.plan ? min((uint32_t)t.plan[t.order_at + at], (uint32_t)t.tokens - 1u) : (uint32_t)at;
+// The token at place `at` of the order: as read, and within its bounds.
+__device__ __forceinline__ uint32_t raw_token(const AdapterTokens& t, int at) {
+  return t.plan ? (uint32_t)t.plan[t.order_at + at] : (uint32_t)at;
 }
+__device__ __forceinline__ uint32_t bounded_token(const AdapterTokens& t, uint32_t token) {
+  return t.plan ? min(token, (uint32_t)t.tokens - 1u) : token;
+}
+__device__ __forceinline__ int64_t token_at(const AdapterTokens& t, int at) { return bounded_token(t, raw_token(t, at)); }
 
 }  // namespace solfp4
