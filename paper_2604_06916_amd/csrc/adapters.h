@@ -52,6 +52,26 @@ struct LaneRun {
       for (int i = 0; i < kCols / 2; ++i) w[i] = v[i];
     }
   }
+  // The same in two steps, so that the first waits for nothing: near the row's end
+  // its last kCols values, which settle() then moves down.
+  __device__ __forceinline__ void load_raw(const uint16_t* row, uint32_t col, uint32_t end) {
+    if (end < kCols) load(row, col, end, false);
+    else w = *reinterpret_cast<const words_at2_t*>(row + min(col, end - kCols));
+  }
+  __device__ __forceinline__ void settle(uint32_t col, uint32_t end) {
+    if (end < kCols) return;
+    const uint32_t by = col - min(col, end - kCols);
+    constexpr int kWords = kCols / 2;
+#pragma unroll
+    for (int hop = kWords / 2; hop; hop /= 2)
+      if (by & 2 * hop)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = i + hop < kWords ? w[i + hop] : 0;
+    if (by & 1)
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = i + 1 < kWords ? __builtin_amdgcn_alignbit(w[i + 1], w[i], 16) : w[i] >> 16;
+    if (by >= kCols) w = words_t{};
+  }
   __device__ __forceinline__ float value(int e) const {
     return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
   }

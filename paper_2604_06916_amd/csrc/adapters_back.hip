@@ -180,15 +180,30 @@ struct Tiles {
 template <int kCols>
 struct Rows {
   LaneRun<kCols> v[8];
+  // kRaw: settle() is called before the first use.
+  template <bool kRaw = false>
   __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, const Tokens& tokens, int col0, int cols,
                                        int m, int g) {
     if (col0 + 16 * kCols <= cols) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i].load(base + tokens.row(g + 4 * i) * stride, col0 + kCols * m, cols, true);
-    } else {
+    } else if constexpr (!kRaw) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i].load(base + tokens.row(g + 4 * i) * stride, col0 + kCols * m, cols, false);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i].load_raw(base + tokens.row(g + 4 * i) * stride, col0 + kCols * m, cols);
     }
+  }
+  // Before the first use, and not at once: that waits for the loads, and all
+  // waves for the one with the row's end (8192 tokens 2240 -> 6720, where it has 64
+  // of its 128 columns, 109 us, so 87).  In the second pass, whose waves do not
+  // wait for each other, rows' ends are moved at once: with this there its rows
+  // of whole lines lost 3%.
+  __device__ __forceinline__ void settle(int col0, int cols, int m) {
+    if (col0 + 16 * kCols <= cols) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i].settle(col0 + kCols * m, cols);
   }
   // to LDS, with zeros in the place of tokens past the tile's end
   __device__ __forceinline__ void put(const TileLds<kCols>& lds, int count, int m, int g) {
@@ -331,7 +346,7 @@ __global__ __launch_bounds__(y_waves(kChunks) * kWave, 2) void adapters_back_y_k
         hv[u][k] = t < tile.count && at < p.rank ? p.hidden[token * p.rank + at] : 0.0f;
       }
     }
-    if (works) dy.load(p.dy, p.dy_stride, tokens, col0, p.N, m, g);
+    if (works) dy.template load<true>(p.dy, p.dy_stride, tokens, col0, p.N, m, g);
   };
   int i = first;
   while (is_real()) {
@@ -339,7 +354,10 @@ __global__ __launch_bounds__(y_waves(kChunks) * kWave, 2) void adapters_back_y_k
     fetch();
     for (bool more = true; more; ++i) {
       tiles_.look(i);
-      if (works) dy.put(lds, tile.count, m, g);
+      if (works) {
+        dy.settle(col0, p.N, m);
+        dy.put(lds, tile.count, m, g);
+      }
       // h as an operand, its tokens in the transposed tile's order
 #pragma unroll
       for (int u = 0; u < kHBlocks; ++u) {
