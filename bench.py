@@ -85,7 +85,10 @@ KERNEL_SOURCES = {
     "mx_gemm.hip": ("mx_gemm.hip", "device_common.h"),
     "quantize.hip": ("quantize.hip", "device_common.h"),
     "mx_quantize.hip": ("mx_quantize.hip", "device_common.h"),
-    "norm.hip": ("norm.hip", "elements.h", "device_common.h"),
+    "norm.hip": ("norm.hip", "norm_common.h", "elements.h", "device_common.h"),
+    "layer_norm.hip": ("layer_norm.hip", "norm_common.h", "elements.h", "device_common.h"),
+    "adapters.hip": ("adapters.hip", "adapters.h", "elements.h", "device_common.h"),
+    "adapters_back.hip": ("adapters_back.hip", "adapters.h", "elements.h", "device_common.h"),
     "rotary.hip": ("rotary.hip", "elements.h", "device_common.h"),
     "weight_linear.hip": ("weight_linear.hip", "elements.h", "device_common.h"),
 }

@@ -1,8 +1,9 @@
 """solfp4: NVFP4 linear layer (quantize, block-scaled GEMM, linear) for
 AMD MI355X, plus its MXFP4 variant on the native scaled FP4 matrix
-instructions, and the operators around it (the norm with the residual's
-addition and its backward pass, rotary positions, linears of few tokens with
-4-bit weights), as a C-ABI HIP library with a thin Python binding.
+instructions, and the operators around it (root-mean-square and layer norm
+with the residual's addition, low-rank adapters beside a linear, the backward
+passes of these, rotary positions, linears of few tokens with 4-bit weights),
+as a C-ABI HIP library with a thin Python binding.
 
 The binding (and so libsolfp4.so) loads on first use of any name below and
 raises ImportError if the library has not been built.

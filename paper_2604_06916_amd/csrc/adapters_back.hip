@@ -11,6 +11,12 @@
 // wave holds 16 kCols columns of da.  The last adds the slices' da and db.
 // All sums have a fixed order, so results are the same on every call.
 //
+// Bound by memory, dy, x and past once in and dx once out, and by how few waves
+// hold it in flight, two workgroups a CU of up to 256 registers: 26574 tokens 2432 ->
+// 7296, rank 32 229 us, 3.4 TB/s (114 to 123 us for dy, 12 for g, 91 for x, 12 for
+// the slices); 8192 tokens 2240 -> 6720 87 us.  With few tokens by the four launches:
+// 1 token 1152 -> 1152 20 us.
+//
 // Both passes multiply by a token's values twice: once with the token's row
 // as it lies in memory (g, dx) and once summed over tokens, for which the row's
 // columns must be lanes and the tokens the reduction: the tile goes through

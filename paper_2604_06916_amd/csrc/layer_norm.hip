@@ -15,7 +15,8 @@
 // since mean(d) is 2^-24 of m.
 //
 // Bound by memory: 8 bytes an element in BF16 with a residual, 7.03 with MXFP8
-// output.
+// output: 8192 x 2240 BF16 in 8 groups 26.8 us, 5.5 TB/s; 26574 x 2432 to MXFP8 93 us,
+// 4.9 TB/s; one row of 1152 4.3 us of which 2.3 are an empty launch.
 #include "norm_common.h"
 
 namespace solfp4 {
@@ -220,8 +221,8 @@ constexpr int kLayerBackRuns = kType == SOLFP4_F32 ? 2 : 6;
 // all of it in registers the kernel spilled (26574 x 2432 BF16 371 us).
 //
 // Bound by memory, 8 bytes an element in BF16 with dsum, and by how few waves
-// hold it in flight: 26574 x 2432 in 6 groups 121 us, 4.3 TB/s; FP32 1009 x 1283
-// 13.4 us.
+// hold it in flight: 26574 x 2432 in 6 groups 120 us, 4.3 TB/s; FP32 1009 x 1283
+// 13.3 us.
 // kWhole: the width is a multiple of 8.
 template <int kType, int kRuns, bool kWhole>
 __global__ __launch_bounds__(kNormMaxWaves * kWave, 2) void layernorm_backward_kernel(LayerNormBackArgs p, RowShape sh) {
