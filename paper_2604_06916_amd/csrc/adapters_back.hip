@@ -37,7 +37,8 @@ namespace {
 // Waves of a workgroup of the first pass: two workgroups a CU that wait for each
 // other's waves less, but more shares of g through the workspace, four times as
 // many values with a rank of 128 (26574 tokens 2432 -> 7296, rank 32: 258 us with 4,
-// 280 with 8; 13000 tokens, rank 64 212 and 201; 6600 tokens, rank 128 392 and 302).
+// 280 with 8; 13000 tokens, rank 64 212 and 201; 6600 tokens, rank 128 392 and 302,
+// before the later steps).
 constexpr int y_waves(int chunks) { return chunks == 1 ? 4 : 8; }
 constexpr int kXWaves = 4;       // of the second, whose waves go by themselves
 
@@ -485,6 +486,9 @@ template <int kChunks>
 __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(BackArgs q) {
   constexpr int kBlocks = 2 * kChunks, kCols = x_cols(kChunks);
   constexpr bool kHeld = kChunks == 1;   // g's pieces fit in registers
+  // g's two pieces half a tile at a time and late, where both halves at once would
+  // spill (8192 tokens 2240 -> 2240, rank 128: 185 us, so 158)
+  constexpr bool kLate = kChunks == 4;
   __shared__ __attribute__((aligned(16))) uint8_t tiles[kXWaves][kAdapterTile * TileLds<kCols>::kRow];
   const AdapterBackArgs& p = q.p;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -557,20 +561,24 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
       const Tile now = tile;
       const Tokens of_now = tokens;
       // g's operands first, past after them: loads come back in order
-      bf16x8_t two[2][kChunks][2], three[kHeld ? kBlocks : 1][3];
+      bf16x8_t two[kLate ? 1 : 2][kChunks][2], three[kHeld ? kBlocks : 1][3];
+      const auto load_two = [&](bf16x8_t(&to)[kChunks][2], int j) {
+#pragma unroll
+        for (int h = 0; h < kChunks; ++h)
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            to[h][s] = __builtin_bit_cast(
+                bf16x8_t, q.ws[q.d.pieces2 + (((int64_t)i * kChunks + h) * 2 + j) * 2 * kWave + s * kWave + lane]);
+      };
       if (real) {
 #pragma unroll
         for (int r = 0; r < (kHeld ? kBlocks : 0); ++r)
 #pragma unroll
           for (int s = 0; s < 3; ++s) three[r][s] = piece3(i, r, s);
-#pragma unroll
-        for (int h = 0; h < kChunks; ++h)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-              two[j][h][s] = __builtin_bit_cast(
-                  bf16x8_t, q.ws[q.d.pieces2 + (((int64_t)i * kChunks + h) * 2 + j) * 2 * kWave + s * kWave + lane]);
+        if constexpr (!kLate) {
+          load_two(two[0], 0);
+          load_two(two[1], 1);
+        }
         wave_order();
         x.put(lds, now.count, m, g);
         wave_order();
@@ -594,6 +602,7 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (real) {
+          if constexpr (kLate) load_two(two[0], j);
           // two columns of a lane's rows at a time
 #pragma unroll
           for (int c = 0; c < kCols; c += 2) {
@@ -603,7 +612,7 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
 #pragma unroll
               for (int s = 1; s >= 0; --s)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) d[u] = mfma(two[j][h][s], at[c + u][h], d[u]);
+                for (int u = 0; u < 2; ++u) d[u] = mfma(two[kLate ? 0 : j][h][s], at[c + u][h], d[u]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               LaneRun<kCols>& o = add.v[4 * j + k];
