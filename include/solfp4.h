@@ -573,7 +573,9 @@ SOLFP4_API size_t solfp4_add_adapters_workspace_bytes(int64_t tokens, int64_t ad
  *   b       [adapters][N][rank] BF16, contiguous
  *   scales  [adapters] FP32; or NULL (all 1)
  *   plan    for these tokens and adapters; or NULL: every token takes the one
- *           adapter (adapters must be 1)
+ *           adapter (adapters must be 1).  A plan that is not written yet (by
+ *           a captured call before its first replay) gives undefined results;
+ *           nothing outside the outputs and the workspace is written
  *   out     [tokens][N] BF16, rows out_stride apart, written; may be y
  *   hidden  [tokens][rank] FP32, written with h (0 for tokens without an
  *           adapter), what the backward pass needs; or NULL
