@@ -498,8 +498,8 @@ SOLFP4_API int solfp4_add_layernorm(int type, const void* x, int64_t x_stride, c
 /*
  * The same with the output quantized in the same pass, width % 32 == 0, codes
  * and scales as mxfp8_add_rmsnorm and mxfp4_add_rmsnorm write them, from the
- * FP32 result.  Squares, rho and a scale that the FP32 result does not decide
- * are formed in 64 bits.
+ * FP32 result.  The mean, squares, rho and, from the unrounded sum, a scale that
+ * the FP32 result does not decide are formed in 64 bits.
  */
 SOLFP4_API int mxfp8_add_layernorm(int type, const void* x, int64_t x_stride, const void* residual,
                    int64_t residual_stride, const void* gain, int64_t gain_stride, const void* shift,

@@ -12,7 +12,8 @@
 // rounded to FP32, so a row far from zero (1000 +- 1) would keep an error of
 // 2^-24 of its mean in every element; with d's own mean taken off, elements
 // are right to 2^-24 of themselves, and mean(d^2) - mean(d)^2 loses nothing,
-// since mean(d) is 2^-24 of m.
+// since mean(d) is 2^-24 of m.  With 8- and 4-bit outputs the sums are in 64 bits,
+// of unrounded differences from a mean that needs no such correction.
 //
 // Bound by memory: 8 bytes an element in BF16 with a residual, 7.03 with MXFP8
 // output: 8192 x 2240 BF16 in 8 groups 26.8 us, 5.5 TB/s; 26574 x 2432 to MXFP8 93 us,
@@ -24,9 +25,11 @@ namespace solfp4 {
 // The E8M0 byte of a 32-element block held by a lane quad, 8 values y = n g + t
 // a lane, as the root-mean-square norm's: floor(log2(amax)) - kEmax + 127, at
 // least 0.  Where y is the difference of two larger numbers its error goes by
-// those: `size` is the lane's largest |n g| + |t|, and y is within 5 roundings
-// of 2^-24 of it (d, its correction, rho, and the product and sum).  An amax
-// within 2^-21 size of a power of two is formed in 64 bits.
+// those: `size` is the lane's largest |n g| + |t| + |off rho g|, off what m lacks
+// to the mean, and y is within 6 roundings of 2^-24 of it (s - m, less off, rho,
+// the two products and the sum; where off outweighs the element, s - m and it
+// once more).  An amax within 2^-21 size of a power of two is formed in 64 bits,
+// from s itself: s - m is rounded, and that alone can reach over the power.
 template <int kEmax, typename F>
 __device__ __forceinline__ uint32_t block_scale(const float (&y)[8], float size, F y64) {
   uint32_t m = 0;
@@ -66,8 +69,9 @@ __device__ __forceinline__ void differences(float (&s)[8], float m, int n, bool 
 template <int kType, int kOut, int kRuns>
 __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(LayerNormArgs p, RowShape sh) {
   using Sum = std::conditional_t<kOut == kNormSame, float, double>;   // block_scale
-  __shared__ Sum lds[kNormMaxWaves][2];
-  __shared__ float lds_mean[kNormMaxWaves][1];
+  constexpr int kSums = kOut == kNormSame ? 2 : 1;   // d where the mean is rounded, and d^2
+  __shared__ Sum lds[kNormMaxWaves][kSums];
+  __shared__ Sum lds_mean[kNormMaxWaves][1];
   const NormArgs& a = p.n;
   const Place<kRuns> at_(sh);
   const int64_t row = a.first + (int64_t)blockIdx.x * sh.waves_slots(blockDim.x / kWave) + at_.slot;
@@ -93,7 +97,7 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(La
     }
   }
   float s[kRuns][8];
-  float mean[1] = {0.0f};
+  Sum mean[1] = {0};
   uint8_t* sr = row_of<kType>(a.sum, at, a.sum_stride);
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
@@ -110,23 +114,39 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(La
     for (int e = 0; e < 8; ++e) mean[0] += s[i][e];
   }
   row_sum<false>(mean, lds_mean, at_.wave, sh);
-  const float m = mean[0] / (float)a.width;
-  Sum q[2] = {0, 0};
+  const Sum mean_ = mean[0] / (Sum)a.width;
+  const float m = (float)mean_;
+  Sum q[kSums] = {};
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    differences(s[i], m, width - (i * step + lane * 8), (a.width & 7) == 0);
+    const int n = width - (i * step + lane * 8);
+    if constexpr (kOut == kNormSame) {
+      differences(s[i], m, n, (a.width & 7) == 0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      q[0] += s[i][e];
-      q[1] = fused(s[i][e], s[i][e], q[1]);
+      for (int e = 0; e < 8; ++e) {
+        q[0] += s[i][e];
+        q[1] = fused(s[i][e], s[i][e], q[1]);
+      }
+    } else {   // a run is inside the row or outside it
+      const double from = n > 0 ? mean_ : 0.0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double d = (double)s[i][e] - from;
+        q[0] = fused(d, d, q[0]);
+      }
     }
   }
   row_sum<false>(q, lds, at_.wave, sh);
-  const Sum off = q[0] / (Sum)a.width, var = not_negative(q[1] / (Sum)a.width - off * off);
+  Sum off, var;   // mean - m
+  if constexpr (kOut == kNormSame) {
+    off = q[0] / (Sum)a.width, var = not_negative(q[1] / (Sum)a.width - off * off);
+  } else {
+    off = mean_ - m, var = q[0] / (Sum)a.width;
+  }
   Sum rho;
   if constexpr (kOut == kNormSame) rho = 1.0f / __builtin_sqrtf(var + a.eps);
   else rho = inverse_root(var + (double)a.eps);
-  const float rho32 = (float)rho, off32 = (float)off;
+  const float rho32 = (float)rho, off32 = (float)off, far = __builtin_fabsf(off32 * rho32);
   uint8_t* outr = row_of<kType>(a.out, at, a.out_stride);
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
@@ -139,9 +159,10 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(La
     float size = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float ng = (s[i][e] - off32) * rho32 * v[e];
+      const float d = kOut == kNormSame ? s[i][e] : s[i][e] - m;
+      const float ng = (d - off32) * rho32 * v[e];
       y[e] = ng + w[e];
-      size = __builtin_fmaxf(size, __builtin_fabsf(ng) + __builtin_fabsf(w[e]));
+      size = __builtin_fmaxf(size, fused(far, __builtin_fabsf(v[e]), __builtin_fabsf(ng) + __builtin_fabsf(w[e])));
     }
     if (n <= 0) continue;
     if constexpr (kOut == kNormSame) {
@@ -149,9 +170,9 @@ __global__ __launch_bounds__(kNormMaxWaves * kWave) void add_layernorm_kernel(La
     } else {
       // the four lanes of a block are inside the row or outside it together
       const uint32_t sc = block_scale<(kOut == kNormMxfp8 ? 8 : 2)>(y, size, [&](int e) {
-        float d = s[i][e];
-        asm volatile("" : "+v"(d));   // converted here, where it is rarely needed, and not kept in 64 bits
-        return ((double)d - off) * rho * (double)v[e] + (double)w[e];
+        float x = s[i][e];
+        asm volatile("" : "+v"(x));   // converted here, where it is rarely needed, and not kept in 64 bits
+        return ((double)x - mean_) * rho * (double)v[e] + (double)w[e];
       });
       const float inv = inverse_scale(sc);
       if constexpr (kOut == kNormMxfp8)
