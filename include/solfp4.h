@@ -583,8 +583,8 @@ SOLFP4_API size_t solfp4_add_adapters_workspace_bytes(int64_t tokens, int64_t ad
  *           aligned (NULL where that is 0)
  *
  * rank from 1 to 128 (adapters of fewer ranks: pad with zeros), N and K below
- * 2^22.  Sums are FP32; h enters the second product with 16 bits and out is
- * rounded once.  Rows and columns that lie between those of out are left as
+ * 2^22.  Sums are FP32, h enters the second product with all its bits, and out
+ * is rounded once.  Rows and columns that lie between those of out are left as
  * they were.  Overlaps other than out == y are refused (SOLFP4_EINVAL).
  */
 SOLFP4_API int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const uint16_t* x,

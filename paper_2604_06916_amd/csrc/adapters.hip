@@ -4,8 +4,7 @@
 //
 // x [tokens][K], y [tokens][N] and the adapters' a [rank][K], b [N][rank] are
 // BF16; h is FP32 (rank values a token) and goes into the second product as
-// two BF16 pieces, 16 of its bits, so that its rounding (2^-17) is far below
-// the output's.
+// three BF16 pieces, all 24 of its bits: y may cancel what the adapters add.
 //
 // A workgroup takes a tile of up to 32 tokens of one adapter (the plan brings
 // them together) and a range of N: its waves share K, add their shares of h in
@@ -197,6 +196,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(Adapter
   constexpr int kShareBytes = (kPart == kFromShares ? 1 : kWaves) * kPlaces * 16;
   // the waves' tiles of x, then their shares of h
   __shared__ __attribute__((aligned(16))) uint8_t room[kXBytes > kShareBytes ? kXBytes : kShareBytes];
+  // the third piece of h, where three in registers would spill (13000 tokens 2432 ->
+  // 7296, rank 64: 180 us)
+  constexpr int kHeld = kChunks == 1 ? 3 : 2;
+  __shared__ bf16x8_t low[kHeld == 3 ? 1 : 2 * kChunks][kWave];
   floatx4_t(*const share)[2 * kBlocks][kWave] = reinterpret_cast<floatx4_t(*)[2 * kBlocks][kWave]>(room);
   // with 8 tiles or more a tile's ranges run on one XCD, whose L2 then has its rows
   const int ranges = kPart == kShares ? p.k_splits : p.splits, at = blockIdx.x / p.xcds;
@@ -215,7 +218,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(Adapter
   // as an operand's row or column, m is row 4 (m % 4) + m / 4 of its block, so that results are of rows g + 4 i
   const int row = m % 4 * 4 + m / 4;
 
-  bf16x8_t h[2][kChunks][2];   // two pieces of h of this lane's tokens
+  bf16x8_t h[2][kChunks][kHeld];   // h's pieces of this lane's tokens
   if (kPart == kFromShares && real) {
     const floatx4_t* from = static_cast<const floatx4_t*>(p.shares) + (int64_t)index * p.k_splits * kPlaces;
     for (int i = threadIdx.x; i < (two ? kPlaces : kPlaces / 2); i += kWaves * kWave) {
@@ -315,8 +318,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(Adapter
           store_run<SOLFP4_F32>(
               reinterpret_cast<uint8_t*>(p.hidden + token_at(p.t, tile.first + row + 16 * j) * p.rank), r0, p.rank - r0,
               from_f32<SOLFP4_F32>(v));
-        split_bf16(v, h[j][c]);
+        bf16x8_t piece[3];
+        split_bf16(v, piece);
+#pragma unroll
+        for (int s = 0; s < kHeld; ++s) h[j][c][s] = piece[s];
+        if (kHeld == 2 && wave == 0) low[j * kChunks + c][lane] = piece[2];
       }
+    if (kHeld == 2) __syncthreads();
   } else if (p.hidden && split == 0) {
     const float v = tile.group == p.t.adapters ? 0.0f : __builtin_nanf("");
     for (int i = threadIdx.x; i < tile.count * p.rank; i += kWaves * kWave)
@@ -373,13 +381,18 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(Adapter
       floatx4_t acc[kLane];
 #pragma unroll
       for (int q = 0; q < kLane; ++q) acc[q] = floatx4_t{0, 0, 0, 0};
-      if (real)
+      if (real) {
+        int at = lane;
+        if (kHeld == 2) asm volatile("" : "+v"(at));   // read here and not kept over the steps
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-          for (int s = 1; s >= 0; --s)
+          for (int s = 2; s >= 0; --s) {
+            const bf16x8_t piece = s < kHeld ? h[j][c][s] : low[j * kChunks + c][at];
 #pragma unroll
-            for (int q = 0; q < kLane; ++q) acc[q] = mfma(h[j][c][s], now_b[q][c], acc[q]);
+            for (int q = 0; q < kLane; ++q) acc[q] = mfma(piece, now_b[q][c], acc[q]);
+          }
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (g + 4 * i + 16 * j >= tile.count) continue;

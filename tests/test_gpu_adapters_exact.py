@@ -1,0 +1,80 @@
+"""Low-rank adapters where every sum is exact in FP32, so that results are the
+definition's to the last bit: h and g have 24 bits and all of them reach what
+is formed from them.
+
+With x = (p, q, r, 0 ..) of whole numbers p from 128 to 254, q and r up to 255,
+rank element 0 holds h = p + q 2^-8 + r 2^-16, which fills FP32's 24 bits; two
+others hold -p and -q 2^-8.  b takes all three once: r 2^-16 is left, 8 bits that
+BF16 holds.  Any order of the sums is exact: all values are multiples of 2^-16
+below 2^8."""
+import pytest
+import torch
+
+import paper_2604_06916_amd as sol
+from gpu_util import device
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+
+
+def parts(seed, tokens, width, places):
+    """[tokens, width] with p, q, r in three columns, and r 2^-16."""
+    g = torch.Generator().manual_seed(seed)
+    v = torch.zeros(tokens, width)
+    for at, (lo, hi) in zip(places, ((128, 255), (0, 256), (0, 256))):
+        v[:, at] = torch.randint(lo, hi, (tokens,), generator=g).float()
+    return v.to(BF16).to(device()), (v[:, places[2]] * 2.0 ** -16).to(device())
+
+
+def columns(rank, width, places, all_of):
+    """(w [rank, width] that gives h, -p, -q 2^-8 from those columns, b's row)."""
+    w, row = torch.zeros(rank, width), torch.zeros(rank)
+    for i, at in enumerate(places):
+        w[all_of[0], at] = 2.0 ** (-8 * i)
+    w[all_of[1], places[0]], w[all_of[2], places[1]] = -1.0, -2.0 ** -8
+    row[list(all_of)] = 1.0
+    return w.to(BF16).to(device()), row.to(BF16).to(device())
+
+
+def index_of(tokens, adapters):
+    g = torch.Generator().manual_seed(tokens)
+    return torch.randint(0, adapters, (tokens,), generator=g, dtype=torch.int32).to(device())
+
+
+@pytest.mark.parametrize("tokens,K,N,rank,adapters", [
+    (1, 3, 1, 3, 1), (5, 40, 70, 8, 2), (70, 200, 131, 24, 3), (33, 64, 128, 32, 2), (300, 90, 64, 33, 5), (64, 100, 200, 64, 1),
+    (40, 300, 200, 100, 3), (50, 129, 333, 128, 2), (12000, 16, 24, 32, 2), (20000, 24, 40, 64, 1), (15000, 9, 16, 128, 3),
+    (9, 9000, 40, 32, 2), (35, 5000, 70, 128, 3)])
+def test_all_bits_of_h_reach_the_output(tokens, K, N, rank, adapters):
+    places, ranks = (0, K // 2, K - 1), (0, rank - 1, rank // 2)
+    x, left = parts(tokens, tokens, K, places)
+    w, row = columns(rank, K, places, ranks)
+    a, b = w.expand(adapters, rank, K).contiguous(), row.expand(adapters, N, rank).contiguous()
+    plan = None if adapters == 1 else sol.adapter_plan(index_of(tokens, adapters), adapters)
+    y = torch.zeros(tokens, N, dtype=BF16, device=device())
+    out, hidden = sol.add_adapters(y, x, a, b, None, plan, hidden=True)
+    assert torch.equal(hidden, x.float() @ w.float().t())
+    assert torch.equal(out.float(), left[:, None].expand(tokens, N))
+
+
+@pytest.mark.parametrize("tokens,K,N,rank", [(1, 1, 1, 1), (7, 40, 33, 8), (90, 65, 130, 24), (40, 200, 64, 64), (33, 72, 96, 128)])
+def test_all_bits_of_g_and_h_reach_da_and_db(tokens, K, N, rank):
+    """A token an adapter.  b is 1 in each column's own rank element, dy and x are 1, the scale fills 24
+    bits: g is the number of a rank element's columns times the scale, here one column or none."""
+    g = torch.Generator().manual_seed(tokens)
+    b = torch.zeros(tokens, N, rank)
+    n = min(N, rank)
+    b[:, torch.arange(n), torch.arange(n)] = 1.0
+    scales = (torch.randint(2 ** 23, 2 ** 24, (tokens,), generator=g).float() * 2.0 ** -23).to(device())
+    hidden = (torch.randint(-2 ** 24, 2 ** 24, (tokens, rank), generator=g).float() * 2.0 ** -20).to(device())
+    a = torch.zeros(tokens, rank, K, dtype=BF16, device=device())
+    dy, x = torch.ones(tokens, N, dtype=BF16, device=device()), torch.ones(tokens, K, dtype=BF16, device=device())
+    index = torch.randperm(tokens, generator=g).int().to(device())
+    plan = sol.adapter_plan(index, tokens)
+    _, da, db = sol.adapters_backward(dy, x, hidden, a, b.to(BF16).to(device()), scales, plan)
+    want = torch.zeros(tokens, rank, K, device=device())
+    want[:, :n] = scales[:, None, None]
+    assert torch.equal(da, want)
+    _, _, db = sol.adapters_backward(dy, x, hidden, a, b.to(BF16).to(device()), None, plan)
+    assert torch.equal(db[index.long()], hidden[:, None].expand(tokens, N, rank))
