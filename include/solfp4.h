@@ -585,7 +585,10 @@ SOLFP4_API size_t solfp4_add_adapters_workspace_bytes(int64_t tokens, int64_t ad
  * rank from 1 to 128 (adapters of fewer ranks: pad with zeros), N and K below
  * 2^22.  Sums are FP32, h enters the second product with all its bits, and out
  * is rounded once.  Rows and columns that lie between those of out are left as
- * they were.  Overlaps other than out == y are refused (SOLFP4_EINVAL).
+ * they were.  A row with an infinity or a NaN spoils itself alone.  An infinite
+ * weight of b gives its adapter's tokens an infinity in that column, or NaN: h
+ * goes in as three pieces, which may have both signs or be 0.  Overlaps other
+ * than out == y are refused (SOLFP4_EINVAL).
  */
 SOLFP4_API int solfp4_add_adapters(const uint16_t* y, int64_t y_stride, const uint16_t* x,
                    int64_t x_stride, const uint16_t* a, const uint16_t* b, const float* scales,

@@ -24,6 +24,8 @@
 // 8192 tokens 2240 -> 6720 51 us, 5.1 TB/s; 64 tokens of 48 adapters 12.8 us, where
 // most tiles have one token and a and b come from HBM once; 1 token 1152 -> 1152,
 // rank 16 5.5 us.
+#include <limits.h>
+
 #include "adapters.h"
 
 namespace solfp4 {
@@ -333,6 +335,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(Adapter
 
   const float scale = !real ? 0.0f : p.scales ? p.scales[tile.group] : 1.0f;
   const uint16_t* b = p.b + (real ? (int64_t)tile.group * p.N * p.rank : 0);
+  const __amdgpu_buffer_rsrc_t whole_b = uniform_rsrc(b, real ? p.N * p.rank * 2 : 0);   // below 2^30 bytes
   const int end = min(p.N, (split + 1) * p.split_cols);
   LaneRun<kLane> y[8];
   const auto load = [&](int n0) {
@@ -352,10 +355,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void add_adapters_kernel(Adapter
       const int n = min(n0 + kLane * m + q, p.N - 1);   // past the last column: any, not stored
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
-        // past the rank: any of the row, times an h of 0
         const int r0 = 32 * c + 8 * g;
-        if constexpr (kWholeRank) bv[q][c] = operand8(b + (int64_t)n * p.rank + min(r0, p.rank - 8));
-        else bv[q][c] = operand8(b + (int64_t)n * p.rank, r0, p.rank);
+        // zeros past the rank, where an infinite weight times an h of 0 would be NaN: from past the buffer
+        if constexpr (kWholeRank)
+          bv[q][c] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(
+                                                      whole_b, n * p.rank * 2 + (r0 < p.rank ? 2 * r0 : INT_MIN), 0, 0));
+        else
+          bv[q][c] = operand8(b + (int64_t)n * p.rank, r0, p.rank);
       }
     }
   };

@@ -1,6 +1,6 @@
 """Low-rank adapters where every sum is exact in FP32, so that results are the
 definition's to the last bit: h and g have 24 bits and all of them reach what
-is formed from them.
+is formed from them; infinite weights.
 
 With x = (p, q, r, 0 ..) of whole numbers p from 128 to 254, q and r up to 255,
 rank element 0 holds h = p + q 2^-8 + r 2^-16, which fills FP32's 24 bits; two
@@ -78,3 +78,37 @@ def test_all_bits_of_g_and_h_reach_da_and_db(tokens, K, N, rank):
     assert torch.equal(da, want)
     _, _, db = sol.adapters_backward(dy, x, hidden, a, b.to(BF16).to(device()), None, plan)
     assert torch.equal(db[index.long()], hidden[:, None].expand(tokens, N, rank))
+
+
+@pytest.mark.parametrize("rank", [1, 4, 8, 12, 24, 40, 72, 128])
+@pytest.mark.parametrize("tokens", [3, 40])
+def test_an_infinite_weight_is_met_once(rank, tokens):
+    """b's last rank element is infinite: the output is what the definition gives, an infinity of
+    h's sign, where all pieces of h have that sign (here positive: p, q and r below 128)."""
+    K, N = 70, 50
+    x = torch.zeros(tokens, K)
+    x[:, :3] = torch.tensor([255.0, 3.0, 5.0])
+    a = torch.zeros(1, rank, K)
+    a[:, -1, :3] = torch.tensor([1.0, 2.0 ** -8, 2.0 ** -16])
+    b = torch.zeros(1, N, rank)
+    b[:, ::2, -1] = float("inf")
+    b[:, 1::4, -1] = -float("inf")
+    y = torch.ones(tokens, N, dtype=BF16, device=device())
+    out, hidden = sol.add_adapters(y, *(t.to(BF16).to(device()) for t in (x, a, b)), hidden=True)
+    want = (1 + b[:, :, -1]).expand(tokens, N).to(device())
+    assert torch.equal(out.float(), want)
+    assert torch.equal(hidden[:, -1].cpu(), torch.full((tokens,), 255 + 3 * 2.0 ** -8 + 5 * 2.0 ** -16))
+
+
+@pytest.mark.parametrize("rank", [8, 24, 32, 40, 128])
+@pytest.mark.parametrize("tokens", [2, 50, 12000])
+def test_weights_at_any_address(rank, tokens):
+    """a and b at odd elements of their memory give what aligned ones give."""
+    K, N = 66, 75
+    g = torch.Generator().manual_seed(rank)
+    room = [torch.randn(n, generator=g).to(BF16).to(device()) for n in (rank * K + 1, N * rank + 1)]
+    a, b = room[0][1:].view(1, rank, K), room[1][1:].view(1, N, rank)
+    x, y = (torch.randn(tokens, w, generator=g).to(BF16).to(device()) for w in (K, N))
+    want = sol.add_adapters(y, x, a.clone(), b.clone(), hidden=True)
+    got = sol.add_adapters(y, x, a, b, hidden=True)
+    assert a.data_ptr() % 4 == b.data_ptr() % 4 == 2 and all(torch.equal(p, q) for p, q in zip(want, got))
