@@ -623,9 +623,9 @@ SOLFP4_API size_t solfp4_adapters_backward_workspace_bytes(int64_t tokens, int64
  *
  * Sums are FP32, in an order that depends on the sizes, the plan and the
  * device alone: results are the same on every call.  g and h enter the products
- * for da and db with all their bits, g that for dx with 16.  A row with an
- * infinity or a NaN spoils its own dx and its adapter's da and db (infinite or
- * NaN), no others.  Overlaps other than dx == past are refused (SOLFP4_EINVAL).
+ * with all their bits.  A row with an infinity or a NaN spoils its own dx and its
+ * adapter's da and db (infinite or NaN), no others.  Overlaps other than dx ==
+ * past are refused (SOLFP4_EINVAL).
  */
 SOLFP4_API int solfp4_adapters_backward(const uint16_t* dy, int64_t dy_stride, const uint16_t* x,
                    int64_t x_stride, const float* hidden, const uint16_t* a, const uint16_t* b,

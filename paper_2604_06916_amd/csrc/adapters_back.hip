@@ -22,8 +22,8 @@
 // columns must be lanes and the tokens the reduction: the tile goes through
 // LDS and comes back transposed (ds_read_b64_tr_b16).
 //
-// FP32 factors (h, g) enter the products as BF16 pieces: three, all 24 bits,
-// for da and db, which are FP32; two for dx, which is BF16.
+// FP32 factors (h, g) enter the products as three BF16 pieces, all 24 bits, also
+// for dx, which is BF16: past may cancel what the adapters add.
 //
 // Slices and tiles: slice s of tiles_each tiles leaves its sums of adapter e in
 // slot s + e.  Tiles are sorted by adapter, so two slices of one adapter or two
@@ -58,7 +58,7 @@ struct Deal {
   int units_n, chunks_n, units_x;       // waves' columns of N and K; workgroups along N
   int slices_n, each_n, slices_x, each_x;
   int64_t slots_n, slots_x;
-  int64_t share, pieces2, pieces3, db, da, bytes;   // offsets of floatx4_t places, bytes at the end
+  int64_t share, rows_g, tokens_g, db, da, bytes;   // offsets of floatx4_t places, bytes at the end
 };
 
 struct BackArgs {
@@ -94,8 +94,8 @@ Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
     return was;
   };
   d.share = take((int64_t)d.chunks_n * d.tiles * 2 * frag);
-  d.pieces2 = take(d.tiles * chunks * 2 * 2 * kWave);
-  d.pieces3 = take(d.tiles * 3 * frag);
+  d.rows_g = take(d.tiles * chunks * 2 * 3 * kWave);
+  d.tokens_g = take(d.tiles * 3 * frag);
   d.db = take(d.slots_n * d.units_n * cols_of(chunks) * frag);
   d.da = take(d.slots_x * d.units_x * x_cols(chunks) * frag);
   d.bytes = at * 16;
@@ -459,11 +459,11 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = gs[m % 4 * 4 + m / 4 + 16 * j][32 * c + e / 4 * 16 + lane / 16 * 4 + e % 4];
-    bf16x8_t piece[2];
+    bf16x8_t piece[3];
     split_bf16(v, piece);
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-      q.ws[q.d.pieces2 + (((int64_t)i * kChunks + c) * 2 + j) * 2 * kWave + s * kWave + lane] =
+    for (int s = 0; s < 3; ++s)
+      q.ws[q.d.rows_g + (((int64_t)i * kChunks + c) * 2 + j) * 3 * kWave + s * kWave + lane] =
           __builtin_bit_cast(floatx4_t, piece[s]);
   }
   for (int k = threadIdx.x; k < kBlocks * kWave; k += 256) {
@@ -475,7 +475,7 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
     split_bf16(v, piece);
 #pragma unroll
     for (int s = 0; s < 3; ++s)
-      q.ws[q.d.pieces3 + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane] =
+      q.ws[q.d.tokens_g + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane] =
           __builtin_bit_cast(floatx4_t, piece[s]);
   }
 }
@@ -486,8 +486,11 @@ template <int kChunks>
 __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(BackArgs q) {
   constexpr int kBlocks = 2 * kChunks, kCols = x_cols(kChunks);
   constexpr bool kHeld = kChunks == 1;   // g's pieces fit in registers
-  // g's two pieces half a tile at a time and late, where both halves at once would
-  // spill (8192 tokens 2240 -> 2240, rank 128: 185 us, so 158)
+  // g's pieces for dx half a tile at a time, and above rank 64 both halves late, where
+  // more at once would spill (13000 tokens 2432 -> 7296, rank 64: 201 us, 214 with both
+  // halves ahead, 205 with both late; 8192 tokens 2240 -> 2240, rank 128: 154 us;
+  // of two pieces 151, and 185 with both halves ahead)
+  constexpr int kHalves = kChunks == 1 ? 2 : 1;
   constexpr bool kLate = kChunks == 4;
   __shared__ __attribute__((aligned(16))) uint8_t tiles[kXWaves][kAdapterTile * TileLds<kCols>::kRow];
   const AdapterBackArgs& p = q.p;
@@ -549,7 +552,7 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
   Tokens& tokens = tiles_.tokens;
   Rows<kCols> x;
   const auto piece3 = [&](int i, int r, int s) {
-    return __builtin_bit_cast(bf16x8_t, q.ws[q.d.pieces3 + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane]);
+    return __builtin_bit_cast(bf16x8_t, q.ws[q.d.tokens_g + ((int64_t)i * 3 + s) * kBlocks * kWave + r * kWave + lane]);
   };
   int i = first;
   while (tile.count) {
@@ -561,24 +564,22 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
       const Tile now = tile;
       const Tokens of_now = tokens;
       // g's operands first, past after them: loads come back in order
-      bf16x8_t two[kLate ? 1 : 2][kChunks][2], three[kHeld ? kBlocks : 1][3];
-      const auto load_two = [&](bf16x8_t(&to)[kChunks][2], int j) {
+      bf16x8_t gd[kHalves][kChunks][3], three[kHeld ? kBlocks : 1][3];
+      const auto load_gd = [&](bf16x8_t(&to)[kChunks][3], int j) {
 #pragma unroll
         for (int h = 0; h < kChunks; ++h)
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
+          for (int s = 0; s < 3; ++s)
             to[h][s] = __builtin_bit_cast(
-                bf16x8_t, q.ws[q.d.pieces2 + (((int64_t)i * kChunks + h) * 2 + j) * 2 * kWave + s * kWave + lane]);
+                bf16x8_t, q.ws[q.d.rows_g + (((int64_t)i * kChunks + h) * 2 + j) * 3 * kWave + s * kWave + lane]);
       };
       if (real) {
 #pragma unroll
         for (int r = 0; r < (kHeld ? kBlocks : 0); ++r)
 #pragma unroll
           for (int s = 0; s < 3; ++s) three[r][s] = piece3(i, r, s);
-        if constexpr (!kLate) {
-          load_two(two[0], 0);
-          load_two(two[1], 1);
-        }
+#pragma unroll
+        for (int j = 0; j < (kLate ? 0 : kHalves); ++j) load_gd(gd[j], j);
         wave_order();
         x.put(lds, now.count, m, g);
         wave_order();
@@ -602,7 +603,7 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (real) {
-          if constexpr (kLate) load_two(two[0], j);
+          if (kHalves == 1 && (kLate || j)) load_gd(gd[0], j);
           // two columns of a lane's rows at a time
 #pragma unroll
           for (int c = 0; c < kCols; c += 2) {
@@ -610,9 +611,9 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
 #pragma unroll
             for (int h = 0; h < kChunks; ++h)
 #pragma unroll
-              for (int s = 1; s >= 0; --s)
+              for (int s = 2; s >= 0; --s)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) d[u] = mfma(two[kLate ? 0 : j][h][s], at[c + u][h], d[u]);
+                for (int u = 0; u < 2; ++u) d[u] = mfma(gd[kHalves == 1 ? 0 : j][h][s], at[c + u][h], d[u]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               LaneRun<kCols>& o = add.v[4 * j + k];

@@ -58,6 +58,21 @@ def test_all_bits_of_h_reach_the_output(tokens, K, N, rank, adapters):
     assert torch.equal(out.float(), left[:, None].expand(tokens, N))
 
 
+@pytest.mark.parametrize("tokens,K,N,rank,adapters", [
+    (1, 1, 3, 3, 1), (5, 70, 40, 8, 2), (70, 131, 200, 24, 3), (33, 128, 64, 32, 2), (300, 64, 90, 33, 5), (64, 200, 100, 64, 1),
+    (40, 200, 300, 100, 3), (50, 333, 1129, 128, 2), (12000, 24, 16, 32, 2), (20000, 40, 24, 64, 1), (15000, 16, 9, 128, 3)])
+def test_all_bits_of_g_reach_dx(tokens, K, N, rank, adapters):
+    places, ranks = (0, N // 2, N - 1), (0, rank - 1, rank // 2)
+    dy, left = parts(tokens, tokens, N, places)
+    w, row = columns(rank, N, places, ranks)
+    b = w.t().contiguous().expand(adapters, N, rank).contiguous()
+    a = row[:, None].expand(adapters, rank, K).contiguous()
+    plan = None if adapters == 1 else sol.adapter_plan(index_of(tokens, adapters), adapters)
+    x, hidden = torch.zeros(tokens, K, dtype=BF16, device=device()), torch.zeros(tokens, rank, device=device())
+    dx, da, db = sol.adapters_backward(dy, x, hidden, a, b, None, plan)
+    assert torch.equal(dx.float(), left[:, None].expand(tokens, K)) and not da.any() and not db.any()
+
+
 @pytest.mark.parametrize("tokens,K,N,rank", [(1, 1, 1, 1), (7, 40, 33, 8), (90, 65, 130, 24), (40, 200, 64, 64), (33, 72, 96, 128)])
 def test_all_bits_of_g_and_h_reach_da_and_db(tokens, K, N, rank):
     """A token an adapter.  b is 1 in each column's own rank element, dy and x are 1, the scale fills 24
