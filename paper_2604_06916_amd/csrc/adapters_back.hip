@@ -28,6 +28,11 @@
 // Slices and tiles: slice s of tiles_each tiles leaves its sums of adapter e in
 // slot s + e.  Tiles are sorted by adapter, so two slices of one adapter or two
 // adapters of one slice never share a slot.
+//
+// Shares and pieces of g grow with the tokens, at a rank of 128 to more than dy
+// (a million tokens 9728 -> 9728 would take 20 GB): past kRunBytes of them the
+// tiles are taken in runs, all launches for each, and a run's sums are added to
+// the da and db of those before it.
 #include "adapters.h"
 
 namespace solfp4 {
@@ -52,19 +57,26 @@ typedef __attribute__((address_space(3))) short4_t* lds_short4_t;
 constexpr int cols_of(int chunks) { return 8 / chunks; }
 constexpr int x_cols(int chunks) { return chunks == 1 ? 4 : cols_of(chunks); }
 
-// How the work is dealt and where everything lies in the workspace.
+// Most bytes of g's shares and pieces of a run (of one tile, if that has more).
+// Rank 128, 2432 -> 7296, 26574 and 50000 tokens: 905 and 1689 us with 256 MiB, 913
+// and 1691 in one run of 0.5 and 0.9 GiB, 959 and 1740 with 128 MiB.
+constexpr int64_t kRunBytes = (int64_t)256 << 20;
+
+// How a run's work is dealt and where everything lies in the workspace.
 struct Deal {
-  int64_t tiles;
+  int64_t tiles;                        // of a run
   int units_n, chunks_n, units_x;       // waves' columns of N and K; workgroups along N
   int slices_n, each_n, slices_x, each_x;
   int64_t slots_n, slots_x;
   int64_t share, rows_g, tokens_g, db, da, bytes;   // offsets of floatx4_t places, bytes at the end
+  int64_t share_each, rows_each, tokens_each;       // places of a tile
 };
 
 struct BackArgs {
   AdapterBackArgs p;
-  Deal d;
+  Deal d;        // share, rows_g and tokens_g: of the plan's first tile, were it in this run
   floatx4_t* ws;
+  int begin, end;   // the run's tiles
 };
 
 Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
@@ -72,11 +84,15 @@ Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
   const int cols = 16 * cols_of(chunks), x_wide = 16 * x_cols(chunks);
   const int64_t cus = device_cu_count();
   Deal d = {};
-  d.tiles = t.max_tiles;
   d.units_n = (int)((N + cols - 1) / cols);
   d.units_x = (int)((K + x_wide - 1) / x_wide);
   const int waves = y_waves(chunks);
   d.chunks_n = (d.units_n + waves - 1) / waves;
+  const int64_t frag = blocks * kWave;
+  d.share_each = 2 * frag, d.rows_each = chunks * 2 * 3 * kWave, d.tokens_each = 3 * frag;
+  const int64_t each = (d.chunks_n * d.share_each + d.rows_each + d.tokens_each) * 16;
+  const int64_t most = each < kRunBytes ? kRunBytes / each : 1, runs = (t.max_tiles + most - 1) / most;
+  d.tiles = runs ? (t.max_tiles + runs - 1) / runs : 0;
   const auto slices = [&](int64_t want, int* each) {
     want = want < 1 ? 1 : want < d.tiles ? want : d.tiles;
     *each = (int)(want > 0 ? (d.tiles + want - 1) / want : 1);
@@ -86,16 +102,15 @@ Deal deal(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
   d.slices_x = slices(d.units_x ? 8 * cus / d.units_x : 1, &d.each_x);
   d.slots_n = d.slices_n + t.adapters;
   d.slots_x = d.slices_x + t.adapters;
-  const int64_t frag = blocks * kWave;
   int64_t at = 0;
   const auto take = [&](int64_t n) {
     const int64_t was = at;
     at += n;
     return was;
   };
-  d.share = take((int64_t)d.chunks_n * d.tiles * 2 * frag);
-  d.rows_g = take(d.tiles * chunks * 2 * 3 * kWave);
-  d.tokens_g = take(d.tiles * 3 * frag);
+  d.share = take(d.chunks_n * d.tiles * d.share_each);
+  d.rows_g = take(d.tiles * d.rows_each);
+  d.tokens_g = take(d.tiles * d.tokens_each);
   d.db = take(d.slots_n * d.units_n * cols_of(chunks) * frag);
   d.da = take(d.slots_x * d.units_x * x_cols(chunks) * frag);
   d.bytes = at * 16;
@@ -333,7 +348,7 @@ __global__ __launch_bounds__(y_waves(kChunks) * kWave, 2) void adapters_back_y_k
     wave_order();
   };
 
-  const int first = slice * q.d.each_n, end = min(first + q.d.each_n, (int)q.d.tiles);
+  const int first = q.begin + slice * q.d.each_n, end = min(first + q.d.each_n, q.end);
   // the next tile's rows and its h come while a tile is worked on
   Tiles tiles_(p.t, first, end, lane);
   Tile& tile = tiles_.tile;
@@ -425,7 +440,7 @@ __global__ __launch_bounds__(256) void adapters_back_g_kernel(BackArgs q) {
   constexpr int kBlocks = 2 * kChunks, kRow = 16 * kBlocks + 1;
   __shared__ float gs[kAdapterTile][kRow];
   const AdapterBackArgs& p = q.p;
-  const int i = blockIdx.x;
+  const int i = q.begin + blockIdx.x;
   const Tile tile = uniform(p.t, load_tile(p.t, i));
   if (tile.count == 0 || tile.group >= p.t.adapters) return;
   const float scale = p.scales ? p.scales[tile.group] : 1.0f;
@@ -545,7 +560,7 @@ __global__ __launch_bounds__(kXWaves * kWave, 2) void adapters_back_x_kernel(Bac
     }
   };
 
-  const int first = slice * q.d.each_x, end = min(first + q.d.each_x, (int)q.d.tiles);
+  const int first = q.begin + slice * q.d.each_x, end = min(first + q.d.each_x, q.end);
   // x ahead as in the pass over dy; past of the tile itself, needed last
   Tiles tiles_(p.t, first, end, lane);
   Tile& tile = tiles_.tile;
@@ -653,8 +668,10 @@ __global__ __launch_bounds__(256) void adapters_back_sums_kernel(BackArgs q) {
     const int64_t k = is_db ? id : id - p.t.adapters * per_n, per = is_db ? per_n : per_x;
     const int e = (int)(k / per);
     const int64_t place = k - e * per;
-    int begin = 0, end = (int)q.d.tiles;   // the adapter's tiles
-    if (p.t.plan) begin = max(p.t.plan[e], 0), end = min(p.t.plan[e + 1], end);
+    int begin = q.begin, end = q.end;   // the adapter's tiles in this run
+    if (p.t.plan) begin = max(p.t.plan[e], begin), end = min(p.t.plan[e + 1], end);
+    if (q.begin && begin >= end) continue;
+    begin -= q.begin, end -= q.begin;
     floatx4_t v = {0, 0, 0, 0};
     if (begin < end) {
       const int each = is_db ? q.d.each_n : q.d.each_x;
@@ -678,26 +695,26 @@ __global__ __launch_bounds__(256) void adapters_back_sums_kernel(BackArgs q) {
       float* to = p.db + ((int64_t)e * p.N + col) * p.rank + at;
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (c < left) to[c] = scale * v[c];
+        if (c < left) to[c] = q.begin ? to[c] + scale * v[c] : scale * v[c];
     } else {
       if (col >= p.K) continue;
       float* to = p.da + ((int64_t)e * p.rank + at) * p.K + col;
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (c < left) to[c * (int64_t)p.K] = v[c];
+        if (c < left) to[c * (int64_t)p.K] = q.begin ? to[c * (int64_t)p.K] + v[c] : v[c];
     }
   }
 }
 
 template <int kChunks>
-hipError_t launch_back(const BackArgs& q, hipStream_t stream) {
+hipError_t launch_run(const BackArgs& q, hipStream_t stream) {
   hipError_t e = hipSuccess;
-  if (q.d.tiles > 0) {
+  if (q.end > q.begin) {
     if (q.d.chunks_n > 0)
       e = launch_kernel(adapters_back_y_kernel<kChunks>, dim3((unsigned)(q.d.chunks_n * q.d.slices_n)),
                         dim3(y_waves(kChunks) * kWave), stream, q);
     if (e == hipSuccess && q.d.units_x > 0)
-      e = launch_kernel(adapters_back_g_kernel<kChunks>, dim3((unsigned)q.d.tiles), dim3(256), stream, q);
+      e = launch_kernel(adapters_back_g_kernel<kChunks>, dim3((unsigned)(q.end - q.begin)), dim3(256), stream, q);
     const int64_t waves = (int64_t)q.d.units_x * q.d.slices_x;
     if (e == hipSuccess && q.d.units_x > 0)
       e = launch_kernel(adapters_back_x_kernel<kChunks>, dim3((unsigned)((waves + kXWaves - 1) / kXWaves)),
@@ -711,6 +728,23 @@ hipError_t launch_back(const BackArgs& q, hipStream_t stream) {
   return launch_kernel(adapters_back_sums_kernel<kChunks>, dim3((unsigned)(wgs < most ? wgs : most)), dim3(256), stream, q);
 }
 
+template <int kChunks>
+hipError_t launch_back(BackArgs q, hipStream_t stream) {
+  const Deal d = q.d;
+  const int64_t tiles = q.p.t.max_tiles;
+  int64_t begin = 0;
+  do {   // once without a tile, for da and db of 0
+    q.begin = (int)begin, q.end = (int)(begin + d.tiles < tiles ? begin + d.tiles : tiles);
+    q.d.share = d.share - begin * d.share_each;
+    q.d.rows_g = d.rows_g - begin * d.rows_each;
+    q.d.tokens_g = d.tokens_g - begin * d.tokens_each;
+    const hipError_t e = launch_run<kChunks>(q, stream);
+    if (e != hipSuccess) return e;
+    begin += d.tiles;
+  } while (begin < tiles);
+  return hipSuccess;
+}
+
 }  // namespace
 
 size_t adapters_backward_bytes(const AdapterTokens& t, int64_t N, int64_t K, int64_t rank) {
@@ -718,7 +752,7 @@ size_t adapters_backward_bytes(const AdapterTokens& t, int64_t N, int64_t K, int
 }
 
 hipError_t launch_adapters_backward(const AdapterBackArgs& a, void* workspace, hipStream_t stream) {
-  const BackArgs q = {a, deal(a.t, a.N, a.K, a.rank), static_cast<floatx4_t*>(workspace)};
+  const BackArgs q = {a, deal(a.t, a.N, a.K, a.rank), static_cast<floatx4_t*>(workspace), 0, 0};
   if (a.rank <= 32) return launch_back<1>(q, stream);
   if (a.rank <= 64) return launch_back<2>(q, stream);
   return launch_back<4>(q, stream);

@@ -1,6 +1,6 @@
 """Low-rank adapters where every sum is exact in FP32, so that results are the
 definition's to the last bit: h and g have 24 bits and all of them reach what
-is formed from them; infinite weights.
+is formed from them; infinite weights; gradients of tokens taken in runs.
 
 With x = (p, q, r, 0 ..) of whole numbers p from 128 to 254, q and r up to 255,
 rank element 0 holds h = p + q 2^-8 + r 2^-16, which fills FP32's 24 bits; two
@@ -12,6 +12,7 @@ import torch
 
 import paper_2604_06916_amd as sol
 from gpu_util import device
+from test_gpu_adapted_maxsize import check_adapters
 
 pytestmark = pytest.mark.gpu
 
@@ -127,3 +128,40 @@ def test_weights_at_any_address(rank, tokens):
     want = sol.add_adapters(y, x, a.clone(), b.clone(), hidden=True)
     got = sol.add_adapters(y, x, a, b, hidden=True)
     assert a.data_ptr() % 4 == b.data_ptr() % 4 == 2 and all(torch.equal(p, q) for p, q in zip(want, got))
+
+
+@pytest.mark.parametrize("tokens,K,N,rank,adapters,sparse", [(70000, 64, 2048, 128, 3, 64), (1300000, 40, 72, 8, 7, 4),
+                                                             (600000, 33, 129, 40, 2, 8)])
+def test_gradients_of_tokens_in_several_runs(tokens, K, N, rank, adapters, sparse):
+    """So many that g's shares take more than a run of tiles holds: sums over runs that end inside an
+    adapter's tiles, adapters of one run alone, tokens without one in the last."""
+    size = sol.adapters_backward_workspace_bytes
+    assert size(tokens, adapters, True, N, K, rank) < size(tokens // 4, adapters, True, N, K, rank) * 2
+    check_adapters(tokens, K, N, rank, adapters, sparse, exact=True)
+
+
+def test_runs_in_a_graph_and_in_place():
+    tokens, K, N, rank, adapters = 70000, 64, 2048, 128, 3
+    g = torch.Generator(device=device()).manual_seed(3)
+    normal = lambda *s: torch.randn(*s, generator=g, device=device()).to(BF16)
+    dy, x, past = normal(tokens, N), normal(tokens, K), normal(tokens, K)
+    a, b, hidden = normal(adapters, rank, K), normal(adapters, N, rank), normal(tokens, rank).float()
+    plan = sol.adapter_plan(index_of(tokens, adapters), adapters)
+    dx = past.clone()
+    call = lambda: sol.adapters_backward(dy, x, hidden, a, b, None, plan, dx, dx=dx)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for _ in range(3):
+        dy.copy_(normal(tokens, N))
+        dx.copy_(past)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = sol.adapters_backward(dy, x, hidden, a, b, None, plan, past)
+        torch.cuda.synchronize()
+        assert held[0] is dx and all(torch.equal(p, q) for p, q in zip(held, want))
