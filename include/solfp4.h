@@ -555,7 +555,9 @@ SOLFP4_API int solfp4_layernorm_backward(int type, const void* dy, int64_t dy_st
  *           Negative: no adapter, the token's out is its y.  adapters or more:
  *           the token's out (and dx) is NaN and it has no part in the gradients
  *
- * tokens below 2^27, at most 65536 adapters.  tokens == 0 is valid.
+ * tokens below 2^27, at most 65536 adapters.  tokens == 0 is valid.  The work grows
+ * with the tokens and, where there are thousands, with the adapters (a million
+ * tokens: 0.1 ms of 4 adapters, 3 ms of 60000).
  */
 SOLFP4_API size_t solfp4_adapter_plan_bytes(int64_t tokens, int64_t adapters);
 SOLFP4_API int solfp4_adapter_plan(const void* index, int index_bytes, int64_t tokens, int64_t adapters,

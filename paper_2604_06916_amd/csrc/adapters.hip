@@ -32,7 +32,40 @@ namespace solfp4 {
 
 // ---- plan -----------------------------------------------------------------
 
-constexpr int kPlanThreads = 1024, kPlanDeep = 8;
+// Tokens come to their groups by a counting sort that keeps their order: they are
+// cut to segments, one a wave, which counts its tokens of every group; one
+// workgroup adds the counts up, group by group and segment by segment, to first
+// places; and each wave puts its tokens there.  A token is read twice, and a
+// count belongs to one wave, so results have no order of atomics in them.
+//
+// Three launches that wait for each other: 13.5 us for 64 tokens of 48 adapters, 17 for
+// 26574 of 6, 91 for a million of 4, 3.1 ms for a million of 60000 (with a workgroup a
+// group that read all of the index 13, 25, 782 and 124 ms).
+constexpr int kPlanThreads = 1024, kPlanDeep = 4;   // fours of counts a thread
+constexpr int kSegmentWaves = 4;   // of a workgroup
+constexpr int64_t kSegment = 128, kMostSegments = 2048, kCounts = 16384;
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+struct Segments {
+  int64_t each, counts_at;   // tokens of a segment; word of the counts in the plan, [group][segment]
+  int count;
+};
+
+// Segments of kSegment tokens or more, and so few that adding up their counts,
+// 0.4 ns each, takes no longer than their waves do, 2.6 us for 64 tokens (a million
+// tokens of 1000 adapters: 230 us, 456 without), and that the counts take no more words than
+// there are tokens (but for kCounts, or one segment's).
+static Segments segments_of(const AdapterTokens& t) {
+  const int64_t groups = t.adapters + 2, fit = (t.tokens + kCounts) / groups;
+  int64_t n = (t.tokens + kSegment - 1) / kSegment;
+  n = n < kMostSegments ? n : kMostSegments;
+  n = n < fit ? n : fit;
+  while (n > 1 && n * n * groups > 128 * t.tokens) n = n * 7 / 8;
+  n = n < 1 ? 1 : n;
+  const int64_t each = ((t.tokens + n - 1) / n + kWave - 1) / kWave * kWave;
+  return {each, t.tiles_at + 4 * t.max_tiles, (int)n};
+}
 
 AdapterTokens adapter_tokens(const void* plan, int64_t tokens, int64_t adapters) {
   AdapterTokens t = {static_cast<const int*>(plan), tokens, (int)adapters, 0, 0, 0, 0};
@@ -47,7 +80,8 @@ AdapterTokens adapter_tokens(const void* plan, int64_t tokens, int64_t adapters)
 
 size_t adapter_plan_bytes(int64_t tokens, int64_t adapters) {
   const AdapterTokens t = adapter_tokens(&t, tokens, adapters);   // any address: as with a plan
-  return (size_t)(t.tiles_at + 4 * t.max_tiles) * 4;
+  const Segments s = segments_of(t);
+  return (size_t)(s.counts_at + ((adapters + 2) * s.count + 3) / 4 * 4) * 4;
 }
 
 template <typename Index>
@@ -56,97 +90,145 @@ __device__ __forceinline__ int group_of(const Index* index, int64_t i, int adapt
   return v < 0 ? adapters : v < adapters ? (int)v : adapters + 1;
 }
 
-// A workgroup a group: counts the tokens of the groups before its own, then
-// puts its tokens behind them in their order.  Each reads the index twice, so
-// no workgroup waits for another.  A plan, its three launches together, takes 14 us
-// for 64 tokens of 48 adapters, 26 for 26574 of 6, and 730 for a million, which
-// each group's one workgroup reads by itself: made once for all layers of a step.
+// The lanes, of those with a token, whose group is this lane's.
+__device__ __forceinline__ uint64_t lanes_alike(int group, bool has, int groups) {
+  uint64_t alike = __ballot(has);
+  for (int bit = 0; groups - 1 >> bit; ++bit) {
+    const bool set = group >> bit & 1;
+    const uint64_t with = __ballot(set);
+    alike &= set ? with : ~with;
+  }
+  return alike;
+}
+
+// f(token, whether there is one, its group, the lanes of that group), 64 tokens at a time.
+template <typename Index, typename F>
+__device__ __forceinline__ void each_of_segment(const Index* index, const AdapterTokens& t, const Segments& s, int segment,
+                                                int lane, F f) {
+  const int64_t first = segment * s.each, end = min(first + s.each, t.tokens);
+  int64_t i = first + lane;
+  int next = i < end ? group_of(index, i, t.adapters) : 0;
+  for (int64_t base = first; base < end; base += kWave, i += kWave) {
+    const int group = next;
+    const bool has = i < end;
+    if (i + kWave < end) next = group_of(index, i + kWave, t.adapters);
+    f((int)i, has, group, lanes_alike(group, has, t.adapters + 2));
+  }
+}
+
 template <typename Index>
-__global__ __launch_bounds__(kPlanThreads) void plan_order_kernel(const Index* __restrict__ index, AdapterTokens t,
-                                                                  int* __restrict__ plan) {
-  constexpr int kWaves = kPlanThreads / kWave;
-  __shared__ int sums[kWaves];
-  const int group = blockIdx.x, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  int before = 0;
-  for (int64_t base = 0; base < t.tokens; base += kPlanThreads * kPlanDeep) {
-    int g[kPlanDeep];
+__global__ __launch_bounds__(kSegmentWaves* kWave) void plan_counts_kernel(const Index* __restrict__ index, AdapterTokens t,
+                                                                          Segments s, int* plan) {
+  const int segment = blockIdx.x * kSegmentWaves + threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  if (segment >= s.count) return;
+  int* const counts = plan + s.counts_at + segment;
+  const int64_t n = (int64_t)(t.adapters + 2) * s.count;
+  for (int64_t g = lane; g < t.adapters + 2; g += kWave) counts[g * s.count] = 0;
+  if (segment == 0 && lane < (-n & 3)) plan[s.counts_at + n + lane] = 0;   // up to whole fours
+  __threadfence();
+  each_of_segment(index, t, s, segment, lane, [&](int, bool has, int group, uint64_t alike) {
+    if (has && lane == __builtin_ctzll(alike)) atomicAdd(counts + (int64_t)group * s.count, __builtin_popcountll(alike));
+  });
+}
+
+// Sums of v over the workgroup's threads before this one; `at` goes on by the sum over all.
+__device__ __forceinline__ int sum_before(int v, int& at, int (&sums)[kPlanThreads / kWave]) {
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  int upto = v;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const int o = __shfl_up(upto, d, kWave);
+    if (lane >= d) upto += o;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) sums[wave] = upto;
+  __syncthreads();
+  int before = at + upto - v;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / kWave; ++w) {
+    if (w < wave) before += sums[w];
+    at += sums[w];
+  }
+  return before;
+}
+
+// One workgroup: the counts become first places, and the groups' first places and
+// first tiles follow from them.
+__global__ __launch_bounds__(kPlanThreads) void plan_starts_kernel(AdapterTokens t, Segments s, int* plan) {
+  __shared__ int sums[kPlanThreads / kWave];
+  const int groups = t.adapters + 2;
+  const int64_t n = (int64_t)groups * s.count;
+  int* const counts = plan + s.counts_at;
+  int at = 0;
+  // a thread's counts follow each other, fours whose last may reach past the end
+  i32x4_t* const fours = reinterpret_cast<i32x4_t*>(counts) + threadIdx.x * kPlanDeep;
+  const int64_t left = (n + 3) / 4 - threadIdx.x * kPlanDeep;
+  i32x4_t v[kPlanDeep];
+  const auto load = [&](int64_t base) {
+#pragma unroll
+    for (int u = 0; u < kPlanDeep; ++u) v[u] = base + u < left ? fours[base + u] : i32x4_t{0, 0, 0, 0};
+  };
+  load(0);
+  for (int64_t base = 0; base < (n + 3) / 4; base += kPlanThreads * kPlanDeep) {
+    i32x4_t now[kPlanDeep];
+    int sum = 0;
 #pragma unroll
     for (int u = 0; u < kPlanDeep; ++u) {
-      const int64_t i = base + u * kPlanThreads + threadIdx.x;
-      g[u] = i < t.tokens ? group_of(index, i, t.adapters) : group;
+      now[u] = v[u];
+      sum += now[u].x + now[u].y + now[u].z + now[u].w;
     }
+    load(base + kPlanThreads * kPlanDeep);
+    int place = sum_before(sum, at, sums);
 #pragma unroll
-    for (int u = 0; u < kPlanDeep; ++u) before += g[u] < group;
+    for (int u = 0; u < kPlanDeep; ++u) {
+      i32x4_t to;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        to[k] = place;
+        place += now[u][k];
+      }
+      if (base + u < left) fours[base + u] = to;
+    }
   }
-  before = lanes_sum(before, kWave);
-  if (lane == 0) sums[wave] = before;
   __syncthreads();
-  int at = 0;
-  for (int w = 0; w < kWaves; ++w) at += sums[w];
-  if (threadIdx.x == 0) plan[t.places_at + group] = at;
-  for (int64_t base = 0; base < t.tokens; base += kPlanThreads * kPlanDeep) {
-    // a thread's kPlanDeep tokens follow each other, so that places ascend with them
-    const int64_t first = base + (int64_t)threadIdx.x * kPlanDeep;
-    uint32_t mine = 0;
-#pragma unroll
-    for (int u = 0; u < kPlanDeep; ++u)
-      if (first + u < t.tokens && group_of(index, first + u, t.adapters) == group) mine |= 1u << u;
-    const int n = __builtin_popcount(mine);
-    int below = n;   // of this lane and the lanes before it
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int o = __shfl_up(below, d, kWave);
-      if (lane >= d) below += o;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) sums[wave] = below;
-    __syncthreads();
-    int place = at + below - n;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) place += sums[w];
-      at += sums[w];
-    }
-#pragma unroll
-    for (int u = 0; u < kPlanDeep; ++u)
-      if (mine >> u & 1) plan[t.order_at + place++] = (int)(first + u);
-  }
-  if (threadIdx.x == 0 && group == t.adapters + 1) plan[t.places_at + group + 1] = at;
-}
-
-// First tile of every group: one workgroup adds up the groups' tiles.
-__global__ __launch_bounds__(kPlanThreads) void plan_starts_kernel(AdapterTokens t, int* __restrict__ plan) {
-  constexpr int kWaves = kPlanThreads / kWave;
-  __shared__ int sums[kWaves];
-  const int groups = t.adapters + 2, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const int* places = plan + t.places_at;
-  int at = 0;
+  int tiles = 0;
   for (int base = 0; base < groups; base += kPlanThreads) {
     const int g = base + threadIdx.x;
-    const int n = g < groups ? (places[g + 1] - places[g] + kAdapterTile - 1) / kAdapterTile : 0;
-    int upto = n;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int o = __shfl_up(upto, d, kWave);
-      if (lane >= d) upto += o;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) sums[wave] = upto;
-    __syncthreads();
-    int first = at + upto - n;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) first += sums[w];
-      at += sums[w];
-    }
-    if (g < groups) plan[g] = first;
+    const int from = g < groups ? counts[(int64_t)g * s.count] : 0;
+    const int to = g + 1 < groups ? counts[(int64_t)(g + 1) * s.count] : (int)t.tokens;
+    const int first = sum_before(g < groups ? (to - from + kAdapterTile - 1) / kAdapterTile : 0, tiles, sums);
+    if (g < groups) plan[g] = first, plan[t.places_at + g] = from;
   }
-  if (threadIdx.x == 0) plan[groups] = at;
+  if (threadIdx.x == 0) plan[groups] = tiles, plan[t.places_at + groups] = (int)t.tokens;
+  if (threadIdx.x < (-n & 3)) counts[n + threadIdx.x] = 0;
 }
 
-// The tiles: a thread finds its tile's group among the groups' first tiles.
-__global__ __launch_bounds__(256) void plan_tiles_kernel(AdapterTokens t, int* __restrict__ plan) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// The tokens to their places; the workgroups after those, a thread a tile, find
+// its group among the groups' first tiles.
+template <typename Index>
+__global__ __launch_bounds__(kSegmentWaves* kWave) void plan_order_kernel(const Index* __restrict__ index, AdapterTokens t,
+                                                                         Segments s, int* plan) {
+  constexpr int kThreads = kSegmentWaves * kWave;
+  const int segment = blockIdx.x * kSegmentWaves + threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int workgroups = (s.count + kSegmentWaves - 1) / kSegmentWaves, groups = t.adapters + 2;
+  if ((int)blockIdx.x < workgroups) {
+    if (segment >= s.count) return;
+    int* const places = plan + s.counts_at + segment;
+    each_of_segment(index, t, s, segment, lane, [&](int token, bool has, int group, uint64_t alike) {
+      const int leader = has ? __builtin_ctzll(alike) : 0;
+      int place = 0;
+      if (has && lane == leader) place = atomicAdd(places + (int64_t)group * s.count, __builtin_popcountll(alike));
+      place = __shfl(place, leader, kWave) + __builtin_popcountll(alike & ((1ull << lane) - 1));
+      asm volatile("" : "+v"(place) : : "memory");   // this round's places before the next's
+      if (has && place < t.tokens) plan[t.order_at + place] = token;
+    });
+    __threadfence();
+    // zeros, as behind the last tile
+    for (int64_t g = lane; g < groups; g += kWave) places[g * s.count] = 0;
+    return;
+  }
+  const int64_t i = (int64_t)(blockIdx.x - workgroups) * kThreads + threadIdx.x;
   if (i >= t.max_tiles) return;
-  const int groups = t.adapters + 2;
   int* tile = plan + t.tiles_at + 4 * i;
   int group = 0, first = 0, count = 0;
   if (i < plan[groups]) {
@@ -163,18 +245,25 @@ __global__ __launch_bounds__(256) void plan_tiles_kernel(AdapterTokens t, int* _
   tile[0] = group, tile[1] = first, tile[2] = count, tile[3] = 0;
 }
 
+template <typename Index>
+static hipError_t launch_plan(const Index* index, const AdapterTokens& t, int* plan, hipStream_t stream) {
+  const Segments s = segments_of(t);
+  constexpr int kThreads = kSegmentWaves * kWave;
+  const unsigned workgroups = (unsigned)((s.count + kSegmentWaves - 1) / kSegmentWaves);
+  const unsigned tiles = (unsigned)((t.max_tiles + kThreads - 1) / kThreads);
+  hipError_t e = launch_kernel(plan_counts_kernel<Index>, dim3(workgroups), dim3(kThreads), stream, index, t, s, plan);
+  if (e == hipSuccess) e = launch_kernel(plan_starts_kernel, dim3(1), dim3(kPlanThreads), stream, t, s, plan);
+  if (e == hipSuccess)
+    e = launch_kernel(plan_order_kernel<Index>, dim3(workgroups + tiles), dim3(kThreads), stream, index, t, s, plan);
+  return e;
+}
+
 hipError_t launch_adapter_plan(const void* index, int index_bytes, int64_t tokens, int64_t adapters, void* plan,
                                hipStream_t stream) {
   const AdapterTokens t = adapter_tokens(plan, tokens, adapters);
   int* p = static_cast<int*>(plan);
-  const dim3 groups((unsigned)(adapters + 2)), block(kPlanThreads);
-  hipError_t e = index_bytes == 4
-                     ? launch_kernel(plan_order_kernel<int32_t>, groups, block, stream, (const int32_t*)index, t, p)
-                     : launch_kernel(plan_order_kernel<int64_t>, groups, block, stream, (const int64_t*)index, t, p);
-  if (e == hipSuccess) e = launch_kernel(plan_starts_kernel, dim3(1), block, stream, t, p);
-  if (e == hipSuccess && t.max_tiles > 0)
-    e = launch_kernel(plan_tiles_kernel, dim3((unsigned)((t.max_tiles + 255) / 256)), dim3(256), stream, t, p);
-  return e;
+  return index_bytes == 4 ? launch_plan(static_cast<const int32_t*>(index), t, p, stream)
+                          : launch_plan(static_cast<const int64_t*>(index), t, p, stream);
 }
 
 // ---- forward --------------------------------------------------------------

@@ -318,9 +318,9 @@ constexpr int64_t kAdapterMaxFeatures = (int64_t)1 << 22;
 
 // The plan, in 4-byte words: first tile of every group, first place of every
 // group, the tokens group by group (in their own order inside a group), and
-// the tiles (group, first place, count, 0; count 0 past the last).  Groups:
-// the adapters, then tokens without one, then tokens whose index is past the
-// last adapter.
+// the tiles (group, first place, count, 0; count 0 past the last), and place for
+// the counts that it is made with, zeros afterwards.  Groups: the adapters, then
+// tokens without one, then tokens whose index is past the last adapter.
 struct AdapterTokens {
   const int* plan;       // NULL: all tokens take the one adapter
   int64_t tokens;

@@ -1,0 +1,83 @@
+"""Plans of many tokens of many adapters at once: the layout that the kernels
+read, whatever the index, and work that grows with the tokens and not with tokens
+times adapters."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_06916_amd as sol
+from gpu_util import device, say
+from test_gpu_adapters import plan_ref
+
+pytestmark = pytest.mark.gpu
+
+
+def check_plan(index, adapters, plan=None):
+    plan = sol.adapter_plan(index, adapters, plan)
+    tokens = index.numel()
+    first, places, order, tiles = plan_ref(index.cpu().numpy().astype(np.int64), adapters)
+    p = plan.buffer.cpu().numpy()
+    heads = (adapters + 3 + 3) // 4 * 4
+    assert np.array_equal(p[:adapters + 3], first) and np.array_equal(p[heads:heads + adapters + 3], places)
+    assert np.array_equal(p[2 * heads:2 * heads + tokens], order)
+    rest = p[2 * heads + (tokens + 3) // 4 * 4:].reshape(-1, 4)
+    assert np.array_equal(rest[:len(tiles), :3], np.array(tiles).reshape(-1, 3)) and np.all(rest[len(tiles):, 2] == 0)
+    return plan
+
+
+def drawn(seed, tokens, adapters, kind, dtype=torch.int32):
+    rng = np.random.default_rng(seed)
+    if kind == "any":
+        i = rng.integers(-2, adapters + 2, tokens)
+    elif kind == "one":            # all tokens of one adapter but a few
+        i = np.full(tokens, adapters - 1)
+        i[rng.integers(0, tokens, 3)] = -1
+    elif kind == "sorted":
+        i = np.sort(rng.integers(0, adapters, tokens))
+    else:                          # neighbours always differ
+        i = np.arange(tokens)[::-1] % adapters
+    return torch.from_numpy(i).to(dtype).to(device())
+
+
+@pytest.mark.parametrize("tokens,adapters", [(63, 1), (64, 2), (65, 65536), (255, 30), (256, 31), (257, 62), (511, 3), (513, 200),
+                                             (4097, 63), (20000, 20000), (131072, 1), (131073, 510), (524287, 7),
+                                             (700001, 4000), ((1 << 20) + 7, 65536)])
+@pytest.mark.parametrize("kind", ["any", "one", "sorted", "apart"])
+def test_layout(tokens, adapters, kind):
+    plan = check_plan(drawn(tokens, tokens, adapters, kind), adapters)
+    check_plan(drawn(tokens + 1, tokens, adapters, "any", torch.int64), adapters, plan)   # over another plan
+
+
+def test_indices_past_32_bits():
+    index = drawn(1, 5000, 9, "any", torch.int64)
+    index[::7] = (1 << 40) + 3
+    index[1::7] = -(1 << 40) + 3
+    index[2::7] = (1 << 32) + 3
+    check_plan(index, 9)
+
+
+@pytest.mark.parametrize("fill", [-1, 2 ** 31 - 1])
+def test_memory_that_held_anything(fill):
+    index = drawn(3, 300001, 801, "any")
+    size = sol.adapter_plan_bytes(300001, 801) // 4
+    plan = sol.AdapterPlan(300001, 801, torch.full((size,), fill, dtype=torch.int32, device=device()))
+    for _ in range(3):
+        check_plan(index, 801, plan)
+
+
+def test_work_does_not_grow_with_tokens_times_adapters():
+    """A million tokens: 60000 adapters cost what their counts take and not, as reading all of the
+    index for each of them, thousands of times what two cost."""
+    tokens, times = 1 << 20, {}
+    for adapters in (2, 60000):
+        index = drawn(4, tokens, adapters, "any")
+        plan = sol.adapter_plan(index, adapters)
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        for _ in range(3):
+            sol.adapter_plan(index, adapters, plan)
+        end.record()
+        torch.cuda.synchronize()
+        times[adapters] = start.elapsed_time(end) / 3
+    say(f"  {times} ms")
+    assert times[60000] < 10.0
