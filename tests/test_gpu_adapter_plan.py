@@ -81,3 +81,31 @@ def test_work_does_not_grow_with_tokens_times_adapters():
         times[adapters] = start.elapsed_time(end) / 3
     say(f"  {times} ms")
     assert times[60000] < 10.0
+
+
+def test_the_most_tokens_of_the_most_adapters():
+    """Groups that do not fall and tokens that rise inside each are T different tokens in their order."""
+    tokens, adapters = (1 << 27) - 1, 65536
+    g = torch.Generator(device=device()).manual_seed(1)
+    index = torch.randint(-1, adapters + 1, (tokens,), generator=g, dtype=torch.int32, device=device())
+    say(f"  plan of {tokens} tokens of {adapters} adapters, {sol.adapter_plan_bytes(tokens, adapters) / 2 ** 30:.1f} GiB")
+    p = sol.adapter_plan(index, adapters).buffer
+    torch.cuda.synchronize()
+    say("  made")
+    group = torch.where(index < 0, adapters, torch.where(index >= adapters, adapters + 1, index))
+    heads = (adapters + 3 + 3) // 4 * 4
+    order = p[2 * heads:2 * heads + tokens]
+    assert int(order.min()) == 0 and int(order.max()) == tokens - 1
+    of = group[order]
+    rises = (of[1:] > of[:-1]) | ((of[1:] == of[:-1]) & (order[1:] > order[:-1]))
+    assert bool(rises.all())
+    counts = torch.bincount(group, minlength=adapters + 2)
+    places = torch.cat((counts.new_zeros(1), counts.cumsum(0)))
+    assert torch.equal(p[heads:heads + adapters + 3].long(), places)
+    first = torch.cat((counts.new_zeros(1), ((counts + 31) // 32).cumsum(0)))
+    assert torch.equal(p[:adapters + 3].long(), first)
+    tiles = p[2 * heads + (tokens + 3) // 4 * 4:].view(-1, 4)
+    n = int(first[-1])
+    assert int(tiles[:n, 2].sum(dtype=torch.int64)) == tokens and not bool(tiles[n:, 2].any())
+    e = tiles[:n, 0].long()
+    assert torch.equal(tiles[:n, 1].long(), places[e] + 32 * (torch.arange(n, device=device()) - first[e]))
