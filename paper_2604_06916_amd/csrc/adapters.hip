@@ -20,10 +20,10 @@
 // row 4 g + i of blocks 2 c and 2 c + 1 is rank element 32 c + 8 g + i and four
 // further on, so h is the second product's operand as it stands.
 //
-// 26574 tokens 2432 -> 7296, rank 32: 218 us, 4.2 TB/s (a copy of its bytes 5.0);
-// 8192 tokens 2240 -> 6720 51 us, 5.1 TB/s; 64 tokens of 48 adapters 12.8 us, where
-// most tiles have one token and a and b come from HBM once; 1 token 1152 -> 1152,
-// rank 16 5.5 us.
+// 26574 tokens 2432 -> 7296, rank 32: 219 us, 4.2 TB/s (a copy of its bytes 5.0);
+// 8192 tokens 2240 -> 6720 50 to 63 us, by what of its 257 MB the 256 MB cache keeps;
+// 64 tokens of 48 adapters 12.9 us, where most tiles have one token and a and b come
+// from HBM once; 1 token 1152 -> 1152, rank 16 5.7 us.
 #include <limits.h>
 
 #include "adapters.h"
@@ -54,8 +54,8 @@ struct Segments {
 
 // Segments of kSegment tokens or more, and so few that adding up their counts,
 // 0.4 ns each, takes no longer than their waves do, 2.6 us for 64 tokens (a million
-// tokens of 1000 adapters: 230 us, 456 without), and that the counts take no more words than
-// there are tokens (but for kCounts, or one segment's).
+// tokens of 1000 adapters: 230 us, 456 without), and that the counts take no more
+// words than there are tokens (but for kCounts, or one segment's).
 static Segments segments_of(const AdapterTokens& t) {
   const int64_t groups = t.adapters + 2, fit = (t.tokens + kCounts) / groups;
   int64_t n = (t.tokens + kSegment - 1) / kSegment;
@@ -523,9 +523,9 @@ static int cut(int64_t size, int64_t step, int64_t want, int* width) {
 
 // h in a launch of its own, its K shared by several workgroups, and the second
 // product in another: where a tile's ranges would each go through a large a
-// again (1 token 9728 -> 9728, rank 64: 39.5 us in one launch and 13.6 in two;
-// 2048 tokens 2240 -> 2240, rank 64 25.5 and 23.8; 64 tokens of 48 adapters 2432 -> 7296,
-// rank 32 12.7 and 12.9; 1 token 1152 -> 1152, rank 16 5.8 and 8.0).
+// again (1 token 9728 -> 9728, rank 64: 38.9 us in one launch and 14.1 in two;
+// 2048 tokens 2240 -> 2240, rank 64 23.1 and 20.5; 64 tokens of 48 adapters 2432 -> 7296,
+// rank 32 12.6 and 13.2; 1 token 1152 -> 1152, rank 16 5.8 and 8.5).
 constexpr int64_t kTwoLaunches = (int64_t)1 << 18;   // elements of one adapter's a
 constexpr int kHWaves = 4, kOutWaves = 8;
 
@@ -545,7 +545,7 @@ size_t add_adapters_bytes(const AdapterTokens& t, int64_t K, int64_t rank) {
 
 // A workgroup a tile where there are more than 1.25 tiles a CU, else ranges of a
 // tile's columns, with more waves and shorter steps (8192 tokens 2240 -> 2240, 266
-// tiles, 30 us so and 37 the other way; 12000 tokens 2432 -> 7296, 377 tiles, 112
+// tiles, 30 us so and 38 the other way; 12000 tokens 2432 -> 7296, 377 tiles, 113
 // and 110).
 template <int kChunks>
 static hipError_t launch_rank(AdapterArgs a, hipStream_t stream) {

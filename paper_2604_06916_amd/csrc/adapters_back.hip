@@ -13,9 +13,11 @@
 //
 // Bound by memory, dy, x and past once in and dx once out, and by how few waves
 // hold it in flight, two workgroups a CU of up to 256 registers: 26574 tokens 2432 ->
-// 7296, rank 32 229 us, 3.4 TB/s (114 to 123 us for dy, 12 for g, 91 for x, 12 for
-// the slices); 8192 tokens 2240 -> 6720 87 us.  With few tokens by the four launches:
-// 1 token 1152 -> 1152 20 us.
+// 7296, rank 32 228 to 232 us, 3.4 TB/s (112 to 118 us for dy, 13 for g, 94 to 96 for
+// x, 12 for the slices); 8192 tokens 2240 -> 6720 87 to 91 us.  With few tokens by the
+// four launches: 1 token 1152 -> 1152 20 us.  At a rank of 128 by g: its shares are as
+// many bytes as dy, and every wave of the pass over x reads 48 KB of its pieces a tile
+// for 2 KB of x (6600 tokens 2432 -> 7296 241 us).
 //
 // Both passes multiply by a token's values twice: once with the token's row
 // as it lies in memory (g, dx) and once summed over tokens, for which the row's
@@ -52,7 +54,7 @@ typedef __attribute__((address_space(3))) short4_t* lds_short4_t;
 
 // Blocks of 16 columns of a wave, so that the sums take 64 registers; in the
 // second pass, which holds x, past and g's pieces beside them, 32 where rows stay
-// whole lines (26574 tokens 2432 -> 7296, rank 32: 229 us with four blocks, 252 with
+// whole lines (26574 tokens 2432 -> 7296, rank 32: 229 us with four blocks, 270 with
 // eight, whose registers spill).
 constexpr int cols_of(int chunks) { return 8 / chunks; }
 constexpr int x_cols(int chunks) { return chunks == 1 ? 4 : cols_of(chunks); }
