@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kSegmentWaves* kWave) void plan_order_kernel(const 
       int place = 0;
       if (has && lane == leader) place = atomicAdd(places + (int64_t)group * s.count, __builtin_popcountll(alike));
       place = __shfl(place, leader, kWave) + __builtin_popcountll(alike & ((1ull << lane) - 1));
-      asm volatile("" : "+v"(place) : : "memory");   // this round's places before the next's
+      asm volatile("" : "+v"(place) : : "memory");   // these places before the next 64 tokens'
       if (has && place < t.tokens) plan[t.order_at + place] = token;
     });
     __threadfence();
